@@ -380,6 +380,140 @@ asgd_status asgd_libsvm_read(const char* path, int32_t one_based, const asgd_lib
                              int32_t* label_indices);
 
 /* ------------------------------------------------------------------------ */
+/* Label logits: a 4-bit label matrix, the k best labels under rules, and    */
+/* distillation from a teacher's top logits                                  */
+/* ------------------------------------------------------------------------ */
+
+/* These entry points take matrices that the caller owns instead of a model
+ * (asgd_predict_topk_rules and asgd_distill_step, below, run them on a
+ * model's own logits).  They enqueue on hip_stream (NULL = the default
+ * stream) of the current device and return at once; nothing is allocated and
+ * nothing waits, so they can be captured into a HIP graph.  Device pointers
+ * must belong to the current device, and so must the stream (EINVAL
+ * otherwise; a host address is EINVAL too).  Sizes, types and alignment are
+ * checked on the host before anything is enqueued.  Scratch memory comes from
+ * the caller: `ws`, at least as many bytes as the matching _workspace call
+ * gives (ERANGE below), 256-byte aligned, and used by one call at a time:
+ * calls that may overlap (other streams, two captured graphs) need one each.
+ * Its content carries nothing from one call to the next. */
+
+/* Element types of a matrix. */
+enum { ASGD_F32 = 0, ASGD_BF16 = 1, ASGD_F16 = 2 };
+
+/* A dense device matrix: element (i, j) at data + i * ld + j, in elements.
+ * data is aligned to its element type; ld >= n_cols and otherwise free (rows
+ * aligned to 16 bytes are fastest).  n_rows in [1, 2^20], n_cols in [1, 2^22). */
+typedef struct asgd_matrix {
+  int32_t n_rows, n_cols;
+  int64_t ld;
+  int32_t dtype; /* ASGD_F32, ASGD_BF16 or ASGD_F16 */
+  void* data;
+} asgd_matrix;
+
+/* A matrix in MXFP4 (the OCP microscaling format): 32 consecutive elements of
+ * a row share one power-of-two scale.  Byte c of a row's codes holds element
+ * 2c in its low and 2c + 1 in its high half, each e2m1 (sign, two exponent
+ * bits, one mantissa bit: 0, 0.5, 1, 1.5, 2, 3, 4, 6); scales[i][j / 32] is
+ * 127 + e for a scale 2^e, 255 for a block that is NaN.  n_cols is a multiple
+ * of 32; n_rows in [1, 2^22), n_rows * n_cols below 2^31.  codes is 16-byte, scales 4-byte aligned. */
+typedef struct asgd_fp4 {
+  int32_t n_rows, n_cols;
+  uint8_t* codes;  /* device, [n_rows x n_cols / 2] */
+  uint8_t* scales; /* device, [n_rows x n_cols / 32] */
+} asgd_fp4;
+
+/* x -> q.  Per block e = floor(log2(largest magnitude)) - 2, kept in
+ * [-127, 127]; elements are x 2^-e rounded to nearest, ties to the even code,
+ * at most 6 in magnitude.  A block of zeros has scale byte 0; a block with an
+ * infinity or a NaN becomes NaN.  x has q's shape (EINVAL otherwise). */
+asgd_status asgd_fp4_quantize(const asgd_matrix* x, const asgd_fp4* q, void* hip_stream);
+
+/* The values that q stands for, rounded once to out's type. */
+asgd_status asgd_fp4_dequantize(const asgd_fp4* q, const asgd_matrix* out, void* hip_stream);
+
+/* Z = A W^T + bias with the label matrix W in MXFP4 [L x 128]: the output
+ * layer of a model whose W2 was quantized.  A [B x 128] is either h (bf16) or
+ * h4 (MXFP4); the other is NULL.  bias: device float [L] or NULL.  Z [B x L]
+ * in any of the three types: products are exact, summed in fp32, and rounded
+ * once.  h's rows are 16-byte aligned (data and ld; EINVAL otherwise). */
+asgd_status asgd_fp4_logits(const asgd_matrix* h, const asgd_fp4* h4, const asgd_fp4* w, const float* bias,
+                            const asgd_matrix* z, void* hip_stream);
+
+/* What is done to the logits of a row before its labels are ranked.  With c_j
+ * the number of times that label j stands in the row's list of `seen`:
+ *   t = z_j; where c_j > 0: t = (t > 0 ? t / repetition : t * repetition)
+ *                               - frequency * c_j - presence
+ *   s_j = t + bias[j] + row_bias of j,  formed in float64, rounded once to float
+ * and labels whose bit of `allowed` is 0 are left out.  Zero-initialise the
+ * struct for no rules (repetition 0 counts as 1).  Ids outside [0, L) are
+ * skipped; of row_bias entries of one row that name the same id the last one
+ * counts. */
+typedef struct asgd_logit_rules {
+  const float* bias;       /* device [L], or NULL */
+  const uint32_t* allowed; /* device bit mask, bit j % 32 of word j / 32 of a row, or NULL: all */
+  int64_t allowed_ld;      /* words from one row's mask to the next, >= ceil(L/32); 0: one mask for all rows */
+  const asgd_csr* seen;    /* ids per row (values ignored; an id may repeat), or NULL */
+  const asgd_csr* row_bias; /* ids and values per row, or NULL */
+  double repetition;       /* > 0, or 0 for none */
+  double frequency, presence;
+} asgd_logit_rules;
+
+/* The k best labels of every row of z by s (ties: smaller id first) under
+ * `rules` (NULL: none), 1 <= k <= 64.  ids: device int32 [B x k]; scores:
+ * device float [B x k] or NULL; lse: device float [B] or NULL, the
+ * log-sum-exp of s over the row's ranked labels, so that score - lse is a
+ * log-probability.  NaN is not ranked; where a row has fewer than k ranked
+ * labels the places left hold id 2^31 - 1 and score -inf, and a row without
+ * any has lse -inf. */
+asgd_status asgd_logits_topk_workspace(int32_t n_rows, int32_t n_cols, int32_t k, size_t* bytes);
+asgd_status asgd_logits_topk(const asgd_matrix* z, const asgd_logit_rules* rules, int32_t k, int32_t* ids,
+                             float* scores, float* lse, void* ws, size_t ws_bytes, void* hip_stream);
+
+/* Distillation from a teacher's top logits: t_ids (device int32 [B x k]) and
+ * t_logits (device float [B x k]) as asgd_predict_topk and asgd_logits_topk
+ * write them.  An entry counts if its id is in [0, L) and its logit finite.
+ * With q the softmax of the row's counted teacher logits over the temperature
+ * T and p the softmax of all of the row's z over T,
+ *   loss_i  = T^2 sum_e q_e (ln q_e - ln p_{id_e})
+ *   dz_ij   = w_i T (p_ij - sum of q_e over the entries with id_e = j)
+ * (the gradient of sum_i w_i loss_i); rows without a counted entry have loss
+ * and gradient 0.  weights: device float [B] or NULL for 1 / B.  loss_rows:
+ * device float [B].  grad: NULL for the loss alone, or a matrix of z's shape
+ * and type, which may be z itself (the same data and ld) but not overlap it
+ * otherwise.  1 <= k <= 512, T > 0 and finite.  A logit that is NaN or +inf makes its row's
+ * loss and gradient NaN; a label of logit -inf has p = 0. */
+asgd_status asgd_distill_workspace(int32_t n_rows, int32_t n_cols, int32_t k, size_t* bytes);
+asgd_status asgd_distill(const asgd_matrix* z, const int32_t* t_ids, const float* t_logits, int32_t k,
+                         float temperature, const float* weights, float* loss_rows, const asgd_matrix* grad,
+                         void* ws, size_t ws_bytes, void* hip_stream);
+
+/* The model's W2 in MXFP4, for asgd_predict_topk_rules: w is [L x 128] and
+ * owned by the caller.  Enqueued on the model's stream; a later training step
+ * does not change it. */
+asgd_status asgd_model_fp4_labels(asgd_model* m, const asgd_fp4* w);
+
+/* asgd_predict_topk with rules, up to 64 labels, optional log-sum-exp, and
+ * optionally through a 4-bit label matrix: rules, k, ids, scores and lse as
+ * for asgd_logits_topk; w NULL for the model's own W2, or [L x 128] (the
+ * hidden rows are then bf16, the biases the model's b2).  The logits pass
+ * through `ws`, as many rows at a time as it holds:
+ * asgd_predict_rules_workspace gives the bytes for n_rows at a time (fewer
+ * rows, a smaller cache footprint), any n_rows >= 1 will do.
+ * Asynchronous on the model's stream; B up to max_batch. */
+asgd_status asgd_predict_rules_workspace(const asgd_model* m, int32_t n_rows, int32_t k, size_t* bytes);
+asgd_status asgd_predict_topk_rules(asgd_model* m, const asgd_csr* x, int32_t k, const asgd_logit_rules* rules,
+                                    const asgd_fp4* w, int32_t* ids_dev, float* scores_dev, float* lse_dev, void* ws,
+                                    size_t ws_bytes);
+
+/* One SGD step on the batch x against a teacher's top logits: asgd_train_step
+ * with the mean of asgd_distill's loss over the batch in the place of the
+ * cross-entropy.  k <= 512.  The logits are stored, so the model must have been
+ * created with ASGD_UNFUSED_OUTPUT (ESTATE otherwise).  loss_out as for
+ * asgd_train_step; asgd_model_last_loss reads it too. */
+asgd_status asgd_distill_step(asgd_model* m, const asgd_csr* x, const int32_t* t_ids, const float* t_logits,
+                              int32_t k, float temperature, float lr, float* loss_out);
+
+/* ------------------------------------------------------------------------ */
 /* Kernel timing (HIP events on the model's stream)                          */
 /* ------------------------------------------------------------------------ */
 

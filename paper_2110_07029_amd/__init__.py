@@ -16,5 +16,8 @@ from ._binding import (  # noqa: F401
     asgd_model_set_timing, asgd_model_get_timing, KERNELS, ASGD_CLOCK_TIMED, ASGD_CLOCK_VIRTUAL,
     asgd_elastic_config, asgd_elastic_log, asgd_elastic_create, asgd_elastic_free, asgd_elastic_round,
     asgd_elastic_model, asgd_libsvm_info, asgd_libsvm_scan, asgd_libsvm_read,
+    ASGD_F32, ASGD_BF16, ASGD_F16, asgd_matrix, asgd_fp4, asgd_logit_rules, asgd_fp4_quantize, asgd_fp4_dequantize,
+    asgd_fp4_logits, asgd_logits_topk_workspace, asgd_logits_topk, asgd_distill_workspace, asgd_distill,
+    asgd_model_fp4_labels, asgd_predict_rules_workspace, asgd_predict_topk_rules, asgd_distill_step,
 )
-from .device_data import DeviceCSR  # noqa: F401
+from .device_data import DeviceCSR, fp4_matrix, logit_rules, matrix  # noqa: F401

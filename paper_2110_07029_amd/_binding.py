@@ -35,7 +35,11 @@ EXPORTS = (
     "asgd_model_set_timing",
     "asgd_model_get_timing", "asgd_elastic_create", "asgd_elastic_free", "asgd_elastic_round",
     "asgd_elastic_model", "asgd_last_error",
+    "asgd_fp4_quantize", "asgd_fp4_dequantize", "asgd_fp4_logits", "asgd_logits_topk_workspace",
+    "asgd_logits_topk", "asgd_distill_workspace", "asgd_distill", "asgd_model_fp4_labels",
+    "asgd_predict_rules_workspace", "asgd_predict_topk_rules", "asgd_distill_step",
 )
+ASGD_F32, ASGD_BF16, ASGD_F16 = 0, 1, 2
 ASGD_CLOCK_TIMED, ASGD_CLOCK_VIRTUAL = 0, 1
 
 # Kernel groups of asgd_model_get_timing.
@@ -71,6 +75,20 @@ class asgd_elastic_config(ctypes.Structure):
 class asgd_libsvm_info(ctypes.Structure):
     _fields_ = [("n_rows", c_int64), ("nnz", c_int64), ("label_nnz", c_int64), ("n_features", c_int64),
                 ("n_labels", c_int64), ("header_rows", c_int64)]
+
+
+class asgd_matrix(ctypes.Structure):
+    _fields_ = [("n_rows", c_int32), ("n_cols", c_int32), ("ld", c_int64), ("dtype", c_int32), ("data", c_void_p)]
+
+
+class asgd_fp4(ctypes.Structure):
+    _fields_ = [("n_rows", c_int32), ("n_cols", c_int32), ("codes", c_void_p), ("scales", c_void_p)]
+
+
+class asgd_logit_rules(ctypes.Structure):
+    _fields_ = [("bias", c_void_p), ("allowed", c_void_p), ("allowed_ld", c_int64), ("seen", POINTER(asgd_csr)),
+                ("row_bias", POINTER(asgd_csr)), ("repetition", c_double), ("frequency", c_double),
+                ("presence", c_double)]
 
 
 class asgd_elastic_log(ctypes.Structure):
@@ -118,6 +136,21 @@ def _declare(lib):
                                          POINTER(asgd_elastic_log)]),
         "asgd_elastic_model": (c_int32, [P, c_int32, POINTER(c_void_p)]),
         "asgd_last_error": (ctypes.c_char_p, []),
+        "asgd_fp4_quantize": (c_int32, [POINTER(asgd_matrix), POINTER(asgd_fp4), P]),
+        "asgd_fp4_dequantize": (c_int32, [POINTER(asgd_fp4), POINTER(asgd_matrix), P]),
+        "asgd_fp4_logits": (c_int32, [POINTER(asgd_matrix), POINTER(asgd_fp4), POINTER(asgd_fp4), P,
+                                      POINTER(asgd_matrix), P]),
+        "asgd_logits_topk_workspace": (c_int32, [c_int32, c_int32, c_int32, POINTER(c_size_t)]),
+        "asgd_logits_topk": (c_int32, [POINTER(asgd_matrix), POINTER(asgd_logit_rules), c_int32, P, P, P, P, c_size_t,
+                                       P]),
+        "asgd_distill_workspace": (c_int32, [c_int32, c_int32, c_int32, POINTER(c_size_t)]),
+        "asgd_distill": (c_int32, [POINTER(asgd_matrix), P, P, c_int32, c_float, P, P, POINTER(asgd_matrix), P,
+                                   c_size_t, P]),
+        "asgd_model_fp4_labels": (c_int32, [P, POINTER(asgd_fp4)]),
+        "asgd_predict_rules_workspace": (c_int32, [P, c_int32, c_int32, POINTER(c_size_t)]),
+        "asgd_predict_topk_rules": (c_int32, [P, POINTER(asgd_csr), c_int32, POINTER(asgd_logit_rules),
+                                              POINTER(asgd_fp4), P, P, P, P, c_size_t]),
+        "asgd_distill_step": (c_int32, [P, POINTER(asgd_csr), P, P, c_int32, c_float, c_float, POINTER(c_float)]),
     }
     for name, (res, args) in sig.items():
         f = getattr(lib, name)
@@ -373,3 +406,78 @@ def asgd_elastic_model(e: int, which: int) -> int:
     h = c_void_p()
     _check(load().asgd_elastic_model(e, which, byref(h)), "asgd_elastic_model")
     return h.value
+
+
+# ------------------------------------------------------------------ label logits
+def _span(ws):
+    """(address, bytes) of scratch memory given as a tensor or None."""
+    return (None, 0) if ws is None else (ws.data_ptr(), ws.numel() * ws.element_size())
+
+
+def asgd_fp4_quantize(x: asgd_matrix, q: asgd_fp4, stream=None):
+    _check(load().asgd_fp4_quantize(byref(x), byref(q), _stream(stream)), "asgd_fp4_quantize")
+
+
+def asgd_fp4_dequantize(q: asgd_fp4, out: asgd_matrix, stream=None):
+    _check(load().asgd_fp4_dequantize(byref(q), byref(out), _stream(stream)), "asgd_fp4_dequantize")
+
+
+def asgd_fp4_logits(h, w: asgd_fp4, z: asgd_matrix, bias=None, stream=None):
+    """h: the hidden rows, an asgd_matrix (bf16) or an asgd_fp4."""
+    h4 = isinstance(h, asgd_fp4)
+    _check(load().asgd_fp4_logits(None if h4 else byref(h), byref(h) if h4 else None, byref(w), _ptr(bias), byref(z),
+                                  _stream(stream)), "asgd_fp4_logits")
+
+
+def asgd_logits_topk_workspace(n_rows: int, n_cols: int, k: int) -> int:
+    v = c_size_t()
+    _check(load().asgd_logits_topk_workspace(n_rows, n_cols, k, byref(v)), "asgd_logits_topk_workspace")
+    return v.value
+
+
+def asgd_logits_topk(z: asgd_matrix, k: int, ids, scores=None, rules=None, lse=None, workspace=None, stream=None):
+    ws, n = _span(workspace)
+    _check(load().asgd_logits_topk(byref(z), None if rules is None else byref(rules), k, _ptr(ids), _ptr(scores),
+                                   _ptr(lse), ws, n, _stream(stream)), "asgd_logits_topk")
+
+
+def asgd_distill_workspace(n_rows: int, n_cols: int, k: int) -> int:
+    v = c_size_t()
+    _check(load().asgd_distill_workspace(n_rows, n_cols, k, byref(v)), "asgd_distill_workspace")
+    return v.value
+
+
+def asgd_distill(z: asgd_matrix, t_ids, t_logits, temperature: float, loss_rows, grad=None, weights=None,
+                 workspace=None, stream=None, k: int = None):
+    """k: teacher entries per row; by default the second dimension of the tensor t_ids."""
+    ws, n = _span(workspace)
+    _check(load().asgd_distill(byref(z), _ptr(t_ids), _ptr(t_logits), t_ids.shape[1] if k is None else k, temperature,
+                               _ptr(weights), _ptr(loss_rows), None if grad is None else byref(grad), ws, n,
+                               _stream(stream)), "asgd_distill")
+
+
+def asgd_model_fp4_labels(m: int, w: asgd_fp4):
+    _check(load().asgd_model_fp4_labels(m, byref(w)), "asgd_model_fp4_labels")
+
+
+def asgd_predict_rules_workspace(m: int, n_rows: int, k: int) -> int:
+    v = c_size_t()
+    _check(load().asgd_predict_rules_workspace(m, n_rows, k, byref(v)), "asgd_predict_rules_workspace")
+    return v.value
+
+
+def asgd_predict_topk_rules(m: int, x: asgd_csr, k: int, ids_dev, scores_dev=None, lse_dev=None, rules=None, w=None,
+                            workspace=None):
+    ws, n = _span(workspace)
+    _check(load().asgd_predict_topk_rules(m, byref(x), k, None if rules is None else byref(rules),
+                                          None if w is None else byref(w), _ptr(ids_dev), _ptr(scores_dev),
+                                          _ptr(lse_dev), ws, n), "asgd_predict_topk_rules")
+
+
+def asgd_distill_step(m: int, x: asgd_csr, t_ids, t_logits, temperature: float, lr: float, want_loss: bool = False,
+                      k: int = None):
+    """k: teacher entries per row; by default the second dimension of the tensor t_ids."""
+    v = c_float()
+    _check(load().asgd_distill_step(m, byref(x), _ptr(t_ids), _ptr(t_logits), t_ids.shape[1] if k is None else k,
+                                    temperature, lr, byref(v) if want_loss else None), "asgd_distill_step")
+    return v.value if want_loss else None

@@ -16,6 +16,7 @@
 
 #include "../../include/asgd.h"
 #include "asgd_kernels.h"
+#include "ops_check.h"
 
 using namespace asgd;
 
@@ -175,6 +176,8 @@ struct asgd_model {
   int ldz = 0;
   float* sm_m = nullptr;  // softmax partials per (column chunk, row)
   float* sm_s = nullptr;
+  char* distill = nullptr;  // scratch of asgd_distill_step (unfused output only)
+  size_t distill_bytes = 0;
   double* tk = nullptr;
   int64_t tk_entries = 0;
 
@@ -261,6 +264,11 @@ int64_t layout_workspace(asgd_model* m, char* base) {
   m->Z = carve<float>(p, m->unfused ? (int64_t)rp * m->ldz : 0);
   m->sm_m = carve<float>(p, sm_rows);
   m->sm_s = carve<float>(p, sm_rows);
+  // Pieces of a distillation step's rows, at most 2,048 + rows of them, and the student's
+  // logits of the teacher's labels.
+  const int64_t train_rows = m->unfused ? std::min(rp, kMaxTrainBatch) : 0;
+  m->distill_bytes = m->unfused ? (size_t)(train_rows + 2048) * 8 + 256 + (size_t)train_rows * DISTILL_MAX_K * 4 : 0;
+  m->distill = carve<char>(p, (int64_t)m->distill_bytes);
   m->tk = carve<double>(p, tk_entries);
   m->tk_entries = tk_entries;
   return (int64_t)(p - base);
@@ -1031,6 +1039,136 @@ asgd_status asgd_debug_touched_rows(asgd_model* m, const asgd_csr* x, int32_t* i
   HIP_TRY(hipMemcpyAsync(&c, m->count, sizeof(c), hipMemcpyDeviceToHost, m->stream));
   HIP_TRY(hipStreamSynchronize(m->stream));
   *count_host = c;
+  return ASGD_OK;
+}
+
+// ---- label logits on a model (the entry points that take matrices are in api_logits.hip) ----
+
+asgd_status asgd_model_fp4_labels(asgd_model* m, const asgd_fp4* w) {
+  if (!m) return fail(ASGD_EINVAL, "model is NULL");
+  asgd_status s = check_fp4(w, "w");
+  if (s) return s;
+  if (w->n_rows != m->L || w->n_cols != HID) return fail(ASGD_EINVAL, "w must be [n_labels x 128]");
+  if ((s = check_device(w->codes, "w.codes")) || (s = check_device(w->scales, "w.scales"))) return s;
+  HIP_TRY(launch_fp4_quantize(ASGD_F32, m->W2(), HID, m->L, HID, w->codes, w->scales, m->stream));
+  return ASGD_OK;
+}
+
+namespace {
+// Scratch of a prediction under rules: fp32 logits of n rows (whole tiles of labels), then
+// the ranking's.
+int64_t rules_ldz(const asgd_model* m) { return round_up(m->L, OUT_TILE); }
+size_t rules_logit_bytes(const asgd_model* m, int64_t n) { return (size_t)round_up(n * rules_ldz(m) * 4, 256); }
+size_t rules_bytes(const asgd_model* m, int n, int k) {
+  return rules_logit_bytes(m, n) + rank_ws_bytes(rank_shape(n, m->L), n, k);
+}
+}  // namespace
+
+asgd_status asgd_predict_rules_workspace(const asgd_model* m, int32_t n_rows, int32_t k, size_t* bytes) {
+  if (!m || !bytes) return fail(ASGD_EINVAL, "NULL argument");
+  if (k < 1 || k > RANK_MAX_K) return fail(ASGD_EINVAL, "k must be in [1, 64]");
+  if (n_rows < 1) return fail(ASGD_EINVAL, "n_rows must be >= 1");
+  if (n_rows > kMaxBatch) return fail(ASGD_ERANGE, "n_rows must be <= 16384");
+  *bytes = rules_bytes(m, n_rows, k);
+  return ASGD_OK;
+}
+
+asgd_status asgd_predict_topk_rules(asgd_model* m, const asgd_csr* x, int32_t k, const asgd_logit_rules* rules,
+                                    const asgd_fp4* w, int32_t* ids_dev, float* scores_dev, float* lse_dev, void* ws,
+                                    size_t ws_bytes) {
+  if (!m) return fail(ASGD_EINVAL, "model is NULL");
+  asgd_status s = check_batch(m, x, nullptr, false);
+  if (s) return s;
+  const int B = x->n_rows;
+  if (k < 1 || k > RANK_MAX_K) return fail(ASGD_EINVAL, "k must be in [1, 64]");
+  if ((s = check_rules(rules, B, m->L))) return s;
+  if (w) {
+    if ((s = check_fp4(w, "w"))) return s;
+    if (w->n_rows != m->L || w->n_cols != HID) return fail(ASGD_EINVAL, "w must be [n_labels x 128]");
+  }
+  if (!ids_dev) return fail(ASGD_EINVAL, "ids_dev is NULL");
+  if (((uintptr_t)ids_dev | (uintptr_t)scores_dev | (uintptr_t)lse_dev) % 4)
+    return fail(ASGD_EINVAL, "ids_dev, scores_dev and lse_dev must be 4-byte aligned");
+  // as many rows at a time as the scratch memory holds
+  int n = (int)std::min<int64_t>(B, ws_bytes / (rules_ldz(m) * 4));
+  while (n > 0 && rules_bytes(m, n, k) > ws_bytes) --n;
+  if (n < 1) return fail(ASGD_ERANGE, "the workspace is smaller than asgd_predict_rules_workspace says for one row");
+  if ((s = check_workspace(ws, ws_bytes, rules_bytes(m, n, k)))) return s;
+  if ((s = check_rules_memory(rules)) || (s = check_device(ids_dev, "ids_dev"))) return s;
+  if (scores_dev && (s = check_device(scores_dev, "scores_dev"))) return s;
+  if (lse_dev && (s = check_device(lse_dev, "lse_dev"))) return s;
+  if (w && ((s = check_device(w->codes, "w.codes")) || (s = check_device(w->scales, "w.scales")))) return s;
+  int rows_pad = 0;
+  m->pipe = false;
+  if ((s = run_gather(m, x, nullptr, m->stream, &rows_pad))) return s;
+  const void* h = m->H1;
+  if (w && !m->bf16) {
+    // fp32 operands: the hidden rows as bf16 into the operands' other copy, which nothing reads
+    // any more (steps that use it are behind this call's work on the stream)
+    void* const to = m->H1b[m->par ^ 1];
+    HIP_TRY(launch_to_bf16((const float*)m->H1, to, (int64_t)rows_pad * HID, m->stream));
+    h = to;
+  }
+  const int64_t ldz = rules_ldz(m);
+  float* const Z = (float*)ws;
+  void* const rank_ws = (char*)ws + rules_logit_bytes(m, n);
+  const RankShape sh = rank_shape(n, m->L);  // (of a full piece, so that the last fits the scratch too)
+  for (int r0 = 0; r0 < B; r0 += n) {
+    const int rows = std::min(n, B - r0);
+    if (w) {
+      const Fp4Rows a{(const char*)h + (size_t)r0 * HID * 2, HID, nullptr, nullptr};
+      HIP_TRY(launch_fp4_logits(a, rows, w->codes, w->scales, m->b2(), m->L, ASGD_F32, Z, ldz, m->stream));
+    } else {
+      // (reads up to 255 operand rows past the piece's: inside H1 or the copy behind it, unused)
+      HIP_TRY(launch_out_logits(m->bf16, m->W2(), m->b2(), m->L, (const char*)h + (size_t)r0 * HID * m->elem, rows, Z,
+                                (int)ldz, 0, m->n_cu, nullptr, nullptr, m->stream));
+    }
+    HIP_TRY(launch_rank(ASGD_F32, Z, ldz, rows, m->L, rules_dev(rules, r0), k, sh, ids_dev + (int64_t)r0 * k,
+                        scores_dev ? scores_dev + (int64_t)r0 * k : nullptr, lse_dev ? lse_dev + r0 : nullptr, rank_ws,
+                        m->stream));
+  }
+  return ASGD_OK;
+}
+
+asgd_status asgd_distill_step(asgd_model* m, const asgd_csr* x, const int32_t* t_ids, const float* t_logits,
+                              int32_t k, float temperature, float lr, float* loss_out) {
+  if (!m) return fail(ASGD_EINVAL, "model is NULL");
+  asgd_status s = check_batch(m, x, nullptr);
+  if (s) return s;
+  if (!m->unfused) return fail(ASGD_ESTATE, "a distillation step needs a model with ASGD_UNFUSED_OUTPUT");
+  if (k < 1 || k > DISTILL_MAX_K) return fail(ASGD_EINVAL, "k must be in [1, 512]");
+  if (!(temperature > 0.0f) || !isfinite(temperature))
+    return fail(ASGD_EINVAL, "temperature must be positive and finite");
+  if (!(lr == lr)) return fail(ASGD_EINVAL, "lr is NaN");
+  if (!t_ids || !t_logits) return fail(ASGD_EINVAL, "t_ids and t_logits must be non-NULL");
+  if (((uintptr_t)t_ids | (uintptr_t)t_logits) % 4) return fail(ASGD_EINVAL, "t_ids and t_logits must be 4-byte aligned");
+  if ((s = check_device(t_ids, "t_ids")) || (s = check_device(t_logits, "t_logits"))) return s;
+  const int B = x->n_rows;
+  const DistillShape sh = distill_shape(B, m->ldz);
+  if (distill_ws_bytes(sh, B, k) > m->distill_bytes) return fail(ASGD_ERANGE, "distillation buffer too small");
+  int rows_pad = 0;
+  m->pipe = false;
+  const SortPlan sort = plan_sort(m, x->nnz);
+  if ((s = run_gather(m, x, nullptr, m->stream, &rows_pad))) return s;
+  if ((s = run_sort(m, m->stream, sort))) return s;
+  TIMED(m, ASGD_K_LOGITS, launch_out_logits(m->bf16, m->W2(), m->b2(), m->L, m->H1, B, m->Z, m->ldz, 0, m->n_cu,
+                                            nullptr, nullptr, m->stream));
+  // the loss, and the gradient in the logits' place (columns past L hold -inf: gradient 0)
+  const DistillJob job{m->Z, m->ldz, B, m->ldz, m->L, t_ids, t_logits, k, temperature, nullptr, m->loss_rows,
+                       m->Z, m->ldz};
+  TIMED(m, ASGD_K_SOFTMAX, launch_distill(ASGD_F32, job, sh, m->distill, m->stream));
+  const int splits = fwd_splits(m, B);
+  if ((int64_t)splits * rows_pad > m->part_rows) return fail(ASGD_ERANGE, "partial buffer too small");
+  TIMED(m, ASGD_K_DH, launch_stored_dh(m->bf16, m->W2(), m->b2(), m->L, m->Z, m->ldz, B, splits, m->o_part, rows_pad,
+                                       m->extra ? m->A2 : m->A1, m->extra ? m->dA2 : m->dA1, m->stream));
+  if (m->extra)
+    TIMED(m, ASGD_K_DENSE_BWD, launch_dense_bwd(m->dA2, m->A1, m->Wh(), m->bh(), B, rows_pad, lr, m->dA1, m->stream));
+  TIMED(m, ASGD_K_W1_UPDATE,
+        launch_sparse_update(m->W1(), m->F, sort.keys_out, sort.vals_out, x->nnz, m->row_of, dev(x), m->dA1, lr, B,
+                             m->b1(), m->loss_rows, m->loss, m->w1_part, nullptr, nullptr, m->stream, nullptr));
+  TIMED(m, ASGD_K_OUT_BWD, launch_stored_wgrad(m->bf16, m->W2(), m->b2(), m->L, m->Z, m->ldz, m->H1, m->H1T,
+                                               m->rows_pad_max, rows_pad, B, lr, m->stream));
+  if (loss_out) return asgd_model_last_loss(m, loss_out);
   return ASGD_OK;
 }
 

@@ -225,6 +225,78 @@ hipError_t launch_softmax_ce(const float* Z, int ldz, int B, float* m_part, floa
 hipError_t launch_unfused_dh(bool use_bf16, const float* W2, const float* b2, int L, const float* Z, int ldz,
                              const float* lse, int B, int splits, float* o_part, int ld_part, const CsrDev& y,
                              const float* rw, const float* A, float* dA, hipStream_t st);
+// dA = (dZ W2) * [A > 0] from a stored gradient dZ [B x ldz] (zero past label L).
+hipError_t launch_stored_dh(bool use_bf16, const float* W2, const float* b2, int L, const float* dZ, int ldz, int B,
+                            int splits, float* o_part, int ld_part, const float* A, float* dA, hipStream_t st);
+// W2 -= lr dZ^T H1 and b2 -= lr 1^T dZ.  H1T: scratch of [128 x ld_t] for bf16 operands, ld_t >= B
+// rounded up to 64; H1 has rows_pad rows, zero from B on.
+hipError_t launch_stored_wgrad(bool use_bf16, float* W2, float* b2, int L, const float* dZ, int ldz, const void* H1,
+                               void* H1T, int ld_t, int rows_pad, int B, float lr, hipStream_t st);
+// n fp32 values as bf16, rounded to nearest.
+hipError_t launch_to_bf16(const float* in, void* out, int64_t n, hipStream_t st);
+
+// ---- label logits (k_rank.hip, k_distill.hip, k_fp4.hip) ----------------------------
+// Element types: 0 float, 1 bfloat16, 2 half.
+// Lists of ids per row: row i spans [indptr[i], indptr[i + 1]), read only inside
+// [*first, *first + nnz).  indptr null: no lists.
+struct IdLists {
+  const int32_t *first, *indptr, *indices;
+  const float* values;
+  int nnz;
+};
+// The k best labels of z [rows x L] under rules.
+struct RankRules {
+  const float* bias;
+  const uint32_t* allowed;
+  int64_t allowed_ld;
+  IdLists seen, row_bias;
+  double repetition, frequency, presence;
+};
+constexpr int RANK_MAX_K = 64;
+struct RankShape {
+  int splits;  // pieces per row
+};
+RankShape rank_shape(int rows, int cols);
+size_t rank_ws_bytes(const RankShape& sh, int rows, int k);
+hipError_t launch_rank(int dtype, const void* z, int64_t ld, int rows, int L, const RankRules& ru, int k,
+                       const RankShape& sh, int32_t* ids, float* scores, float* lse, void* ws, hipStream_t st);
+
+// Loss against a teacher's k logits per row and, with grad, its gradient (grad may be z).
+struct DistillJob {
+  const void* z;
+  int64_t ld;
+  int n_rows, n_cols;
+  int n_labels;  // ids below it count (columns from it on hold -inf)
+  const int32_t* t_ids;
+  const float* t_logits;
+  int k;
+  float temperature;
+  const float* weights;  // per row, or null: 1 / n_rows
+  float* loss_rows;
+  void* grad;
+  int64_t ld_grad;
+};
+constexpr int DISTILL_MAX_K = 512;
+struct DistillShape {
+  int splits;
+};
+DistillShape distill_shape(int rows, int cols);
+size_t distill_ws_bytes(const DistillShape& sh, int rows, int k);
+hipError_t launch_distill(int dtype, const DistillJob& j, const DistillShape& sh, void* ws, hipStream_t st);
+
+// MXFP4: codes [rows x cols / 2], scales [rows x cols / 32].
+hipError_t launch_fp4_quantize(int dtype, const void* x, int64_t ld, int rows, int cols, uint8_t* codes,
+                               uint8_t* scales, hipStream_t st);
+hipError_t launch_fp4_dequantize(const uint8_t* codes, const uint8_t* scales, int rows, int cols, int dtype, void* out,
+                                 int64_t ld, hipStream_t st);
+// Z = A W^T + bias, W [L x 128] in MXFP4, A either bf16 rows (h, 16-byte aligned) or MXFP4.
+struct Fp4Rows {
+  const void* h;
+  int64_t ld;
+  const uint8_t *codes, *scales;
+};
+hipError_t launch_fp4_logits(const Fp4Rows& a, int B, const uint8_t* codes, const uint8_t* scales, const float* bias,
+                             int L, int dtype, void* z, int64_t ldz, hipStream_t st);
 
 // ---- prediction ---------------------------------------------------------------
 // A prediction's launch shape: 32 nb rows per wave, nrb row blocks of 8 waves,

@@ -321,9 +321,10 @@ int softmax_splits(int ldz) { return (ldz + SM_CHUNK - 1) / SM_CHUNK; }
 // O = P W2 from the stored logits.  The workgroup shape of the logits kernel;
 // per tile a wave loads its 32 rows x 32 labels of Z, forms p = 2^(z log2 e - lse log2 e) in the
 // accumulator layout, and adds W2_tile^T P^T into its O^T accumulators.  Z and W2 tiles
-// are loaded two ahead (670,091 labels, 256 rows: 250 us, one ahead 265).
+// are loaded two ahead (670,091 labels, 256 rows: 250 us, one ahead 265).  GIVEN: Z holds
+// dZ and is taken as it is (distillation), and no lse.
 // ---------------------------------------------------------------------------
-template <bool BF16>
+template <bool BF16, bool GIVEN>
 __global__ __launch_bounds__(FWD_THREADS) void k_unfused_dh(const float* __restrict__ W2,
                                                             const float* __restrict__ b2, int L,
                                                             const float* __restrict__ Z, int ldz,
@@ -348,7 +349,7 @@ __global__ __launch_bounds__(FWD_THREADS) void k_unfused_dh(const float* __restr
   const bool live = row < B;
   const W2Src src = w2_src(W2, b2, L);
   const int cbase[2] = {tw_col_base(lane, 0), tw_col_base(lane, 1)};
-  const float nl2 = live ? -lse[row] * LOG2E : 0.0f;
+  const float nl2 = !GIVEN && live ? -lse[row] * LOG2E : 0.0f;
   const float* zrow = Z + (size_t)(live ? row : 0) * ldz + 4 * g;
 
   f32x16 acc_o[4];
@@ -364,8 +365,10 @@ __global__ __launch_bounds__(FWD_THREADS) void k_unfused_dh(const float* __restr
       // non-temporal loads let the line go before the other three quarters
       // are read: 1.5x the bytes from HBM, measured)
       zv[q] = live ? *reinterpret_cast<const float4*>(zrow + t * OUT_TILE + 8 * q)
-                   : make_float4(-INFINITY, -INFINITY, -INFINITY, -INFINITY);
+                   : GIVEN ? make_float4(0.0f, 0.0f, 0.0f, 0.0f)
+                           : make_float4(-INFINITY, -INFINITY, -INFINITY, -INFINITY);
   };
+  auto p_of = [&](float v) { return GIVEN ? v : __builtin_amdgcn_exp2f(fmaf(v, LOG2E, nl2)); };
   // Z and W2 two tiles ahead (one ahead, a CU has 48 KB in flight, which the memory's
   // latency does not cover): the iteration of tile t uses zc, moves tile t+1 of W2 into the
   // other LDS buffer and loads tile t+3 of W2 and t+2 of Z in their places.  The last three
@@ -389,10 +392,10 @@ __global__ __launch_bounds__(FWD_THREADS) void k_unfused_dh(const float* __restr
     float p[16];
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
-      p[4 * q + 0] = __builtin_amdgcn_exp2f(fmaf(zc[q].x, LOG2E, nl2));
-      p[4 * q + 1] = __builtin_amdgcn_exp2f(fmaf(zc[q].y, LOG2E, nl2));
-      p[4 * q + 2] = __builtin_amdgcn_exp2f(fmaf(zc[q].z, LOG2E, nl2));
-      p[4 * q + 3] = __builtin_amdgcn_exp2f(fmaf(zc[q].w, LOG2E, nl2));
+      p[4 * q + 0] = p_of(zc[q].x);
+      p[4 * q + 1] = p_of(zc[q].y);
+      p[4 * q + 2] = p_of(zc[q].z);
+      p[4 * q + 3] = p_of(zc[q].w);
     }
     if constexpr (LEFT >= 2) load_z(t + 2, zc);
     Fr pf[NCH];
@@ -477,13 +480,143 @@ hipError_t launch_unfused_dh(bool use_bf16, const float* W2, const float* b2, in
   const int RB = out_rows_per_block(use_bf16);
   const dim3 grid(s_eff * ((B + RB - 1) / RB)), block(FWD_THREADS);
   if (use_bf16)
-    hipLaunchKernelGGL(k_unfused_dh<true>, grid, block, 0, st, W2, b2, L, Z, ldz, lse, B, tps, n_tiles, s_eff,
+    hipLaunchKernelGGL((k_unfused_dh<true, false>), grid, block, 0, st, W2, b2, L, Z, ldz, lse, B, tps, n_tiles, s_eff,
                        o_part, ld_part);
   else
-    hipLaunchKernelGGL(k_unfused_dh<false>, grid, block, 0, st, W2, b2, L, Z, ldz, lse, B, tps, n_tiles, s_eff,
+    hipLaunchKernelGGL((k_unfused_dh<false, false>), grid, block, 0, st, W2, b2, L, Z, ldz, lse, B, tps, n_tiles, s_eff,
                        o_part, ld_part);
   hipLaunchKernelGGL(k_dh_combine, dim3(B), dim3(HID * DHC_GROUPS), 0, st, o_part, ld_part, s_eff, W2, L, y, rw,
                      A, 1.0f / (float)B, dA);
+  return hipGetLastError();
+}
+
+// ---------------------------------------------------------------------------
+// The backward from a stored gradient of the logits.
+// ---------------------------------------------------------------------------
+// dA = (sum of the splits' dZ W2) where A > 0, splits summed as k_dh_combine does.
+__global__ __launch_bounds__(HID * DHC_GROUPS) void k_stored_dh_sum(const float* __restrict__ o_part, int ld_part,
+                                                                    int splits, const float* __restrict__ A,
+                                                                    float* __restrict__ dA) {
+  __shared__ float part[DHC_GROUPS][HID];
+  const int row = blockIdx.x, j = threadIdx.x % HID, grp = threadIdx.x / HID;
+  float og = 0.0f;
+  for (int k = grp; k < splits; k += DHC_GROUPS) og += o_part[((size_t)k * ld_part + row) * HID + j];
+  part[grp][j] = og;
+  __syncthreads();
+  if (grp) return;
+  float o = part[0][j];
+#pragma unroll
+  for (int c = 1; c < DHC_GROUPS; ++c) o += part[c][j];
+  dA[(size_t)row * HID + j] = A[(size_t)row * HID + j] > 0.0f ? o : 0.0f;
+}
+
+hipError_t launch_stored_dh(bool use_bf16, const float* W2, const float* b2, int L, const float* dZ, int ldz, int B,
+                            int splits, float* o_part, int ld_part, const float* A, float* dA, hipStream_t st) {
+  const int n_tiles = (L + OUT_TILE - 1) / OUT_TILE;
+  if (ldz < n_tiles * OUT_TILE) return hipErrorInvalidValue;
+  const int tps = (n_tiles + splits - 1) / splits;
+  const int s_eff = (n_tiles + tps - 1) / tps;
+  const int RB = out_rows_per_block(use_bf16);
+  const dim3 grid(s_eff * ((B + RB - 1) / RB)), block(FWD_THREADS);
+  if (use_bf16)
+    hipLaunchKernelGGL((k_unfused_dh<true, true>), grid, block, 0, st, W2, b2, L, dZ, ldz, (const float*)nullptr, B,
+                       tps, n_tiles, s_eff, o_part, ld_part);
+  else
+    hipLaunchKernelGGL((k_unfused_dh<false, true>), grid, block, 0, st, W2, b2, L, dZ, ldz, (const float*)nullptr, B,
+                       tps, n_tiles, s_eff, o_part, ld_part);
+  hipLaunchKernelGGL(k_stored_dh_sum, dim3(B), dim3(HID * DHC_GROUPS), 0, st, o_part, ld_part, s_eff, A, dA);
+  return hipGetLastError();
+}
+
+// H1T [128 x ld_t] from H1 [rows x 128], 64 rows per workgroup.
+__global__ __launch_bounds__(256) void k_transpose_h(const bf16* __restrict__ H1, bf16* __restrict__ H1T, int ld_t) {
+  __shared__ bf16 t[64][HID + 2];
+  const int r0 = (int)blockIdx.x * 64;
+  for (int i = threadIdx.x; i < 64 * HID; i += 256) t[i / HID][i % HID] = H1[(size_t)r0 * HID + i];
+  __syncthreads();
+  for (int i = threadIdx.x; i < 64 * HID; i += 256) H1T[(size_t)(i / 64) * ld_t + r0 + i % 64] = t[i % 64][i / 64];
+}
+
+// dW2 = dZ^T H1 for the 32 labels of one wave, rows as the product's inner index: lane (g, n)
+// reads label n of the rows that its group holds (whole 128-byte runs of a row of dZ per 32 lanes), rounds them
+// to the operand type, and the accumulator holds W2's own layout, hidden units across the
+// lanes.  b2's gradient is summed from the unrounded values, in row order per group.
+constexpr int WG_THREADS = 256;
+template <bool BF16>
+__global__ __launch_bounds__(WG_THREADS) void k_stored_wgrad(float* __restrict__ W2, float* __restrict__ b2, int L,
+                                                             const float* __restrict__ dZ, int ldz,
+                                                             const typename Mma<BF16>::elem* __restrict__ H,
+                                                             int ld_t, int B, float lr) {
+  using M = Mma<BF16>;
+  constexpr int KL = M::KL;  // rows per lane and product
+  const int lane = threadIdx.x & 63, g = lane >> 5, n = lane & 31;
+  const int tile = (int)blockIdx.x * (WG_THREADS / 64) + (int)(threadIdx.x >> 6);
+  if (tile * OUT_TILE >= L) return;
+  const int label = tile * OUT_TILE + n;  // (dZ's rows reach past L: ldz covers whole tiles)
+  f32x16 acc[4];
+#pragma unroll
+  for (int hb = 0; hb < 4; ++hb)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) acc[hb][r] = 0.0f;
+  float db = 0.0f;
+  for (int i0 = 0; i0 < B; i0 += M::KC) {
+    float d[KL];
+#pragma unroll
+    for (int j = 0; j < KL; ++j) {
+      const int i = i0 + KL * g + j;
+      d[j] = i < B ? dZ[(size_t)i * ldz + label] : 0.0f;
+      db += d[j];
+    }
+    if constexpr (BF16) {
+      bf16x8 a;
+#pragma unroll
+      for (int j = 0; j < KL; ++j) a[j] = (bf16)d[j];
+#pragma unroll
+      for (int hb = 0; hb < 4; ++hb) {
+        const bf16x8 b = *reinterpret_cast<const bf16x8*>(H + (size_t)(32 * hb + n) * ld_t + i0 + KL * g);
+        acc[hb] = M::mma(a, b, acc[hb]);
+      }
+    } else {
+      const int i = i0 + g;
+#pragma unroll
+      for (int hb = 0; hb < 4; ++hb) acc[hb] = M::mma(d[0], i < B ? H[(size_t)i * HID + 32 * hb + n] : 0.0f, acc[hb]);
+    }
+  }
+  db += __shfl_xor(db, 32);
+  if (g == 0 && label < L) b2[label] = fmaf(-lr, db, b2[label]);
+#pragma unroll
+  for (int hb = 0; hb < 4; ++hb)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      const int l = tile * OUT_TILE + 8 * (r >> 2) + 4 * g + (r & 3);
+      if (l < L) {
+        float* w = W2 + (size_t)l * HID + 32 * hb + n;
+        *w = fmaf(-lr, acc[hb][r], *w);
+      }
+    }
+}
+
+hipError_t launch_stored_wgrad(bool use_bf16, float* W2, float* b2, int L, const float* dZ, int ldz, const void* H1,
+                               void* H1T, int ld_t, int rows_pad, int B, float lr, hipStream_t st) {
+  const int n_tiles = (L + OUT_TILE - 1) / OUT_TILE, rt = (B + 63) / 64 * 64;
+  if (ldz < n_tiles * OUT_TILE || rt > ld_t || rt > rows_pad) return hipErrorInvalidValue;
+  const dim3 grid((n_tiles + WG_THREADS / 64 - 1) / (WG_THREADS / 64)), block(WG_THREADS);
+  if (use_bf16) {
+    hipLaunchKernelGGL(k_transpose_h, dim3(rt / 64), dim3(256), 0, st, (const bf16*)H1, (bf16*)H1T, ld_t);
+    hipLaunchKernelGGL(k_stored_wgrad<true>, grid, block, 0, st, W2, b2, L, dZ, ldz, (const bf16*)H1T, ld_t, B, lr);
+  } else {
+    hipLaunchKernelGGL(k_stored_wgrad<false>, grid, block, 0, st, W2, b2, L, dZ, ldz, (const float*)H1, ld_t, B, lr);
+  }
+  return hipGetLastError();
+}
+
+__global__ __launch_bounds__(256) void k_to_bf16(const float* __restrict__ in, bf16* __restrict__ out, int64_t n) {
+  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (i < n) out[i] = (bf16)in[i];
+}
+
+hipError_t launch_to_bf16(const float* in, void* out, int64_t n, hipStream_t st) {
+  hipLaunchKernelGGL(k_to_bf16, dim3((unsigned)((n + 255) / 256)), dim3(256), 0, st, in, (bf16*)out, n);
   return hipGetLastError();
 }
 

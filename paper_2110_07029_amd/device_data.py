@@ -1,4 +1,5 @@
-"""Device-resident CSR datasets whose batches are zero-copy row slices.
+"""Device-resident CSR datasets whose batches are zero-copy row slices, and torch
+tensors as the library's dense arguments.
 
 The whole synthetic dataset is staged once in HBM (torch tensors are used only
 as device memory); a batch handed to the library is a pointer into the
@@ -6,9 +7,11 @@ dataset's indptr plus the host's nnz count for that slice.
 """
 from __future__ import annotations
 
+import ctypes
+
 import numpy as np
 
-from ._binding import asgd_csr
+from ._binding import ASGD_BF16, ASGD_F16, ASGD_F32, asgd_csr, asgd_fp4, asgd_logit_rules, asgd_matrix
 
 
 class DeviceCSR:
@@ -36,3 +39,41 @@ class DeviceCSR:
 
     def nnz(self, r0: int, r1: int) -> int:
         return int(self.indptr_host[r1] - self.indptr_host[r0])
+
+
+_TYPES = {"torch.float32": ASGD_F32, "torch.bfloat16": ASGD_BF16, "torch.float16": ASGD_F16}
+
+
+def matrix(t) -> asgd_matrix:
+    """A 2-d tensor (unit stride along a row) as an asgd_matrix; the tensor must outlive its use."""
+    if t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1):
+        raise ValueError("a matrix needs two dimensions and unit stride along a row")
+    dtype = _TYPES.get(str(t.dtype))
+    if dtype is None:
+        raise ValueError(f"no matrix of {t.dtype}")
+    rows, cols = t.shape
+    return asgd_matrix(rows, cols, t.stride(0) if rows > 1 else max(cols, 1), dtype, t.data_ptr())
+
+
+def fp4_matrix(codes, scales) -> asgd_fp4:
+    """uint8 tensors, codes [rows, cols / 2] and scales [rows, cols / 32], as an asgd_fp4."""
+    rows, half = codes.shape
+    if str(codes.dtype) != "torch.uint8" or str(scales.dtype) != "torch.uint8" or half % 16:
+        raise ValueError("codes and scales are uint8, codes with a multiple of 16 columns")
+    if tuple(scales.shape) != (rows, half // 16) or not (codes.is_contiguous() and scales.is_contiguous()):
+        raise ValueError("codes [rows, cols / 2] and scales [rows, cols / 32] must be contiguous")
+    return asgd_fp4(rows, 2 * half, codes.data_ptr(), scales.data_ptr())
+
+
+def logit_rules(bias=None, allowed=None, seen=None, repetition: float = 1.0, frequency: float = 0.0,
+                presence: float = 0.0, row_bias=None) -> asgd_logit_rules:
+    """Rules from tensors (bias: float32 [L]; allowed: int32 / uint32 words, [rows, words] or
+    [words] for one mask for all rows) and asgd_csr lists."""
+    ld = 0 if allowed is None or allowed.dim() == 1 else allowed.stride(0) if allowed.shape[0] > 1 else allowed.shape[1]
+    r = asgd_logit_rules(None if bias is None else bias.data_ptr(), None if allowed is None else allowed.data_ptr(), ld,
+                         None, None, repetition, frequency, presence)
+    if seen is not None:
+        r.seen = ctypes.pointer(seen)
+    if row_bias is not None:
+        r.row_bias = ctypes.pointer(row_bias)
+    return r
