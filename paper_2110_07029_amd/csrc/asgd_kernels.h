@@ -255,6 +255,7 @@ struct RankRules {
 constexpr int RANK_MAX_K = 64;
 struct RankShape {
   int splits;  // pieces per row
+  int ranges;  // ranges of listed labels per row at most
 };
 RankShape rank_shape(int rows, int cols);
 size_t rank_ws_bytes(const RankShape& sh, int rows, int k);

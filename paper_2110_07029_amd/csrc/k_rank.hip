@@ -4,15 +4,24 @@
 // its waves keeps the 64 best (score, label) pairs that it has met, one per
 // lane in descending order, as 64-bit keys: the score's bits in an order that
 // integers share, above the label's complement, so that one comparison ranks by
-// score and then by smaller label, and 0 is below every label.  A label passes
-// if its key is above the wave's k-th; those that pass gather in LDS, and 64 of
-// them at a time are sorted across the lanes and merged into the list.  The lists of
-// the waves are merged in LDS, those of a row's pieces by k_rank_join.
+// score and then by smaller label, and 0 is below every label.  A lane's largest score of
+// a round of loads is compared with the k-th best so far (of any wave of the
+// workgroup); only a round that has something above it looks at its labels one by
+// one.  Those gather in LDS, are sorted across the lanes 64 at a time, and merge into the list.
+// The first round starts from the k-th largest of its lanes' maxima, so that few of its labels
+// pass.  The lists of the waves are merged in LDS, those of a row's pieces by k_rank_join.
+// A label that is not ranked (not allowed, NaN) carries a NaN through the arithmetic, which
+// maxima and comparisons leave out.
 //
-// Penalties touch few labels: the occurrences of a row's `seen` ids are counted
-// in LDS (integers: any order gives the same count) for SUB columns at a time, as are the last entries of row_bias,
-// and labels that neither list names take none of that arithmetic.
+// Penalties touch few labels.  The pieces skip every label that `seen` or `row_bias`
+// name (one bit per column in LDS), and more workgroups per row, each with a range of labels, look only at those: a
+// hash table in LDS counts occurrences (integers: any order gives the same count), keeps
+// the last row_bias entry and the first entry that names a label, and that entry's thread
+// forms the label's score in float64, so sums follow the lists' order.  A range with more
+// labels than the table holds is counted 1,024 columns at a time.
 #include <math.h>
+
+#include <algorithm>
 
 #include "asgd_dev.h"
 #include "asgd_kernels.h"
@@ -24,8 +33,12 @@ namespace {
 
 constexpr int RK_THREADS = 256;
 constexpr int RK_WAVES = RK_THREADS / 64;
-constexpr int RK_U = 2;       // vectors per lane and round
-constexpr int RK_SUB = 4096;  // columns whose penalties are in LDS at a time
+constexpr int RK_U = 2;            // vectors per lane and round
+constexpr int RK_BITS = 1 << 16;   // columns of a piece at most where lists are given
+constexpr int RK_SLOTS = 1024;     // the table of listed labels
+constexpr int RK_PROBES = 32;
+constexpr int RK_RANGES = 32;     // ranges of listed labels per row at most
+constexpr int RK_WGS = 1024;      // workgroups wanted
 constexpr int RK_NONE = 0x7fffffff;
 
 // Bits of a float in an order that unsigned integers share; every number's is above 0.
@@ -38,46 +51,83 @@ __device__ __forceinline__ float of_order(unsigned o) {
 }
 __device__ __forceinline__ u64 key_of(float v, int label) { return ((u64)order_of(v) << 32) | (unsigned)~label; }
 
-__device__ __forceinline__ u64 swap_lanes(u64 v, int x) { return __shfl_xor(v, x); }
-
-// Sorts the lanes' keys in descending order.
-__device__ __forceinline__ u64 sort64(u64 v, int lane) {
-#pragma unroll
-  for (int size = 2; size <= 64; size *= 2)
-#pragma unroll
-    for (int d = size / 2; d >= 1; d /= 2) {
-      const u64 o = swap_lanes(v, d);
-      const bool big = ((lane & d) == 0) == ((lane & size) == 0);
-      v = (o > v) == big ? o : v;
-    }
-  return v;
+// v of lane ^ X, without a trip through LDS.
+template <int CTRL>
+__device__ __forceinline__ unsigned dpp(unsigned v) {
+  return (unsigned)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, 0xf, 0xf, true);
 }
-
-// The 64 best of two lists in descending order.
-__device__ __forceinline__ u64 merge64(u64 a, u64 b, int lane) {
-  const u64 r = __shfl(b, 63 - lane);
-  u64 v = a > r ? a : r;
-#pragma unroll
-  for (int d = 32; d >= 1; d /= 2) {
-    const u64 o = swap_lanes(v, d);
-    v = (o > v) == ((lane & d) == 0) ? o : v;
+template <int X>
+__device__ __forceinline__ unsigned lane_xor(unsigned v, int lane) {
+  if constexpr (X == 1) return dpp<0xb1>(v);         // quad_perm [1, 0, 3, 2]
+  else if constexpr (X == 2) return dpp<0x4e>(v);    // quad_perm [2, 3, 0, 1]
+  else if constexpr (X == 4) return dpp<0x1b>(dpp<0x141>(v));  // half row mirrored (xor 7), then xor 3
+  else if constexpr (X == 8) return dpp<0x128>(v);   // row rotated by 8
+  else if constexpr (X == 16) {
+    const auto s = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+    const unsigned a = s[0], b = s[1];
+    return lane & 16 ? a : b;
+  } else {
+    const auto s = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+    const unsigned a = s[0], b = s[1];
+    return lane & 32 ? a : b;
   }
+}
+template <int X>
+__device__ __forceinline__ u64 lane_xor(u64 v, int lane) {
+  return ((u64)lane_xor<X>((unsigned)(v >> 32), lane) << 32) | lane_xor<X>((unsigned)v, lane);
+}
+__device__ __forceinline__ unsigned lane_of(unsigned v, int l) { return (unsigned)__builtin_amdgcn_readlane((int)v, l); }
+__device__ __forceinline__ u64 lane_of(u64 v, int l) {
+  return ((u64)lane_of((unsigned)(v >> 32), l) << 32) | lane_of((unsigned)v, l);
+}
+
+// One step of a bitonic network over the lanes, D apart, in runs of SIZE that alternate
+// between descending and ascending.
+template <int D, int SIZE, typename K>
+__device__ __forceinline__ K bitonic_step(K v, int lane) {
+  const K o = lane_xor<D>(v, lane);
+  const bool big = ((lane & D) == 0) == ((lane & SIZE) == 0);
+  return (o > v) == big ? o : v;
+}
+template <int D, int SIZE, typename K>
+__device__ __forceinline__ K bitonic_merge(K v, int lane) {
+  v = bitonic_step<D, SIZE>(v, lane);
+  if constexpr (D > 1) v = bitonic_merge<D / 2, SIZE>(v, lane);
   return v;
 }
+// Sorts the lanes' keys in descending order.
+template <typename K>
+__device__ __forceinline__ K sort64(K v, int lane) {
+  v = bitonic_merge<1, 2>(v, lane);
+  v = bitonic_merge<2, 4>(v, lane);
+  v = bitonic_merge<4, 8>(v, lane);
+  v = bitonic_merge<8, 16>(v, lane);
+  v = bitonic_merge<16, 32>(v, lane);
+  return bitonic_merge<32, 64>(v, lane);
+}
+
+// The 64 best of two lists, the second one in ascending order.
+__device__ __forceinline__ u64 merge64(u64 a, u64 r, int lane) {
+  return bitonic_merge<32, 64>(a > r ? a : r, lane);
+}
+__device__ __forceinline__ u64 reverse64(u64 v, int lane) { return __shfl(v, 63 - lane); }
 
 struct Best {
-  u64 list;  // lane i: the i-th best
-  u64 least;  // the k-th best
-  int n;     // keys waiting in buf
-  u64* buf;  // LDS, 128 keys of this wave
+  u64 list;   // lane i: the i-th best
+  u64 least;  // the k-th best; keys up to it need not be looked at
+  int n;      // keys waiting in buf
+  u64* buf;   // LDS, 128 keys of this wave
+  u64* shared;  // LDS, the largest `least` of the workgroup's waves
 
   __device__ void flush(int lane, int k, int count) {
     __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "wavefront");
     const u64 v = lane < count ? buf[n - count + lane] : 0;
     __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "wavefront");
     n -= count;
-    list = merge64(list, sort64(v, lane), lane);
-    least = __shfl(list, k - 1);
+    list = merge64(list, reverse64(sort64(v, lane), lane), lane);
+    const u64 kth = lane_of(list, k - 1);
+    least = kth > least ? kth : least;
+    if (lane == 0) atomicMax(shared, least);
   }
   // All lanes call it; key 0 never passes.
   __device__ void offer(u64 key, int lane, int k) {
@@ -87,6 +137,20 @@ struct Best {
     if (in) buf[n + __builtin_amdgcn_mbcnt_hi((unsigned)(who >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)who, 0))] = key;
     n += __popcll(who);
     if (n >= 64) flush(lane, k, 64);
+  }
+  // Enough keys wait to raise the bound: after k of them about half of what passes no longer would.
+  __device__ void settle(int lane, int k) {
+    if (n >= max(k, 8)) flush(lane, k, n);
+  }
+  // Scores below it do not pass.
+  __device__ float bound() const {
+    const unsigned o = (unsigned)(least >> 32);
+    return o > 0x007fffffu ? of_order(o) : -INFINITY;  // (0x007fffff: -inf)
+  }
+  __device__ void look() {
+    const u64 o = *(volatile u64*)shared;
+    const u64 t = lane_of(o, 0);
+    least = t > least ? t : least;
   }
 };
 
@@ -112,91 +176,245 @@ __device__ __forceinline__ float lse_of(float m, float s) {
   return m + __builtin_amdgcn_logf(s) * LN2;
 }
 
+// The lists of the waves of a workgroup as one, on wave 0; likewise (m, s).
+__device__ __forceinline__ bool gather_waves(Best& best, float& m, float& s, u64 (*lists)[128], float2* red, int lane,
+                                             int wave) {
+#pragma unroll
+  for (int o = 32; o >= 1; o >>= 1) soft_merge(m, s, __shfl_xor(m, o), __shfl_xor(s, o), LOG2E);
+  if (lane == 0) red[wave] = make_float2(m, s);
+  lists[wave][63 - lane] = best.list;
+  __syncthreads();
+  if (wave) return false;
+  for (int w = 1; w < RK_WAVES; ++w) {
+    best.list = merge64(best.list, lists[w][lane], lane);
+    soft_merge(m, s, red[w].x, red[w].y, LOG2E);
+  }
+  return true;
+}
+
+struct Table {
+  int id[RK_SLOTS], count[RK_SLOTS], last[RK_SLOTS], first[RK_SLOTS];
+};
+
+__device__ __forceinline__ unsigned slot_of(int id) { return ((unsigned)id * 2654435761u) >> 22; }
+// The slot that holds id (put there if absent), or -1 after RK_PROBES others.
+__device__ __forceinline__ int table_put(Table& t, int id) {
+  unsigned h = slot_of(id);
+  for (int p = 0; p < RK_PROBES; ++p, h = (h + 1) & (RK_SLOTS - 1)) {
+    const int was = atomicCAS(&t.id[h], -1, id);
+    if (was == -1 || was == id) return (int)h;
+  }
+  return -1;
+}
+
+// Score of a label that the row's lists name: n occurrences in seen, and the last of the
+// row_bias entries from b0 on (1-based, 0: none).  NaN if it is not ranked.
 template <typename T>
+__device__ __forceinline__ float listed_score(const T* zrow, const RankRules& ru, const uint32_t* mask, int id, int n,
+                                              int last, int b0) {
+  if (mask && !((mask[id >> 5] >> (id & 31)) & 1)) return NAN;
+  double t = (double)(float)zrow[id];
+  if (n) t = (t > 0.0 ? t / ru.repetition : t * ru.repetition) - ru.frequency * (double)n - ru.presence;
+  if (ru.bias) t += (double)ru.bias[id];
+  if (last) t += (double)ru.row_bias.values[b0 + last - 1];
+  return (float)t + 0.0f;
+}
+
+// The listed labels in [lo, hi).
+template <typename T>
+__device__ void rank_listed(const T* zrow, const RankRules& ru, const uint32_t* mask, int lo, int hi, int s0, int s1,
+                            int b0, int b1, int k, Table& t, int* overflow, Best& best, float& m, float& s, int lane) {
+  const int tid = threadIdx.x, ns = s1 - s0, n = ns + (b1 - b0);
+  auto entry = [&](int i) {
+    const int id = i < ns ? ru.seen.indices[s0 + i] : ru.row_bias.indices[b0 + i - ns];
+    return id >= lo && id < hi ? id : -1;
+  };
+  auto take = [&](float v, int id) {
+    best.offer(v == v ? key_of(v, id) : 0, lane, k);
+    if (v == v) soft_merge(m, s, v, 1.0f, LOG2E);
+  };
+  for (int i = tid; i < RK_SLOTS; i += RK_THREADS) {
+    t.id[i] = -1;
+    t.count[i] = t.last[i] = 0;
+    t.first[i] = n;
+  }
+  if (tid == 0) *overflow = 0;
+  __syncthreads();
+  for (int i = tid; i < n; i += RK_THREADS) {
+    const int id = entry(i);
+    if (id < 0) continue;
+    const int h = table_put(t, id);
+    if (h < 0) {
+      *overflow = 1;
+      break;
+    }
+    atomicMin(&t.first[h], i);
+    if (i < ns)
+      atomicAdd(&t.count[h], 1);
+    else
+      atomicMax(&t.last[h], i - ns + 1);
+  }
+  __syncthreads();
+  if (!*overflow) {
+    for (int i0 = 0; i0 < n; i0 += RK_THREADS) {
+      const int i = i0 + tid, id = i < n ? entry(i) : -1;
+      float v = NAN;
+      if (id >= 0) {
+        unsigned h = slot_of(id);
+        while (t.id[h] != id) h = (h + 1) & (RK_SLOTS - 1);  // (it is there)
+        if (t.first[h] == i) v = listed_score(zrow, ru, mask, id, t.count[h], t.last[h], b0);
+      }
+      take(v, id);
+    }
+    return;
+  }
+  for (int c0 = lo; c0 < hi; c0 += RK_SLOTS) {
+    __syncthreads();
+    for (int i = tid; i < RK_SLOTS; i += RK_THREADS) t.count[i] = t.last[i] = 0;
+    __syncthreads();
+    for (int i = tid; i < n; i += RK_THREADS) {
+      const int id = entry(i);
+      if (id < 0 || (unsigned)(id - c0) >= (unsigned)RK_SLOTS) continue;
+      if (i < ns)
+        atomicAdd(&t.count[id - c0], 1);
+      else
+        atomicMax(&t.last[id - c0], i - ns + 1);
+    }
+    __syncthreads();
+    for (int i = tid; i < RK_SLOTS; i += RK_THREADS) {
+      const int c = t.count[i], l = t.last[i];
+      take(c | l ? listed_score(zrow, ru, mask, c0 + i, c, l, b0) : NAN, c0 + i);
+    }
+  }
+}
+
+template <int N>
+struct __attribute__((packed, aligned(4))) Floats {
+  float v[N];
+};
+
+// Workgroup = (piece, row): `splits` pieces of columns and, with LISTS, `ranges` ranges of
+// listed labels.
+template <typename T, bool LISTS>
 __global__ __launch_bounds__(RK_THREADS) void k_rank(const T* __restrict__ z, int64_t ld, int L, RankRules ru, int k,
-                                                     int splits, int vec_split, u64* __restrict__ part,
+                                                     int splits, int ranges, int vec_split, u64* __restrict__ part,
                                                      float2* __restrict__ part_ms, int32_t* __restrict__ ids,
                                                      float* __restrict__ scores, float* __restrict__ lse) {
   using R = Row<T>;
-  constexpr int V = R::V;
-  constexpr int SUBV = RK_SUB / V;
+  constexpr int V = R::V, ROUND = RK_THREADS * RK_U;
+  constexpr unsigned ALL = (1u << V) - 1;
   __shared__ u64 buf[RK_WAVES][128];
   __shared__ float2 red[RK_WAVES];
-  extern __shared__ int touched[];  // counts [RK_SUB], then last row_bias entries [RK_SUB]
-  int* const count = touched;
-  int* const last = touched + RK_SUB;
+  __shared__ u64 shared_least;
+  __shared__ union Lists {
+    unsigned bits[LISTS ? RK_BITS / 32 + 1 : 1];
+    char table[LISTS ? sizeof(Table) : 1];
+  } in;
+  __shared__ int overflow;
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int row = blockIdx.x / splits, split = blockIdx.x % splits;
+  const int parts = splits + ranges;
+  const int row = blockIdx.x / parts, piece = blockIdx.x % parts;
   const R zr(const_cast<T*>(z), ld, row, L);
-  const int v0 = split * vec_split, v1 = min(zr.n_vec, v0 + vec_split);
   const uint32_t* mask = ru.allowed ? ru.allowed + (int64_t)row * ru.allowed_ld : nullptr;
   const int words = (L + 31) >> 5;
-  int s0 = 0, s1 = 0, b0 = 0, b1 = 0;
-  if (ru.seen.indptr) list_range(ru.seen, row, &s0, &s1);
-  if (ru.row_bias.indptr) list_range(ru.row_bias, row, &b0, &b1);
-  const bool lists = s1 > s0 || b1 > b0;
-
-  Best best{0, 0, 0, buf[wave]};
+  Best best{0, 0, 0, buf[wave], &shared_least};
   float m = -INFINITY, s = 0.0f;
-  for (int w0 = v0; w0 < v1; w0 += SUBV) {
-    const int w1 = min(v1, w0 + SUBV), c0 = zr.col(w0);
+  if (threadIdx.x == 0) shared_least = 0;
+
+  int s0 = 0, s1 = 0, b0 = 0, b1 = 0;
+  bool lists = false;
+  if constexpr (LISTS) {
+    if (ru.seen.indptr) list_range(ru.seen, row, &s0, &s1);
+    if (ru.row_bias.indptr) list_range(ru.row_bias, row, &b0, &b1);
+    lists = s1 > s0 || b1 > b0;
+  }
+  if (LISTS && piece >= splits) {
+    const int width = (L + ranges - 1) / ranges, lo = (piece - splits) * width;
+    __syncthreads();
+    if (lists)
+      rank_listed(zr.base + zr.phase, ru, mask, lo, min(L, lo + width), s0, s1, b0, b1, k,
+                  *reinterpret_cast<Table*>(in.table), &overflow, best, m, s, lane);
+  } else {
+    const int v0 = piece * vec_split, v1 = max(v0, min(zr.n_vec, v0 + vec_split)), c0 = zr.col(v0);
     if (lists) {
+      for (int i = threadIdx.x; i <= RK_BITS / 32; i += RK_THREADS) in.bits[i] = 0;
       __syncthreads();
-      for (int i = threadIdx.x; i < 2 * RK_SUB; i += RK_THREADS) touched[i] = 0;
-      __syncthreads();
+      const unsigned width = (unsigned)(v1 - v0) * V;
       for (int q = s0 + (int)threadIdx.x; q < s1; q += RK_THREADS) {
-        const int id = ru.seen.indices[q];
-        if (id >= 0 && id < L && (unsigned)(id - c0) < (unsigned)RK_SUB) atomicAdd(&count[id - c0], 1);
+        const unsigned c = (unsigned)(ru.seen.indices[q] - c0);
+        if (c < width) atomicOr(&in.bits[c >> 5], 1u << (c & 31));
       }
       for (int q = b0 + (int)threadIdx.x; q < b1; q += RK_THREADS) {
-        const int id = ru.row_bias.indices[q];
-        if (id >= 0 && id < L && (unsigned)(id - c0) < (unsigned)RK_SUB) atomicMax(&last[id - c0], q - b0 + 1);
+        const unsigned c = (unsigned)(ru.row_bias.indices[q] - c0);
+        if (c < width) atomicOr(&in.bits[c >> 5], 1u << (c & 31));
       }
-      __syncthreads();
     }
-    for (int base = w0; base < w1; base += RK_THREADS * RK_U) {
-      float x[RK_U][V];
-      unsigned ok[RK_U];
+    __syncthreads();
+    // a round of loads: the logits and biases of the columns to look at
+    typename R::vec x[RK_U];
+    Floats<V> bias[RK_U];
+    unsigned ok[RK_U];
+    auto load = [&](int base) {
 #pragma unroll
       for (int u = 0; u < RK_U; ++u) {
-        const int i = base + u * RK_THREADS + (int)threadIdx.x;
-        ok[u] = i < w1 ? zr.in_row(i) : 0;
-        if (mask && ok[u]) ok[u] &= mask_bits(mask, words, zr.col(i), V);
-        if (ok[u]) zr.load(i, ok[u], x[u]);
+        const int i = base + u * RK_THREADS + (int)threadIdx.x, c = zr.col(i);
+        const unsigned in_row = i < v1 ? zr.in_row(i) : 0;
+        unsigned o = in_row;
+        if (mask && o) o &= mask_bits(mask, words, c, V);
+        if (LISTS && lists && o) o &= ~(in.bits[(i - v0) * V >> 5] >> ((i - v0) * V & 31));
+        ok[u] = o;
+        if (!o) continue;
+        if (in_row == ALL) {
+          x[u] = __builtin_nontemporal_load(reinterpret_cast<const typename R::vec*>(zr.base + (int64_t)V * i));
+          if (ru.bias) bias[u] = *reinterpret_cast<const Floats<V>*>(ru.bias + c);
+        } else {
+#pragma unroll
+          for (int e = 0; e < V; ++e)
+            if ((in_row >> e) & 1) {
+              x[u][e] = zr.base[(int64_t)V * i + e];
+              if (ru.bias) bias[u].v[e] = ru.bias[c + e];
+            }
+        }
       }
+    };
+    const int rounds = v1 > v0 ? (v1 - v0 + ROUND - 1) / ROUND : 0;
+    if (rounds) load(v0);
+    for (int r = 0; r < rounds; ++r) {
+      const int base = v0 + r * ROUND;
+      float w[RK_U][V];
       float mx = -INFINITY;
 #pragma unroll
       for (int u = 0; u < RK_U; ++u) {
-        const int c = zr.col(base + u * RK_THREADS + (int)threadIdx.x);
 #pragma unroll
-        for (int e = 0; e < V; ++e) {
-          const bool on = (ok[u] >> e) & 1;
-          float v = on ? x[u][e] : 0.0f;
-          // (+ 0: a negative zero ties with zero)
-          const float b = ru.bias && on ? ru.bias[c + e] : 0.0f;
-          int n = 0, l = 0;
-          if (lists && on) {
-            n = count[c + e - c0];
-            l = last[c + e - c0];
-          }
-          if (n | l) {
-            double t = v;
-            if (n) t = (t > 0.0 ? t / ru.repetition : t * ru.repetition) - ru.frequency * (double)n - ru.presence;
-            t += (double)b;
-            if (l) t += (double)ru.row_bias.values[b0 + l - 1];
-            v = (float)t + 0.0f;
-          } else {
-            v += b;
-          }
-          if (!on || v != v) {
-            ok[u] &= ~(1u << e);
-            v = -INFINITY;
-          }
-          x[u][e] = v;
-          mx = fmaxf(mx, v);
-          best.offer((ok[u] >> e) & 1 ? key_of(v, c + e) : 0, lane, k);
+        for (int e = 0; e < V; ++e) w[u][e] = (float)x[u][e] + (ru.bias ? bias[u].v[e] : 0.0f);
+        if (__ballot(ok[u] != ALL)) {
+          const int off = (int)~ok[u];
+#pragma unroll
+          for (int e = 0; e < V; ++e)
+            w[u][e] = __int_as_float(__float_as_int(w[u][e]) | (off << (31 - e) >> 31));  // a NaN
         }
+#pragma unroll
+        for (int e = 0; e < V; ++e) mx = fmaxf(mx, w[u][e]);
+      }
+      if (r + 1 < rounds) load(base + ROUND);
+      if (r == 0) {
+        const unsigned kth = lane_of(sort64(order_of(mx), lane), k - 1);
+        best.least = ((u64)kth << 32) - 1;  // (keys of that score are above it)
+        if (lane == 0) atomicMax(&shared_least, best.least);
+      }
+      best.look();
+      if (__ballot(mx >= best.bound())) {
+#pragma unroll
+        for (int u = 0; u < RK_U; ++u) {
+          const int c = zr.col(base + u * RK_THREADS + (int)threadIdx.x);
+#pragma unroll
+          for (int e = 0; e < V; ++e) {
+            const float v = w[u][e];
+            if (__ballot(v >= best.bound())) best.offer(v == v ? key_of(v, c + e) : 0, lane, k);
+          }
+        }
+        best.settle(lane, k);
       }
       if (lse) {
         if (mx > m) {
@@ -207,26 +425,14 @@ __global__ __launch_bounds__(RK_THREADS) void k_rank(const T* __restrict__ z, in
 #pragma unroll
           for (int u = 0; u < RK_U; ++u)
 #pragma unroll
-            for (int e = 0; e < V; ++e)
-              s += x[u][e] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((x[u][e] - m) * LOG2E);
+            for (int e = 0; e < V; ++e) s += __builtin_amdgcn_exp2f((fmaxf(w[u][e], -INFINITY) - m) * LOG2E);
         }
       }
     }
   }
   if (best.n) best.flush(lane, k, best.n);
-  if (lse) {
-#pragma unroll
-    for (int o = 32; o >= 1; o >>= 1) soft_merge(m, s, __shfl_xor(m, o), __shfl_xor(s, o), LOG2E);
-    if (lane == 0) red[wave] = make_float2(m, s);
-  }
-  buf[wave][lane] = best.list;
-  __syncthreads();
-  if (wave) return;
-  for (int w = 1; w < RK_WAVES; ++w) {
-    best.list = merge64(best.list, buf[w][lane], lane);
-    if (lse) soft_merge(m, s, red[w].x, red[w].y, LOG2E);
-  }
-  if (splits == 1) {
+  if (!gather_waves(best, m, s, buf, red, lane, wave)) return;
+  if (parts == 1) {
     put_best(best.list, lane, k, row, ids, scores);
     if (lse && lane == 0) lse[row] = lse_of(m, s);
   } else {
@@ -236,7 +442,7 @@ __global__ __launch_bounds__(RK_THREADS) void k_rank(const T* __restrict__ z, in
 }
 
 // Per row: the k best of its pieces' lists, and lse of their sums, in a fixed order.
-__global__ __launch_bounds__(RK_THREADS) void k_rank_join(int splits, int k, const u64* __restrict__ part,
+__global__ __launch_bounds__(RK_THREADS) void k_rank_join(int parts, int k, const u64* __restrict__ part,
                                                           const float2* __restrict__ part_ms,
                                                           int32_t* __restrict__ ids, float* __restrict__ scores,
                                                           float* __restrict__ lse) {
@@ -244,26 +450,26 @@ __global__ __launch_bounds__(RK_THREADS) void k_rank_join(int splits, int k, con
   __shared__ float2 red[RK_WAVES];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int64_t row = blockIdx.x;
-  const int n = splits * k;
+  const int n = parts * k;
   const u64* p = part + row * n;
   u64 list = 0, least = 0;
   for (int i = wave * 64; i < n; i += RK_THREADS) {
     const u64 v = i + lane < n ? p[i + lane] : 0;
     if (!__ballot(v > least)) continue;
-    list = merge64(list, sort64(v, lane), lane);
-    least = __shfl(list, k - 1);
+    list = merge64(list, reverse64(sort64(v, lane), lane), lane);
+    least = lane_of(list, k - 1);
   }
   float m = -INFINITY, s = 0.0f;
   if (lse) {
-    for (int i = threadIdx.x; i < splits; i += RK_THREADS) {
-      const float2 ms = part_ms[row * splits + i];
+    for (int i = threadIdx.x; i < parts; i += RK_THREADS) {
+      const float2 ms = part_ms[row * parts + i];
       soft_merge(m, s, ms.x, ms.y, LOG2E);
     }
 #pragma unroll
     for (int o = 32; o >= 1; o >>= 1) soft_merge(m, s, __shfl_xor(m, o), __shfl_xor(s, o), LOG2E);
     if (lane == 0) red[wave] = make_float2(m, s);
   }
-  buf[wave][lane] = list;
+  buf[wave][63 - lane] = list;
   __syncthreads();
   if (wave) return;
   for (int w = 1; w < RK_WAVES; ++w) {
@@ -274,24 +480,30 @@ __global__ __launch_bounds__(RK_THREADS) void k_rank_join(int splits, int k, con
   if (lse && lane == 0) lse[row] = lse_of(m, s);
 }
 
-// Pieces per row: enough workgroups to fill the GPU, each with at least one full round.
-RankShape shape_of(int rows, int cols) {
-  RankShape sh;
-  const int want = (2048 + rows - 1) / rows;
-  const int most = (cols + RK_SUB - 1) / RK_SUB;
-  sh.splits = want < most ? want : most;
-  if (sh.splits < 1) sh.splits = 1;
-  return sh;
-}
-
 }  // namespace
 
-RankShape rank_shape(int rows, int cols) { return shape_of(rows, cols); }
+// Pieces per row: enough workgroups to fill the GPU, each with at least a round of 16-bit
+// loads per wave, and no more columns than a workgroup has bits for.
+RankShape rank_shape(int rows, int cols) {
+  const int want = (RK_WGS + rows - 1) / rows, most = (cols + 2047) / 2048;
+  const int least = (cols + 8 + RK_BITS - 1) / RK_BITS;
+  return RankShape{std::max(std::min(want, most), least), std::max(1, std::min(RK_RANGES, 2048 / rows))};
+}
+
+// Ranges of listed labels per row: about 256 entries each.  (The scratch memory has room for
+// the most, whatever the lists.)
+static int rank_ranges(const RankShape& sh, const RankRules& ru, int rows) {
+  const int64_t n = (ru.seen.indptr ? ru.seen.nnz : 0) + (int64_t)(ru.row_bias.indptr ? ru.row_bias.nnz : 0);
+  if (!n) return 0;
+  return (int)std::min<int64_t>(sh.ranges, (n + 256 * (int64_t)rows - 1) / (256 * (int64_t)rows));
+}
+
+static size_t key_bytes(const RankShape& sh, int rows, int k) {
+  return ((size_t)rows * (sh.splits + sh.ranges) * k * sizeof(u64) + 255) / 256 * 256;
+}
 
 size_t rank_ws_bytes(const RankShape& sh, int rows, int k) {
-  if (sh.splits == 1) return 0;
-  const size_t keys = ((size_t)rows * sh.splits * k * sizeof(u64) + 255) / 256 * 256;
-  return keys + (size_t)rows * sh.splits * sizeof(float2);
+  return key_bytes(sh, rows, k) + (size_t)rows * (sh.splits + sh.ranges) * sizeof(float2);
 }
 
 template <typename T>
@@ -300,13 +512,19 @@ static hipError_t rank_as(const void* z, int64_t ld, int rows, int L, const Rank
   // vectors of a row of any phase, and per piece
   const int n_vec = (L + 2 * Row<T>::V - 2) / Row<T>::V;
   const int vps = (n_vec + sh.splits - 1) / sh.splits;
+  const int ranges = rank_ranges(sh, ru, rows), parts = sh.splits + ranges;
+  if (ranges && vps * Row<T>::V > RK_BITS) return hipErrorInvalidValue;
   u64* part = (u64*)ws;
-  float2* ms = (float2*)((char*)ws + ((size_t)rows * sh.splits * k * sizeof(u64) + 255) / 256 * 256);
-  const int lds = ru.seen.indptr || ru.row_bias.indptr ? 2 * RK_SUB * (int)sizeof(int) : 0;
-  hipLaunchKernelGGL(k_rank<T>, dim3((unsigned)rows * sh.splits), dim3(RK_THREADS), lds, st, (const T*)z, ld, L, ru,
-                     k, sh.splits, vps, part, ms, ids, scores, lse);
-  if (sh.splits > 1)
-    hipLaunchKernelGGL(k_rank_join, dim3(rows), dim3(RK_THREADS), 0, st, sh.splits, k, part, ms, ids, scores, lse);
+  float2* ms = (float2*)((char*)ws + key_bytes(sh, rows, k));
+  const dim3 grid((unsigned)rows * parts), block(RK_THREADS);
+  if (ranges)
+    hipLaunchKernelGGL((k_rank<T, true>), grid, block, 0, st, (const T*)z, ld, L, ru, k, sh.splits, ranges, vps, part, ms,
+                       ids, scores, lse);
+  else
+    hipLaunchKernelGGL((k_rank<T, false>), grid, block, 0, st, (const T*)z, ld, L, ru, k, sh.splits, 0, vps, part, ms, ids,
+                       scores, lse);
+  if (parts > 1)
+    hipLaunchKernelGGL(k_rank_join, dim3(rows), dim3(RK_THREADS), 0, st, parts, k, part, ms, ids, scores, lse);
   return hipGetLastError();
 }
 

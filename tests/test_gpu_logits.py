@@ -569,9 +569,11 @@ def test_memory_that_is_not_the_devices_is_refused():
     z = dev(np.zeros((2, 100), np.float32))
     ids = torch.empty((2, 1), dtype=torch.int32, device="cuda")
     on_host = torch.zeros((2, 100))
-    cases = [lambda: asgd.asgd_logits_topk(asgd.matrix(on_host), 1, ids),
-             lambda: asgd.asgd_logits_topk(asgd.matrix(z), 1, ids.cpu()),
-             lambda: asgd.asgd_logits_topk(asgd.matrix(z), 1, ids, rules=asgd.logit_rules(bias=torch.zeros(100))),
+    ws = scratch(asgd.asgd_logits_topk_workspace(2, 100, 1))
+    cases = [lambda: asgd.asgd_logits_topk(asgd.matrix(on_host), 1, ids, workspace=ws),
+             lambda: asgd.asgd_logits_topk(asgd.matrix(z), 1, ids.cpu(), workspace=ws),
+             lambda: asgd.asgd_logits_topk(asgd.matrix(z), 1, ids, rules=asgd.logit_rules(bias=torch.zeros(100)),
+                                           workspace=ws),
              lambda: asgd.asgd_distill(asgd.matrix(z), ids.cpu(), z, 1.0, z, k=1,
                                        workspace=scratch(asgd.asgd_distill_workspace(2, 100, 1))),
              lambda: asgd.asgd_distill(asgd.matrix(z), ids, z, 1.0, z, k=1, workspace=torch.zeros(1 << 16, dtype=torch.uint8)
