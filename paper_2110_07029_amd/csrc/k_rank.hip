@@ -57,7 +57,7 @@ __device__ __forceinline__ unsigned dpp(unsigned v) {
   return (unsigned)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, 0xf, 0xf, true);
 }
 template <int X>
-__device__ __forceinline__ unsigned lane_xor(unsigned v, int lane) {
+__device__ __forceinline__ unsigned lane_xor(unsigned v, int) {
   if constexpr (X == 1) return dpp<0xb1>(v);         // quad_perm [1, 0, 3, 2]
   else if constexpr (X == 2) return dpp<0x4e>(v);    // quad_perm [2, 3, 0, 1]
   else if constexpr (X == 4) return dpp<0x1b>(dpp<0x141>(v));  // half row mirrored (xor 7), then xor 3
@@ -65,11 +65,11 @@ __device__ __forceinline__ unsigned lane_xor(unsigned v, int lane) {
   else if constexpr (X == 16) {
     const auto s = __builtin_amdgcn_permlane16_swap(v, v, false, false);
     const unsigned a = s[0], b = s[1];
-    return lane & 16 ? a : b;
+    return __builtin_amdgcn_inverse_ballot_w64(0xffff0000ffff0000ull) ? a : b;
   } else {
     const auto s = __builtin_amdgcn_permlane32_swap(v, v, false, false);
     const unsigned a = s[0], b = s[1];
-    return lane & 32 ? a : b;
+    return __builtin_amdgcn_inverse_ballot_w64(0xffffffff00000000ull) ? a : b;
   }
 }
 template <int X>
@@ -81,12 +81,20 @@ __device__ __forceinline__ u64 lane_of(u64 v, int l) {
   return ((u64)lane_of((unsigned)(v >> 32), l) << 32) | lane_of((unsigned)v, l);
 }
 
-// One step of a bitonic network over the lanes, D apart, in runs of SIZE that alternate
-// between descending and ascending.
+// Bit l: of lanes l and l ^ D, l keeps the larger key, in runs of SIZE that alternate between
+// descending and ascending.
+constexpr u64 keeps_larger(int D, int SIZE) {
+  u64 b = 0;
+  for (int l = 0; l < 64; ++l) b |= (u64)(((l & D) == 0) == ((l & SIZE) == 0)) << l;
+  return b;
+}
+// One step of a bitonic network over the lanes, D apart.  (The lanes' roles as a constant: as
+// comparisons of the lane they would take a scalar register pair each through the whole kernel.)
 template <int D, int SIZE, typename K>
 __device__ __forceinline__ K bitonic_step(K v, int lane) {
   const K o = lane_xor<D>(v, lane);
-  const bool big = ((lane & D) == 0) == ((lane & SIZE) == 0);
+  constexpr u64 KEEPS = keeps_larger(D, SIZE);
+  const bool big = __builtin_amdgcn_inverse_ballot_w64(KEEPS);
   return (o > v) == big ? o : v;
 }
 template <int D, int SIZE, typename K>
@@ -112,56 +120,88 @@ __device__ __forceinline__ u64 merge64(u64 a, u64 r, int lane) {
 }
 __device__ __forceinline__ u64 reverse64(u64 v, int lane) { return __shfl(v, 63 - lane); }
 
+// What the waves of a workgroup have found, in LDS: k labels of a wave are as good as `kth`,
+// ceil(k / waves) as good as `part`.  So the workgroup's k-th best is at least the largest
+// kth and the smallest part, and labels below that need not be looked at by any wave.
+template <int WAVES>
+struct Found {
+  u64 kth[WAVES], part[WAVES];
+};
+
 struct Best {
   u64 list;   // lane i: the i-th best
-  u64 least;  // the k-th best; keys up to it need not be looked at
+  u64 least;  // keys up to it need not be looked at
+  u64 part;   // what this wave published
   int n;      // keys waiting in buf
   u64* buf;   // LDS, 128 keys of this wave
-  u64* shared;  // LDS, the largest `least` of the workgroup's waves
 
-  __device__ void flush(int lane, int k, int count) {
+  // Appends the lanes' keys that are above the bound (0 never is): at most 64 more.
+  __device__ void append(u64 key) {
+    const bool in = key > least;
+    const u64 who = __ballot(in);
+    if (in) buf[n + __builtin_amdgcn_mbcnt_hi((unsigned)(who >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)who, 0))] = key;
+    n += __popcll(who);
+  }
+  // Takes up to 64 waiting keys into the list.
+  __device__ void flush(int lane) {
+    const int count = min(n, 64);
     __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "wavefront");
     const u64 v = lane < count ? buf[n - count + lane] : 0;
     __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "wavefront");
     n -= count;
     list = merge64(list, reverse64(sort64(v, lane), lane), lane);
-    const u64 kth = lane_of(list, k - 1);
+  }
+  template <int WAVES>
+  __device__ void publish(Found<WAVES>& f, u64 kth, u64 p, int lane, int wave) {
     least = kth > least ? kth : least;
-    if (lane == 0) atomicMax(shared, least);
+    part = p > part ? p : part;
+    if (lane == 0) {
+      f.kth[wave] = least;
+      f.part[wave] = part;
+    }
   }
-  // All lanes call it; key 0 never passes.
-  __device__ void offer(u64 key, int lane, int k) {
-    const bool in = key > least;
-    const u64 who = __ballot(in);
-    if (!who) return;
-    if (in) buf[n + __builtin_amdgcn_mbcnt_hi((unsigned)(who >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)who, 0))] = key;
-    n += __popcll(who);
-    if (n >= 64) flush(lane, k, 64);
+  template <int WAVES>
+  __device__ void publish_list(Found<WAVES>& f, int lane, int wave, int k) {
+    publish(f, lane_of(list, k - 1), lane_of(list, (k + WAVES - 1) / WAVES - 1), lane, wave);
   }
-  // Enough keys wait to raise the bound: after k of them about half of what passes no longer would.
-  __device__ void settle(int lane, int k) {
-    if (n >= max(k, 8)) flush(lane, k, n);
+  template <int WAVES>
+  __device__ void look(const Found<WAVES>& f, int lane) {
+    static_assert(WAVES == 4);
+    u64 a = *(const volatile u64*)&f.kth[lane & 3], b = *(const volatile u64*)&f.part[lane & 3];
+    u64 o = lane_xor<1>(a, lane);
+    a = o > a ? o : a;
+    o = lane_xor<2>(a, lane);
+    a = o > a ? o : a;
+    o = lane_xor<1>(b, lane);
+    b = o < b ? o : b;
+    o = lane_xor<2>(b, lane);
+    b = o < b ? o : b;
+    b = b ? b - 1 : 0;  // (keys equal to it pass: they may be the k-th)
+    const u64 t = lane_of(a > b ? a : b, 0);
+    least = t > least ? t : least;
   }
   // Scores below it do not pass.
   __device__ float bound() const {
     const unsigned o = (unsigned)(least >> 32);
     return o > 0x007fffffu ? of_order(o) : -INFINITY;  // (0x007fffff: -inf)
   }
-  __device__ void look() {
-    const u64 o = *(volatile u64*)shared;
-    const u64 t = lane_of(o, 0);
-    least = t > least ? t : least;
-  }
 };
 
-// Bits of the columns c .. c + v - 1 in a row's mask of `words` words.
-__device__ __forceinline__ unsigned mask_bits(const uint32_t* m, int words, int c, int v) {
-  if (c < 0) return m[0] << -c;
-  const int w = c >> 5, sh = c & 31;
-  if (w >= words) return 0;
-  u64 b = m[w];
-  if (sh + v > 32 && w + 1 < words) b |= (u64)m[w + 1] << 32;
-  return (unsigned)(b >> sh);
+// The words of a row's mask that hold the bits of 4 or 8 columns from c on (a few of them may
+// lie before the row), and those bits.
+struct MaskWords {
+  u64 w;
+  int shift;
+};
+struct __attribute__((packed, aligned(4))) TwoWords {
+  u64 v;
+};
+__device__ __forceinline__ MaskWords mask_load(const uint32_t* m, int words, int c) {
+  const int at = max(0, min(c >> 5, words - 2));
+  return {words > 1 ? reinterpret_cast<const TwoWords*>(m + at)->v : m[0], c - 32 * at};
+}
+__device__ __forceinline__ unsigned mask_bits(const MaskWords& m) {
+  return (unsigned)(m.shift < 0 ? m.w << -m.shift : m.shift < 64 ? m.w >> m.shift : 0);
 }
 
 // Writes the first k of a wave's list as ids and scores, or as keys.
@@ -171,25 +211,58 @@ __device__ __forceinline__ void put_best(u64 key, int lane, int k, int64_t row, 
   if (scores) scores[row * k + lane] = key ? of_order((unsigned)(key >> 32)) : -INFINITY;
 }
 
-__device__ __forceinline__ float lse_of(float m, float s) {
-  if (m == -INFINITY || m == INFINITY) return m;
-  return m + __builtin_amdgcn_logf(s) * LN2;
+// A row's sum of e^score as (m, s): the sum is s 2^m.  m is a whole number (or infinite), so a
+// term 2^(score log2 e - m) takes one fused product and one exponential, and is at most
+// 1: its clamp to [0, 1] turns the NaN of a label that is not ranked into 0.
+__device__ __forceinline__ float term2(float v, float m) {
+  return __builtin_amdgcn_fmed3f(__builtin_amdgcn_exp2f(fmaf(v, LOG2E, -m)), 0.0f, 1.0f);
+}
+__device__ __forceinline__ void raise2(float v, float& m, float& s) {
+  const float c = ceilf(v * LOG2E);
+  if (c > m) {
+    s = m == -INFINITY ? 0.0f : s * __builtin_amdgcn_exp2f(m - c);
+    m = c;
+  }
+}
+__device__ __forceinline__ void merge2(float& m, float& s, float m2, float s2) { soft_merge(m, s, m2, s2, 1.0f); }
+// The row's log-sum-exp; best: its best key.  Beyond 2^32 the sum's logarithm, at most
+// ln 2^22, is below half a step of the best score (and the score's product with log2 e may overflow).
+__device__ __forceinline__ float lse_of(u64 best, float m, float s) {
+  if (!best) return -INFINITY;
+  const float top = of_order((unsigned)(best >> 32));
+  return fabsf(top) < 4294967296.0f ? (m + __builtin_amdgcn_logf(s)) * LN2 : top;
 }
 
-// The lists of the waves of a workgroup as one, on wave 0; likewise (m, s).
-__device__ __forceinline__ bool gather_waves(Best& best, float& m, float& s, u64 (*lists)[128], float2* red, int lane,
-                                             int wave) {
-#pragma unroll
-  for (int o = 32; o >= 1; o >>= 1) soft_merge(m, s, __shfl_xor(m, o), __shfl_xor(s, o), LOG2E);
-  if (lane == 0) red[wave] = make_float2(m, s);
-  lists[wave][63 - lane] = best.list;
-  __syncthreads();
-  if (wave) return false;
-  for (int w = 1; w < RK_WAVES; ++w) {
-    best.list = merge64(best.list, lists[w][lane], lane);
-    soft_merge(m, s, red[w].x, red[w].y, LOG2E);
+template <int X>
+__device__ __forceinline__ void merge2_lanes(float& m, float& s, int lane) {
+  const float mo = __uint_as_float(lane_xor<X>(__float_as_uint(m), lane));
+  const float so = __uint_as_float(lane_xor<X>(__float_as_uint(s), lane));
+  merge2(m, s, mo, so);
+}
+// The lists of the waves of a workgroup as one, on wave 0; likewise (m, s) on its lanes.
+template <int WAVES, int STRIDE>
+__device__ __forceinline__ void gather_waves(u64& list, float& m, float& s, bool sums, u64 (*lists)[STRIDE], float2* red,
+                                             int lane, int wave) {
+  if (sums) {
+    merge2_lanes<1>(m, s, lane);
+    merge2_lanes<2>(m, s, lane);
+    merge2_lanes<4>(m, s, lane);
+    merge2_lanes<8>(m, s, lane);
+    merge2_lanes<16>(m, s, lane);
+    merge2_lanes<32>(m, s, lane);
   }
-  return true;
+#pragma unroll 1
+  for (int d = 1; d < WAVES; d *= 2) {
+    if ((wave & (2 * d - 1)) == d) {
+      lists[wave][63 - lane] = list;
+      if (lane == 0) red[wave] = make_float2(m, s);
+    }
+    __syncthreads();
+    if ((wave & (2 * d - 1)) == 0) {
+      list = merge64(list, lists[wave + d][lane], lane);
+      if (sums) merge2(m, s, red[wave + d].x, red[wave + d].y);
+    }
+  }
 }
 
 struct Table {
@@ -223,15 +296,19 @@ __device__ __forceinline__ float listed_score(const T* zrow, const RankRules& ru
 // The listed labels in [lo, hi).
 template <typename T>
 __device__ void rank_listed(const T* zrow, const RankRules& ru, const uint32_t* mask, int lo, int hi, int s0, int s1,
-                            int b0, int b1, int k, Table& t, int* overflow, Best& best, float& m, float& s, int lane) {
+                            int b0, int b1, Table& t, int* overflow, Best& best, float& m, float& s, int lane) {
   const int tid = threadIdx.x, ns = s1 - s0, n = ns + (b1 - b0);
   auto entry = [&](int i) {
     const int id = i < ns ? ru.seen.indices[s0 + i] : ru.row_bias.indices[b0 + i - ns];
     return id >= lo && id < hi ? id : -1;
   };
   auto take = [&](float v, int id) {
-    best.offer(v == v ? key_of(v, id) : 0, lane, k);
-    if (v == v) soft_merge(m, s, v, 1.0f, LOG2E);
+    best.append(v == v ? key_of(v, id) : 0);
+    if (best.n >= 64) best.flush(lane);
+    if (v == v) {
+      raise2(v, m, s);
+      if (m != -INFINITY) s += term2(v, m);
+    }
   };
   for (int i = tid; i < RK_SLOTS; i += RK_THREADS) {
     t.id[i] = -1;
@@ -305,7 +382,7 @@ __global__ __launch_bounds__(RK_THREADS) void k_rank(const T* __restrict__ z, in
   constexpr unsigned ALL = (1u << V) - 1;
   __shared__ u64 buf[RK_WAVES][128];
   __shared__ float2 red[RK_WAVES];
-  __shared__ u64 shared_least;
+  __shared__ Found<RK_WAVES> found;
   __shared__ union Lists {
     unsigned bits[LISTS ? RK_BITS / 32 + 1 : 1];
     char table[LISTS ? sizeof(Table) : 1];
@@ -318,9 +395,9 @@ __global__ __launch_bounds__(RK_THREADS) void k_rank(const T* __restrict__ z, in
   const R zr(const_cast<T*>(z), ld, row, L);
   const uint32_t* mask = ru.allowed ? ru.allowed + (int64_t)row * ru.allowed_ld : nullptr;
   const int words = (L + 31) >> 5;
-  Best best{0, 0, 0, buf[wave], &shared_least};
+  Best best{0, 0, 0, 0, buf[wave]};
   float m = -INFINITY, s = 0.0f;
-  if (threadIdx.x == 0) shared_least = 0;
+  if (threadIdx.x < RK_WAVES) found.kth[threadIdx.x] = found.part[threadIdx.x] = 0;
 
   int s0 = 0, s1 = 0, b0 = 0, b1 = 0;
   bool lists = false;
@@ -333,7 +410,7 @@ __global__ __launch_bounds__(RK_THREADS) void k_rank(const T* __restrict__ z, in
     const int width = (L + ranges - 1) / ranges, lo = (piece - splits) * width;
     __syncthreads();
     if (lists)
-      rank_listed(zr.base + zr.phase, ru, mask, lo, min(L, lo + width), s0, s1, b0, b1, k,
+      rank_listed(zr.base + zr.phase, ru, mask, lo, min(L, lo + width), s0, s1, b0, b1,
                   *reinterpret_cast<Table*>(in.table), &overflow, best, m, s, lane);
   } else {
     const int v0 = piece * vec_split, v1 = max(v0, min(zr.n_vec, v0 + vec_split)), c0 = zr.col(v0);
@@ -351,21 +428,31 @@ __global__ __launch_bounds__(RK_THREADS) void k_rank(const T* __restrict__ z, in
       }
     }
     __syncthreads();
-    // a round of loads: the logits and biases of the columns to look at
+    // Rounds of loads: a round's logits and biases are on their way while the one before it is
+    // worked on, and its words of the mask while the one before that is.
     typename R::vec x[RK_U];
     Floats<V> bias[RK_U];
     unsigned ok[RK_U];
-    auto load = [&](int base) {
+    MaskWords mw[RK_U];
+    const int rounds = (v1 - v0 + ROUND - 1) / ROUND, settle = max(k, 8);
+    auto load_mask = [&](int base) {
+#pragma unroll
+      for (int u = 0; u < RK_U; ++u) mw[u] = mask_load(mask, words, zr.col(base + u * RK_THREADS + (int)threadIdx.x));
+    };
+    auto load = [&](int r) {
+      const int base = v0 + r * ROUND;
+      // only these two rounds meet an end of the row or of the piece
+      const bool inside = r > 0 && r < rounds - 1;
 #pragma unroll
       for (int u = 0; u < RK_U; ++u) {
         const int i = base + u * RK_THREADS + (int)threadIdx.x, c = zr.col(i);
-        const unsigned in_row = i < v1 ? zr.in_row(i) : 0;
+        const unsigned in_row = inside ? ALL : i < v1 ? zr.in_row(i) : 0;
         unsigned o = in_row;
-        if (mask && o) o &= mask_bits(mask, words, c, V);
-        if (LISTS && lists && o) o &= ~(in.bits[(i - v0) * V >> 5] >> ((i - v0) * V & 31));
+        if (mask) o &= mask_bits(mw[u]);
+        if (LISTS && lists && (inside || o)) o &= ~(in.bits[(i - v0) * V >> 5] >> ((i - v0) * V & 31));
         ok[u] = o;
         if (!o) continue;
-        if (in_row == ALL) {
+        if (inside || in_row == ALL) {
           x[u] = __builtin_nontemporal_load(reinterpret_cast<const typename R::vec*>(zr.base + (int64_t)V * i));
           if (ru.bias) bias[u] = *reinterpret_cast<const Floats<V>*>(ru.bias + c);
         } else {
@@ -378,16 +465,25 @@ __global__ __launch_bounds__(RK_THREADS) void k_rank(const T* __restrict__ z, in
         }
       }
     };
-    const int rounds = v1 > v0 ? (v1 - v0 + ROUND - 1) / ROUND : 0;
-    if (rounds) load(v0);
+    if (rounds) {
+      if (mask) load_mask(v0);
+      load(0);
+      if (mask && rounds > 1) load_mask(v0 + ROUND);
+    }
     for (int r = 0; r < rounds; ++r) {
       const int base = v0 + r * ROUND;
+      if (r) best.look(found, lane);
       float w[RK_U][V];
       float mx = -INFINITY;
 #pragma unroll
       for (int u = 0; u < RK_U; ++u) {
+        if (ru.bias) {
 #pragma unroll
-        for (int e = 0; e < V; ++e) w[u][e] = (float)x[u][e] + (ru.bias ? bias[u].v[e] : 0.0f);
+          for (int e = 0; e < V; ++e) w[u][e] = (float)x[u][e] + bias[u].v[e];
+        } else {
+#pragma unroll
+          for (int e = 0; e < V; ++e) w[u][e] = (float)x[u][e] + 0.0f;  // (-0 ties with 0)
+        }
         if (__ballot(ok[u] != ALL)) {
           const int off = (int)~ok[u];
 #pragma unroll
@@ -397,44 +493,58 @@ __global__ __launch_bounds__(RK_THREADS) void k_rank(const T* __restrict__ z, in
 #pragma unroll
         for (int e = 0; e < V; ++e) mx = fmaxf(mx, w[u][e]);
       }
-      if (r + 1 < rounds) load(base + ROUND);
-      if (r == 0) {
-        const unsigned kth = lane_of(sort64(order_of(mx), lane), k - 1);
-        best.least = ((u64)kth << 32) - 1;  // (keys of that score are above it)
-        if (lane == 0) atomicMax(&shared_least, best.least);
+      if (r + 1 < rounds) {
+        load(r + 1);
+        if (mask && r + 2 < rounds) load_mask(base + 2 * ROUND);
       }
-      best.look();
-      if (__ballot(mx >= best.bound())) {
+      if (r == 0) {
+        // (keys of the k-th largest maximum's score are above the bound)
+        const unsigned tops = sort64(order_of(mx), lane);
+        best.publish(found, ((u64)lane_of(tops, k - 1) << 32) - 1,
+                     (u64)lane_of(tops, (k + RK_WAVES - 1) / RK_WAVES - 1) << 32, lane, wave);
+      }
+      const float bound = best.bound();
+      if (__ballot(mx >= bound)) {
+        unsigned pass = 0;
 #pragma unroll
-        for (int u = 0; u < RK_U; ++u) {
-          const int c = zr.col(base + u * RK_THREADS + (int)threadIdx.x);
+        for (int u = 0; u < RK_U; ++u)
 #pragma unroll
-          for (int e = 0; e < V; ++e) {
-            const float v = w[u][e];
-            if (__ballot(v >= best.bound())) best.offer(v == v ? key_of(v, c + e) : 0, lane, k);
+          for (int e = 0; e < V; ++e) pass |= w[u][e] >= bound ? 1u << (u * V + e) : 0u;
+        // one label of each lane at a time; the list takes them 64 at a time, or when enough
+        // wait to raise the bound: of what passes after k of them, about half no longer would
+        do {
+          const int at = pass ? __builtin_ctz(pass) : 0;
+          float v = w[0][0];
+#pragma unroll
+          for (int j = 1; j < RK_U * V; ++j) v = at == j ? w[j / V][j % V] : v;
+          const int c = zr.col(base + at / V * RK_THREADS + (int)threadIdx.x) + at % V;
+          best.append(pass ? key_of(v, c) : 0);
+          pass &= pass - 1;
+          const bool more = __ballot(pass != 0);
+          if (best.n >= 64 || (!more && best.n >= settle)) {
+            best.flush(lane);
+            best.publish_list(found, lane, wave, k);
           }
-        }
-        best.settle(lane, k);
+          if (!more) break;
+        } while (true);
       }
       if (lse) {
-        if (mx > m) {
-          s = m == -INFINITY ? 0.0f : s * __builtin_amdgcn_exp2f((m - mx) * LOG2E);
-          m = mx;
-        }
+        raise2(mx, m, s);
         if (m != -INFINITY) {
 #pragma unroll
           for (int u = 0; u < RK_U; ++u)
 #pragma unroll
-            for (int e = 0; e < V; ++e) s += __builtin_amdgcn_exp2f((fmaxf(w[u][e], -INFINITY) - m) * LOG2E);
+            for (int e = 0; e < V; ++e) s += term2(w[u][e], m);
         }
       }
     }
   }
-  if (best.n) best.flush(lane, k, best.n);
-  if (!gather_waves(best, m, s, buf, red, lane, wave)) return;
+  if (best.n) best.flush(lane);
+  gather_waves<RK_WAVES>(best.list, m, s, lse != nullptr, buf, red, lane, wave);
+  if (wave) return;
   if (parts == 1) {
     put_best(best.list, lane, k, row, ids, scores);
-    if (lse && lane == 0) lse[row] = lse_of(m, s);
+    if (lse && lane == 0) lse[row] = lse_of(best.list, m, s);
   } else {
     if (lane < k) part[(int64_t)blockIdx.x * k + lane] = best.list;
     if (lse && lane == 0) part_ms[blockIdx.x] = make_float2(m, s);
@@ -442,42 +552,39 @@ __global__ __launch_bounds__(RK_THREADS) void k_rank(const T* __restrict__ z, in
 }
 
 // Per row: the k best of its pieces' lists, and lse of their sums, in a fixed order.
-__global__ __launch_bounds__(RK_THREADS) void k_rank_join(int parts, int k, const u64* __restrict__ part,
+template <int WAVES>
+__global__ __launch_bounds__(64 * WAVES) void k_rank_join(int parts, int k, const u64* __restrict__ part,
                                                           const float2* __restrict__ part_ms,
                                                           int32_t* __restrict__ ids, float* __restrict__ scores,
                                                           float* __restrict__ lse) {
-  __shared__ u64 buf[RK_WAVES][64];
-  __shared__ float2 red[RK_WAVES];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  __shared__ u64 buf[WAVES][64];
+  __shared__ float2 red[WAVES];
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int64_t row = blockIdx.x;
   const int n = parts * k;
   const u64* p = part + row * n;
+  float m = -INFINITY, s = 0.0f;
+  if (lse)
+    for (int i = threadIdx.x; i < parts; i += 64 * WAVES) {
+      const float2 ms = part_ms[row * parts + i];
+      merge2(m, s, ms.x, ms.y);
+    }
   u64 list = 0, least = 0;
-  for (int i = wave * 64; i < n; i += RK_THREADS) {
-    const u64 v = i + lane < n ? p[i + lane] : 0;
+  int i = wave * 64 + lane;
+  u64 next = i < n ? p[i] : 0;
+  for (; i - lane < n; i += 64 * WAVES) {
+    const u64 v = next;
+    if (i + 64 * WAVES < n) next = p[i + 64 * WAVES];
+    else next = 0;
     if (!__ballot(v > least)) continue;
     list = merge64(list, reverse64(sort64(v, lane), lane), lane);
     least = lane_of(list, k - 1);
   }
-  float m = -INFINITY, s = 0.0f;
-  if (lse) {
-    for (int i = threadIdx.x; i < parts; i += RK_THREADS) {
-      const float2 ms = part_ms[row * parts + i];
-      soft_merge(m, s, ms.x, ms.y, LOG2E);
-    }
-#pragma unroll
-    for (int o = 32; o >= 1; o >>= 1) soft_merge(m, s, __shfl_xor(m, o), __shfl_xor(s, o), LOG2E);
-    if (lane == 0) red[wave] = make_float2(m, s);
-  }
-  buf[wave][63 - lane] = list;
-  __syncthreads();
+  gather_waves<WAVES>(list, m, s, lse != nullptr, buf, red, lane, wave);
   if (wave) return;
-  for (int w = 1; w < RK_WAVES; ++w) {
-    list = merge64(list, buf[w][lane], lane);
-    if (lse) soft_merge(m, s, red[w].x, red[w].y, LOG2E);
-  }
   put_best(list, lane, k, row, ids, scores);
-  if (lse && lane == 0) lse[row] = lse_of(m, s);
+  if (lse && lane == 0) lse[row] = lse_of(list, m, s);
 }
 
 }  // namespace
@@ -523,8 +630,10 @@ static hipError_t rank_as(const void* z, int64_t ld, int rows, int L, const Rank
   else
     hipLaunchKernelGGL((k_rank<T, false>), grid, block, 0, st, (const T*)z, ld, L, ru, k, sh.splits, 0, vps, part, ms, ids,
                        scores, lse);
-  if (parts > 1)
-    hipLaunchKernelGGL(k_rank_join, dim3(rows), dim3(RK_THREADS), 0, st, parts, k, part, ms, ids, scores, lse);
+  if (parts > 1 && parts * k > 512 && rows <= 256)
+    hipLaunchKernelGGL(k_rank_join<16>, dim3(rows), dim3(1024), 0, st, parts, k, part, ms, ids, scores, lse);
+  else if (parts > 1)
+    hipLaunchKernelGGL(k_rank_join<4>, dim3(rows), dim3(256), 0, st, parts, k, part, ms, ids, scores, lse);
   return hipGetLastError();
 }
 
