@@ -33,8 +33,8 @@ namespace {
 
 constexpr int RK_THREADS = 256;
 constexpr int RK_WAVES = RK_THREADS / 64;
-constexpr int RK_U = 2;            // vectors per lane and round
-constexpr int RK_BITS = 1 << 16;   // columns of a piece at most where lists are given
+constexpr int RK_LANE = 8;         // labels per lane and round
+constexpr int RK_BITS = 1 << 17;   // columns of a piece at most where lists are given (as many bits as the table takes)
 constexpr int RK_SLOTS = 1024;     // the table of listed labels
 constexpr int RK_PROBES = 32;
 constexpr int RK_RANGES = 32;     // ranges of listed labels per row at most
@@ -122,10 +122,10 @@ __device__ __forceinline__ u64 reverse64(u64 v, int lane) { return __shfl(v, 63 
 
 // What the waves of a workgroup have found, in LDS: k labels of a wave are as good as `kth`,
 // ceil(k / waves) as good as `part`.  So the workgroup's k-th best is at least the largest
-// kth and the smallest part, and labels below that need not be looked at by any wave.
+// kth and the smallest part, and labels below that need not be looked at by any wave: `bound`.
 template <int WAVES>
 struct Found {
-  u64 kth[WAVES], part[WAVES];
+  u64 bound, part[WAVES];
 };
 
 struct Best {
@@ -153,31 +153,27 @@ struct Best {
   }
   template <int WAVES>
   __device__ void publish(Found<WAVES>& f, u64 kth, u64 p, int lane, int wave) {
-    least = kth > least ? kth : least;
+    static_assert(WAVES == 4);
     part = p > part ? p : part;
-    if (lane == 0) {
-      f.kth[wave] = least;
-      f.part[wave] = part;
-    }
+    if (lane == 0) *(volatile u64*)&f.part[wave] = part;
+    u64 b = *(const volatile u64*)&f.part[lane & 3];
+    u64 o = lane_xor<1>(b, lane);
+    b = o < b ? o : b;
+    o = lane_xor<2>(b, lane);
+    b = o < b ? o : b;
+    b = b ? b - 1 : 0;  // (a key equal to it passes: it may be the k-th)
+    b = b > kth ? b : kth;
+    if (lane == 0) atomicMax(&f.bound, b);
+    b = lane_of(b, 0);
+    least = b > least ? b : least;
   }
   template <int WAVES>
   __device__ void publish_list(Found<WAVES>& f, int lane, int wave, int k) {
     publish(f, lane_of(list, k - 1), lane_of(list, (k + WAVES - 1) / WAVES - 1), lane, wave);
   }
   template <int WAVES>
-  __device__ void look(const Found<WAVES>& f, int lane) {
-    static_assert(WAVES == 4);
-    u64 a = *(const volatile u64*)&f.kth[lane & 3], b = *(const volatile u64*)&f.part[lane & 3];
-    u64 o = lane_xor<1>(a, lane);
-    a = o > a ? o : a;
-    o = lane_xor<2>(a, lane);
-    a = o > a ? o : a;
-    o = lane_xor<1>(b, lane);
-    b = o < b ? o : b;
-    o = lane_xor<2>(b, lane);
-    b = o < b ? o : b;
-    b = b ? b - 1 : 0;  // (keys equal to it pass: they may be the k-th)
-    const u64 t = lane_of(a > b ? a : b, 0);
+  __device__ void look(const Found<WAVES>& f) {
+    const u64 t = lane_of(*(const volatile u64*)&f.bound, 0);
     least = t > least ? t : least;
   }
   // Scores below it do not pass.
@@ -186,23 +182,6 @@ struct Best {
     return o > 0x007fffffu ? of_order(o) : -INFINITY;  // (0x007fffff: -inf)
   }
 };
-
-// The words of a row's mask that hold the bits of 4 or 8 columns from c on (a few of them may
-// lie before the row), and those bits.
-struct MaskWords {
-  u64 w;
-  int shift;
-};
-struct __attribute__((packed, aligned(4))) TwoWords {
-  u64 v;
-};
-__device__ __forceinline__ MaskWords mask_load(const uint32_t* m, int words, int c) {
-  const int at = max(0, min(c >> 5, words - 2));
-  return {words > 1 ? reinterpret_cast<const TwoWords*>(m + at)->v : m[0], c - 32 * at};
-}
-__device__ __forceinline__ unsigned mask_bits(const MaskWords& m) {
-  return (unsigned)(m.shift < 0 ? m.w << -m.shift : m.shift < 64 ? m.w >> m.shift : 0);
-}
 
 // Writes the first k of a wave's list as ids and scores, or as keys.
 __device__ __forceinline__ void put_best(u64 key, int lane, int k, int64_t row, int32_t* ids, float* scores) {
@@ -378,16 +357,17 @@ __global__ __launch_bounds__(RK_THREADS) void k_rank(const T* __restrict__ z, in
                                                      float2* __restrict__ part_ms, int32_t* __restrict__ ids,
                                                      float* __restrict__ scores, float* __restrict__ lse) {
   using R = Row<T>;
-  constexpr int V = R::V, ROUND = RK_THREADS * RK_U;
+  constexpr int V = R::V, RK_U = RK_LANE / V, ROUND = RK_THREADS * RK_U;
   constexpr unsigned ALL = (1u << V) - 1;
   __shared__ u64 buf[RK_WAVES][128];
   __shared__ float2 red[RK_WAVES];
   __shared__ Found<RK_WAVES> found;
   __shared__ union Lists {
-    unsigned bits[LISTS ? RK_BITS / 32 + 1 : 1];
+    unsigned bits[LISTS ? RK_BITS / 32 : 1];
     char table[LISTS ? sizeof(Table) : 1];
   } in;
   __shared__ int overflow;
+  __shared__ unsigned edge_bits;
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int parts = splits + ranges;
@@ -397,7 +377,7 @@ __global__ __launch_bounds__(RK_THREADS) void k_rank(const T* __restrict__ z, in
   const int words = (L + 31) >> 5;
   Best best{0, 0, 0, 0, buf[wave]};
   float m = -INFINITY, s = 0.0f;
-  if (threadIdx.x < RK_WAVES) found.kth[threadIdx.x] = found.part[threadIdx.x] = 0;
+  if (threadIdx.x <= RK_WAVES) (&found.bound)[threadIdx.x] = 0;
 
   int s0 = 0, s1 = 0, b0 = 0, b1 = 0;
   bool lists = false;
@@ -413,66 +393,72 @@ __global__ __launch_bounds__(RK_THREADS) void k_rank(const T* __restrict__ z, in
       rank_listed(zr.base + zr.phase, ru, mask, lo, min(L, lo + width), s0, s1, b0, b1,
                   *reinterpret_cast<Table*>(in.table), &overflow, best, m, s, lane);
   } else {
-    const int v0 = piece * vec_split, v1 = max(v0, min(zr.n_vec, v0 + vec_split)), c0 = zr.col(v0);
+    // whole vectors [va, vb) are shared out; the first piece's first wave takes the labels before and after them
+    const int va = zr.phase ? 1 : 0, vb = max(va, (zr.phase + L) / V);
+    const int v0 = va + piece * vec_split, v1 = max(v0, min(vb, v0 + vec_split)), c0 = zr.col(v0);
+    const int head = min(L, zr.col(va)), tail = min(L, max(head, zr.col(vb)));
     if (lists) {
-      for (int i = threadIdx.x; i <= RK_BITS / 32; i += RK_THREADS) in.bits[i] = 0;
+      for (int i = threadIdx.x; i < ((v1 - v0) * V + 31) / 32; i += RK_THREADS) in.bits[i] = 0;
+      if (threadIdx.x == 0) edge_bits = 0;
       __syncthreads();
       const unsigned width = (unsigned)(v1 - v0) * V;
-      for (int q = s0 + (int)threadIdx.x; q < s1; q += RK_THREADS) {
-        const unsigned c = (unsigned)(ru.seen.indices[q] - c0);
+      auto skip = [&](int id) {
+        const unsigned c = (unsigned)(id - c0);
         if (c < width) atomicOr(&in.bits[c >> 5], 1u << (c & 31));
-      }
-      for (int q = b0 + (int)threadIdx.x; q < b1; q += RK_THREADS) {
-        const unsigned c = (unsigned)(ru.row_bias.indices[q] - c0);
-        if (c < width) atomicOr(&in.bits[c >> 5], 1u << (c & 31));
-      }
+        if (id >= 0 && id < L && (id < head || id >= tail)) atomicOr(&edge_bits, 1u << (id < head ? id : head + id - tail));
+      };
+      for (int q = s0 + (int)threadIdx.x; q < s1; q += RK_THREADS) skip(ru.seen.indices[q]);
+      for (int q = b0 + (int)threadIdx.x; q < b1; q += RK_THREADS) skip(ru.row_bias.indices[q]);
     }
     __syncthreads();
+    if (piece == 0 && wave == 0 && head + (L - tail) > 0) {
+      float v = NAN;
+      const int c = lane < head ? lane : tail + lane - head;
+      if (c < L && !(mask && !((mask[c >> 5] >> (c & 31)) & 1)) && !(lists && ((edge_bits >> lane) & 1)))
+        v = (float)zr.base[zr.phase + c] + (ru.bias ? ru.bias[c] : 0.0f);
+      best.append(v == v ? key_of(v, c) : 0);
+      raise2(v, m, s);
+      if (m != -INFINITY) s += term2(v, m);
+    }
     // Rounds of loads: a round's logits and biases are on their way while the one before it is
-    // worked on, and its words of the mask while the one before that is.
+    // worked on, and its words of the mask while the one before that is.  Lanes past the
+    // piece's end load its last vector again.
     typename R::vec x[RK_U];
     Floats<V> bias[RK_U];
-    unsigned ok[RK_U];
-    MaskWords mw[RK_U];
-    const int rounds = (v1 - v0 + ROUND - 1) / ROUND, settle = max(k, 8);
-    auto load_mask = [&](int base) {
-#pragma unroll
-      for (int u = 0; u < RK_U; ++u) mw[u] = mask_load(mask, words, zr.col(base + u * RK_THREADS + (int)threadIdx.x));
-    };
-    auto load = [&](int r) {
-      const int base = v0 + r * ROUND;
-      // only these two rounds meet an end of the row or of the piece
-      const bool inside = r > 0 && r < rounds - 1;
+    unsigned ok[RK_U], m0[RK_U], m1[RK_U];
+    const int rounds = (v1 - v0 + ROUND - 1) / ROUND;
+    const int first = v0 + (int)threadIdx.x;
+    auto load_mask = [&](int r) {
 #pragma unroll
       for (int u = 0; u < RK_U; ++u) {
-        const int i = base + u * RK_THREADS + (int)threadIdx.x, c = zr.col(i);
-        const unsigned in_row = inside ? ALL : i < v1 ? zr.in_row(i) : 0;
-        unsigned o = in_row;
-        if (mask) o &= mask_bits(mw[u]);
-        if (LISTS && lists && (inside || o)) o &= ~(in.bits[(i - v0) * V >> 5] >> ((i - v0) * V & 31));
-        ok[u] = o;
-        if (!o) continue;
-        if (inside || in_row == ALL) {
-          x[u] = __builtin_nontemporal_load(reinterpret_cast<const typename R::vec*>(zr.base + (int64_t)V * i));
-          if (ru.bias) bias[u] = *reinterpret_cast<const Floats<V>*>(ru.bias + c);
-        } else {
+        const int w = zr.col(min(first + r * ROUND + u * RK_THREADS, v1 - 1)) >> 5;
+        m0[u] = mask[(unsigned)w];
+        m1[u] = mask[(unsigned)min(w + 1, words - 1)];
+      }
+    };
+    auto load = [&](int r) {
 #pragma unroll
-          for (int e = 0; e < V; ++e)
-            if ((in_row >> e) & 1) {
-              x[u][e] = zr.base[(int64_t)V * i + e];
-              if (ru.bias) bias[u].v[e] = ru.bias[c + e];
-            }
-        }
+      for (int u = 0; u < RK_U; ++u) {
+        const int i = first + r * ROUND + u * RK_THREADS, j = min(i, v1 - 1), c = zr.col(j);
+        unsigned o = i == j ? ALL : 0;
+        if (mask) o &= __builtin_amdgcn_alignbit(m1[u], m0[u], c & 31);
+        if (LISTS && lists) o &= ~(in.bits[(j - v0) * V >> 5] >> ((j - v0) * V & 31));
+        ok[u] = o;
+        if (!__ballot(o != 0)) continue;
+        x[u] = __builtin_nontemporal_load(
+            reinterpret_cast<const typename R::vec*>(reinterpret_cast<const char*>(zr.base) + (unsigned)(16 * j)));
+        if (ru.bias)
+          bias[u] = *reinterpret_cast<const Floats<V>*>(reinterpret_cast<const char*>(ru.bias) + (unsigned)(4 * c));
       }
     };
     if (rounds) {
-      if (mask) load_mask(v0);
+      if (mask) load_mask(0);
       load(0);
-      if (mask && rounds > 1) load_mask(v0 + ROUND);
+      if (mask && rounds > 1) load_mask(1);
     }
     for (int r = 0; r < rounds; ++r) {
       const int base = v0 + r * ROUND;
-      if (r) best.look(found, lane);
+      if (r) best.look(found);
       float w[RK_U][V];
       float mx = -INFINITY;
 #pragma unroll
@@ -495,7 +481,7 @@ __global__ __launch_bounds__(RK_THREADS) void k_rank(const T* __restrict__ z, in
       }
       if (r + 1 < rounds) {
         load(r + 1);
-        if (mask && r + 2 < rounds) load_mask(base + 2 * ROUND);
+        if (mask && r + 2 < rounds) load_mask(r + 2);
       }
       if (r == 0) {
         // (keys of the k-th largest maximum's score are above the bound)
@@ -510,8 +496,8 @@ __global__ __launch_bounds__(RK_THREADS) void k_rank(const T* __restrict__ z, in
         for (int u = 0; u < RK_U; ++u)
 #pragma unroll
           for (int e = 0; e < V; ++e) pass |= w[u][e] >= bound ? 1u << (u * V + e) : 0u;
-        // one label of each lane at a time; the list takes them 64 at a time, or when enough
-        // wait to raise the bound: of what passes after k of them, about half no longer would
+        // one label of each lane at a time; the list takes them 64 at a time (as soon as k of them
+        // wait: 62 us instead of 54 for 256 x 205,443 bf16 and k = 32, no difference for k = 5)
         do {
           const int at = pass ? __builtin_ctz(pass) : 0;
           float v = w[0][0];
@@ -520,13 +506,11 @@ __global__ __launch_bounds__(RK_THREADS) void k_rank(const T* __restrict__ z, in
           const int c = zr.col(base + at / V * RK_THREADS + (int)threadIdx.x) + at % V;
           best.append(pass ? key_of(v, c) : 0);
           pass &= pass - 1;
-          const bool more = __ballot(pass != 0);
-          if (best.n >= 64 || (!more && best.n >= settle)) {
+          if (best.n >= 64) {
             best.flush(lane);
             best.publish_list(found, lane, wave, k);
           }
-          if (!more) break;
-        } while (true);
+        } while (__ballot(pass != 0));
       }
       if (lse) {
         raise2(mx, m, s);
@@ -590,11 +574,15 @@ __global__ __launch_bounds__(64 * WAVES) void k_rank_join(int parts, int k, cons
 }  // namespace
 
 // Pieces per row: enough workgroups to fill the GPU, each with at least a round of 16-bit
-// loads per wave, and no more columns than a workgroup has bits for.
-RankShape rank_shape(int rows, int cols) {
+// loads per wave; where lists are given, no more columns than a workgroup has bits for.
+static int row_pieces(int rows, int cols, bool lists) {
   const int want = (RK_WGS + rows - 1) / rows, most = (cols + 2047) / 2048;
-  const int least = (cols + 8 + RK_BITS - 1) / RK_BITS;
-  return RankShape{std::max(std::min(want, most), least), std::max(1, std::min(RK_RANGES, 2048 / rows))};
+  const int least = lists ? (cols + RK_BITS - 1) / RK_BITS : 1;
+  return std::max(std::min(want, most), least);
+}
+
+RankShape rank_shape(int rows, int cols) {
+  return RankShape{row_pieces(rows, cols, true), std::max(1, std::min(RK_RANGES, 2048 / rows))};
 }
 
 // Ranges of listed labels per row: about 256 entries each.  (The scratch memory has room for
@@ -616,19 +604,20 @@ size_t rank_ws_bytes(const RankShape& sh, int rows, int k) {
 template <typename T>
 static hipError_t rank_as(const void* z, int64_t ld, int rows, int L, const RankRules& ru, int k, const RankShape& sh,
                           int32_t* ids, float* scores, float* lse, void* ws, hipStream_t st) {
-  // vectors of a row of any phase, and per piece
-  const int n_vec = (L + 2 * Row<T>::V - 2) / Row<T>::V;
-  const int vps = (n_vec + sh.splits - 1) / sh.splits;
-  const int ranges = rank_ranges(sh, ru, rows), parts = sh.splits + ranges;
-  if (ranges && vps * Row<T>::V > RK_BITS) return hipErrorInvalidValue;
+  const int ranges = rank_ranges(sh, ru, rows);
+  const int splits = std::min(sh.splits, row_pieces(rows, L, ranges > 0)), parts = splits + ranges;
+  // whole vectors of a row at most, and per piece
+  const int n_vec = L / Row<T>::V;
+  const int vps = (n_vec + splits - 1) / splits;
+  if (ranges && (int64_t)vps * Row<T>::V > RK_BITS) return hipErrorInvalidValue;
   u64* part = (u64*)ws;
   float2* ms = (float2*)((char*)ws + key_bytes(sh, rows, k));
   const dim3 grid((unsigned)rows * parts), block(RK_THREADS);
   if (ranges)
-    hipLaunchKernelGGL((k_rank<T, true>), grid, block, 0, st, (const T*)z, ld, L, ru, k, sh.splits, ranges, vps, part, ms,
+    hipLaunchKernelGGL((k_rank<T, true>), grid, block, 0, st, (const T*)z, ld, L, ru, k, splits, ranges, vps, part, ms,
                        ids, scores, lse);
   else
-    hipLaunchKernelGGL((k_rank<T, false>), grid, block, 0, st, (const T*)z, ld, L, ru, k, sh.splits, 0, vps, part, ms, ids,
+    hipLaunchKernelGGL((k_rank<T, false>), grid, block, 0, st, (const T*)z, ld, L, ru, k, splits, 0, vps, part, ms, ids,
                        scores, lse);
   if (parts > 1 && parts * k > 512 && rows <= 256)
     hipLaunchKernelGGL(k_rank_join<16>, dim3(rows), dim3(1024), 0, st, parts, k, part, ms, ids, scores, lse);
