@@ -52,10 +52,15 @@ __device__ __forceinline__ void store8(T* p, const float (&x)[8]) {
   }
 }
 
+// 2^(byte - 127), or NaN for 255.
+__device__ __forceinline__ float scale_of(unsigned byte) {
+  return __uint_as_float(byte == 0 ? 0x00400000u : byte == 255 ? 0x7fc00000u : byte << 23);
+}
+
 // Four lanes hold a block of 32.  The scale's exponent is the largest magnitude's less 2,
 // taken from its bits (which order magnitudes as integers, infinities and NaN on top).
-// Elements are scaled by a power of two (exact) and compared with the midpoints of the
-// e2m1 grid; which side a midpoint falls on is the even code's.
+// The conversion divides by the scale (a power of two, the exponent bits of a float: 2^-127
+// is the field's 0) and rounds to nearest, ties to the even code, at most 6 in magnitude.
 template <typename T, bool ALIGNED>
 __global__ __launch_bounds__(Q_THREADS) void k_quantize(const T* __restrict__ x, int64_t ld, int64_t n8, int row8,
                                                         uint32_t* __restrict__ codes, uint8_t* __restrict__ scales) {
@@ -71,22 +76,14 @@ __global__ __launch_bounds__(Q_THREADS) void k_quantize(const T* __restrict__ x,
   big = max(big, (unsigned)__shfl_xor((int)big, 2));
   const int ex = (int)(big >> 23);
   const int byte = big == 0 ? 0 : ex == 255 ? 255 : max(ex - 2, 0);
-  // 2^(127 - byte)
-  const float up = __uint_as_float(byte >= 254 ? 0x00400000u >> (byte - 254) : (unsigned)(254 - byte) << 23);
+  const float scale = scale_of((unsigned)byte);
   unsigned out = 0;
-#pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    const float m = fabsf(v[e] * up);
-    unsigned code = (m > 0.25f) + (m >= 0.75f) + (m > 1.25f) + (m >= 1.75f) + (m > 2.5f) + (m >= 3.5f) + (m > 5.0f);
-    if (v[e] < 0.0f) code |= 8;
-    out |= code << (4 * e);
-  }
+  out = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(out, v[0], v[1], scale, 0);
+  out = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(out, v[2], v[3], scale, 1);
+  out = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(out, v[4], v[5], scale, 2);
+  out = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(out, v[6], v[7], scale, 3);
   codes[i] = byte == 255 ? 0 : out;
   if ((i & 3) == 0) scales[i >> 2] = (uint8_t)byte;
-}
-
-__device__ __forceinline__ float scale_of(unsigned byte) {
-  return __uint_as_float(byte == 0 ? 0x00400000u : byte == 255 ? 0x7fc00000u : byte << 23);
 }
 
 template <typename T, bool ALIGNED>
@@ -99,91 +96,193 @@ __global__ __launch_bounds__(Q_THREADS) void k_dequantize(const uint32_t* __rest
   const unsigned w = codes[i];
   const float s = scale_of(scales[i >> 2]);
   float v[8];
-#pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    const unsigned code = w >> (4 * e);
-    const unsigned m = code & 7;
-    // e2m1: 0, 0.5, then (1 + mantissa / 2) 2^(exponent - 1)
-    const float a = m < 2 ? 0.5f * (float)m : __uint_as_float((126 + (m >> 1)) << 23 | (m & 1) << 22);
-    v[e] = (code & 8 ? -a : a) * s;
-  }
+  const bool nan = scales[i >> 2] == 255;
+  auto two = [&](f32x2 p, int at) {
+    v[at] = nan ? NAN : p[0];
+    v[at + 1] = nan ? NAN : p[1];
+  };
+  two(__builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, s, 0), 0);
+  two(__builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, s, 1), 2);
+  two(__builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, s, 2), 4);
+  two(__builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, s, 3), 6);
   store8<T, ALIGNED>(out + row * ld + c * 8, v);
 }
 
 // ---------------------------------------------------------------------------
-// Logits.  One wave per 32 labels, the label as the product's column: lane
-// (g, n) holds label n's codes of hidden units 64c + 32g .. + 31 (c = 0, 1), 16
-// bytes each, and so the accumulator holds four rows of 32 consecutive labels
-// per register quad.  With 4-bit rows the codes go into the scaled product
-// as they are; with bf16 rows they are widened to bf16 (exact) once, for all the rows.
+// Logits.  A wave's tile is 32 labels, the product's columns: lane (g, n) holds label n's codes
+// of hidden units 64g .. 64g + 63, 32 contiguous bytes, and takes units 64g + 32c .. + 31 into
+// half c of the product (the order of the inner index is free as long as both
+// operands share it).  The accumulator then holds, per register, one row of 32 consecutive
+// labels on each half of the wave.  With 4-bit rows the codes go into the scaled product as
+// they are, a lane's 32 elements under its block's scale; with bf16 rows they are
+// widened to bf16 (exactly) first.
 // ---------------------------------------------------------------------------
 constexpr int FL_THREADS = 256;
+constexpr int FL_WAVES = FL_THREADS / 64;
+constexpr int FL_FEW_WGS = 1024;
 
-template <typename T, bool H4>
-__global__ __launch_bounds__(FL_THREADS) void k_fp4_logits(const bf16* __restrict__ h, int64_t ldh,
-                                                           const uint8_t* __restrict__ h_codes,
-                                                           const uint8_t* __restrict__ h_scales, int B,
-                                                           const uint8_t* __restrict__ codes,
-                                                           const uint8_t* __restrict__ scales,
-                                                           const float* __restrict__ bias, int L, T* __restrict__ z,
-                                                           int64_t ldz) {
-  const int lane = threadIdx.x & 63, g = lane >> 5, n = lane & 31;
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int tile = (int)blockIdx.x * (FL_THREADS / 64) + wave;
-  if (tile * 32 >= L) return;
-  const int label = tile * 32 + n;
-  const int safe = min(label, L - 1);
-  i32x4 wc[2];
+// 32 labels of W: codes, scales (halves c = 0, 1 in bytes 0, 1) and bias, as loaded.
+struct LabelTile {
+  i32x4 c[2];
+  unsigned scale;
+  float bias;
+};
+__device__ __forceinline__ void label_load(LabelTile& t, const uint8_t* codes, const uint8_t* scales, const float* bias,
+                                           int tile, int L, int g, int n) {
+  const int label = min(tile * 32 + n, L - 1);
+  const i32x4* p = reinterpret_cast<const i32x4*>(codes + (unsigned)label * (HID / 2) + 32 * g);
+  t.c[0] = p[0];
+  t.c[1] = p[1];
+  t.scale = *reinterpret_cast<const unsigned*>(scales + (unsigned)label * (HID / 32)) >> (16 * g);
+  t.bias = bias ? bias[label] : 0.0f;
+}
+
+typedef bf16 bf16x2_ __attribute__((ext_vector_type(2)));
+// The tile's weights as operands of the bf16 product.
+__device__ __forceinline__ void widen(const LabelTile& t, bf16x8 (&w)[8]) {
 #pragma unroll
-  for (int c = 0; c < 2; ++c)
-    wc[c] = *reinterpret_cast<const i32x4*>(codes + (int64_t)safe * (HID / 2) + 32 * c + 16 * g);
-  const unsigned ws = *reinterpret_cast<const unsigned*>(scales + (int64_t)safe * (HID / 32)) >> (8 * g);
-  const float b = bias ? bias[safe] : 0.0f;
-  bf16x8 wf[H4 ? 1 : 8];
-  if constexpr (!H4) {
+  for (int c = 0; c < 2; ++c) {
+    const float s = scale_of((t.scale >> (8 * c)) & 255);
 #pragma unroll
-    for (int c = 0; c < 2; ++c) {
-      const float s = scale_of((ws >> (16 * c)) & 255);
-#pragma unroll
-      for (int j = 0; j < 4; ++j)
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const unsigned code = (unsigned)wc[c][j] >> (4 * e);
-          const unsigned m = code & 7;
-          const float a = m < 2 ? 0.5f * (float)m : __uint_as_float((126 + (m >> 1)) << 23 | (m & 1) << 22);
-          wf[4 * c + j][e] = (bf16)((code & 8 ? -a : a) * s);
-        }
+    for (int j = 0; j < 4; ++j) {
+      const unsigned v = (unsigned)t.c[c][j];
+      const bf16x2_ a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(v, s, 0), b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(v, s, 1),
+                    d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(v, s, 2), e = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(v, s, 3);
+      w[4 * c + j] = bf16x8{a[0], a[1], b[0], b[1], d[0], d[1], e[0], e[1]};
     }
   }
-  for (int r0 = (int)blockIdx.y * 32; r0 < B; r0 += (int)gridDim.y * 32) {
-    const int row = min(r0 + n, B - 1);
+}
+
+// 32 hidden rows as the other operand.
+template <bool H4>
+struct RowTile;
+template <>
+struct RowTile<false> {
+  bf16x8 a[8];
+  __device__ void load(const Fp4Rows& h, int row, int g) {
+    const bf16* p = (const bf16*)h.h + (int64_t)row * h.ld + 64 * g;
+#pragma unroll
+    for (int c = 0; c < 8; ++c) a[c] = *reinterpret_cast<const bf16x8*>(p + 8 * c);
+  }
+};
+template <>
+struct RowTile<true> {
+  i32x4 c[2];
+  unsigned scale;
+  __device__ void load(const Fp4Rows& h, int row, int g) {
+    const i32x4* p = reinterpret_cast<const i32x4*>(h.codes + (unsigned)row * (HID / 2) + 32 * g);
+    c[0] = p[0];
+    c[1] = p[1];
+    scale = *reinterpret_cast<const unsigned*>(h.scales + (unsigned)row * (HID / 32)) >> (16 * g);
+  }
+};
+
+__device__ __forceinline__ f32x16 product(const RowTile<false>& h, const bf16x8 (&w)[8], f32x16 acc) {
+#pragma unroll
+  for (int c = 0; c < 8; ++c) acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(h.a[c], w[c], acc, 0, 0, 0);
+  return acc;
+}
+__device__ __forceinline__ f32x16 product(const RowTile<true>& h, const LabelTile& w, f32x16 acc) {
+#pragma unroll
+  for (int c = 0; c < 2; ++c) {
+    const i32x8 a = {h.c[c][0], h.c[c][1], h.c[c][2], h.c[c][3], 0, 0, 0, 0};
+    const i32x8 b = {w.c[c][0], w.c[c][1], w.c[c][2], w.c[c][3], 0, 0, 0, 0};
+    if (c == 0)
+      acc = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a, b, acc, 4, 4, 0, (int)h.scale, 0, (int)w.scale);
+    else
+      acc = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a, b, acc, 4, 4, 1, (int)h.scale, 1, (int)w.scale);
+  }
+  // The product takes part of every lane; this compiler would otherwise move it, and the loads
+  // of its operands, under a later branch that some lanes do not take.
+  asm volatile("" : "+v"(acc));
+  return acc;
+}
+__device__ __forceinline__ f32x16 splat(float v) {
+  f32x16 a;
+#pragma unroll
+  for (int r = 0; r < 16; ++r) a[r] = v;
+  return a;
+}
+
+// At most 32 rows: the rows stay in registers, and a wave goes through its tiles of labels with
+// the next one on its way.
+template <typename T, bool H4>
+__global__ __launch_bounds__(FL_THREADS) void k_fp4_logits_few(Fp4Rows h, int B, const uint8_t* __restrict__ codes,
+                                                               const uint8_t* __restrict__ scales,
+                                                               const float* __restrict__ bias, int L, int n_tiles,
+                                                               T* __restrict__ z, int64_t ldz) {
+  const int lane = threadIdx.x & 63, g = lane >> 5, n = lane & 31;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int step = (int)gridDim.x * FL_WAVES;
+  int tile = (int)blockIdx.x * FL_WAVES + wave;
+  if (tile >= n_tiles) return;
+  LabelTile next;
+  label_load(next, codes, scales, bias, tile, L, g, n);
+  RowTile<H4> rows;
+  rows.load(h, min(n, B - 1), g);
+  for (; tile < n_tiles; tile += step) {
+    const LabelTile w = next;
+    if (tile + step < n_tiles) label_load(next, codes, scales, bias, tile + step, L, g, n);
     f32x16 acc;
-#pragma unroll
-    for (int r = 0; r < 16; ++r) acc[r] = 0.0f;
     if constexpr (H4) {
-      const unsigned hs = *reinterpret_cast<const unsigned*>(h_scales + (int64_t)row * (HID / 32)) >> (8 * g);
-#pragma unroll
-      for (int c = 0; c < 2; ++c) {
-        const i32x4 hc = *reinterpret_cast<const i32x4*>(h_codes + (int64_t)row * (HID / 2) + 32 * c + 16 * g);
-        const i32x8 a = {hc[0], hc[1], hc[2], hc[3], 0, 0, 0, 0}, w = {wc[c][0], wc[c][1], wc[c][2], wc[c][3], 0, 0, 0, 0};
-        acc = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a, w, acc, 4, 4, 0, (int)(hs >> (16 * c)), 0,
-                                                              (int)(ws >> (16 * c)));
-      }
-      // The product takes part of every lane; this compiler would otherwise move it, and the
-      // loads of its operands, under the branch below, which some lanes of the last tile skip.
-      asm volatile("" : "+v"(acc));
+      acc = product(rows, w, splat(0.0f));
     } else {
-#pragma unroll
-      for (int c = 0; c < 8; ++c) {
-        const bf16x8 a = *reinterpret_cast<const bf16x8*>(h + (int64_t)row * ldh + 64 * (c >> 2) + 32 * g + 8 * (c & 3));
-        acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, wf[c], acc, 0, 0, 0);
-      }
+      bf16x8 f[8];
+      widen(w, f);
+      acc = product(rows, f, splat(0.0f));
     }
+    const int label = tile * 32 + n;
     if (label < L) {
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
-        const int i = r0 + 8 * (r >> 2) + 4 * g + (r & 3);
-        if (i < B) z[(int64_t)i * ldz + label] = (T)(acc[r] + b);
+        const int i = 8 * (r >> 2) + 4 * g + (r & 3);
+        if (i < B) z[(int64_t)i * ldz + label] = (T)(acc[r] + w.bias);
+      }
+    }
+  }
+}
+
+// Many rows: a wave keeps 64 labels and goes through blocks of 32 rows.
+template <typename T, bool H4>
+__global__ __launch_bounds__(FL_THREADS) void k_fp4_logits(Fp4Rows h, int B, const uint8_t* __restrict__ codes,
+                                                           const uint8_t* __restrict__ scales,
+                                                           const float* __restrict__ bias, int L, int n_wg,
+                                                           T* __restrict__ z, int64_t ldz) {
+  const int lane = threadIdx.x & 63, g = lane >> 5, n = lane & 31;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  // neighbouring labels on one XCD: their rows' segments share memory lines
+  const int per = (n_wg + 7) / 8;
+  const int wg = (int)(blockIdx.x % 8) * per + (int)blockIdx.x / 8;
+  if (wg >= n_wg) return;
+  const int tile = 2 * (wg * FL_WAVES + wave);
+  if (tile * 32 >= L) return;
+  LabelTile w[2];
+  bf16x8 f[2][8];
+#pragma unroll
+  for (int t = 0; t < 2; ++t) {
+    label_load(w[t], codes, scales, bias, tile + t, L, g, n);
+    if constexpr (!H4) widen(w[t], f[t]);
+  }
+  const int step = (int)gridDim.y * 32;
+  RowTile<H4> next;
+  next.load(h, min((int)blockIdx.y * 32 + n, B - 1), g);
+  for (int r0 = (int)blockIdx.y * 32; r0 < B; r0 += step) {
+    const RowTile<H4> rows = next;
+    next.load(h, min(r0 + step + n, B - 1), g);
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      f32x16 acc;
+      if constexpr (H4)
+        acc = product(rows, w[t], splat(0.0f));
+      else
+        acc = product(rows, f[t], splat(0.0f));
+      const int label = (tile + t) * 32 + n;
+      if (label < L) {
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          const int i = r0 + 8 * (r >> 2) + 4 * g + (r & 3);
+          if (i < B) z[(int64_t)i * ldz + label] = (T)(acc[r] + w[t].bias);
+        }
       }
     }
   }
@@ -214,20 +313,22 @@ hipError_t dequantize_as(const uint8_t* codes, const uint8_t* scales, int rows, 
   return hipGetLastError();
 }
 
-template <typename T>
+template <typename T, bool H4>
 hipError_t logits_as(const Fp4Rows& a, int B, const uint8_t* codes, const uint8_t* scales, const float* bias, int L,
                      void* z, int64_t ldz, hipStream_t st) {
-  const int wgs = (L + 32 * (FL_THREADS / 64) - 1) / (32 * (FL_THREADS / 64));
-  const int blocks = (B + 31) / 32;
-  int gy = (2048 + wgs - 1) / wgs;
-  if (gy > blocks) gy = blocks;
-  const dim3 grid(wgs, gy), block(FL_THREADS);
-  if (a.codes)
-    hipLaunchKernelGGL((k_fp4_logits<T, true>), grid, block, 0, st, (const bf16*)nullptr, (int64_t)0, a.codes, a.scales,
-                       B, codes, scales, bias, L, (T*)z, ldz);
-  else
-    hipLaunchKernelGGL((k_fp4_logits<T, false>), grid, block, 0, st, (const bf16*)a.h, a.ld, a.codes, a.scales, B, codes,
-                       scales, bias, L, (T*)z, ldz);
+  const int n_tiles = (L + 31) / 32;
+  const dim3 block(FL_THREADS);
+  if (B <= 32) {
+    const int wgs = (n_tiles + FL_WAVES - 1) / FL_WAVES;
+    hipLaunchKernelGGL((k_fp4_logits_few<T, H4>), dim3(wgs < FL_FEW_WGS ? wgs : FL_FEW_WGS), block, 0, st, a, B, codes, scales,
+                       bias, L, n_tiles, (T*)z, ldz);
+  } else {
+    const int wgs = (n_tiles + 2 * FL_WAVES - 1) / (2 * FL_WAVES), blocks = (B + 31) / 32;
+    int gy = (2048 + wgs - 1) / wgs;
+    if (gy > blocks) gy = blocks;
+    hipLaunchKernelGGL((k_fp4_logits<T, H4>), dim3((wgs + 7) / 8 * 8, gy), block, 0, st, a, B, codes, scales, bias, L, wgs,
+                       (T*)z, ldz);
+  }
   return hipGetLastError();
 }
 
@@ -249,9 +350,14 @@ hipError_t launch_fp4_dequantize(const uint8_t* codes, const uint8_t* scales, in
 
 hipError_t launch_fp4_logits(const Fp4Rows& a, int B, const uint8_t* codes, const uint8_t* scales, const float* bias,
                              int L, int dtype, void* z, int64_t ldz, hipStream_t st) {
-  if (dtype == 0) return logits_as<float>(a, B, codes, scales, bias, L, z, ldz, st);
-  if (dtype == 1) return logits_as<bf16>(a, B, codes, scales, bias, L, z, ldz, st);
-  return logits_as<f16>(a, B, codes, scales, bias, L, z, ldz, st);
+  if (a.codes) {
+    if (dtype == 0) return logits_as<float, true>(a, B, codes, scales, bias, L, z, ldz, st);
+    if (dtype == 1) return logits_as<bf16, true>(a, B, codes, scales, bias, L, z, ldz, st);
+    return logits_as<f16, true>(a, B, codes, scales, bias, L, z, ldz, st);
+  }
+  if (dtype == 0) return logits_as<float, false>(a, B, codes, scales, bias, L, z, ldz, st);
+  if (dtype == 1) return logits_as<bf16, false>(a, B, codes, scales, bias, L, z, ldz, st);
+  return logits_as<f16, false>(a, B, codes, scales, bias, L, z, ldz, st);
 }
 
 }  // namespace asgd
