@@ -121,15 +121,15 @@ constexpr int FL_THREADS = 256;
 constexpr int FL_WAVES = FL_THREADS / 64;
 constexpr int FL_FEW_WGS = 1024;
 
-// 32 labels of W: codes, scales (halves c = 0, 1 in bytes 0, 1) and bias, as loaded.
+// A label's share of a tile, on its two lanes: codes, scales (halves c = 0, 1 in bytes 0, 1) and bias, as loaded.
 struct LabelTile {
   i32x4 c[2];
   unsigned scale;
   float bias;
 };
 __device__ __forceinline__ void label_load(LabelTile& t, const uint8_t* codes, const uint8_t* scales, const float* bias,
-                                           int tile, int L, int g, int n) {
-  const int label = min(tile * 32 + n, L - 1);
+                                           int label, int L, int g) {
+  label = max(0, min(label, L - 1));
   const i32x4* p = reinterpret_cast<const i32x4*>(codes + (unsigned)label * (HID / 2) + 32 * g);
   t.c[0] = p[0];
   t.c[1] = p[1];
@@ -217,12 +217,12 @@ __global__ __launch_bounds__(FL_THREADS) void k_fp4_logits_few(Fp4Rows h, int B,
   int tile = (int)blockIdx.x * FL_WAVES + wave;
   if (tile >= n_tiles) return;
   LabelTile next;
-  label_load(next, codes, scales, bias, tile, L, g, n);
+  label_load(next, codes, scales, bias, tile * 32 + n, L, g);
   RowTile<H4> rows;
   rows.load(h, min(n, B - 1), g);
   for (; tile < n_tiles; tile += step) {
     const LabelTile w = next;
-    if (tile + step < n_tiles) label_load(next, codes, scales, bias, tile + step, L, g, n);
+    if (tile + step < n_tiles) label_load(next, codes, scales, bias, (tile + step) * 32 + n, L, g);
     f32x16 acc;
     if constexpr (H4) {
       acc = product(rows, w, splat(0.0f));
@@ -242,49 +242,110 @@ __global__ __launch_bounds__(FL_THREADS) void k_fp4_logits_few(Fp4Rows h, int B,
   }
 }
 
-// Many rows: a wave keeps 64 labels and goes through blocks of 32 rows.
+// Many rows: bound by writing Z, whose rows of an odd number of labels start anywhere in a memory
+// line.  A line that two workgroups write part of costs the memory a read, so each row is
+// divided at its own line boundaries: the workgroup of labels from t0 on stores, of a row whose element
+// t0 lies p elements into its line, the labels t0 - p .. t0 - p + FM_KEEP - 1, and forms the labels
+// of one line more for that.  Eight waves with 64 labels each (the weights stay in
+// registers) go through blocks of 32 rows; a block passes through LDS, shifted so that
+// 16-byte pieces of memory are 16-byte pieces there, and leaves as whole lines.  bf16 rows come
+// in through LDS as well (read by every wave as operands, they are 16 bytes out of each of 64 lines).
+constexpr int FM_THREADS = 512;
+constexpr int FM_WGS = 1024;  // workgroups wanted
+constexpr int FM_LABELS = 64 * (FM_THREADS / 64);
+
 template <typename T, bool H4>
-__global__ __launch_bounds__(FL_THREADS) void k_fp4_logits(Fp4Rows h, int B, const uint8_t* __restrict__ codes,
-                                                           const uint8_t* __restrict__ scales,
-                                                           const float* __restrict__ bias, int L, int n_wg,
-                                                           T* __restrict__ z, int64_t ldz) {
+__global__ __launch_bounds__(FM_THREADS, 4) void k_fp4_logits(Fp4Rows h, int B, const uint8_t* __restrict__ codes,
+                                                              const uint8_t* __restrict__ scales,
+                                                              const float* __restrict__ bias, int L, int n_wg,
+                                                              T* __restrict__ z, int64_t ldz) {
+  constexpr int V = 16 / (int)sizeof(T), LINE = 128 / (int)sizeof(T), KEEP = FM_LABELS - LINE;
+  typedef T vec __attribute__((ext_vector_type(V)));
+  constexpr int S = FM_LABELS + 8;  // (4 rows of it apart, the halves of a wave write other banks)
+  constexpr int HS = HID + 8;   // row stride of the hidden rows: 16 lanes read 16 different bank groups
+  __shared__ __attribute__((aligned(16))) T stage[32 * S];
+  __shared__ __attribute__((aligned(16))) bf16 hid[H4 ? 8 : 32 * HS];
   const int lane = threadIdx.x & 63, g = lane >> 5, n = lane & 31;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  // neighbouring labels on one XCD: their rows' segments share memory lines
+  // neighbouring labels on one XCD
   const int per = (n_wg + 7) / 8;
   const int wg = (int)(blockIdx.x % 8) * per + (int)blockIdx.x / 8;
   if (wg >= n_wg) return;
-  const int tile = 2 * (wg * FL_WAVES + wave);
-  if (tile * 32 >= L) return;
+  const int t0 = wg * KEEP, from = t0 - LINE;  // labels from .. from + FM_LABELS - 1 are formed
+  // row i's element t0 lies (at0 + i ld_line) % LINE elements into its line
+  const int at0 = (int)((uintptr_t)z / sizeof(T) + (unsigned)t0) & (LINE - 1), ld_line = (int)ldz & (LINE - 1);
+  const bool inner = t0 >= LINE && t0 + KEEP <= L;  // every label that it stores exists
   LabelTile w[2];
   bf16x8 f[2][8];
 #pragma unroll
   for (int t = 0; t < 2; ++t) {
-    label_load(w[t], codes, scales, bias, tile + t, L, g, n);
+    // (labels before the first and past the last are read as some other, and not stored)
+    label_load(w[t], codes, scales, bias, from + 64 * wave + 32 * t + n, L, g);
     if constexpr (!H4) widen(w[t], f[t]);
   }
   const int step = (int)gridDim.y * 32;
-  RowTile<H4> next;
-  next.load(h, min((int)blockIdx.y * 32 + n, B - 1), g);
+  // thread t brings 16 bytes of row t / 16; or, 4-bit rows, a lane its operand
+  bf16x8 piece;
+  RowTile<true> rows;
+  auto fetch = [&](int r) {
+    if constexpr (H4)
+      rows.load(h, min(r + n, B - 1), g);
+    else
+      piece = *reinterpret_cast<const bf16x8*>((const bf16*)h.h + (int64_t)min(r + (int)threadIdx.x / 16, B - 1) * h.ld +
+                                               8 * (threadIdx.x % 16));
+  };
+  auto put = [&]() {
+    if constexpr (!H4) *reinterpret_cast<bf16x8*>(hid + (threadIdx.x / 16) * HS + 8 * (threadIdx.x % 16)) = piece;
+  };
+  fetch((int)blockIdx.y * 32);
+  put();
+  if constexpr (!H4) __syncthreads();
   for (int r0 = (int)blockIdx.y * 32; r0 < B; r0 += step) {
-    const RowTile<H4> rows = next;
-    next.load(h, min(r0 + step + n, B - 1), g);
+    f32x16 acc[2] = {splat(0.0f), splat(0.0f)};
+    if constexpr (H4) {
+      acc[0] = product(rows, w[0], acc[0]);
+      acc[1] = product(rows, w[1], acc[1]);
+    } else {
 #pragma unroll
-    for (int t = 0; t < 2; ++t) {
-      f32x16 acc;
-      if constexpr (H4)
-        acc = product(rows, w[t], splat(0.0f));
-      else
-        acc = product(rows, f[t], splat(0.0f));
-      const int label = (tile + t) * 32 + n;
-      if (label < L) {
-#pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          const int i = r0 + 8 * (r >> 2) + 4 * g + (r & 3);
-          if (i < B) z[(int64_t)i * ldz + label] = (T)(acc[r] + w[t].bias);
-        }
+      for (int c = 0; c < 8; ++c) {
+        const bf16x8 a = *reinterpret_cast<const bf16x8*>(hid + n * HS + 64 * g + 8 * c);
+        acc[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, f[0][c], acc[0], 0, 0, 0);
+        acc[1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, f[1][c], acc[1], 0, 0, 0);
       }
     }
+    fetch(r0 + step);
+    T* const to = stage + 4 * g * S + 64 * wave + n;
+    const int at = at0 + (r0 + 4 * g) * ld_line;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      const int i = 8 * (r >> 2) + (r & 3);
+      const int shift = (at + i * ld_line) & (V - 1);
+      to[i * S + shift] = (T)(acc[0][r] + w[0].bias);
+      to[i * S + shift + 32] = (T)(acc[1][r] + w[1].bias);
+    }
+    __syncthreads();
+    put();  // (before the stores, or it would wait for them)
+#pragma unroll 1
+    for (int q = 0; q < 32 / (FM_THREADS / 64); ++q) {
+      const int i = wave * (32 / (FM_THREADS / 64)) + q, row = r0 + i;
+      if (row >= B) break;
+      const int p = (at0 + row * ld_line) & (LINE - 1);
+      const int first = t0 - p;  // the row's first label here: column LINE - p + p % V of the stage
+      T* const out = z + ((int64_t)row * ldz + first);
+      const T* const in = stage + i * S + LINE - (p & ~(V - 1));
+      if (inner) {
+#pragma unroll
+        for (int v = 0; v < (KEEP / V + 63) / 64; ++v)
+          if (v * 64 + lane < KEEP / V)
+            __builtin_nontemporal_store(*reinterpret_cast<const vec*>(in + (v * 64 + lane) * V),
+                                        reinterpret_cast<vec*>(out + (v * 64 + lane) * V));
+      } else {
+#pragma unroll 1
+        for (int c = lane; c < KEEP; c += 64)
+          if (first + c >= 0 && first + c < L) out[c] = in[c];
+      }
+    }
+    __syncthreads();
   }
 }
 
@@ -323,11 +384,12 @@ hipError_t logits_as(const Fp4Rows& a, int B, const uint8_t* codes, const uint8_
     hipLaunchKernelGGL((k_fp4_logits_few<T, H4>), dim3(wgs < FL_FEW_WGS ? wgs : FL_FEW_WGS), block, 0, st, a, B, codes, scales,
                        bias, L, n_tiles, (T*)z, ldz);
   } else {
-    const int wgs = (n_tiles + 2 * FL_WAVES - 1) / (2 * FL_WAVES), blocks = (B + 31) / 32;
-    int gy = (2048 + wgs - 1) / wgs;
+    constexpr int LINE = 128 / (int)sizeof(T);
+    const int wgs = (L + LINE - 1 + FM_LABELS - LINE - 1) / (FM_LABELS - LINE), blocks = (B + 31) / 32;
+    int gy = (FM_WGS + wgs - 1) / wgs;
     if (gy > blocks) gy = blocks;
-    hipLaunchKernelGGL((k_fp4_logits<T, H4>), dim3((wgs + 7) / 8 * 8, gy), block, 0, st, a, B, codes, scales, bias, L, wgs,
-                       (T*)z, ldz);
+    hipLaunchKernelGGL((k_fp4_logits<T, H4>), dim3((wgs + 7) / 8 * 8, gy), dim3(FM_THREADS), 0, st, a, B, codes, scales,
+                       bias, L, wgs, (T*)z, ldz);
   }
   return hipGetLastError();
 }
