@@ -279,7 +279,8 @@ struct DistillJob {
 };
 constexpr int DISTILL_MAX_K = 512;
 struct DistillShape {
-  int splits;
+  int slabs;   // of rows, one after the other
+  int splits;  // pieces per row
 };
 DistillShape distill_shape(int rows, int cols);
 size_t distill_ws_bytes(const DistillShape& sh, int rows, int k);
