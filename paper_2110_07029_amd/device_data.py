@@ -41,25 +41,36 @@ class DeviceCSR:
         return int(self.indptr_host[r1] - self.indptr_host[r0])
 
 
-_TYPES = {"torch.float32": ASGD_F32, "torch.bfloat16": ASGD_BF16, "torch.float16": ASGD_F16}
+class _Types(dict):
+    """torch's element types as the library's, looked up without importing torch before it is needed."""
+
+    def __missing__(self, dtype):
+        code = {"torch.float32": ASGD_F32, "torch.bfloat16": ASGD_BF16, "torch.float16": ASGD_F16}.get(str(dtype))
+        if code is None:
+            raise ValueError(f"no matrix of {dtype}")
+        self[dtype] = code
+        return code
+
+
+_TYPES = _Types()
 
 
 def matrix(t) -> asgd_matrix:
     """A 2-d tensor (unit stride along a row) as an asgd_matrix; the tensor must outlive its use."""
-    if t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1):
-        raise ValueError("a matrix needs two dimensions and unit stride along a row")
-    dtype = _TYPES.get(str(t.dtype))
-    if dtype is None:
-        raise ValueError(f"no matrix of {t.dtype}")
+    if t.dim() != 2:
+        raise ValueError("a matrix has two dimensions")
     rows, cols = t.shape
-    return asgd_matrix(rows, cols, t.stride(0) if rows > 1 else max(cols, 1), dtype, t.data_ptr())
+    ld, step = t.stride()
+    if step != 1 and cols > 1:
+        raise ValueError("a matrix needs unit stride along a row")
+    return asgd_matrix(rows, cols, ld if rows > 1 else cols, _TYPES[t.dtype], t.data_ptr())
 
 
 def fp4_matrix(codes, scales) -> asgd_fp4:
     """uint8 tensors, codes [rows, cols / 2] and scales [rows, cols / 32], as an asgd_fp4."""
     rows, half = codes.shape
-    if str(codes.dtype) != "torch.uint8" or str(scales.dtype) != "torch.uint8" or half % 16:
-        raise ValueError("codes and scales are uint8, codes with a multiple of 16 columns")
+    if codes.element_size() != 1 or scales.element_size() != 1 or half % 16:
+        raise ValueError("codes and scales are bytes, codes with a multiple of 16 columns")
     if tuple(scales.shape) != (rows, half // 16) or not (codes.is_contiguous() and scales.is_contiguous()):
         raise ValueError("codes [rows, cols / 2] and scales [rows, cols / 32] must be contiguous")
     return asgd_fp4(rows, 2 * half, codes.data_ptr(), scales.data_ptr())
