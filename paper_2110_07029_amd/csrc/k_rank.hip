@@ -212,35 +212,47 @@ __device__ __forceinline__ float lse_of(u64 best, float m, float s) {
   return fabsf(top) < 4294967296.0f ? (m + __builtin_amdgcn_logf(s)) * LN2 : top;
 }
 
+// (m, s) of all lanes as one, on all of them: the largest m, and the sums under it.
 template <int X>
-__device__ __forceinline__ void merge2_lanes(float& m, float& s, int lane) {
-  const float mo = __uint_as_float(lane_xor<X>(__float_as_uint(m), lane));
-  const float so = __uint_as_float(lane_xor<X>(__float_as_uint(s), lane));
-  merge2(m, s, mo, so);
+__device__ __forceinline__ float float_xor(float v, int lane) {
+  return __uint_as_float(lane_xor<X>(__float_as_uint(v), lane));
+}
+__device__ __forceinline__ void merge2_wave(float& m, float& s, int lane) {
+  float t = m;
+  t = fmaxf(t, float_xor<1>(t, lane));
+  t = fmaxf(t, float_xor<2>(t, lane));
+  t = fmaxf(t, float_xor<4>(t, lane));
+  t = fmaxf(t, float_xor<8>(t, lane));
+  t = fmaxf(t, float_xor<16>(t, lane));
+  t = fmaxf(t, float_xor<32>(t, lane));
+  s = m == -INFINITY ? 0.0f : s * __builtin_amdgcn_exp2f(m - t);
+  m = t;
+  s += float_xor<1>(s, lane);
+  s += float_xor<2>(s, lane);
+  s += float_xor<4>(s, lane);
+  s += float_xor<8>(s, lane);
+  s += float_xor<16>(s, lane);
+  s += float_xor<32>(s, lane);
 }
 // The lists of the waves of a workgroup as one, on wave 0; likewise (m, s) on its lanes.
 template <int WAVES, int STRIDE>
 __device__ __forceinline__ void gather_waves(u64& list, float& m, float& s, bool sums, u64 (*lists)[STRIDE], float2* red,
                                              int lane, int wave) {
   if (sums) {
-    merge2_lanes<1>(m, s, lane);
-    merge2_lanes<2>(m, s, lane);
-    merge2_lanes<4>(m, s, lane);
-    merge2_lanes<8>(m, s, lane);
-    merge2_lanes<16>(m, s, lane);
-    merge2_lanes<32>(m, s, lane);
+    merge2_wave(m, s, lane);
+    if (lane == 0) red[wave] = make_float2(m, s);
   }
 #pragma unroll 1
   for (int d = 1; d < WAVES; d *= 2) {
-    if ((wave & (2 * d - 1)) == d) {
-      lists[wave][63 - lane] = list;
-      if (lane == 0) red[wave] = make_float2(m, s);
-    }
+    if ((wave & (2 * d - 1)) == d) lists[wave][63 - lane] = list;
     __syncthreads();
-    if ((wave & (2 * d - 1)) == 0) {
-      list = merge64(list, lists[wave + d][lane], lane);
-      if (sums) merge2(m, s, red[wave + d].x, red[wave + d].y);
-    }
+    if ((wave & (2 * d - 1)) == 0) list = merge64(list, lists[wave + d][lane], lane);
+  }
+  if (sums && wave == 0) {
+    const float2 r = lane < WAVES ? red[lane] : make_float2(-INFINITY, 0.0f);
+    m = r.x;
+    s = r.y;
+    merge2_wave(m, s, lane);
   }
 }
 
@@ -259,15 +271,22 @@ __device__ __forceinline__ int table_put(Table& t, int id) {
   return -1;
 }
 
-// Score of a label that the row's lists name: n occurrences in seen, and the last of the
-// row_bias entries from b0 on (1-based, 0: none).  NaN if it is not ranked.
+// A listed label's logit and bias, and whether it is allowed.
+struct Listed {
+  float z, bias;
+  bool allowed;
+};
 template <typename T>
-__device__ __forceinline__ float listed_score(const T* zrow, const RankRules& ru, const uint32_t* mask, int id, int n,
-                                              int last, int b0) {
-  if (mask && !((mask[id >> 5] >> (id & 31)) & 1)) return NAN;
-  double t = (double)(float)zrow[id];
+__device__ __forceinline__ Listed listed_load(const T* zrow, const RankRules& ru, const uint32_t* mask, int id) {
+  return {(float)zrow[id], ru.bias ? ru.bias[id] : 0.0f, !mask || ((mask[id >> 5] >> (id & 31)) & 1)};
+}
+// Its score: n occurrences in seen, and the last of the row_bias entries from b0 on (1-based, 0:
+// none).  NaN if it is not ranked.
+__device__ __forceinline__ float listed_score(const Listed& l, const RankRules& ru, int n, int last, int b0) {
+  if (!l.allowed) return NAN;
+  double t = (double)l.z;
   if (n) t = (t > 0.0 ? t / ru.repetition : t * ru.repetition) - ru.frequency * (double)n - ru.presence;
-  if (ru.bias) t += (double)ru.bias[id];
+  t += (double)l.bias;
   if (last) t += (double)ru.row_bias.values[b0 + last - 1];
   return (float)t + 0.0f;
 }
@@ -289,6 +308,10 @@ __device__ void rank_listed(const T* zrow, const RankRules& ru, const uint32_t* 
       if (m != -INFINITY) s += term2(v, m);
     }
   };
+  // (a thread's first entry and what it leads to are on their way while the table is made)
+  const int id0 = tid < n ? entry(tid) : -1;
+  Listed l0{};
+  if (id0 >= 0) l0 = listed_load(zrow, ru, mask, id0);
   for (int i = tid; i < RK_SLOTS; i += RK_THREADS) {
     t.id[i] = -1;
     t.count[i] = t.last[i] = 0;
@@ -297,7 +320,7 @@ __device__ void rank_listed(const T* zrow, const RankRules& ru, const uint32_t* 
   if (tid == 0) *overflow = 0;
   __syncthreads();
   for (int i = tid; i < n; i += RK_THREADS) {
-    const int id = entry(i);
+    const int id = i == tid ? id0 : entry(i);
     if (id < 0) continue;
     const int h = table_put(t, id);
     if (h < 0) {
@@ -313,12 +336,13 @@ __device__ void rank_listed(const T* zrow, const RankRules& ru, const uint32_t* 
   __syncthreads();
   if (!*overflow) {
     for (int i0 = 0; i0 < n; i0 += RK_THREADS) {
-      const int i = i0 + tid, id = i < n ? entry(i) : -1;
+      const int i = i0 + tid, id = i0 == 0 ? id0 : i < n ? entry(i) : -1;
       float v = NAN;
       if (id >= 0) {
         unsigned h = slot_of(id);
         while (t.id[h] != id) h = (h + 1) & (RK_SLOTS - 1);  // (it is there)
-        if (t.first[h] == i) v = listed_score(zrow, ru, mask, id, t.count[h], t.last[h], b0);
+        if (t.first[h] == i)
+          v = listed_score(i0 == 0 ? l0 : listed_load(zrow, ru, mask, id), ru, t.count[h], t.last[h], b0);
       }
       take(v, id);
     }
@@ -339,7 +363,7 @@ __device__ void rank_listed(const T* zrow, const RankRules& ru, const uint32_t* 
     __syncthreads();
     for (int i = tid; i < RK_SLOTS; i += RK_THREADS) {
       const int c = t.count[i], l = t.last[i];
-      take(c | l ? listed_score(zrow, ru, mask, c0 + i, c, l, b0) : NAN, c0 + i);
+      take(c | l ? listed_score(listed_load(zrow, ru, mask, c0 + i), ru, c, l, b0) : NAN, c0 + i);
     }
   }
 }
@@ -397,6 +421,41 @@ __global__ __launch_bounds__(RK_THREADS) void k_rank(const T* __restrict__ z, in
     const int va = zr.phase ? 1 : 0, vb = max(va, (zr.phase + L) / V);
     const int v0 = va + piece * vec_split, v1 = max(v0, min(vb, v0 + vec_split)), c0 = zr.col(v0);
     const int head = min(L, zr.col(va)), tail = min(L, max(head, zr.col(vb)));
+    // Rounds of loads: a round's logits and biases are on their way while the one before it is
+    // worked on, and its words of the mask while the one before that is.  Lanes past the
+    // piece's end load its last vector again.
+    typename R::vec x[RK_U];
+    Floats<V> bias[RK_U];
+    unsigned ok[RK_U], m0[RK_U], m1[RK_U];
+    const int rounds = (v1 - v0 + ROUND - 1) / ROUND;
+    const int first = v0 + (int)threadIdx.x;
+    auto load_mask = [&](int r) {
+#pragma unroll
+      for (int u = 0; u < RK_U; ++u) {
+        const int w = zr.col(min(first + r * ROUND + u * RK_THREADS, v1 - 1)) >> 5;
+        m0[u] = mask[(unsigned)w];
+        m1[u] = mask[(unsigned)min(w + 1, words - 1)];
+      }
+    };
+    auto load = [&](int r) {
+#pragma unroll
+      for (int u = 0; u < RK_U; ++u) {
+        const int i = first + r * ROUND + u * RK_THREADS, j = min(i, v1 - 1), c = zr.col(j);
+        unsigned o = i == j ? ALL : 0;
+        if (mask) o &= __builtin_amdgcn_alignbit(m1[u], m0[u], c & 31);
+        ok[u] = o;
+        if (!__ballot(o != 0)) continue;
+        x[u] = __builtin_nontemporal_load(
+            reinterpret_cast<const typename R::vec*>(reinterpret_cast<const char*>(zr.base) + (unsigned)(16 * j)));
+        if (ru.bias)
+          bias[u] = *reinterpret_cast<const Floats<V>*>(reinterpret_cast<const char*>(ru.bias) + (unsigned)(4 * c));
+      }
+    };
+    if (rounds) {
+      if (mask) load_mask(0);
+      load(0);
+      if (mask && rounds > 1) load_mask(1);
+    }
     if (lists) {
       for (int i = threadIdx.x; i < ((v1 - v0) * V + 31) / 32; i += RK_THREADS) in.bits[i] = 0;
       if (threadIdx.x == 0) edge_bits = 0;
@@ -420,42 +479,6 @@ __global__ __launch_bounds__(RK_THREADS) void k_rank(const T* __restrict__ z, in
       raise2(v, m, s);
       if (m != -INFINITY) s += term2(v, m);
     }
-    // Rounds of loads: a round's logits and biases are on their way while the one before it is
-    // worked on, and its words of the mask while the one before that is.  Lanes past the
-    // piece's end load its last vector again.
-    typename R::vec x[RK_U];
-    Floats<V> bias[RK_U];
-    unsigned ok[RK_U], m0[RK_U], m1[RK_U];
-    const int rounds = (v1 - v0 + ROUND - 1) / ROUND;
-    const int first = v0 + (int)threadIdx.x;
-    auto load_mask = [&](int r) {
-#pragma unroll
-      for (int u = 0; u < RK_U; ++u) {
-        const int w = zr.col(min(first + r * ROUND + u * RK_THREADS, v1 - 1)) >> 5;
-        m0[u] = mask[(unsigned)w];
-        m1[u] = mask[(unsigned)min(w + 1, words - 1)];
-      }
-    };
-    auto load = [&](int r) {
-#pragma unroll
-      for (int u = 0; u < RK_U; ++u) {
-        const int i = first + r * ROUND + u * RK_THREADS, j = min(i, v1 - 1), c = zr.col(j);
-        unsigned o = i == j ? ALL : 0;
-        if (mask) o &= __builtin_amdgcn_alignbit(m1[u], m0[u], c & 31);
-        if (LISTS && lists) o &= ~(in.bits[(j - v0) * V >> 5] >> ((j - v0) * V & 31));
-        ok[u] = o;
-        if (!__ballot(o != 0)) continue;
-        x[u] = __builtin_nontemporal_load(
-            reinterpret_cast<const typename R::vec*>(reinterpret_cast<const char*>(zr.base) + (unsigned)(16 * j)));
-        if (ru.bias)
-          bias[u] = *reinterpret_cast<const Floats<V>*>(reinterpret_cast<const char*>(ru.bias) + (unsigned)(4 * c));
-      }
-    };
-    if (rounds) {
-      if (mask) load_mask(0);
-      load(0);
-      if (mask && rounds > 1) load_mask(1);
-    }
     for (int r = 0; r < rounds; ++r) {
       const int base = v0 + r * ROUND;
       if (r) best.look(found);
@@ -469,6 +492,10 @@ __global__ __launch_bounds__(RK_THREADS) void k_rank(const T* __restrict__ z, in
         } else {
 #pragma unroll
           for (int e = 0; e < V; ++e) w[u][e] = (float)x[u][e] + 0.0f;  // (-0 ties with 0)
+        }
+        if (LISTS && lists) {
+          const int at = (min(first + r * ROUND + u * RK_THREADS, v1 - 1) - v0) * V;
+          ok[u] &= ~(in.bits[at >> 5] >> (at & 31));
         }
         if (__ballot(ok[u] != ALL)) {
           const int off = (int)~ok[u];
@@ -573,10 +600,10 @@ __global__ __launch_bounds__(64 * WAVES) void k_rank_join(int parts, int k, cons
 
 }  // namespace
 
-// Pieces per row: enough workgroups to fill the GPU, each with at least a round of 16-bit
-// loads per wave; where lists are given, no more columns than a workgroup has bits for.
+// Pieces per row: enough workgroups to fill the GPU, each with two rounds of loads or more (one row of
+// 670,091 under rules, at least 2,048 | 4,096 | 8,192 columns: 14.9 | 14.0 | 15.7 us); where lists are given, no more columns than a workgroup has bits for.
 static int row_pieces(int rows, int cols, bool lists) {
-  const int want = (RK_WGS + rows - 1) / rows, most = (cols + 2047) / 2048;
+  const int want = (RK_WGS + rows - 1) / rows, most = (cols + 4095) / 4096;
   const int least = lists ? (cols + RK_BITS - 1) / RK_BITS : 1;
   return std::max(std::min(want, most), least);
 }
