@@ -16,96 +16,120 @@ typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef int i32x4 __attribute__((ext_vector_type(4)));
 typedef int i32x8 __attribute__((ext_vector_type(8)));
 
-// Eight consecutive elements of a row from element p on; ALIGNED: p is 16-byte aligned.
-template <typename T, bool ALIGNED>
-__device__ __forceinline__ void load8(const T* p, float (&x)[8]) {
-  if constexpr (ALIGNED) {
-    constexpr int V = 16 / (int)sizeof(T);
-    typedef T vec __attribute__((ext_vector_type(V)));
-#pragma unroll
-    for (int a = 0; a < 8 / V; ++a) {
-      const vec v = reinterpret_cast<const vec*>(p)[a];
-#pragma unroll
-      for (int e = 0; e < V; ++e) x[a * V + e] = (float)v[e];
-    }
-  } else {
-#pragma unroll
-    for (int e = 0; e < 8; ++e) x[e] = (float)p[e];
+// A thread takes 16 bytes of the dense matrix at a time, Q_U of them in flight; EACH elements,
+// whose codes are EACH / 2 bytes.  Rows that follow each other without a gap are one run of
+// pieces; otherwise the piece's row is looked up.  ALIGNED: every piece of the dense matrix is 16-byte aligned.
+constexpr int Q_U = 4;
+template <typename T>
+struct Piece {
+  static constexpr int EACH = 16 / (int)sizeof(T), LANES = 32 / EACH;  // lanes per block
+  typedef T vec __attribute__((ext_vector_type(EACH)));
+  static __device__ __forceinline__ int64_t offset(unsigned i, unsigned per_row, int64_t ld) {
+    if (per_row == 0) return (int64_t)i * EACH;
+    const unsigned row = i / per_row;
+    return (int64_t)row * ld + (i - row * per_row) * EACH;
   }
-}
-
-template <typename T, bool ALIGNED>
-__device__ __forceinline__ void store8(T* p, const float (&x)[8]) {
-  if constexpr (ALIGNED) {
-    constexpr int V = 16 / (int)sizeof(T);
-    typedef T vec __attribute__((ext_vector_type(V)));
-#pragma unroll
-    for (int a = 0; a < 8 / V; ++a) {
-      vec v;
-#pragma unroll
-      for (int e = 0; e < V; ++e) v[e] = (T)x[a * V + e];
-      reinterpret_cast<vec*>(p)[a] = v;
-    }
-  } else {
-#pragma unroll
-    for (int e = 0; e < 8; ++e) p[e] = (T)x[e];
-  }
-}
+};
 
 // 2^(byte - 127), or NaN for 255.
 __device__ __forceinline__ float scale_of(unsigned byte) {
   return __uint_as_float(byte == 0 ? 0x00400000u : byte == 255 ? 0x7fc00000u : byte << 23);
 }
 
-// Four lanes hold a block of 32.  The scale's exponent is the largest magnitude's less 2,
+// Eight lanes (16-bit types: four) hold a block of 32.  The scale's exponent is the largest magnitude's less 2,
 // taken from its bits (which order magnitudes as integers, infinities and NaN on top).
 // The conversion divides by the scale (a power of two, the exponent bits of a float: 2^-127
 // is the field's 0) and rounds to nearest, ties to the even code, at most 6 in magnitude.
 template <typename T, bool ALIGNED>
-__global__ __launch_bounds__(Q_THREADS) void k_quantize(const T* __restrict__ x, int64_t ld, int64_t n8, int row8,
-                                                        uint32_t* __restrict__ codes, uint8_t* __restrict__ scales) {
-  const int64_t i = (int64_t)blockIdx.x * Q_THREADS + threadIdx.x;
-  if (i >= n8) return;  // (whole blocks: n8 is a multiple of 4)
-  const int64_t row = i / row8, c = i - row * row8;
-  float v[8];
-  load8<T, ALIGNED>(x + row * ld + c * 8, v);
-  unsigned big = 0;
+__global__ __launch_bounds__(Q_THREADS) void k_quantize(const T* __restrict__ x, int64_t ld, unsigned n, unsigned per_row,
+                                                        void* __restrict__ codes, uint8_t* __restrict__ scales) {
+  using P = Piece<T>;
+  const unsigned first = blockIdx.x * (Q_THREADS * Q_U) + threadIdx.x;
+  const int lane = threadIdx.x & 63;
+  typename P::vec v[Q_U];
 #pragma unroll
-  for (int e = 0; e < 8; ++e) big = max(big, __float_as_uint(v[e]) & 0x7fffffffu);
-  big = max(big, (unsigned)__shfl_xor((int)big, 1));
-  big = max(big, (unsigned)__shfl_xor((int)big, 2));
-  const int ex = (int)(big >> 23);
-  const int byte = big == 0 ? 0 : ex == 255 ? 255 : max(ex - 2, 0);
-  const float scale = scale_of((unsigned)byte);
-  unsigned out = 0;
-  out = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(out, v[0], v[1], scale, 0);
-  out = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(out, v[2], v[3], scale, 1);
-  out = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(out, v[4], v[5], scale, 2);
-  out = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(out, v[6], v[7], scale, 3);
-  codes[i] = byte == 255 ? 0 : out;
-  if ((i & 3) == 0) scales[i >> 2] = (uint8_t)byte;
+  for (int u = 0; u < Q_U; ++u) {
+    const unsigned i = first + u * Q_THREADS;
+    if (i >= n) break;  // (whole blocks: n is a multiple of their lanes)
+    const T* p = x + P::offset(i, per_row, ld);
+    if constexpr (ALIGNED) {
+      v[u] = __builtin_nontemporal_load(reinterpret_cast<const typename P::vec*>(p));
+    } else {
+#pragma unroll
+      for (int e = 0; e < P::EACH; ++e) v[u][e] = p[e];
+    }
+  }
+#pragma unroll
+  for (int u = 0; u < Q_U; ++u) {
+    const unsigned i = first + u * Q_THREADS;
+    if (i >= n) break;
+    float f[P::EACH];
+    unsigned big = 0;
+#pragma unroll
+    for (int e = 0; e < P::EACH; ++e) {
+      f[e] = (float)v[u][e];
+      big = max(big, __float_as_uint(f[e]) & 0x7fffffffu);
+    }
+    big = max(big, lane_xor<1>(big, lane));
+    big = max(big, lane_xor<2>(big, lane));
+    if constexpr (P::LANES == 8) big = max(big, lane_xor<4>(big, lane));
+    const int ex = (int)(big >> 23);
+    const int byte = big == 0 ? 0 : ex == 255 ? 255 : max(ex - 2, 0);
+    const float scale = scale_of((unsigned)byte);
+    unsigned out = 0;
+    out = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(out, f[0], f[1], scale, 0);
+    out = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(out, f[2], f[3], scale, 1);
+    if constexpr (P::EACH == 8) {
+      out = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(out, f[4], f[5], scale, 2);
+      out = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(out, f[6], f[7], scale, 3);
+    }
+    if (byte == 255) out = 0;
+    if constexpr (P::EACH == 8)
+      reinterpret_cast<uint32_t*>(codes)[i] = out;
+    else
+      reinterpret_cast<uint16_t*>(codes)[i] = (uint16_t)out;
+    if (i % P::LANES == 0) scales[i / P::LANES] = (uint8_t)byte;
+  }
 }
 
 template <typename T, bool ALIGNED>
-__global__ __launch_bounds__(Q_THREADS) void k_dequantize(const uint32_t* __restrict__ codes,
-                                                          const uint8_t* __restrict__ scales, int64_t n8, int row8,
-                                                          T* __restrict__ out, int64_t ld) {
-  const int64_t i = (int64_t)blockIdx.x * Q_THREADS + threadIdx.x;
-  if (i >= n8) return;
-  const int64_t row = i / row8, c = i - row * row8;
-  const unsigned w = codes[i];
-  const float s = scale_of(scales[i >> 2]);
-  float v[8];
-  const bool nan = scales[i >> 2] == 255;
-  auto two = [&](f32x2 p, int at) {
-    v[at] = nan ? NAN : p[0];
-    v[at + 1] = nan ? NAN : p[1];
-  };
-  two(__builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, s, 0), 0);
-  two(__builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, s, 1), 2);
-  two(__builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, s, 2), 4);
-  two(__builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, s, 3), 6);
-  store8<T, ALIGNED>(out + row * ld + c * 8, v);
+__global__ __launch_bounds__(Q_THREADS) void k_dequantize(const void* __restrict__ codes, const uint8_t* __restrict__ scales,
+                                                          unsigned n, unsigned per_row, T* __restrict__ out, int64_t ld) {
+  using P = Piece<T>;
+  const unsigned first = blockIdx.x * (Q_THREADS * Q_U) + threadIdx.x;
+  unsigned w[Q_U], byte[Q_U];
+#pragma unroll
+  for (int u = 0; u < Q_U; ++u) {
+    const unsigned i = first + u * Q_THREADS;
+    if (i >= n) break;
+    w[u] = P::EACH == 8 ? reinterpret_cast<const uint32_t*>(codes)[i] : reinterpret_cast<const uint16_t*>(codes)[i];
+    byte[u] = scales[i / P::LANES];
+  }
+#pragma unroll
+  for (int u = 0; u < Q_U; ++u) {
+    const unsigned i = first + u * Q_THREADS;
+    if (i >= n) break;
+    const float s = scale_of(byte[u]);
+    const bool nan = byte[u] == 255;
+    typename P::vec v;
+    auto two = [&](f32x2 p, int at) {
+      v[at] = (T)(nan ? NAN : p[0]);
+      v[at + 1] = (T)(nan ? NAN : p[1]);
+    };
+    two(__builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w[u], s, 0), 0);
+    two(__builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w[u], s, 1), 2);
+    if constexpr (P::EACH == 8) {
+      two(__builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w[u], s, 2), 4);
+      two(__builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w[u], s, 3), 6);
+    }
+    T* p = out + P::offset(i, per_row, ld);
+    if constexpr (ALIGNED) {
+      __builtin_nontemporal_store(v, reinterpret_cast<typename P::vec*>(p));
+    } else {
+#pragma unroll
+      for (int e = 0; e < P::EACH; ++e) p[e] = v[e];
+    }
+  }
 }
 
 // ---------------------------------------------------------------------------
@@ -351,26 +375,28 @@ __global__ __launch_bounds__(FM_THREADS, 4) void k_fp4_logits(Fp4Rows h, int B, 
 
 template <typename T>
 hipError_t quantize_as(const void* x, int64_t ld, int rows, int cols, uint8_t* codes, uint8_t* scales, hipStream_t st) {
-  const int64_t n8 = (int64_t)rows * cols / 8;
-  const bool al = ((uintptr_t)x & 15) == 0 && ld * sizeof(T) % 16 == 0;
-  const dim3 grid((unsigned)((n8 + Q_THREADS - 1) / Q_THREADS)), block(Q_THREADS);
+  const unsigned n = (unsigned)((int64_t)rows * cols / Piece<T>::EACH);
+  const unsigned per_row = ld == cols ? 0 : (unsigned)(cols / Piece<T>::EACH);
+  const bool al = ((uintptr_t)x & 15) == 0 && (ld * sizeof(T) % 16 == 0 || rows == 1);
+  const dim3 grid((n + Q_THREADS * Q_U - 1) / (Q_THREADS * Q_U)), block(Q_THREADS);
   if (al)
-    hipLaunchKernelGGL((k_quantize<T, true>), grid, block, 0, st, (const T*)x, ld, n8, cols / 8, (uint32_t*)codes, scales);
+    hipLaunchKernelGGL((k_quantize<T, true>), grid, block, 0, st, (const T*)x, ld, n, per_row, codes, scales);
   else
-    hipLaunchKernelGGL((k_quantize<T, false>), grid, block, 0, st, (const T*)x, ld, n8, cols / 8, (uint32_t*)codes, scales);
+    hipLaunchKernelGGL((k_quantize<T, false>), grid, block, 0, st, (const T*)x, ld, n, per_row, codes, scales);
   return hipGetLastError();
 }
 
 template <typename T>
 hipError_t dequantize_as(const uint8_t* codes, const uint8_t* scales, int rows, int cols, void* out, int64_t ld,
                          hipStream_t st) {
-  const int64_t n8 = (int64_t)rows * cols / 8;
-  const bool al = ((uintptr_t)out & 15) == 0 && ld * sizeof(T) % 16 == 0;
-  const dim3 grid((unsigned)((n8 + Q_THREADS - 1) / Q_THREADS)), block(Q_THREADS);
+  const unsigned n = (unsigned)((int64_t)rows * cols / Piece<T>::EACH);
+  const unsigned per_row = ld == cols ? 0 : (unsigned)(cols / Piece<T>::EACH);
+  const bool al = ((uintptr_t)out & 15) == 0 && (ld * sizeof(T) % 16 == 0 || rows == 1);
+  const dim3 grid((n + Q_THREADS * Q_U - 1) / (Q_THREADS * Q_U)), block(Q_THREADS);
   if (al)
-    hipLaunchKernelGGL((k_dequantize<T, true>), grid, block, 0, st, (const uint32_t*)codes, scales, n8, cols / 8, (T*)out, ld);
+    hipLaunchKernelGGL((k_dequantize<T, true>), grid, block, 0, st, codes, scales, n, per_row, (T*)out, ld);
   else
-    hipLaunchKernelGGL((k_dequantize<T, false>), grid, block, 0, st, (const uint32_t*)codes, scales, n8, cols / 8, (T*)out, ld);
+    hipLaunchKernelGGL((k_dequantize<T, false>), grid, block, 0, st, codes, scales, n, per_row, (T*)out, ld);
   return hipGetLastError();
 }
 

@@ -63,6 +63,32 @@ struct Row {
   }
 };
 
+// v of lane ^ X, without a trip through LDS.
+template <int CTRL>
+__device__ __forceinline__ unsigned dpp(unsigned v) {
+  return (unsigned)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, 0xf, 0xf, true);
+}
+template <int X>
+__device__ __forceinline__ unsigned lane_xor(unsigned v, int) {
+  if constexpr (X == 1) return dpp<0xb1>(v);         // quad_perm [1, 0, 3, 2]
+  else if constexpr (X == 2) return dpp<0x4e>(v);    // quad_perm [2, 3, 0, 1]
+  else if constexpr (X == 4) return dpp<0x1b>(dpp<0x141>(v));  // half row mirrored (xor 7), then xor 3
+  else if constexpr (X == 8) return dpp<0x128>(v);   // row rotated by 8
+  else if constexpr (X == 16) {
+    const auto s = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+    const unsigned a = s[0], b = s[1];
+    return __builtin_amdgcn_inverse_ballot_w64(0xffff0000ffff0000ull) ? a : b;
+  } else {
+    const auto s = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+    const unsigned a = s[0], b = s[1];
+    return __builtin_amdgcn_inverse_ballot_w64(0xffffffff00000000ull) ? a : b;
+  }
+}
+template <int X>
+__device__ __forceinline__ u64 lane_xor(u64 v, int lane) {
+  return ((u64)lane_xor<X>((unsigned)(v >> 32), lane) << 32) | lane_xor<X>((unsigned)v, lane);
+}
+
 // Entries [*q0, *q1) of row i of a list, kept inside [*first, *first + nnz) whatever
 // indptr holds.
 __device__ __forceinline__ void list_range(const IdLists& a, int i, int* q0, int* q1) {
