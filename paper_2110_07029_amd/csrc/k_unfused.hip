@@ -548,9 +548,12 @@ __global__ __launch_bounds__(WG_THREADS) void k_stored_wgrad(float* __restrict__
                                                              const typename Mma<BF16>::elem* __restrict__ H,
                                                              int ld_t, int B, float lr) {
   using M = Mma<BF16>;
-  constexpr int KL = M::KL;  // rows per lane and product
+  constexpr int KL = M::KL;                        // rows per lane and product
+  constexpr int ROWS = 64, NR = ROWS / 2;          // rows per round, and a lane's of them
   const int lane = threadIdx.x & 63, g = lane >> 5, n = lane & 31;
-  const int tile = (int)blockIdx.x * (WG_THREADS / 64) + (int)(threadIdx.x >> 6);
+  // neighbouring tiles on one XCD: a row of dZ's runs of 128 bytes lie side by side
+  const int per = (int)gridDim.x / 8, wg = (int)(blockIdx.x % 8) * per + (int)blockIdx.x / 8;
+  const int tile = wg * (WG_THREADS / 64) + (int)(threadIdx.x >> 6);
   if (tile * OUT_TILE >= L) return;
   const int label = tile * OUT_TILE + n;  // (dZ's rows reach past L: ldz covers whole tiles)
   f32x16 acc[4];
@@ -559,48 +562,68 @@ __global__ __launch_bounds__(WG_THREADS) void k_stored_wgrad(float* __restrict__
 #pragma unroll
     for (int r = 0; r < 16; ++r) acc[hb][r] = 0.0f;
   float db = 0.0f;
-  for (int i0 = 0; i0 < B; i0 += M::KC) {
-    float d[KL];
+  float next[NR];
+  auto load = [&](int i0) {
 #pragma unroll
-    for (int j = 0; j < KL; ++j) {
-      const int i = i0 + KL * g + j;
-      d[j] = i < B ? dZ[(size_t)i * ldz + label] : 0.0f;
+    for (int j = 0; j < NR; ++j) {
+      const int i = i0 + M::KC * (j / KL) + KL * g + j % KL;
+      next[j] = i < B ? __builtin_nontemporal_load(dZ + (size_t)i * ldz + label) : 0.0f;
+    }
+  };
+  load(0);
+  for (int i0 = 0; i0 < B; i0 += ROWS) {
+    float d[NR];
+#pragma unroll
+    for (int j = 0; j < NR; ++j) {
+      d[j] = next[j];
       db += d[j];
     }
+    if (i0 + ROWS < B) load(i0 + ROWS);
     if constexpr (BF16) {
-      bf16x8 a;
 #pragma unroll
-      for (int j = 0; j < KL; ++j) a[j] = (bf16)d[j];
+      for (int c = 0; c < ROWS / M::KC; ++c) {
+        bf16x8 a;
 #pragma unroll
-      for (int hb = 0; hb < 4; ++hb) {
-        const bf16x8 b = *reinterpret_cast<const bf16x8*>(H + (size_t)(32 * hb + n) * ld_t + i0 + KL * g);
-        acc[hb] = M::mma(a, b, acc[hb]);
+        for (int j = 0; j < 8; ++j) a[j] = (bf16)d[8 * c + j];
+#pragma unroll
+        for (int hb = 0; hb < 4; ++hb) {
+          const bf16x8 b = *reinterpret_cast<const bf16x8*>(H + (size_t)(32 * hb + n) * ld_t + i0 + M::KC * c + KL * g);
+          acc[hb] = M::mma(a, b, acc[hb]);
+        }
       }
     } else {
-      const int i = i0 + g;
 #pragma unroll
-      for (int hb = 0; hb < 4; ++hb) acc[hb] = M::mma(d[0], i < B ? H[(size_t)i * HID + 32 * hb + n] : 0.0f, acc[hb]);
+      for (int c = 0; c < ROWS / M::KC; ++c) {
+        const int i = i0 + M::KC * c + g;
+#pragma unroll
+        for (int hb = 0; hb < 4; ++hb) acc[hb] = M::mma(d[c], i < B ? H[(size_t)i * HID + 32 * hb + n] : 0.0f, acc[hb]);
+      }
     }
   }
   db += __shfl_xor(db, 32);
   if (g == 0 && label < L) b2[label] = fmaf(-lr, db, b2[label]);
 #pragma unroll
-  for (int hb = 0; hb < 4; ++hb)
+  for (int hb = 0; hb < 4; ++hb) {
+    float w[16];
 #pragma unroll
     for (int r = 0; r < 16; ++r) {
       const int l = tile * OUT_TILE + 8 * (r >> 2) + 4 * g + (r & 3);
-      if (l < L) {
-        float* w = W2 + (size_t)l * HID + 32 * hb + n;
-        *w = fmaf(-lr, acc[hb][r], *w);
-      }
+      w[r] = l < L ? W2[(size_t)l * HID + 32 * hb + n] : 0.0f;
     }
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      const int l = tile * OUT_TILE + 8 * (r >> 2) + 4 * g + (r & 3);
+      if (l < L) W2[(size_t)l * HID + 32 * hb + n] = fmaf(-lr, acc[hb][r], w[r]);
+    }
+  }
 }
 
 hipError_t launch_stored_wgrad(bool use_bf16, float* W2, float* b2, int L, const float* dZ, int ldz, const void* H1,
                                void* H1T, int ld_t, int rows_pad, int B, float lr, hipStream_t st) {
   const int n_tiles = (L + OUT_TILE - 1) / OUT_TILE, rt = (B + 63) / 64 * 64;
   if (ldz < n_tiles * OUT_TILE || rt > ld_t || rt > rows_pad) return hipErrorInvalidValue;
-  const dim3 grid((n_tiles + WG_THREADS / 64 - 1) / (WG_THREADS / 64)), block(WG_THREADS);
+  const int wgs = (n_tiles + WG_THREADS / 64 - 1) / (WG_THREADS / 64);
+  const dim3 grid((wgs + 7) / 8 * 8), block(WG_THREADS);
   if (use_bf16) {
     hipLaunchKernelGGL(k_transpose_h, dim3(rt / 64), dim3(256), 0, st, (const bf16*)H1, (bf16*)H1T, ld_t);
     hipLaunchKernelGGL(k_stored_wgrad<true>, grid, block, 0, st, W2, b2, L, dZ, ldz, (const bf16*)H1T, ld_t, B, lr);

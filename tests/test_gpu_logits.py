@@ -342,6 +342,43 @@ def test_topk_lists_with_malformed_indptr_are_read_inside_their_entries():
     check_rank(got, ref.scores(x, seen=seen, presence=3.0), 5)
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("L,low,count,k", [(200_000, 0, 3000, 64), (200_000, 150_000, 9000, 5), (3000, 0, 2900, 64),
+                                           (4100, 4000, 100, 64)])
+def test_topk_lists_that_crowd_a_range(dtype, L, low, count, k):
+    # more distinct ids side by side than a table holds, in both lists, each of them up to three times
+    r = np.random.default_rng(L + count)
+    ids = low + r.permutation(count)[:count]
+    seen = [np.concatenate([ids, ids[::2], ids[::7]]), [], ids[:3]]
+    row_bias = [(ids[::3], r.normal(0, 3, len(ids[::3])).astype(np.float32)), ([low], np.array([9.0], np.float32)), ([], [])]
+    z = strided(r.normal(0, 2, (3, L)), dtype, 1, 3)
+    c, keep = lists(seen, L)
+    c2, keep2 = lists(row_bias, L, values=True)
+    kw = dict(repetition=1.1, frequency=0.3, presence=0.1)
+    check_rank(rank(z, k, asgd.logit_rules(seen=c, row_bias=c2, **kw)),
+               ref.scores(host(z), seen=seen, row_bias=row_bias, **kw), k)
+
+
+def test_topk_twice_is_bitwise_the_same_and_stays_in_its_rows():
+    B, L, k = 30, 50_000, 20
+    r = np.random.default_rng(77)
+    z = dev(r.normal(0, 2, (B, L)).astype(np.float32))
+    o, rules, allowed, keep = random_rules(r, B, L, 400, True, 30, 0.8)
+    big = [torch.full((B + 2, k), -7, dtype=torch.int32, device="cuda"), torch.full((B + 2, k), 7.0, device="cuda"),
+           torch.full((B + 2,), 7.0, device="cuda")]
+    ids, sc, lse = (t[1:B + 1] for t in big)
+    first = None
+    for _ in range(4):
+        ws = scratch(asgd.asgd_logits_topk_workspace(B, L, k))
+        asgd.asgd_logits_topk(asgd.matrix(z), k, ids, sc, rules=rules, lse=lse, workspace=ws)
+        now = [t.clone() for t in (ids, sc, lse)]
+        assert first is None or all(torch.equal(a, b) for a, b in zip(first, now))
+        first = first or now
+    for t, v in zip(big, (-7, 7.0, 7.0)):
+        assert bool((t[0] == v).all() and (t[-1] == v).all())
+    check_rank(first, ref.scores(host(z), **o), k, allowed)
+
+
 # ---------------------------------------------------------------- distillation
 def teacher(r, B, L, k, empty=0.2):
     ids = np.stack([r.permutation(max(L, k))[:k] for _ in range(B)]).astype(np.int32)
@@ -503,6 +540,34 @@ def test_rows_past_two_to_the_31_elements():
     loss = distill(near, dev(ids), dev(t), 1.0, alone)
     assert torch.equal(distill(z, dev(ids), dev(t), 1.0, z), loss)
     assert torch.equal(z, alone)
+
+
+def test_fp4_rows_past_two_to_the_31_elements():
+    B, L, ld = 520, 1000, (1 << 22) + 8
+    flush("  allocating 8.8 GB")
+    big = torch.zeros((B, ld), dtype=torch.bfloat16, device="cuda")
+    r = np.random.default_rng(5)
+    x = big[:, 5:133]
+    x.copy_(torch.from_numpy(r.normal(0, 1, (B, 128))))
+    codes = torch.empty((B, 64), dtype=torch.uint8, device="cuda")
+    scales = torch.empty((B, 4), dtype=torch.uint8, device="cuda")
+    h = asgd.fp4_matrix(codes, scales)
+    asgd.asgd_fp4_quantize(asgd.matrix(x), h)
+    v, c, s = ref.quantize(host(x))
+    assert np.array_equal(ref.values_of(codes.cpu().numpy(), scales.cpu().numpy()), v)
+    wc, wsc = (dev(t) for t in label_matrix(L, 9))
+    w = asgd.fp4_matrix(wc, wsc)
+    for n in (B, 20):  # many rows and few
+        z = big[:n, 200:200 + L] if n > 32 else big[-n:, 200:200 + L]
+        a = asgd.fp4_matrix(codes[:n] if n > 32 else codes[-n:], scales[:n] if n > 32 else scales[-n:])
+        asgd.asgd_fp4_logits(a, w, asgd.matrix(z))
+        near = torch.empty((n, L), dtype=torch.bfloat16, device="cuda")
+        asgd.asgd_fp4_logits(a, w, asgd.matrix(near))
+        assert torch.equal(z, near)
+        assert bool((big[:, 200 + L:200 + L + 64] == 0).all() and (big[:, 133:200] == 0).all())
+    big[:, 5:133].zero_()
+    asgd.asgd_fp4_dequantize(h, asgd.matrix(x))
+    assert torch.equal(x.cpu(), torch.from_numpy(v).bfloat16())
 
 
 def test_two_streams_at_once():
