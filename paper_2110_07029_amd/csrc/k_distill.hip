@@ -3,7 +3,7 @@
 // With p the softmax of a row of z over the temperature T and q that of the teacher's
 // k logits, loss = T^2 sum q (ln q - ln p) and dz = w T (p - q).  The gradient needs the row's
 // sum, so a row is read twice unless something holds it meanwhile:
-//   k_distill_row    a row that a workgroup's registers hold (128 KB): one read, one write;
+//   k_distill_row    a row that a workgroup's registers hold (128 KB, many rows: 256 KB): one read, one write;
 //   k_distill_sums   longer rows, first pass: (max, sum of exponentials) per piece of a row, and
 //                    the student's logits of the teacher's labels (the gradient may take z's place);
 //   k_distill_grad   second pass: joins the pieces' sums and writes the piece's gradient.
@@ -23,6 +23,7 @@ namespace {
 constexpr int KD_THREADS = 256;
 constexpr int KD_WAVES = KD_THREADS / 64;
 constexpr int KD_WGS = 2048;  // workgroups wanted per pass of a slab
+constexpr int KD_ROWS = 512;
 constexpr int64_t KD_SLAB = 192 << 20;
 
 __device__ __forceinline__ bool finite(float v) { return (__float_as_uint(v) & 0x7f800000u) != 0x7f800000u; }
@@ -449,6 +450,10 @@ static hipError_t distill_as(const DistillJob& j, const DistillShape& sh, void* 
   if (n_vec <= 2 * 256) return distill_rows<T, 256, 2>(j, ce, ce_lo, st);
   if (n_vec <= 8 * 256) return distill_rows<T, 256, 8>(j, ce, ce_lo, st);
   if (n_vec <= 8 * 1024) return distill_rows<T, 1024, 8>(j, ce, ce_lo, st);
+  // 256 KB: half of a compute unit's registers, so one row at a time on each, and worth it from two rows for
+  // each on (two passes | this: 512 x 60,000 fp32 65 | 51 us, 300 x 100,000 bf16 43 | 47 us; rows of 400 KB in the
+  // same way no longer gain: 512 x 205,443 bf16 120 | 121 us)
+  if (j.n_rows >= KD_ROWS && n_vec <= 16 * 1024) return distill_rows<T, 1024, 16>(j, ce, ce_lo, st);
   const int vps = (n_vec + sh.splits - 1) / sh.splits;
   float2* part = (float2*)ws;
   float* z_t = (float*)((char*)ws + part_bytes(sh, j.n_rows));

@@ -418,7 +418,8 @@ def distill_bounds(z, ids, t, T, w, p, q, dtype):
 
 
 DISTILL = [(1, 1, 1, 1.0), (1, 7, 3, 2.0), (3, 64, 5, 0.5), (4, 1000, 32, 1.0), (128, 1000, 5, 2.0), (5, 8193, 512, 4.0),
-           (2, 30_000, 32, 1.0), (3, 65_537, 64, 1.5), (1, 205_443, 100, 2.0), (2100, 65, 4, 1.0)]
+           (2, 30_000, 32, 1.0), (3, 65_537, 64, 1.5), (1, 205_443, 100, 2.0), (2100, 65, 4, 1.0),
+           (520, 33_001, 6, 1.0), (40, 8200, 9, 3.0), (30, 2049, 3, 1.0)]
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
