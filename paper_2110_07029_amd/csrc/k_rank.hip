@@ -369,7 +369,8 @@ __global__ __launch_bounds__(RK_THREADS) void k_rank(const T* __restrict__ z, in
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int parts = splits + ranges;
-  const int row = blockIdx.x / parts, piece = blockIdx.x % parts;
+  // (rows side by side: workgroups that run together read the same columns' biases)
+  const int n_rows = (int)(gridDim.x / (unsigned)parts), row = blockIdx.x % n_rows, piece = blockIdx.x / n_rows;
   const R zr(const_cast<T*>(z), ld, row, L);
   const uint32_t* mask = ru.allowed ? ru.allowed + (int64_t)row * ru.allowed_ld : nullptr;
   const int words = (L + 31) >> 5;
@@ -533,8 +534,8 @@ __global__ __launch_bounds__(RK_THREADS) void k_rank(const T* __restrict__ z, in
     put_best(best.list, lane, k, row, ids, scores);
     if (lse && lane == 0) lse[row] = lse_of(best.list, m, s);
   } else {
-    if (lane < k) part[(int64_t)blockIdx.x * k + lane] = best.list;
-    if (lse && lane == 0) part_ms[blockIdx.x] = make_float2(m, s);
+    if (lane < k) part[((int64_t)row * parts + piece) * k + lane] = best.list;
+    if (lse && lane == 0) part_ms[(int64_t)row * parts + piece] = make_float2(m, s);
   }
 }
 
