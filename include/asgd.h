@@ -445,8 +445,8 @@ asgd_status asgd_fp4_logits(const asgd_matrix* h, const asgd_fp4* h4, const asgd
  *                               - frequency * c_j - presence
  *   s_j = t + bias[j] + row_bias of j,  formed in float64, rounded once to float
  * and labels whose bit of `allowed` is 0 are left out.  Zero-initialise the
- * struct for no rules (repetition 0 counts as 1).  Ids outside [0, L) are
- * skipped; of row_bias entries of one row that name the same id the last one
+ * struct for no rules (repetition 0 counts as 1).  Lists hold below 2^30
+ * entries; ids outside [0, L) are skipped; of row_bias entries of one row that name the same id the last one
  * counts. */
 typedef struct asgd_logit_rules {
   const float* bias;       /* device [L], or NULL */
@@ -480,7 +480,7 @@ asgd_status asgd_logits_topk(const asgd_matrix* z, const asgd_logit_rules* rules
  * and gradient 0.  weights: device float [B] or NULL for 1 / B.  loss_rows:
  * device float [B].  grad: NULL for the loss alone, or a matrix of z's shape
  * and type, which may be z itself (the same data and ld) but not overlap it
- * otherwise.  1 <= k <= 512, T > 0 and finite.  A logit that is NaN or +inf makes its row's
+ * otherwise.  1 <= k <= 512, T in [1e-6, 1e6].  A logit that is NaN or +inf makes its row's
  * loss and gradient NaN; a label of logit -inf has p = 0. */
 asgd_status asgd_distill_workspace(int32_t n_rows, int32_t n_cols, int32_t k, size_t* bytes);
 asgd_status asgd_distill(const asgd_matrix* z, const int32_t* t_ids, const float* t_logits, int32_t k,

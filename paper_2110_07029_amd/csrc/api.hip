@@ -1137,8 +1137,7 @@ asgd_status asgd_distill_step(asgd_model* m, const asgd_csr* x, const int32_t* t
   if (s) return s;
   if (!m->unfused) return fail(ASGD_ESTATE, "a distillation step needs a model with ASGD_UNFUSED_OUTPUT");
   if (k < 1 || k > DISTILL_MAX_K) return fail(ASGD_EINVAL, "k must be in [1, 512]");
-  if (!(temperature > 0.0f) || !isfinite(temperature))
-    return fail(ASGD_EINVAL, "temperature must be positive and finite");
+  if ((s = check_temperature(temperature))) return s;
   if (!(lr == lr)) return fail(ASGD_EINVAL, "lr is NaN");
   if (!t_ids || !t_logits) return fail(ASGD_EINVAL, "t_ids and t_logits must be non-NULL");
   if (((uintptr_t)t_ids | (uintptr_t)t_logits) % 4) return fail(ASGD_EINVAL, "t_ids and t_logits must be 4-byte aligned");

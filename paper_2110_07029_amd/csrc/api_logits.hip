@@ -33,6 +33,7 @@ asgd_status check_list(const asgd_csr* a, const char* name, int rows, int cols, 
   if (a->n_rows != rows) return set_error_named(ASGD_EINVAL, name, ".n_rows differs from the logits' rows");
   if (a->n_cols != cols) return set_error_named(ASGD_EINVAL, name, ".n_cols differs from the logits' columns");
   if (a->nnz < 0) return set_error_named(ASGD_EINVAL, name, ".nnz must be >= 0");
+  if (a->nnz >= (1 << 30)) return set_error_named(ASGD_ERANGE, name, ".nnz must be < 2^30");
   if (!a->indptr) return set_error_named(ASGD_EINVAL, name, ".indptr is NULL");
   if (a->nnz > 0 && !a->indices) return set_error_named(ASGD_EINVAL, name, ".indices is NULL");
   if (values && a->nnz > 0 && !a->values) return set_error_named(ASGD_EINVAL, name, ".values is NULL");
@@ -97,6 +98,12 @@ asgd_status check_rules(const asgd_logit_rules* r, int rows, int cols) {
     return set_error(ASGD_EINVAL, "rules.frequency and rules.presence must be finite");
   TRY(check_list(r->seen, "rules.seen", rows, cols, false));
   return check_list(r->row_bias, "rules.row_bias", rows, cols, true);
+}
+
+asgd_status check_temperature(float t) {
+  if (!(t > 0.0f) || !isfinite(t)) return set_error(ASGD_EINVAL, "temperature must be positive and finite");
+  if (t < 1e-6f || t > 1e6f) return set_error(ASGD_ERANGE, "temperature must be in [1e-6, 1e6]");
+  return ASGD_OK;
 }
 
 RankRules rules_dev(const asgd_logit_rules* r, int row0) {
@@ -272,8 +279,7 @@ asgd_status asgd_distill(const asgd_matrix* z, const int32_t* t_ids, const float
                          void* ws, size_t ws_bytes, void* hip_stream) {
   TRY(check_matrix(z, "z"));
   if (k < 1 || k > DISTILL_MAX_K) return set_error(ASGD_EINVAL, "k must be in [1, 512]");
-  if (!(temperature > 0.0f) || !isfinite(temperature))
-    return set_error(ASGD_EINVAL, "temperature must be positive and finite");
+  TRY(check_temperature(temperature));
   if (!t_ids || !t_logits || !loss_rows) return set_error(ASGD_EINVAL, "t_ids, t_logits and loss_rows must be non-NULL");
   if (((uintptr_t)t_ids | (uintptr_t)t_logits | (uintptr_t)loss_rows | (uintptr_t)weights) % 4)
     return set_error(ASGD_EINVAL, "t_ids, t_logits, weights and loss_rows must be 4-byte aligned");

@@ -77,8 +77,8 @@ __device__ __forceinline__ float soft(float x, float m, float f, float ce, float
     const float t = d * ce;
     const float r = fmaf(d, ce, -t) + d * ce_lo;
     const float p = __builtin_amdgcn_exp2f(t);
-    // (a label of -inf: p = 0, r is NaN; a row whose f is NaN stays NaN)
-    return f * (d == -INFINITY ? 0.0f : fmaf(p, r * LN2, p));
+    // (far below the maximum, or -inf: p = 0 and r is none; a row whose f is NaN stays NaN)
+    return f * (t == -INFINITY ? 0.0f : fmaf(p, r * LN2, p));
   } else {
     return f * __builtin_amdgcn_exp2f(d * ce);
   }

@@ -48,7 +48,10 @@ __device__ __forceinline__ unsigned order_of(float v) {
 __device__ __forceinline__ float of_order(unsigned o) {
   return __uint_as_float((int)o < 0 ? o & 0x7fffffffu : ~o);
 }
-__device__ __forceinline__ u64 key_of(float v, int label) { return ((u64)order_of(v) << 32) | (unsigned)~label; }
+// (+ 0: a negative zero ties with zero)
+__device__ __forceinline__ u64 key_of(float v, int label) {
+  return ((u64)order_of(v + 0.0f) << 32) | (unsigned)~label;
+}
 
 __device__ __forceinline__ unsigned lane_of(unsigned v, int l) { return (unsigned)__builtin_amdgcn_readlane((int)v, l); }
 __device__ __forceinline__ u64 lane_of(u64 v, int l) {
@@ -262,7 +265,7 @@ __device__ __forceinline__ float listed_score(const Listed& l, const RankRules& 
   if (n) t = (t > 0.0 ? t / ru.repetition : t * ru.repetition) - ru.frequency * (double)n - ru.presence;
   t += (double)l.bias;
   if (last) t += (double)ru.row_bias.values[b0 + last - 1];
-  return (float)t + 0.0f;
+  return (float)t;
 }
 
 // The listed labels in [lo, hi).
@@ -468,7 +471,7 @@ __global__ __launch_bounds__(RK_THREADS) void k_rank(const T* __restrict__ z, in
           for (int e = 0; e < V; ++e) w[u][e] = (float)x[u][e] + bias[u].v[e];
         } else {
 #pragma unroll
-          for (int e = 0; e < V; ++e) w[u][e] = (float)x[u][e] + 0.0f;  // (-0 ties with 0)
+          for (int e = 0; e < V; ++e) w[u][e] = (float)x[u][e];
         }
         if (LISTS && lists) {
           const int at = (min(first + r * ROUND + u * RK_THREADS, v1 - 1) - v0) * V;

@@ -18,6 +18,7 @@ asgd_status check_matrix(const asgd_matrix* a, const char* name);
 asgd_status check_fp4(const asgd_fp4* q, const char* name);
 // The rules for rows of `cols` labels, `rows` of them.
 asgd_status check_rules(const asgd_logit_rules* r, int rows, int cols);
+asgd_status check_temperature(float t);
 // The rules as the kernels take them, from row `row0` on.
 RankRules rules_dev(const asgd_logit_rules* r, int row0);
 // The device memory that the rules name belongs to the current device.

@@ -195,6 +195,20 @@ def test_fp4_logits_of_nan_blocks_stay_in_their_rows_and_labels():
     want = np.zeros((40, 70), bool)
     want[33], want[:, 5] = True, True
     assert np.array_equal(nan, want)
+    # bf16 rows, many and few: NaN and infinities of a row stay in it
+    h = torch.ones((40, 128), dtype=torch.bfloat16, device="cuda")
+    h[3, 7], h[4, 100] = NAN, INF
+    for n in (40, 20):
+        z = torch.empty((n, 70), device="cuda")
+        asgd.asgd_fp4_logits(asgd.matrix(h[:n]), asgd.fp4_matrix(*keep[:2]), asgd.matrix(z))
+        got = host(z)
+        want = np.zeros((n, 70), bool)
+        want[3], want[:, 5] = True, True
+        weights = ref.values_of(codes, scales)[:, 100]
+        want[4] |= weights == 0  # 0 * inf
+        assert np.array_equal(np.isnan(got), want)
+        ok = ~want[4]
+        assert np.array_equal(got[4][ok], np.sign(weights[ok]) * INF)
 
 
 # ---------------------------------------------------------------- ranking under rules
@@ -328,6 +342,17 @@ def test_topk_seen_ids_that_repeat_and_cancel():
     kw = dict(repetition=1.7, frequency=0.001, presence=-0.5)
     got = rank(dev(x), 64, asgd.logit_rules(seen=c, row_bias=c2, **kw))
     check_rank(got, ref.scores(x, seen=seen, row_bias=row_bias, **kw), 64)
+
+
+def test_topk_negative_zeros_tie_with_zeros():
+    L = 3000
+    r = np.random.default_rng(1)
+    z = np.where(r.random((2, L)) < 0.5, -0.0, 0.0).astype(np.float32)
+    bias = np.where(r.random(L) < 0.7, -0.0, 0.0).astype(np.float32)
+    b = dev(bias)
+    got = rank(dev(z), 64, asgd.logit_rules(bias=b))
+    assert np.array_equal(got[0].cpu().numpy(), np.tile(np.arange(64), (2, 1)))
+    assert bool((got[1] == 0).all())
 
 
 def test_topk_lists_with_malformed_indptr_are_read_inside_their_entries():
@@ -500,6 +525,26 @@ def test_distill_infinite_logits():
         assert np.abs(g[i] - wg[i]).max() <= 64 * 2 * U, i
     assert (g[2, 30:40] == 0).all()
     assert abs(loss[4] - want[4]) <= 64 * 2 * U * 16 and abs(loss[5] - want[5]) <= 64 * 2 * U * 4
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("L", [300, 40_000, 200_000])
+@pytest.mark.parametrize("T", [1e-6, 1e-3, 1e3, 1e6])
+def test_distill_at_the_ends_of_the_temperatures(dtype, L, T):
+    r = np.random.default_rng(L)
+    x = np.round(r.normal(0, 2, (2, L)), 1)  # (gaps of 0.1 at the least between different logits)
+    x[0, 7] = -INF
+    z = strided(x, dtype, 1, 3)
+    ids = r.integers(0, L, (2, 3)).astype(np.int32)
+    t = np.array([[1.0, 2.0, 3.0], [0.0, 0.0, 1.0]], np.float32)
+    grad = torch.empty((2, L), dtype=z.dtype, device="cuda")
+    distill(z, dev(ids), dev(t), T, grad)
+    xx = host(z)
+    _, g, p, q = ref.distill(xx, ids, t, float(np.float32(T)))
+    # (an exponent of thousands has an error of its own; there p is below 1e-30 on both sides)
+    bound = distill_bounds(np.where(p > 1e-30, xx, -INF), ids, t, T, np.full(2, 0.5), p, q, dtype) + T * 1e-30
+    err = np.abs(host(grad) - g)
+    assert np.isfinite(host(grad)).all() and (err <= bound).all(), (err / bound).max()
 
 
 def test_distill_gradient_against_differences():

@@ -123,6 +123,7 @@ def test_rule_masks_and_outputs_are_checked():
     E, R = asgd.ASGD_EINVAL, asgd.ASGD_ERANGE
     r = asgd.asgd_logit_rules(allowed=A, allowed_ld=3)
     refused(E, "allowed_ld", asgd.asgd_logits_topk, mat(), 1, A, rules=r, workspace=BIG)
+    refused(R, "2^30", asgd.asgd_logits_topk, mat(), 1, A, rules=asgd.logit_rules(seen=csr(nnz=1 << 30)), workspace=BIG)
     r = asgd.asgd_logit_rules(allowed=A, allowed_ld=-1)
     refused(E, "allowed_ld", asgd.asgd_logits_topk, mat(), 1, A, rules=r, workspace=BIG)
     refused(E, "aligned", asgd.asgd_logits_topk, mat(), 1, A, rules=asgd.asgd_logit_rules(bias=A + 2), workspace=BIG)
@@ -151,6 +152,8 @@ def test_distill_arguments_are_checked():
         refused(E, "k must", asgd.asgd_distill_workspace, 4, 100, k)
     for T in (0.0, -1.0, float("nan"), float("inf")):
         refused(E, "temperature", call, T=T)
+    for T in (1e-7, 2e6):
+        refused(R, "temperature", call, T=T)
     for o in (dict(ids=None), dict(t=None), dict(loss=None)):
         refused(E, "non-NULL", call, **o)
     refused(E, "aligned", call, loss=A + 2)
