@@ -264,10 +264,13 @@ int64_t layout_workspace(asgd_model* m, char* base) {
   m->Z = carve<float>(p, m->unfused ? (int64_t)rp * m->ldz : 0);
   m->sm_m = carve<float>(p, sm_rows);
   m->sm_s = carve<float>(p, sm_rows);
-  // Pieces of a distillation step's rows, at most 2,048 + rows of them, and the student's
-  // logits of the teacher's labels.
-  const int64_t train_rows = m->unfused ? std::min(rp, kMaxTrainBatch) : 0;
-  m->distill_bytes = m->unfused ? (size_t)(train_rows + 2048) * 8 + 256 + (size_t)train_rows * DISTILL_MAX_K * 4 : 0;
+  // A distillation step's scratch memory: the most that any number of its rows takes.
+  m->distill_bytes = 0;
+  if (m->unfused) {
+    const int ldz = n_tiles * OUT_TILE, most = std::min(rp, kMaxTrainBatch);
+    for (int r = 1; r <= most; ++r)
+      m->distill_bytes = std::max(m->distill_bytes, distill_ws_bytes(distill_shape(r, ldz), r, DISTILL_MAX_K));
+  }
   m->distill = carve<char>(p, (int64_t)m->distill_bytes);
   m->tk = carve<double>(p, tk_entries);
   m->tk_entries = tk_entries;

@@ -4,13 +4,16 @@
 // k logits, loss = T^2 sum q (ln q - ln p) and dz = w T (p - q).  The gradient needs the row's
 // sum, so a row is read twice unless something holds it meanwhile:
 //   k_distill_row    a row that a workgroup's registers hold (128 KB, many rows: 256 KB): one read, one write;
-//   k_distill_sums   longer rows, first pass: (max, sum of exponentials) per piece of a row, and
-//                    the student's logits of the teacher's labels (the gradient may take z's place);
-//   k_distill_grad   second pass: joins the pieces' sums and writes the piece's gradient.
+//   k_distill_sums   longer rows, first pass: (max, sum of exponentials) per piece of a row, and q and
+//                    the student's logits at the teacher's labels (the gradient may take z's place);
+//   k_distill_grad   second pass: joins the pieces' sums and writes the gradient.
 // The gradient is w T p everywhere and then, after the workgroup's other stores, once more
 // at the labels that the teacher names: the first of the entries that name a label writes it,
 // with the sum of q over all of them.
 #include <math.h>
+
+#include <algorithm>
+#include <type_traits>
 
 #include "asgd_dev.h"
 #include "asgd_kernels.h"
@@ -22,7 +25,10 @@ namespace {
 
 constexpr int KD_THREADS = 256;
 constexpr int KD_WAVES = KD_THREADS / 64;
-constexpr int KD_WGS = 2048;  // workgroups wanted per pass of a slab
+constexpr int KD_WGS = 1024;  // workgroups wanted for the first pass of a slab
+// Vectors a thread of the second pass, 12 KB a workgroup; 2 | 3 | 4 | 8 of them: 256 x 670,091 bf16 187 | 181 |
+// 178 | 182 us, 512 x 205,443 fp32 216 | 205 | 220 | 309.
+constexpr int KD_U = 3;
 constexpr int KD_ROWS = 512;
 constexpr int64_t KD_SLAB = 192 << 20;
 
@@ -111,6 +117,11 @@ __device__ __forceinline__ bool teacher(const int32_t* t_ids, const float* t_log
   return some;
 }
 
+// (a row of -inf gives no label any probability)
+__device__ __forceinline__ float whole_loss(float sum, float m, float temp, bool some) {
+  return !some ? 0.0f : m == -INFINITY ? INFINITY : temp * temp * sum;
+}
+
 // T^2 sum q (ln q - ln p) from the student's logits of the entries (the thread's own entries' q).
 template <int THREADS>
 __device__ __forceinline__ float row_loss(const float* q, const float* z_t, int k, float m, float s, float temp, bool some,
@@ -119,28 +130,22 @@ __device__ __forceinline__ float row_loss(const float* q, const float* z_t, int 
   float part = 0.0f;
   for (int e = threadIdx.x; e < k; e += THREADS)
     if (q[e] > 0.0f) part += q[e] * (logf(q[e]) - ((z_t[e] - m) / temp - log_s));
-  part = wg_sum<THREADS / 64>(part, red);
-  // (a row of -inf gives no label any probability)
-  return !some ? 0.0f : m == -INFINITY ? INFINITY : temp * temp * part;
+  return whole_loss(wg_sum<THREADS / 64>(part, red), m, temp, some);
 }
 
-// The gradient at the teacher's labels in [c0, c1), after the workgroup's other stores.
-template <typename T, int THREADS>
-__device__ __forceinline__ void put_teacher(T* grow, const float* q, const int* q_id, const float* z_t, int k, int c0,
-                                            int c1, float m, float f, float scale, float ce, float ce_lo) {
-  __syncthreads();
-  for (int e = threadIdx.x; e < k; e += THREADS) {
-    const int id = q_id[e];
-    if (id < 0 || id < c0 || id >= c1) continue;
-    float sum = 0.0f;
-    bool first = true;
-    for (int j = 0; j < k; ++j)
-      if (q_id[j] == id) {
-        first = first && j >= e;
-        sum += q[j];
-      }
-    if (first) grow[id] = (T)((m == -INFINITY ? 0.0f : soft<T>(z_t[e], m, f, ce, ce_lo)) - scale * sum);
-  }
+// Whether entry e is the first of those that name its label; *sum: q over all of them.
+__device__ __forceinline__ bool teacher_sum(const float* q, const int* q_id, int k, int e, float* sum) {
+  const int id = q_id[e];
+  if (id < 0) return false;
+  bool first = true;
+  float t = 0.0f;
+  for (int j = 0; j < k; ++j)
+    if (q_id[j] == id) {
+      first = first && j >= e;
+      t += q[j];
+    }
+  *sum = t;
+  return first;
 }
 
 template <typename T>
@@ -225,30 +230,30 @@ __global__ __launch_bounds__(THREADS) void k_distill_row(DistillJob job, float c
       store_vec<T>(gr, same, i, zr.col(i), y);
     }
   }
-  if (some) put_teacher<T, THREADS>(gr.base + gr.phase, q, q_id, z_t, k, 0, job.n_cols, m, f, scale, ce, ce_lo);
+  if (!some) return;
+  __syncthreads();  // (the workgroup's other stores come first)
+  for (int e = tid; e < k; e += THREADS) {
+    float sum = 0.0f;
+    if (teacher_sum(q, q_id, k, e, &sum))
+      gr.base[gr.phase + q_id[e]] = (T)((m == -INFINITY ? 0.0f : soft<T>(z_t[e], m, f, ce, ce_lo)) - scale * sum);
+  }
 }
 
 // First pass over one piece of a row.
 template <typename T>
 __device__ __forceinline__ void piece_sums(const DistillJob& job, int row, int split, float ce, int splits, int vec_split,
-                                           float2* part, float* z_t, float2* red) {
+                                           float2* part, float2* red) {
   using R = Row<T>;
   constexpr int V = R::V, U = 16 / V;
-  const int tid = threadIdx.x, k = job.k;
+  const int tid = threadIdx.x;
   const R zr((T*)const_cast<void*>(job.z), job.ld, row, job.n_cols);
   const Parts<T> at(zr);
   const int v0 = at.va + split * vec_split, v1 = min(at.vb, v0 + vec_split);
   float m = -INFINITY, s = 0.0f;
-  if (split == 0) {
-    for (int e = tid; e < k; e += KD_THREADS) {
-      const int id = job.t_ids[(int64_t)row * k + e];
-      z_t[(int64_t)row * k + e] = id >= 0 && id < job.n_labels ? (float)zr.base[zr.phase + id] : 0.0f;
-    }
-    if (tid < at.edges) {
-      m = (float)zr.base[zr.phase + at.edge(tid)];
-      if (m != m) m = INFINITY;
-      s = m == -INFINITY ? 0.0f : m == INFINITY ? NAN : 1.0f;
-    }
+  if (split == 0 && tid < at.edges) {
+    m = (float)zr.base[zr.phase + at.edge(tid)];
+    if (m != m) m = INFINITY;
+    s = m == -INFINITY ? 0.0f : m == INFINITY ? NAN : 1.0f;
   }
   typename R::vec x[U];
   auto load = [&](int base) {
@@ -300,120 +305,144 @@ __device__ __forceinline__ void piece_sums(const DistillJob& job, int row, int s
   __syncthreads();
   if (tid == 0) {
     for (int i = 1; i < KD_WAVES; ++i) soft_merge(m, s, red[i].x, red[i].y, ce);
-    part[(int64_t)row * splits + split] = make_float2(m, s);
+    part[(int64_t)row * (splits + 1) + split] = make_float2(m, s);
   }
 }
 
-// Second pass: the row's loss, and with GRAD the gradient of one piece of it.
-template <typename T, bool GRAD>
-__device__ __forceinline__ void piece_grad(const DistillJob& job, int row, int split, float ce, float ce_lo,
-                                           float mean_weight, int n_part, int vec_split, const float2* part,
-                                           const float* z_t, float2* red2) {
-  using R = Row<T>;
-  constexpr int V = R::V, U = 2;
+// An entry of a teacher's list: its q, the student's logit of its label, and if it is the
+// first that names this label the label and the sum of q over all that do (otherwise id -1).
+struct __align__(16) Entry {
+  int id;
+  float q, sum, z;
+};
+
+// First pass.  The first workgroups make the rows' entries, beside the others' reading.
+template <typename T>
+__global__ __launch_bounds__(KD_THREADS) void k_distill_sums(DistillJob job, int row0, int rows, float ce, int splits,
+                                                             int vec_split, float2* __restrict__ part,
+                                                             Entry* __restrict__ entries) {
+  __shared__ float2 red2[KD_WAVES];
   __shared__ float red[KD_WAVES];
   __shared__ float q[DISTILL_MAX_K];
   __shared__ int q_id[DISTILL_MAX_K];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, k = job.k;
-  const R zr((T*)const_cast<void*>(job.z), job.ld, row, job.n_cols);
-  const Parts<T> at(zr);
-  const int v0 = at.va + split * vec_split, v1 = max(v0, min(at.vb, v0 + vec_split));
-  typename R::vec x[U];
-  auto load = [&](int base) {
-#pragma unroll
-    for (int u = 0; u < U; ++u)
-      x[u] = *reinterpret_cast<const typename R::vec*>(zr.base + (int64_t)V * min(base + u * KD_THREADS + tid, v1 - 1));
-  };
-  if (GRAD && v0 < v1) load(v0);
-
-  // the row's maximum and sum from its pieces
-  float m = -INFINITY, s = 0.0f;
-  for (int i = tid; i < n_part; i += KD_THREADS) {
-    const float2 ms = part[(int64_t)row * n_part + i];
-    soft_merge(m, s, ms.x, ms.y, ce);
+  const int block = (int)blockIdx.x - rows;
+  if (block >= 0) {
+    piece_sums<T>(job, row0 + block / splits, block % splits, ce, splits, vec_split, part, red2);
+    return;
   }
-#pragma unroll
-  for (int o = 32; o >= 1; o >>= 1) soft_merge(m, s, __shfl_xor(m, o), __shfl_xor(s, o), ce);
-  if (lane == 0) red2[wave] = make_float2(m, s);
-  __syncthreads();
-  m = red2[0].x;
-  s = red2[0].y;
-  for (int i = 1; i < KD_WAVES; ++i) soft_merge(m, s, red2[i].x, red2[i].y, ce);
-
-  z_t += (int64_t)row * k;
+  const int row = row0 + blockIdx.x, tid = threadIdx.x, k = job.k;
+  const Row<T> zr((T*)const_cast<void*>(job.z), job.ld, row, job.n_cols);
   const bool some = teacher<KD_THREADS>(job.t_ids + (int64_t)row * k, job.t_logits + (int64_t)row * k, k, job.n_labels,
                                         job.temperature, q, q_id, red);
-  if (split == 0) {
-    const float loss = row_loss<KD_THREADS>(q, z_t, k, m, s, job.temperature, some, red);
-    if (tid == 0) job.loss_rows[row] = loss;
+  __syncthreads();
+  for (int e = tid; e < k; e += KD_THREADS) {
+    Entry t{-1, q[e], 0.0f, q_id[e] >= 0 ? (float)zr.base[zr.phase + q_id[e]] : 0.0f};
+    if (teacher_sum(q, q_id, k, e, &t.sum)) t.id = q_id[e];
+    entries[(int64_t)row * k + e] = t;
   }
-  if constexpr (!GRAD) return;
-  const float scale = (job.weights ? job.weights[row] : mean_weight) * job.temperature;
-  const float f = some && s != 0.0f ? scale / s : 0.0f;
-  const R gr((T*)job.grad, job.ld_grad, row, job.n_cols);
-  const bool same = gr.phase == zr.phase, zero = m == -INFINITY || !some;
-  auto value = [&](float v) { return zero ? 0.0f : soft<T>(v, m, f, ce, ce_lo); };
-  if (split == 0 && tid < at.edges) {
-    const int c = at.edge(tid);
-    gr.base[gr.phase + c] = (T)value((float)zr.base[zr.phase + c]);
+  // (behind the row's pieces: whether any entry counts)
+  if (tid == 0) part[(int64_t)row * (splits + 1) + splits] = make_float2(some ? 1.0f : 0.0f, 0.0f);
+}
+
+// Second pass: a workgroup writes KD_U vectors a thread of a row, then the teacher's entries among
+// them; the first of a row's also finds its loss (without GRAD the only one).  Workgroups go through the rows from
+// the last one back: what the first pass read last is what the memory's cache still holds.
+template <typename T, bool GRAD>
+__global__ __launch_bounds__(KD_THREADS) void k_distill_grad(DistillJob job, int row0, int rows, int chunks, float ce,
+                                                             float ce_lo, float mean_weight, int splits,
+                                                             const float2* __restrict__ part,
+                                                             const Entry* __restrict__ entries) {
+  using R = Row<T>;
+  constexpr int V = R::V;
+  __shared__ float red[KD_WAVES];
+  const int tid = threadIdx.x, lane = tid & 63, k = job.k;
+  const int row = row0 + rows - 1 - (int)(blockIdx.x / chunks), chunk = chunks - 1 - (int)(blockIdx.x % chunks);
+  const R zr((T*)const_cast<void*>(job.z), job.ld, row, job.n_cols);
+  const Parts<T> at(zr);
+  const int v0 = at.va + chunk * (KD_THREADS * KD_U), v1 = max(v0, min(at.vb, v0 + KD_THREADS * KD_U));
+  typename R::vec x[KD_U];
+  float edge = 0.0f;
+  const bool has_edge = chunk == 0 && tid < at.edges;
+  if constexpr (GRAD) {
+#pragma unroll
+    for (int u = 0; u < KD_U; ++u) {
+      const int i = v0 + u * KD_THREADS + tid;
+      if (i < v1) x[u] = *reinterpret_cast<const typename R::vec*>(zr.base + (int64_t)V * i);
+    }
+    if (has_edge) edge = (float)zr.base[zr.phase + at.edge(tid)];
   }
-  for (int base = v0; base < v1; base += KD_THREADS * U) {
-    float y[U][V];
+  constexpr int E = DISTILL_MAX_K / KD_THREADS;
+  Entry t[E];
 #pragma unroll
-    for (int u = 0; u < U; ++u)
+  for (int j = 0; j < E; ++j) {
+    t[j] = Entry{-1, 0.0f, 0.0f, 0.0f};
+    if (tid + j * KD_THREADS < k) t[j] = entries[(int64_t)row * k + tid + j * KD_THREADS];
+  }
+  // The pieces' sums as one, in every wave for itself.
+  part += (int64_t)row * (splits + 1);
+  const bool some = part[splits].x != 0.0f;
+  float m = -INFINITY, s = 0.0f;
+  for (int i = lane; i < splits; i += 64) {
+    const float2 ms = part[i];
+    soft_merge(m, s, ms.x, ms.y, ce);
+  }
+  auto merge = [&](auto x) {
+    const float m2 = __uint_as_float(lane_xor<decltype(x)::value>(__float_as_uint(m), lane));
+    const float s2 = __uint_as_float(lane_xor<decltype(x)::value>(__float_as_uint(s), lane));
+    soft_merge(m, s, m2, s2, ce);
+  };
+  merge(std::integral_constant<int, 1>());
+  merge(std::integral_constant<int, 2>());
+  merge(std::integral_constant<int, 4>());
+  merge(std::integral_constant<int, 8>());
+  merge(std::integral_constant<int, 16>());
+  merge(std::integral_constant<int, 32>());
+  if (chunk == 0) {
+    const float log_s = logf(s);
+    float sum = 0.0f;
 #pragma unroll
-      for (int e = 0; e < V; ++e) y[u][e] = (float)x[u][e];
-    if (base + KD_THREADS * U < v1) load(base + KD_THREADS * U);
+    for (int j = 0; j < E; ++j)
+      if (t[j].q > 0.0f) sum += t[j].q * (logf(t[j].q) - ((t[j].z - m) / job.temperature - log_s));
+    sum = wg_sum<KD_WAVES>(sum, red);
+    if (tid == 0) job.loss_rows[row] = whole_loss(sum, m, job.temperature, some);
+  }
+  if constexpr (GRAD) {
+    const R gr((T*)job.grad, job.ld_grad, row, job.n_cols);
+    const float scale = (job.weights ? job.weights[row] : mean_weight) * job.temperature;
+    const float f = some && s != 0.0f ? scale / s : 0.0f;
+    const bool zero = !some || m == -INFINITY, same = gr.phase == zr.phase;
+    if (zero)  // (the products below are none, or not 0 for a logit that is none)
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int i = base + u * KD_THREADS + tid;
-      if (i < v1) {
+      for (int u = 0; u < KD_U; ++u) x[u] = (typename R::vec)(T)0.0f;
 #pragma unroll
-        for (int e = 0; e < V; ++e) y[u][e] = value(y[u][e]);
-        store_vec<T>(gr, same, i, zr.col(i), y[u]);
-      }
+    for (int u = 0; u < KD_U; ++u) {
+      const int i = v0 + u * KD_THREADS + tid;
+      if (i >= v1) continue;
+      float y[V];
+#pragma unroll
+      for (int e = 0; e < V; ++e) y[e] = soft<T>((float)x[u][e], zero ? 0.0f : m, f, ce, ce_lo);
+      store_vec<T>(gr, same, i, zr.col(i), y);
+    }
+    T* const grow = gr.base + gr.phase;
+    if (has_edge) grow[at.edge(tid)] = (T)(zero ? 0.0f : soft<T>(edge, m, f, ce, ce_lo));
+    __syncthreads();  // (the workgroup's other stores come first)
+    const int c0 = zr.col(v0), c1 = zr.col(v1);
+#pragma unroll
+    for (int j = 0; j < E; ++j) {
+      const int id = t[j].id;
+      if (id >= 0 && ((id >= c0 && id < c1) || (chunk == 0 && (id < at.head || id >= at.tail))))
+        grow[id] = (T)((zero ? 0.0f : soft<T>(t[j].z, m, f, ce, ce_lo)) - scale * t[j].sum);
     }
   }
-  if (!some) return;
-  // the piece's labels; the first one's edges too (its own stores, like the others of the piece)
-  const int c0 = split == 0 ? 0 : zr.col(v0), c1 = zr.col(v1);
-  T* const grow = gr.base + gr.phase;
-  put_teacher<T, KD_THREADS>(grow, q, q_id, z_t, k, c0, c1, m, f, scale, ce, ce_lo);
-  if (split == 0) put_teacher<T, KD_THREADS>(grow, q, q_id, z_t, k, max(c1, at.tail), job.n_cols, m, f, scale, ce, ce_lo);
-}
-
-// The passes over `rows` rows from row0 on.  The second one takes the rows last first: those
-// that the first pass read last are the ones that the memory's cache still holds.
-template <typename T>
-__global__ __launch_bounds__(KD_THREADS) void k_distill_sums(DistillJob job, int row0, float ce, int splits, int vec_split,
-                                                             float2* part, float* z_t) {
-  __shared__ float2 red[KD_WAVES];
-  piece_sums<T>(job, row0 + blockIdx.x / splits, blockIdx.x % splits, ce, splits, vec_split, part, z_t, red);
-}
-template <typename T>
-__global__ __launch_bounds__(KD_THREADS) void k_distill_grad(DistillJob job, int row0, int rows, float ce, float ce_lo,
-                                                             float mean_weight, int splits, int vec_split,
-                                                             const float2* part, const float* z_t) {
-  __shared__ float2 red[KD_WAVES];
-  piece_grad<T, true>(job, row0 + rows - 1 - blockIdx.x / splits, blockIdx.x % splits, ce, ce_lo, mean_weight, splits,
-                      vec_split, part, z_t, red);
-}
-
-// The loss alone, after the first pass.
-template <typename T>
-__global__ __launch_bounds__(KD_THREADS) void k_distill_loss(DistillJob job, float ce, int n_part, const float2* part,
-                                                             const float* z_t) {
-  __shared__ float2 red[KD_WAVES];
-  piece_grad<T, false>(job, blockIdx.x, 0, ce, 0.0f, 0.0f, n_part, 0, part, z_t, red);
 }
 
 }  // namespace
 
 // Slabs of rows whose logits the memory's cache (256 MB) holds between the two passes, and
 // pieces per row so that a slab's fill the GPU.  Measured, one slab | slabs of 192 MB (16-bit logits): 256 x
-// 670,091 bf16 202 | 196 us (first pass 70, second 127, which is what a copy of z takes; rows in the same order in
-// both passes, one slab: 219), 512 x 205,443 fp32 243 | 226; slabs of 64 MB, the first pass of one beside the
-// second of another in a launch: 226 and 257.
+// 670,091 bf16 202 | 196 us (rows in the same order in both passes, one slab: 219), 512 x 205,443 fp32 243 | 226;
+// slabs of 64 MB, the first pass of one beside the second of another in a launch: 226 and 257.  512 | 1,024 |
+// 2,048 workgroups for a slab's first pass: 183 | 176 | 183 us and 223 | 220 | 226.
 DistillShape distill_shape(int rows, int cols) {
   DistillShape sh;
   const int64_t n = ((int64_t)rows * cols * 2 + KD_SLAB - 1) / KD_SLAB;
@@ -424,13 +453,11 @@ DistillShape distill_shape(int rows, int cols) {
   return sh;
 }
 
+// Scratch memory: per row the pieces' sums and whether its teacher counts, then the teachers' entries.
 static size_t part_bytes(const DistillShape& sh, int rows) {
-  return ((size_t)rows * sh.splits * sizeof(float2) + 255) / 256 * 256;
+  return ((size_t)rows * (sh.splits + 1) * sizeof(float2) + 255) / 256 * 256;
 }
-
-size_t distill_ws_bytes(const DistillShape& sh, int rows, int k) {
-  return part_bytes(sh, rows) + (size_t)rows * k * sizeof(float);
-}
+size_t distill_ws_bytes(const DistillShape& sh, int rows, int k) { return part_bytes(sh, rows) + (size_t)rows * k * sizeof(Entry); }
 
 template <typename T, int THREADS, int NV>
 static hipError_t distill_rows(const DistillJob& j, float ce, float ce_lo, hipStream_t st) {
@@ -451,23 +478,27 @@ static hipError_t distill_as(const DistillJob& j, const DistillShape& sh, void* 
   if (n_vec <= 8 * 256) return distill_rows<T, 256, 8>(j, ce, ce_lo, st);
   if (n_vec <= 8 * 1024) return distill_rows<T, 1024, 8>(j, ce, ce_lo, st);
   // 256 KB: half of a compute unit's registers, so one row at a time on each, and worth it from two rows for
-  // each on (two passes | this: 512 x 60,000 fp32 65 | 51 us, 300 x 100,000 bf16 43 | 47 us; rows of 400 KB in the
-  // same way no longer gain: 512 x 205,443 bf16 120 | 121 us)
+  // each on (two passes | this: 512 x 60,000 fp32 63 | 51 us, 300 x 100,000 bf16 36 | 47 us; rows of 400 KB in the
+  // same way do not gain: 512 x 205,443 bf16 109 | 121 us)
   if (j.n_rows >= KD_ROWS && n_vec <= 16 * 1024) return distill_rows<T, 1024, 16>(j, ce, ce_lo, st);
   const int vps = (n_vec + sh.splits - 1) / sh.splits;
   float2* part = (float2*)ws;
-  float* z_t = (float*)((char*)ws + part_bytes(sh, j.n_rows));
+  Entry* entries = (Entry*)((char*)ws + part_bytes(sh, j.n_rows));
   const float mean = 1.0f / (float)j.n_rows;
   const int per = j.grad ? (j.n_rows + sh.slabs - 1) / sh.slabs : j.n_rows;
+  const int chunks = (n_vec + KD_THREADS * KD_U - 1) / (KD_THREADS * KD_U);
+  const dim3 block(KD_THREADS);
   for (int r0 = 0; r0 < j.n_rows; r0 += per) {
-    const int rows = per < j.n_rows - r0 ? per : j.n_rows - r0;
-    const dim3 grid((unsigned)rows * sh.splits), block(KD_THREADS);
-    hipLaunchKernelGGL(k_distill_sums<T>, grid, block, 0, st, j, r0, ce, sh.splits, vps, part, z_t);
+    const int rows = std::min(per, j.n_rows - r0);
+    hipLaunchKernelGGL(k_distill_sums<T>, dim3((unsigned)rows * (sh.splits + 1)), block, 0, st, j, r0, rows, ce, sh.splits,
+                       vps, part, entries);
     if (j.grad)
-      hipLaunchKernelGGL(k_distill_grad<T>, grid, block, 0, st, j, r0, rows, ce, ce_lo, mean, sh.splits, vps, part, z_t);
+      hipLaunchKernelGGL((k_distill_grad<T, true>), dim3((unsigned)rows * chunks), block, 0, st, j, r0, rows, chunks, ce,
+                         ce_lo, mean, sh.splits, part, entries);
+    else
+      hipLaunchKernelGGL((k_distill_grad<T, false>), dim3(rows), block, 0, st, j, r0, rows, 1, ce, ce_lo, mean, sh.splits,
+                         part, entries);
   }
-  if (!j.grad)
-    hipLaunchKernelGGL(k_distill_loss<T>, dim3(j.n_rows), dim3(KD_THREADS), 0, st, j, ce, sh.splits, part, z_t);
   return hipGetLastError();
 }
 
