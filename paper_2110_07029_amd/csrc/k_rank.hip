@@ -112,7 +112,7 @@ struct Best {
   int n;      // keys waiting in buf
   u64* buf;   // LDS, 128 keys of this wave
 
-  // Appends the lanes' keys that are above the bound (0 never is): at most 64 more.
+  // Appends the lanes' keys that are above the bound (0 never is): at most 64 to at most 63.
   __device__ void append(u64 key) {
     const bool in = key > least;
     const u64 who = __ballot(in);
@@ -456,6 +456,7 @@ __global__ __launch_bounds__(RK_THREADS) void k_rank(const T* __restrict__ z, in
       if (c < L && !(mask && !((mask[c >> 5] >> (c & 31)) & 1)) && !(lists && ((edge_bits >> lane) & 1)))
         v = (float)zr.base[zr.phase + c] + (ru.bias ? ru.bias[c] : 0.0f);
       best.append(v == v ? key_of(v, c) : 0);
+      if (best.n >= 64) best.flush(lane);  // (listed labels may wait too)
       raise2(v, m, s);
       if (m != -INFINITY) s += term2(v, m);
     }

@@ -384,6 +384,19 @@ def test_topk_lists_that_crowd_a_range(dtype, L, low, count, k):
                ref.scores(host(z), seen=seen, row_bias=row_bias, **kw), k)
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("listed", [50, 63])
+def test_topk_short_rows_with_listed_labels_and_unaligned_ends(dtype, listed):
+    # rows of one piece: listed labels wait, then the labels before and after the whole vectors, then a round that
+    # passes one label of every lane
+    r = np.random.default_rng(listed)
+    L = 3998
+    z = strided(r.normal(0, 2, (40, L)), dtype, 1, 9)
+    seen = [r.permutation(np.arange(20, L - 20))[:listed] for _ in range(40)]
+    c, keep = lists(seen, L)
+    check_rank(rank(z, 64, asgd.logit_rules(seen=c, presence=-1.0)), ref.scores(host(z), seen=seen, presence=-1.0), 64)
+
+
 def test_topk_twice_is_bitwise_the_same_and_stays_in_its_rows():
     B, L, k = 30, 50_000, 20
     r = np.random.default_rng(77)
