@@ -19,6 +19,11 @@
 // the last row_bias entry and the first entry that names a label, and that entry's thread
 // forms the label's score in float64, so sums follow the lists' order.  A range with more
 // labels than the table holds is counted 1,024 columns at a time.
+//
+// Measured: 1,024 x 670,091 fp32, k = 5, all rules, 551 us for 2.83 GB (5.1 TB/s: memory; the biases of rows that
+// start at odd places are not aligned, with aligned rows 478); 256 x 205,443 bf16, k = 32, all rules, 48 us, of
+// which k_rank_join 4 (112 MB at 2.4 TB/s: vector work, of which 2/5 the exponentials of lse and the mask, the
+// rest maxima and lists); one row of 670,091 13 to 15 us in two launches of 8.6 and 4.8.
 #include <math.h>
 
 #include <algorithm>
@@ -632,6 +637,8 @@ static hipError_t rank_as(const void* z, int64_t ld, int rows, int L, const Rank
   else
     hipLaunchKernelGGL((k_rank<T, false>), grid, block, 0, st, (const T*)z, ld, L, ru, k, splits, 0, vps, part, ms, ids,
                        scores, lse);
+  // (4 | 16 waves: 1 x 670,091, k = 64, 55 | 27 us, 16 x 205,443, k = 32, 18.4 | 14.8; from 256 rows on, where
+  // the rows fill the GPU, 43.2 | 44.0)
   if (parts > 1 && parts * k > 512 && rows <= 256)
     hipLaunchKernelGGL(k_rank_join<16>, dim3(rows), dim3(1024), 0, st, parts, k, part, ms, ids, scores, lse);
   else if (parts > 1)

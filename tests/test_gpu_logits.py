@@ -154,7 +154,8 @@ def product_bound(a, w, bias):
 @pytest.mark.parametrize("B,L,shift,pad,with_bias", [(1, 1, 0, 0, True), (1, 33, 0, 0, False), (2, 31, 1, 3, True),
                                                      (31, 1000, 0, 0, True), (33, 1001, 2, 9, True),
                                                      (64, 257, 0, 0, False), (129, 4099, 1, 1, True),
-                                                     (5, 30_000, 0, 0, True), (300, 515, 0, 5, True)])
+                                                     (5, 30_000, 0, 0, True), (300, 515, 0, 5, True),
+                                                     (16, 700, 3, 4, True), (17, 700, 1, 1, True)])
 def test_fp4_logits(acts, out, B, L, shift, pad, with_bias):
     r = np.random.default_rng(B * 7 + L)
     codes, scales = label_matrix(L, L)
