@@ -509,7 +509,9 @@ asgd_status asgd_predict_topk_rules(asgd_model* m, const asgd_csr* x, int32_t k,
  * with the mean of asgd_distill's loss over the batch in the place of the
  * cross-entropy.  k <= 512.  The logits are stored, so the model must have been
  * created with ASGD_UNFUSED_OUTPUT (ESTATE otherwise).  loss_out as for
- * asgd_train_step; asgd_model_last_loss reads it too. */
+ * asgd_train_step; asgd_model_last_loss reads it too.  Its kernels are timed as
+ * ASGD_K_GATHER, SORT, LOGITS, SOFTMAX (loss and gradient), DH, DENSE_BWD,
+ * W1_UPDATE and OUT_BWD (W2 and b2, with the step's transposed hidden rows). */
 asgd_status asgd_distill_step(asgd_model* m, const asgd_csr* x, const int32_t* t_ids, const float* t_logits,
                               int32_t k, float temperature, float lr, float* loss_out);
 

@@ -21,9 +21,10 @@
 // labels than the table holds is counted 1,024 columns at a time.
 //
 // Measured: 1,024 x 670,091 fp32, k = 5, all rules, 551 us for 2.83 GB (5.1 TB/s: memory; the biases of rows that
-// start at odd places are not aligned, with aligned rows 478); 256 x 205,443 bf16, k = 32, all rules, 48 us, of
-// which k_rank_join 4 (112 MB at 2.4 TB/s: vector work, of which 2/5 the exponentials of lse and the mask, the
-// rest maxima and lists); one row of 670,091 13 to 15 us in two launches of 8.6 and 4.8.
+// start at odd places are not aligned: without biases 430, with aligned rows 478; aligned loads whose elements
+// neighbouring lanes pass on took 747, their branches end the loads' overlap); 256 x 205,443 bf16, k = 32, all
+// rules, 48 us, of which k_rank_join 4 (112 MB at 2.4 TB/s: vector work; without rules 41, without lse too 33, with
+// k = 1 besides 24); one row of 670,091 13 to 15 us in two launches of 8.6 and 4.8.
 #include <math.h>
 
 #include <algorithm>
