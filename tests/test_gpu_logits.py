@@ -541,6 +541,47 @@ def test_distill_infinite_logits():
     assert abs(loss[4] - want[4]) <= 64 * 2 * U * 16 and abs(loss[5] - want[5]) <= 64 * 2 * U * 4
 
 
+@pytest.mark.parametrize("shift", [0, 1])
+@pytest.mark.parametrize("L", [40_003, 300_002])
+def test_distill_infinities_repeats_and_empty_teachers_of_long_rows(L, shift):
+    B, T = 8, 2.0
+    x = np.random.default_rng(L).normal(0, 1, (B, L)).astype(np.float32)
+    x[0, L // 2] = NAN
+    x[1, L - 1] = INF
+    x[2, 30:L // 2] = -INF                # masked labels, one of them the teacher's
+    x[3, :] = -INF
+    x[4, :] = np.finfo(np.float32).min
+    x[5, 1:] = -INF
+    x[6, 5] = NAN                         # and no teacher
+    ids = np.tile(np.array([5, 40, 0, L - 1, L - 2, 17], np.int32), (B, 1))
+    t = np.random.default_rng(1).normal(0, 1, (B, 6)).astype(np.float32)
+    ids[2] = [40, 3, 3, L, -1, L - 1]
+    ids[5] = 0
+    ids[6] = ref.EMPTY
+    ids[7] = [L - 1, 0, L - 1, 0, 20_000, 20_000]
+    big = torch.full((B, L + 9), 7.0, device="cuda")
+    grad = big[:, 4:4 + L]
+    loss = distill(strided(x, "f32", shift, 3), dev(ids), dev(t), T, grad)
+    assert bool((big[:, :4] == 7.0).all() and (big[:, 4 + L:] == 7.0).all())
+    assert torch.equal(distill(strided(x, "f32", shift, 3), dev(ids), dev(t), T)[2:], loss[2:])
+    loss, g = host(loss), host(grad)
+    want, wg, p, q = ref.distill(x, ids, t, T)
+    assert np.isnan(loss[:2]).all() and np.isnan(g[:2]).all()
+    assert loss[2] == INF and loss[3] == INF and loss[6] == 0 and (g[6] == 0).all()
+    assert (g[2, 30:40] == 0).all() and (g[3, 100:1000] == 0).all()
+    some = [2, 3, 7]
+    on = (ids >= 0) & (ids < L)
+    bound = distill_bounds(x[some], ids[some], np.where(on, t, -INF)[some], T, np.full(3, 1 / B), p[some], q[some], "f32")
+    err = np.abs(g[some] - wg[some])
+    assert (err <= bound).all(), (err / bound).max()
+    # equal logits, and a single one: exponentials of 0, the sum's additions, a division, q's roundings, a difference
+    bound = T / B * (L / 256 + 96 + 16 + 24) * 2 * U * (p[4:6] + q[4:6])
+    err = np.abs(g[4:6] - wg[4:6])
+    assert (err <= bound).all(), (err / bound).max()
+    size = T * T * (8 / T * 2 + np.log(L) + 16)
+    assert (np.abs(loss[[4, 5, 7]] - want[[4, 5, 7]]) <= size * (16 + 1 + L / 512) * 2 * U).all()
+
+
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("L", [300, 40_000, 200_000])
 @pytest.mark.parametrize("T", [1e-6, 1e-3, 1e3, 1e6])
@@ -617,7 +658,7 @@ def test_fp4_rows_past_two_to_the_31_elements():
     assert np.array_equal(ref.values_of(codes.cpu().numpy(), scales.cpu().numpy()), v)
     wc, wsc = (dev(t) for t in label_matrix(L, 9))
     w = asgd.fp4_matrix(wc, wsc)
-    for n in (B, 20):  # many rows and few
+    for n in (B, 20, 10):  # many rows and few
         z = big[:n, 200:200 + L] if n > 32 else big[-n:, 200:200 + L]
         a = asgd.fp4_matrix(codes[:n] if n > 32 else codes[-n:], scales[:n] if n > 32 else scales[-n:])
         asgd.asgd_fp4_logits(a, w, asgd.matrix(z))
