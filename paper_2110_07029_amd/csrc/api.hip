@@ -269,7 +269,7 @@ int64_t layout_workspace(asgd_model* m, char* base) {
   if (m->unfused) {
     const int ldz = n_tiles * OUT_TILE, most = std::min(rp, kMaxTrainBatch);
     for (int r = 1; r <= most; ++r)
-      m->distill_bytes = std::max(m->distill_bytes, distill_ws_bytes(distill_shape(r, ldz), r, DISTILL_MAX_K));
+      m->distill_bytes = std::max(m->distill_bytes, distill_ws_bytes(distill_splits(r, ldz), r, DISTILL_MAX_K));
   }
   m->distill = carve<char>(p, (int64_t)m->distill_bytes);
   m->tk = carve<double>(p, tk_entries);
@@ -1146,8 +1146,8 @@ asgd_status asgd_distill_step(asgd_model* m, const asgd_csr* x, const int32_t* t
   if (((uintptr_t)t_ids | (uintptr_t)t_logits) % 4) return fail(ASGD_EINVAL, "t_ids and t_logits must be 4-byte aligned");
   if ((s = check_device(t_ids, "t_ids")) || (s = check_device(t_logits, "t_logits"))) return s;
   const int B = x->n_rows;
-  const DistillShape sh = distill_shape(B, m->ldz);
-  if (distill_ws_bytes(sh, B, k) > m->distill_bytes) return fail(ASGD_ERANGE, "distillation buffer too small");
+  const int pieces = distill_splits(B, m->ldz);
+  if (distill_ws_bytes(pieces, B, k) > m->distill_bytes) return fail(ASGD_ERANGE, "distillation buffer too small");
   int rows_pad = 0;
   m->pipe = false;
   const SortPlan sort = plan_sort(m, x->nnz);
@@ -1158,7 +1158,7 @@ asgd_status asgd_distill_step(asgd_model* m, const asgd_csr* x, const int32_t* t
   // the loss, and the gradient in the logits' place (columns past L hold -inf: gradient 0)
   const DistillJob job{m->Z, m->ldz, B, m->ldz, m->L, t_ids, t_logits, k, temperature, nullptr, m->loss_rows,
                        m->Z, m->ldz};
-  TIMED(m, ASGD_K_SOFTMAX, launch_distill(ASGD_F32, job, sh, m->distill, m->stream));
+  TIMED(m, ASGD_K_SOFTMAX, launch_distill(ASGD_F32, job, pieces, m->distill, m->stream));
   const int splits = fwd_splits(m, B);
   if ((int64_t)splits * rows_pad > m->part_rows) return fail(ASGD_ERANGE, "partial buffer too small");
   TIMED(m, ASGD_K_DH, launch_stored_dh(m->bf16, m->W2(), m->b2(), m->L, m->Z, m->ldz, B, splits, m->o_part, rows_pad,

@@ -270,7 +270,7 @@ asgd_status asgd_logits_topk(const asgd_matrix* z, const asgd_logit_rules* rules
 
 asgd_status asgd_distill_workspace(int32_t n_rows, int32_t n_cols, int32_t k, size_t* bytes) {
   TRY(check_sizes(n_rows, n_cols, k, DISTILL_MAX_K, bytes));
-  *bytes = distill_ws_bytes(distill_shape(n_rows, n_cols), n_rows, k);
+  *bytes = distill_ws_bytes(distill_splits(n_rows, n_cols), n_rows, k);
   return ASGD_OK;
 }
 
@@ -291,8 +291,8 @@ asgd_status asgd_distill(const asgd_matrix* z, const int32_t* t_ids, const float
     if (!same && (uintptr_t)grad->data < end_of(z) && (uintptr_t)z->data < end_of(grad))
       return set_error(ASGD_EINVAL, "grad overlaps z without being z");
   }
-  const DistillShape sh = distill_shape(z->n_rows, z->n_cols);
-  TRY(check_workspace(ws, ws_bytes, distill_ws_bytes(sh, z->n_rows, k)));
+  const int splits = distill_splits(z->n_rows, z->n_cols);
+  TRY(check_workspace(ws, ws_bytes, distill_ws_bytes(splits, z->n_rows, k)));
   TRY(check_stream(hip_stream));
   TRY(check_device(z->data, "z.data"));
   TRY(check_device(t_ids, "t_ids"));
@@ -302,7 +302,7 @@ asgd_status asgd_distill(const asgd_matrix* z, const int32_t* t_ids, const float
   if (grad) TRY(check_device(grad->data, "grad.data"));
   const DistillJob j{z->data, z->ld, z->n_rows, z->n_cols, z->n_cols, t_ids, t_logits, k, temperature, weights, loss_rows,
                      grad ? grad->data : nullptr, grad ? grad->ld : 0};
-  LAUNCH(launch_distill(z->dtype, j, sh, ws, (hipStream_t)hip_stream));
+  LAUNCH(launch_distill(z->dtype, j, splits, ws, (hipStream_t)hip_stream));
   return ASGD_OK;
 }
 

@@ -278,13 +278,10 @@ struct DistillJob {
   int64_t ld_grad;
 };
 constexpr int DISTILL_MAX_K = 512;
-struct DistillShape {
-  int slabs;   // of rows, one after the other
-  int splits;  // pieces per row
-};
-DistillShape distill_shape(int rows, int cols);
-size_t distill_ws_bytes(const DistillShape& sh, int rows, int k);
-hipError_t launch_distill(int dtype, const DistillJob& j, const DistillShape& sh, void* ws, hipStream_t st);
+// Pieces per row.
+int distill_splits(int rows, int cols);
+size_t distill_ws_bytes(int splits, int rows, int k);
+hipError_t launch_distill(int dtype, const DistillJob& j, int splits, void* ws, hipStream_t st);
 
 // MXFP4: codes [rows x cols / 2], scales [rows x cols / 32].
 hipError_t launch_fp4_quantize(int dtype, const void* x, int64_t ld, int rows, int cols, uint8_t* codes,

@@ -12,12 +12,11 @@
 // with the sum of q over all of them.
 //
 // Measured: 128 x 1,000 fp32 10 us (a launch and three dependent reductions); 256 x 30,000 fp32 16 us (61 MB, 3.8
-// TB/s: one workgroup per compute unit holds its row between reading and writing); 256 x 670,091 bf16 176 to 181
-// us, twice a first pass of 34 (5.0 TB/s) and a second of 56 (343 MB read and written in all, where a copy of z
-// alone takes 127).
+// TB/s: one workgroup per compute unit holds its row between reading and writing); 256 x 670,091 bf16 170 us, a
+// first pass of 57 (6.0 TB/s) and a second of 107 (343 MB read and written; a copy of z alone takes 127, here the
+// memory's cache holds part of z).
 #include <math.h>
 
-#include <algorithm>
 #include <type_traits>
 
 #include "asgd_dev.h"
@@ -30,12 +29,12 @@ namespace {
 
 constexpr int KD_THREADS = 256;
 constexpr int KD_WAVES = KD_THREADS / 64;
-constexpr int KD_WGS = 1024;  // workgroups wanted for the first pass of a slab
+constexpr int KD_WGS = 1024;  // workgroups wanted for the first pass
 // Vectors a thread of the second pass, 12 KB a workgroup; 2 | 3 | 4 | 8 of them: 256 x 670,091 bf16 187 | 181 |
-// 178 | 182 us, 512 x 205,443 fp32 216 | 205 | 220 | 309.
+// 178 | 182 us, 512 x 205,443 fp32 216 | 205 | 220 | 309 (in slabs; without, 2 | 3 | 4: 184 | 171 | 170 and 207 | 199 | 216).
 constexpr int KD_U = 3;
 constexpr int KD_ROWS = 512;
-constexpr int64_t KD_SLAB = 192 << 20;
+constexpr int KD_GRID = 1 << 20;  // workgroups along x at most (a dimension has below 2^32 threads)
 
 __device__ __forceinline__ bool finite(float v) { return (__float_as_uint(v) & 0x7f800000u) != 0x7f800000u; }
 
@@ -323,19 +322,19 @@ struct __align__(16) Entry {
 
 // First pass.  The first workgroups make the rows' entries, beside the others' reading.
 template <typename T>
-__global__ __launch_bounds__(KD_THREADS) void k_distill_sums(DistillJob job, int row0, int rows, float ce, int splits,
+__global__ __launch_bounds__(KD_THREADS) void k_distill_sums(DistillJob job, float ce, int splits,
                                                              int vec_split, float2* __restrict__ part,
                                                              Entry* __restrict__ entries) {
   __shared__ float2 red2[KD_WAVES];
   __shared__ float red[KD_WAVES];
   __shared__ float q[DISTILL_MAX_K];
   __shared__ int q_id[DISTILL_MAX_K];
-  const int block = (int)blockIdx.x - rows;
+  const int block = (int)blockIdx.x - job.n_rows;
   if (block >= 0) {
-    piece_sums<T>(job, row0 + block / splits, block % splits, ce, splits, vec_split, part, red2);
+    piece_sums<T>(job, block / splits, block % splits, ce, splits, vec_split, part, red2);
     return;
   }
-  const int row = row0 + blockIdx.x, tid = threadIdx.x, k = job.k;
+  const int row = blockIdx.x, tid = threadIdx.x, k = job.k;
   const Row<T> zr((T*)const_cast<void*>(job.z), job.ld, row, job.n_cols);
   const bool some = teacher<KD_THREADS>(job.t_ids + (int64_t)row * k, job.t_logits + (int64_t)row * k, k, job.n_labels,
                                         job.temperature, q, q_id, red);
@@ -353,7 +352,7 @@ __global__ __launch_bounds__(KD_THREADS) void k_distill_sums(DistillJob job, int
 // them; the first of a row's also finds its loss (without GRAD the only one).  Workgroups go through the rows from
 // the last one back: what the first pass read last is what the memory's cache still holds.
 template <typename T, bool GRAD>
-__global__ __launch_bounds__(KD_THREADS) void k_distill_grad(DistillJob job, int row0, int rows, int chunks, float ce,
+__global__ __launch_bounds__(KD_THREADS) void k_distill_grad(DistillJob job, int chunks, float ce,
                                                              float ce_lo, float mean_weight, int splits,
                                                              const float2* __restrict__ part,
                                                              const Entry* __restrict__ entries) {
@@ -361,7 +360,9 @@ __global__ __launch_bounds__(KD_THREADS) void k_distill_grad(DistillJob job, int
   constexpr int V = R::V;
   __shared__ float red[KD_WAVES];
   const int tid = threadIdx.x, lane = tid & 63, k = job.k;
-  const int row = row0 + rows - 1 - (int)(blockIdx.x / chunks), chunk = chunks - 1 - (int)(blockIdx.x % chunks);
+  const unsigned block = blockIdx.y * gridDim.x + blockIdx.x;
+  const int row = job.n_rows - 1 - (int)(block / (unsigned)chunks), chunk = chunks - 1 - (int)(block % (unsigned)chunks);
+  if (row < 0) return;
   const R zr((T*)const_cast<void*>(job.z), job.ld, row, job.n_cols);
   const Parts<T> at(zr);
   const int v0 = at.va + chunk * (KD_THREADS * KD_U), v1 = max(v0, min(at.vb, v0 + KD_THREADS * KD_U));
@@ -443,26 +444,21 @@ __global__ __launch_bounds__(KD_THREADS) void k_distill_grad(DistillJob job, int
 
 }  // namespace
 
-// Slabs of rows whose logits the memory's cache (256 MB) holds between the two passes, and
-// pieces per row so that a slab's fill the GPU.  Measured, one slab | slabs of 192 MB (16-bit logits): 256 x
-// 670,091 bf16 202 | 196 us (rows in the same order in both passes, one slab: 219), 512 x 205,443 fp32 243 | 226;
-// slabs of 64 MB, the first pass of one beside the second of another in a launch: 226 and 257.  512 | 1,024 |
-// 2,048 workgroups for a slab's first pass: 183 | 176 | 183 us and 223 | 220 | 226.
-DistillShape distill_shape(int rows, int cols) {
-  DistillShape sh;
-  const int64_t n = ((int64_t)rows * cols * 2 + KD_SLAB - 1) / KD_SLAB;
-  sh.slabs = (int)(n < rows ? n : rows);
-  const int per = (rows + sh.slabs - 1) / sh.slabs;
-  const int want = (KD_WGS + per - 1) / per, most = (cols + 8191) / 8192;
-  sh.splits = want < most ? want : most;
-  return sh;
+// Pieces per row so that the first pass fills the GPU.  The second pass starts where the
+// first one ended, on what the memory's cache (256 MB) still holds.  Slabs of 192 MB, both passes of one before
+// the next, | none: 256 x 670,091 bf16 180 | 173 us, 512 x 205,443 fp32 205 | 200, bf16 109 | 100; both passes from the
+// first row on (one slab): 219 for the first of these at the time when the way back took 202.  512 | 1,024 |
+// 2,048 workgroups wanted: 180 | 171 | 172 us for the first, and no difference beyond 2 us for the others.
+int distill_splits(int rows, int cols) {
+  const int want = (KD_WGS + rows - 1) / rows, most = (cols + 8191) / 8192;
+  return want < most ? want : most;
 }
 
 // Scratch memory: per row the pieces' sums and whether its teacher counts, then the teachers' entries.
-static size_t part_bytes(const DistillShape& sh, int rows) {
-  return ((size_t)rows * (sh.splits + 1) * sizeof(float2) + 255) / 256 * 256;
+static size_t part_bytes(int splits, int rows) {
+  return ((size_t)rows * (splits + 1) * sizeof(float2) + 255) / 256 * 256;
 }
-size_t distill_ws_bytes(const DistillShape& sh, int rows, int k) { return part_bytes(sh, rows) + (size_t)rows * k * sizeof(Entry); }
+size_t distill_ws_bytes(int splits, int rows, int k) { return part_bytes(splits, rows) + (size_t)rows * k * sizeof(Entry); }
 
 template <typename T, int THREADS, int NV>
 static hipError_t distill_rows(const DistillJob& j, float ce, float ce_lo, hipStream_t st) {
@@ -475,7 +471,7 @@ static hipError_t distill_rows(const DistillJob& j, float ce, float ce_lo, hipSt
 }
 
 template <typename T>
-static hipError_t distill_as(const DistillJob& j, const DistillShape& sh, void* ws, hipStream_t st) {
+static hipError_t distill_as(const DistillJob& j, int splits, void* ws, hipStream_t st) {
   const double c = 1.4426950408889634 / (double)j.temperature;
   const float ce = (float)c, ce_lo = (float)(c - (double)ce);
   const int n_vec = j.n_cols / Row<T>::V;  // whole vectors of a row at most
@@ -486,31 +482,29 @@ static hipError_t distill_as(const DistillJob& j, const DistillShape& sh, void* 
   // each on (two passes | this: 512 x 60,000 fp32 63 | 51 us, 300 x 100,000 bf16 36 | 47 us; rows of 400 KB in the
   // same way do not gain: 512 x 205,443 bf16 109 | 121 us)
   if (j.n_rows >= KD_ROWS && n_vec <= 16 * 1024) return distill_rows<T, 1024, 16>(j, ce, ce_lo, st);
-  const int vps = (n_vec + sh.splits - 1) / sh.splits;
+  const int vps = (n_vec + splits - 1) / splits;
   float2* part = (float2*)ws;
-  Entry* entries = (Entry*)((char*)ws + part_bytes(sh, j.n_rows));
+  Entry* entries = (Entry*)((char*)ws + part_bytes(splits, j.n_rows));
   const float mean = 1.0f / (float)j.n_rows;
-  const int per = j.grad ? (j.n_rows + sh.slabs - 1) / sh.slabs : j.n_rows;
-  const int chunks = (n_vec + KD_THREADS * KD_U - 1) / (KD_THREADS * KD_U);
   const dim3 block(KD_THREADS);
-  for (int r0 = 0; r0 < j.n_rows; r0 += per) {
-    const int rows = std::min(per, j.n_rows - r0);
-    hipLaunchKernelGGL(k_distill_sums<T>, dim3((unsigned)rows * (sh.splits + 1)), block, 0, st, j, r0, rows, ce, sh.splits,
-                       vps, part, entries);
-    if (j.grad)
-      hipLaunchKernelGGL((k_distill_grad<T, true>), dim3((unsigned)rows * chunks), block, 0, st, j, r0, rows, chunks, ce,
-                         ce_lo, mean, sh.splits, part, entries);
-    else
-      hipLaunchKernelGGL((k_distill_grad<T, false>), dim3(rows), block, 0, st, j, r0, rows, 1, ce, ce_lo, mean, sh.splits,
-                         part, entries);
+  hipLaunchKernelGGL(k_distill_sums<T>, dim3((unsigned)j.n_rows * (splits + 1)), block, 0, st, j, ce, splits, vps, part,
+                     entries);
+  if (j.grad) {
+    const int chunks = (n_vec + KD_THREADS * KD_U - 1) / (KD_THREADS * KD_U);
+    const int64_t n = (int64_t)j.n_rows * chunks, y = (n + KD_GRID - 1) / KD_GRID;
+    hipLaunchKernelGGL((k_distill_grad<T, true>), dim3((unsigned)((n + y - 1) / y), (unsigned)y), block, 0, st, j, chunks,
+                       ce, ce_lo, mean, splits, part, entries);
+  } else {
+    hipLaunchKernelGGL((k_distill_grad<T, false>), dim3(j.n_rows), block, 0, st, j, 1, ce, ce_lo, mean, splits, part,
+                       entries);
   }
   return hipGetLastError();
 }
 
-hipError_t launch_distill(int dtype, const DistillJob& j, const DistillShape& sh, void* ws, hipStream_t st) {
-  if (dtype == 0) return distill_as<float>(j, sh, ws, st);
-  if (dtype == 1) return distill_as<bf16>(j, sh, ws, st);
-  return distill_as<f16>(j, sh, ws, st);
+hipError_t launch_distill(int dtype, const DistillJob& j, int splits, void* ws, hipStream_t st) {
+  if (dtype == 0) return distill_as<float>(j, splits, ws, st);
+  if (dtype == 1) return distill_as<bf16>(j, splits, ws, st);
+  return distill_as<f16>(j, splits, ws, st);
 }
 
 }  // namespace asgd

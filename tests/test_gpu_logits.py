@@ -643,6 +643,25 @@ def test_rows_past_two_to_the_31_elements():
     assert torch.equal(z, alone)
 
 
+def test_distill_past_a_million_workgroups():
+    B, L, T = 1600, (1 << 22) - 3, 1.0
+    flush("  allocating 13.4 GB")
+    r = np.random.default_rng(7)
+    row = r.normal(0, 2, L)
+    z = torch.empty((B, L), dtype=torch.bfloat16, device="cuda")
+    z.copy_(dev(row))
+    ids, t = teacher(r, B, 1000, 5)
+    at = [0, 2, 799, B - 1]
+    x = host(z[:1]).repeat(len(at), 0)
+    w = r.uniform(0.5, 2.0, B).astype(np.float32)
+    loss = host(distill(z, dev(ids), dev(t), T, z, dev(w)))[at]
+    want, g, p, q = ref.distill(x, ids[at], t[at], T, w[at])
+    err = np.abs(host(z[at]) - g)
+    assert (err <= distill_bounds(x, ids[at], t[at], T, w[at], p, q, "bf16")).all()
+    size = T * T * (np.abs(x).max(1) / T * 2 + np.log(L) + 16)
+    assert (np.abs(loss - want) <= size * (16 + 1 + L / 512) * 2 * U).all()
+
+
 def test_fp4_rows_past_two_to_the_31_elements():
     B, L, ld = 520, 1000, (1 << 22) + 8
     flush("  allocating 8.8 GB")
