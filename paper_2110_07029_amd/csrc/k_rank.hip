@@ -187,12 +187,14 @@ __device__ __forceinline__ void raise2(float v, float& m, float& s) {
   }
 }
 __device__ __forceinline__ void merge2(float& m, float& s, float m2, float s2) { soft_merge(m, s, m2, s2, 1.0f); }
-// The row's log-sum-exp; best: its best key.  Beyond 2^32 the sum's logarithm, at most
-// ln 2^22, is below half a step of the best score (and the score's product with log2 e may overflow).
+// The row's log-sum-exp; best: its best key.  From 2^28 on the sum's logarithm, at most ln 2^22 = 15.3, is below
+// half a step (16; a step above -2^28 itself) of the best score, which is then the answer.  Below that the product that m is
+// taken from is below 2^29 and its rounding at most 16, so the best label's term neither vanishes nor
+// loses more to its clamp than a step of the score; far above it that rounding passes the exponents of floats.
 __device__ __forceinline__ float lse_of(u64 best, float m, float s) {
   if (!best) return -INFINITY;
   const float top = of_order((unsigned)(best >> 32));
-  return fabsf(top) < 4294967296.0f ? (m + __builtin_amdgcn_logf(s)) * LN2 : top;
+  return fabsf(top) < 268435456.0f ? (m + __builtin_amdgcn_logf(s)) * LN2 : top;
 }
 
 // (m, s) of all lanes as one, on all of them: the largest m, and the sums under it.

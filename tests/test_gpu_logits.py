@@ -418,6 +418,47 @@ def test_topk_twice_is_bitwise_the_same_and_stays_in_its_rows():
     check_rank(first, ref.scores(host(z), **o), k, allowed)
 
 
+# Where ceil(v log2 e), formed from the rounded product, lay far above the exact one.
+FAR = [3000000512.0, -3000000768.0, 3182850800.0, 3.0366761e9, -3.0031217e9, 1.6e9, -1.9e9, 4.2e9, 2.0 ** 28, -(2.0 ** 28),
+       2.0 ** 32, -(2.0 ** 32)]
+
+
+def far_scores(r, B):
+    """Best scores of either sign from 2^23 to 2^34."""
+    v = np.exp2(r.uniform(23, 34, B)) * r.choice([-1, 1], B)
+    v[:len(FAR)] = FAR[:B]
+    return v
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("B,L", [(300, 1), (300, 130), (64, 9001), (40, 140_000)])
+def test_topk_lse_of_very_large_scores(dtype, B, L):
+    r = np.random.default_rng(L)
+    top = far_scores(r, B)
+    # labels at the best score, next to it, and far below
+    x = top[:, None] - np.abs(top[:, None]) * r.choice([0.0, 2.0 ** -22, 2.0 ** -7, 0.1, 1.0], (B, L), p=[.1, .2, .2, .2, .3])
+    x[:, L // 2] = top
+    z = strided(x, dtype, 1, 3)
+    check_rank(rank(z, 5), ref.scores(host(z)), 5)
+
+
+@pytest.mark.parametrize("B,L", [(100, 300), (20, 60_000)])
+def test_topk_lse_of_very_large_listed_scores(B, L):
+    # the best label is one that the lists name: its score goes through their own sum
+    r = np.random.default_rng(B)
+    top = far_scores(r, B)
+    x = r.normal(0, 2, (B, L)).astype(np.float32)
+    x[top < 0] += 2 * top[top < 0, None].astype(np.float32)
+    at = r.integers(0, L, B)
+    row_bias = [(np.array([j]), np.array([t], np.float32)) for j, t in zip(at, top)]
+    x[np.arange(B), at] = 0.5
+    c, keep = lists(row_bias, L, values=True)
+    seen = [np.array([j, j]) for j in at]
+    c2, keep2 = lists(seen, L)
+    check_rank(rank(dev(x), 3, asgd.logit_rules(seen=c2, row_bias=c, frequency=0.25)),
+               ref.scores(x, seen=seen, row_bias=row_bias, frequency=0.25), 3)
+
+
 # ---------------------------------------------------------------- distillation
 def teacher(r, B, L, k, empty=0.2):
     ids = np.stack([r.permutation(max(L, k))[:k] for _ in range(B)]).astype(np.int32)
