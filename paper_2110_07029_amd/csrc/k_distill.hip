@@ -121,20 +121,26 @@ __device__ __forceinline__ bool teacher(const int32_t* t_ids, const float* t_log
   return some;
 }
 
+// An entry's part of the loss, T^2 q (ln q - ln p) with ln p = (z - m) / T - ln s.  (z - m) / T may pass the type's
+// range where T times it does not (z of the lowest value as a mask, T below 1), and z - m itself may: so the
+// distance is taken at half its size and meets q first, then 2 T.
+__device__ __forceinline__ float entry_loss(float q, float z, float m, float log_s, float temp) {
+  return fmaf(2.0f * temp, q * (0.5f * m - 0.5f * z), temp * temp * (q * (logf(q) + log_s)));
+}
 // (a row of -inf gives no label any probability)
-__device__ __forceinline__ float whole_loss(float sum, float m, float temp, bool some) {
-  return !some ? 0.0f : m == -INFINITY ? INFINITY : temp * temp * sum;
+__device__ __forceinline__ float whole_loss(float sum, float m, bool some) {
+  return !some ? 0.0f : m == -INFINITY ? INFINITY : sum;
 }
 
-// T^2 sum q (ln q - ln p) from the student's logits of the entries (the thread's own entries' q).
+// The loss from the student's logits of the entries (the thread's own entries' q).
 template <int THREADS>
 __device__ __forceinline__ float row_loss(const float* q, const float* z_t, int k, float m, float s, float temp, bool some,
                                           float* red) {
   const float log_s = logf(s);
   float part = 0.0f;
   for (int e = threadIdx.x; e < k; e += THREADS)
-    if (q[e] > 0.0f) part += q[e] * (logf(q[e]) - ((z_t[e] - m) / temp - log_s));
-  return whole_loss(wg_sum<THREADS / 64>(part, red), m, temp, some);
+    if (q[e] > 0.0f) part += entry_loss(q[e], z_t[e], m, log_s, temp);
+  return whole_loss(wg_sum<THREADS / 64>(part, red), m, some);
 }
 
 // Whether entry e is the first of those that name its label; *sum: q over all of them.
@@ -408,9 +414,9 @@ __global__ __launch_bounds__(KD_THREADS) void k_distill_grad(DistillJob job, int
     float sum = 0.0f;
 #pragma unroll
     for (int j = 0; j < E; ++j)
-      if (t[j].q > 0.0f) sum += t[j].q * (logf(t[j].q) - ((t[j].z - m) / job.temperature - log_s));
+      if (t[j].q > 0.0f) sum += entry_loss(t[j].q, t[j].z, m, log_s, job.temperature);
     sum = wg_sum<KD_WAVES>(sum, red);
-    if (tid == 0) job.loss_rows[row] = whole_loss(sum, m, job.temperature, some);
+    if (tid == 0) job.loss_rows[row] = whole_loss(sum, m, some);
   }
   if constexpr (GRAD) {
     const R gr((T*)job.grad, job.ld_grad, row, job.n_cols);

@@ -643,6 +643,38 @@ def test_distill_at_the_ends_of_the_temperatures(dtype, L, T):
     assert np.isfinite(host(grad)).all() and (err <= bound).all(), (err / bound).max()
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("L", [9, 300, 40_003, 200_000])
+@pytest.mark.parametrize("T", [1e-6, 0.25, 0.5, 1.0, 3.0])
+def test_distill_loss_of_teachers_labels_masked_by_the_lowest_value(dtype, L, T):
+    # T^2 times (gap / T) is finite where gap / T is not
+    r = np.random.default_rng(L)
+    low = float(torch.finfo(ref.DTYPES[dtype]).min)
+    x = r.normal(0, 2, (5, L))
+    x[0, 3] = x[1, L // 2:] = low
+    x[2, L - 1] = 0.75 * low
+    x[3, 1:] = low
+    x[3, 0], x[4, 0], x[4, 2] = 0.9 * -low, 0.5 * -low, 0.5 * low  # (and gaps beyond the type)
+    z = strided(x, dtype, 1, 3)
+    ids = np.array([[3, 0], [L - 1, 1], [L - 1, L - 1], [2, 0], [2, 0]], np.int32)
+    t = (np.array([[0.0, 0.5], [1.0, 0.0], [-1.0, 0.0], [0.0, 2.0], [0.0, 0.0]]) * min(T, 1.0)).astype(np.float32)
+    grad = torch.empty((5, L), dtype=z.dtype, device="cuda")
+    loss = distill(z, dev(ids), dev(t), T, grad)
+    assert torch.equal(distill(z, dev(ids), dev(t), T), loss)
+    xx = host(z)
+    want, g, p, q = ref.distill(xx, ids, t, float(np.float32(T)))
+    with np.errstate(over="ignore"):
+        infinite = np.isinf(want.astype(np.float32))
+    got = host(loss)
+    assert np.array_equal(np.isinf(got), infinite) and (got[infinite] == INF).all()
+    # in half steps: q has its argument's (at most 2) two, its exponential's two, the sum's as many again, weighted, and
+    # one, and a division's and a product's: 15; the gap's rounding, three products and two additions are six more
+    ok = ~infinite
+    assert (np.abs(got - want)[ok] <= 24 * U * want[ok]).all(), (got, want)
+    assert (np.abs(host(grad) - g) <= distill_bounds(np.where(p > 1e-30, xx, -INF), ids, t, T, np.full(5, 0.2), p, q, dtype)
+            + T * 1e-30).all()
+
+
 def test_distill_gradient_against_differences():
     # the loss in fp32 moves by its gradient times the step, up to the loss's own rounding
     B, L, T = 3, 50, 1.3
