@@ -160,6 +160,39 @@ def test_distill_step_updates(bf16, extra, B, L, k, T):
         s.free()
 
 
+@pytest.mark.parametrize("bf16", [False, True])
+@pytest.mark.parametrize("B,L", [(40, 40_003), (3, 150_001)])
+def test_distill_step_of_long_rows(bf16, B, L):
+    # rows beyond a workgroup's registers, gradient in place on the model's padded rows, label tiles over all XCDs
+    k, T, lr = 20, 2.0, 0.25
+    s = Setup(workload(L), 64, 64, bf16=bf16, flags=asgd.ASGD_UNFUSED_OUTPUT)
+    try:
+        trained_scale(s, 4)
+        before = s.params()
+        r = np.random.default_rng(L)
+        ids = r.integers(0, L, (B, k)).astype(np.int32)
+        t = r.normal(3, 1, (B, k)).astype(np.float32)
+        ids[0, 0], ids[0, 1], ids[0, 2] = L, L - 1, 0  # a padding column, the last label and the first
+        ids[1], t[1] = ref.EMPTY, -np.inf              # no teacher
+        ids[2, 4:] = ids[2, 0]                         # one label seventeen times
+        x, _ = s.host_batch(0, B)
+        loss = asgd.asgd_distill_step(s.m, s.xb(0, B), dev(ids), dev(t), T, lr, want_loss=True)
+        after = s.params()
+        want, want_loss, mag, _ = distill_oracle(before, x, ids, t, T, lr, 0)
+        rtol = RTOL_BF16 if bf16 else RTOL_FP32
+        assert abs(loss - want_loss) <= rtol * abs(want_loss), (loss, want_loss)
+        for n in want:
+            assert_update_close(n, before[n], after[n], want[n], rtol, mag[n])
+        from gpu_util import SELECT
+        for n, v in before.items():
+            asgd.asgd_model_set_params(s.m, SELECT[n], v)
+        asgd.asgd_distill_step(s.m, s.xb(0, B), dev(ids), dev(t), T, lr)
+        again = s.params()
+        assert all(np.array_equal(again[n], after[n]) for n in after)
+    finally:
+        s.free()
+
+
 def test_distill_step_needs_stored_logits_and_checks_its_arguments():
     s = Setup(workload(100), 20, 20)
     u = Setup(workload(100), 20, 20, flags=asgd.ASGD_UNFUSED_OUTPUT)
