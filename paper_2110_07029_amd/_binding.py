@@ -89,6 +89,8 @@ class asgd_logit_rules(ctypes.Structure):
     _fields_ = [("bias", c_void_p), ("allowed", c_void_p), ("allowed_ld", c_int64), ("seen", POINTER(asgd_csr)),
                 ("row_bias", POINTER(asgd_csr)), ("repetition", c_double), ("frequency", c_double),
                 ("presence", c_double)]
+    # (rows, columns) of logits that the tensors behind bias and allowed reach for, where they are known.
+    covers = None
 
 
 class asgd_elastic_log(ctypes.Structure):
@@ -214,11 +216,13 @@ def asgd_model_init(n_features: int, n_labels: int, max_batch: int, max_nnz: int
     h = c_void_p()
     _check(load().asgd_model_init(byref(h), byref(cfg), c_uint64(seed & (2 ** 64 - 1)), _stream(stream)),
            "asgd_model_init")
+    _n_labels[h.value] = n_labels
     return h.value
 
 
 def asgd_model_free(m: int):
     _check(load().asgd_model_free(m), "asgd_model_free")
+    _n_labels.pop(m, None)
 
 
 def asgd_model_set_stream(m: int, stream):
@@ -370,11 +374,13 @@ def asgd_elastic_create(cfg: asgd_elastic_config, model_cfg: asgd_config, seed: 
     h = c_void_p()
     _check(load().asgd_elastic_create(byref(h), byref(cfg), byref(model_cfg), c_uint64(seed), arr,
                                       _stream(global_stream)), "asgd_elastic_create")
+    _n_labels[h.value] = model_cfg.n_labels
     return h.value
 
 
 def asgd_elastic_free(e: int):
     _check(load().asgd_elastic_free(e), "asgd_elastic_free")
+    _n_labels.pop(e, None)
 
 
 def asgd_elastic_round(e: int, x_all: asgd_csr, y_all: asgd_csr, x_indptr_host: np.ndarray,
@@ -405,10 +411,21 @@ def asgd_elastic_round(e: int, x_all: asgd_csr, y_all: asgd_csr, x_indptr_host: 
 def asgd_elastic_model(e: int, which: int) -> int:
     h = c_void_p()
     _check(load().asgd_elastic_model(e, which, byref(h)), "asgd_elastic_model")
+    _n_labels[h.value] = _n_labels.get(e, 0)
     return h.value
 
 
 # ------------------------------------------------------------------ label logits
+# Labels of the models that this module created, by handle.
+_n_labels = {}
+
+
+def _too_short(r: asgd_logit_rules, rows: int, cols: int):
+    """The library sees addresses only, so the sizes behind them are checked here."""
+    raise ValueError(f"rules.bias and rules.allowed reach for {r.covers[0]} rows of {r.covers[1]} labels at most, "
+                     f"the logits have {rows} of {cols}")
+
+
 def _span(ws):
     """(address, bytes) of scratch memory given as a tensor or None."""
     return (None, 0) if ws is None else (ws.data_ptr(), ws.numel() * ws.element_size())
@@ -436,6 +453,8 @@ def asgd_logits_topk_workspace(n_rows: int, n_cols: int, k: int) -> int:
 
 
 def asgd_logits_topk(z: asgd_matrix, k: int, ids, scores=None, rules=None, lse=None, workspace=None, stream=None):
+    if rules is not None and rules.covers is not None and (rules.covers[0] < z.n_rows or rules.covers[1] < z.n_cols):
+        _too_short(rules, z.n_rows, z.n_cols)
     ws, n = _span(workspace)
     _check(load().asgd_logits_topk(byref(z), None if rules is None else byref(rules), k, _ptr(ids), _ptr(scores),
                                    _ptr(lse), ws, n, _stream(stream)), "asgd_logits_topk")
@@ -468,6 +487,10 @@ def asgd_predict_rules_workspace(m: int, n_rows: int, k: int) -> int:
 
 def asgd_predict_topk_rules(m: int, x: asgd_csr, k: int, ids_dev, scores_dev=None, lse_dev=None, rules=None, w=None,
                             workspace=None):
+    if rules is not None and rules.covers is not None:
+        cols = _n_labels.get(m, 0)
+        if rules.covers[0] < x.n_rows or rules.covers[1] < cols:
+            _too_short(rules, x.n_rows, cols)
     ws, n = _span(workspace)
     _check(load().asgd_predict_topk_rules(m, byref(x), k, None if rules is None else byref(rules),
                                           None if w is None else byref(w), _ptr(ids_dev), _ptr(scores_dev),

@@ -52,14 +52,30 @@ class _Types(dict):
         return code
 
 
+class _Is(dict):
+    """Whether one of torch's element types is among the named."""
+
+    def __init__(self, *names):
+        self.names = names
+
+    def __missing__(self, dtype):
+        self[dtype] = str(dtype) in self.names
+        return self[dtype]
+
+
 _TYPES = _Types()
+_FLOAT = _Is("torch.float32")
+_WORD = _Is("torch.int32", "torch.uint32")
+_LIST = ctypes.POINTER(asgd_csr)
+_ANY = 1 << 31  # more rows or columns than any matrix has
 
 
 def matrix(t) -> asgd_matrix:
     """A 2-d tensor (unit stride along a row) as an asgd_matrix; the tensor must outlive its use."""
-    if t.dim() != 2:
+    shape = t.shape
+    if len(shape) != 2:
         raise ValueError("a matrix has two dimensions")
-    rows, cols = t.shape
+    rows, cols = shape
     ld, step = t.stride()
     if step != 1 and cols > 1:
         raise ValueError("a matrix needs unit stride along a row")
@@ -79,12 +95,24 @@ def fp4_matrix(codes, scales) -> asgd_fp4:
 def logit_rules(bias=None, allowed=None, seen=None, repetition: float = 1.0, frequency: float = 0.0,
                 presence: float = 0.0, row_bias=None) -> asgd_logit_rules:
     """Rules from tensors (bias: float32 [L]; allowed: int32 / uint32 words, [rows, words] or
-    [words] for one mask for all rows) and asgd_csr lists."""
-    ld = 0 if allowed is None or allowed.dim() == 1 else allowed.stride(0) if allowed.shape[0] > 1 else allowed.shape[1]
-    r = asgd_logit_rules(None if bias is None else bias.data_ptr(), None if allowed is None else allowed.data_ptr(), ld,
-                         None, None, repetition, frequency, presence)
-    if seen is not None:
-        r.seen = ctypes.pointer(seen)
-    if row_bias is not None:
-        r.row_bias = ctypes.pointer(row_bias)
+    [words] for one mask for all rows) and asgd_csr lists.  Other types and strides raise ValueError, as
+    do tensors too short for the logits where the rules meet them.  The tensors must outlive the rules' use."""
+    at = mask = None
+    ld, rows, cols = 0, _ANY, _ANY
+    if bias is not None:
+        if bias.stride() != (1,) and (bias.dim() != 1 or bias.numel() > 1) or not _FLOAT[bias.dtype]:
+            raise ValueError("rules.bias is a contiguous float32 tensor of one dimension")
+        at, cols = bias.data_ptr(), bias.numel()
+    if allowed is not None:
+        shape, step = allowed.shape, allowed.stride()
+        if len(shape) not in (1, 2) or (step[-1] != 1 and shape[-1] > 1) or not _WORD[allowed.dtype]:
+            raise ValueError("rules.allowed holds int32 or uint32 words, [rows, words] or [words], with unit stride along a row")
+        mask, cols = allowed.data_ptr(), min(cols, 32 * shape[-1])
+        if len(shape) == 2:
+            rows = shape[0]
+            ld = step[0] if rows > 1 else shape[1]
+    r = asgd_logit_rules(at, mask, ld, None if seen is None else _LIST(seen), None if row_bias is None else _LIST(row_bias),
+                         repetition, frequency, presence)
+    if cols != _ANY:
+        r.covers = rows, cols
     return r

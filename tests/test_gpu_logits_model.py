@@ -193,6 +193,19 @@ def test_distill_step_of_long_rows(bf16, B, L):
         s.free()
 
 
+def test_rules_too_short_for_the_models_labels_are_refused():
+    s = Setup(workload(100), 20, 20)
+    try:
+        for kw in (dict(bias=torch.zeros(99, device="cuda")), dict(allowed=torch.zeros(3, dtype=torch.int32, device="cuda")),
+                   dict(allowed=torch.zeros((1, 4), dtype=torch.int32, device="cuda"))):
+            with pytest.raises(ValueError):
+                predict(s, 4, 2, asgd.logit_rules(**kw))
+        b = torch.zeros(100, device="cuda")
+        predict(s, 4, 2, asgd.logit_rules(bias=b))
+    finally:
+        s.free()
+
+
 def test_distill_step_needs_stored_logits_and_checks_its_arguments():
     s = Setup(workload(100), 20, 20)
     u = Setup(workload(100), 20, 20, flags=asgd.ASGD_UNFUSED_OUTPUT)

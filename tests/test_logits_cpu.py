@@ -196,6 +196,39 @@ def test_tensor_helpers_check_layout():
     assert asgd.logit_rules(allowed=w[:1]).allowed_ld == 7
 
 
+def test_rule_tensors_of_other_types_and_strides_are_refused():
+    b, w = torch.zeros(100), torch.zeros(4, 7, dtype=torch.int32)
+    for bad in (b.bfloat16(), b.half(), b.double(), b.int(), b[::2], b[None], b[0]):
+        with pytest.raises(ValueError, match="bias"):
+            asgd.logit_rules(bias=bad)
+    for bad in (w.long(), w.short(), w.bool(), w.float(), w[:, ::2], w[0, ::2], w.T, w[None], w[0, 0]):
+        with pytest.raises(ValueError, match="allowed"):
+            asgd.logit_rules(allowed=bad)
+    r = asgd.logit_rules(bias=b[3:], allowed=w[1:, 2:5])
+    assert (r.bias, r.allowed, r.allowed_ld) == (b.data_ptr() + 12, w.data_ptr() + 4 * 9, 7)
+    assert asgd.logit_rules(allowed=w.view(torch.uint32)).allowed_ld == 7
+    assert asgd.logit_rules(allowed=w[:1].expand(4, 7)).allowed_ld == 0  # one mask for all rows
+    assert asgd.logit_rules(bias=b[::50][:1]).bias == b.data_ptr()       # one entry has no stride
+    assert asgd.logit_rules(allowed=w[:, ::7]).allowed_ld == 7
+
+
+def test_rule_tensors_too_short_for_the_logits_are_refused(monkeypatch):
+    w = torch.zeros(4, 4, dtype=torch.int32)
+    bad = [(dict(bias=torch.zeros(99)), "of 99 labels"), (dict(allowed=w[:3]), "for 3 rows"),
+           (dict(allowed=w[:1]), "for 1 rows"), (dict(allowed=w[:, :3]), "of 96 labels"),
+           (dict(allowed=w[0, :3]), "of 96 labels")]
+    monkeypatch.setitem(asgd._binding._n_labels, None, 100)
+    for kw, word in bad:
+        rules = asgd.logit_rules(**kw)
+        with pytest.raises(ValueError, match=word):
+            asgd.asgd_logits_topk(mat(), 1, A, rules=rules, workspace=BIG)
+        with pytest.raises(ValueError, match=word):
+            asgd.asgd_predict_topk_rules(None, csr(), 1, A, rules=rules, workspace=BIG)
+    # what covers the logits goes on to the library, which refuses something else
+    for kw in (dict(bias=torch.zeros(100), allowed=w), dict(allowed=w[0]), dict(allowed=w[:1].expand(4, 4))):
+        refused(asgd.ASGD_EINVAL, "k must", asgd.asgd_logits_topk, mat(), 0, A, rules=asgd.logit_rules(**kw), workspace=BIG)
+
+
 def test_reference_pins():
     # hand-computed: the largest magnitude 7.1 gives scale 2^0, 5 and 0.25 are midpoints
     x = np.zeros((1, 32))
