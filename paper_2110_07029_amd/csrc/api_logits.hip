@@ -37,6 +37,8 @@ asgd_status check_list(const asgd_csr* a, const char* name, int rows, int cols, 
   if (!a->indptr) return set_error_named(ASGD_EINVAL, name, ".indptr is NULL");
   if (a->nnz > 0 && !a->indices) return set_error_named(ASGD_EINVAL, name, ".indices is NULL");
   if (values && a->nnz > 0 && !a->values) return set_error_named(ASGD_EINVAL, name, ".values is NULL");
+  if (((uintptr_t)a->indptr | (uintptr_t)a->indices | (values ? (uintptr_t)a->values : 0)) % 4)
+    return set_error_named(ASGD_EINVAL, name, ": indptr, indices and values must be 4-byte aligned");
   return ASGD_OK;
 }
 

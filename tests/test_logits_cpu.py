@@ -119,6 +119,13 @@ def test_bad_rules_are_refused(change, word):
     refused(asgd.ASGD_EINVAL, word, asgd.asgd_logits_topk, mat(), 1, A, rules=asgd.logit_rules(**change), workspace=BIG)
 
 
+@pytest.mark.parametrize("change", [dict(seen=csr(indptr=A + 2)), dict(seen=csr(indices=A + 1)), dict(row_bias=csr(values=A + 2)),
+                                    dict(row_bias=csr(indices=A + 3))])
+def test_misaligned_lists_are_refused(change):
+    refused(asgd.ASGD_EINVAL, "4-byte aligned", asgd.asgd_logits_topk, mat(), 1, A, rules=asgd.logit_rules(**change),
+            workspace=BIG)
+
+
 def test_rule_masks_and_outputs_are_checked():
     E, R = asgd.ASGD_EINVAL, asgd.ASGD_ERANGE
     r = asgd.asgd_logit_rules(allowed=A, allowed_ld=3)
