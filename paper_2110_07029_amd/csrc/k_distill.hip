@@ -12,9 +12,9 @@
 // with the sum of q over all of them.
 //
 // Measured: 128 x 1,000 fp32 10 us (a launch and three dependent reductions); 256 x 30,000 fp32 16 us (61 MB, 3.8
-// TB/s: one workgroup per compute unit holds its row between reading and writing); 256 x 670,091 bf16 170 us, a
-// first pass of 57 (6.0 TB/s) and a second of 107 (343 MB read and written; a copy of z alone takes 127, here the
-// memory's cache holds part of z).
+// TB/s: one workgroup per compute unit holds its row between reading and writing); 256 x 670,091 bf16 163 to 170 us, a
+// first pass of 57 (6.0 TB/s) and a second of 107 (343 MB read and as many written, 6.4 TB/s; both passes ask the
+// memory for the whole of z).
 #include <math.h>
 
 #include <type_traits>
@@ -30,8 +30,8 @@ namespace {
 constexpr int KD_THREADS = 256;
 constexpr int KD_WAVES = KD_THREADS / 64;
 constexpr int KD_WGS = 1024;  // workgroups wanted for the first pass
-// Vectors a thread of the second pass, 12 KB a workgroup; 2 | 3 | 4 | 8 of them: 256 x 670,091 bf16 187 | 181 |
-// 178 | 182 us, 512 x 205,443 fp32 216 | 205 | 220 | 309 (in slabs; without, 2 | 3 | 4: 184 | 171 | 170 and 207 | 199 | 216).
+// Vectors a thread of the second pass, 12 KB a workgroup; 2 | 3 | 4 of them: 256 x 670,091 bf16 184 | 171 | 170 us,
+// 512 x 205,443 fp32 207 | 199 | 216.
 constexpr int KD_U = 3;
 constexpr int KD_ROWS = 512;
 constexpr int KD_GRID = 1 << 20;  // workgroups along x at most (a dimension has below 2^32 threads)
@@ -356,7 +356,8 @@ __global__ __launch_bounds__(KD_THREADS) void k_distill_sums(DistillJob job, flo
 
 // Second pass: a workgroup writes KD_U vectors a thread of a row, then the teacher's entries among
 // them; the first of a row's also finds its loss (without GRAD the only one).  Workgroups go through the rows from
-// the last one back: what the first pass read last is what the memory's cache still holds.
+// the last one back, beginning with what the first pass read last (from the first row on | from the last one back:
+// 256 x 670,091 bf16 167 | 163 us; 512 x 205,443 fp32 202 | 201, bf16 99 | 100).
 template <typename T, bool GRAD>
 __global__ __launch_bounds__(KD_THREADS) void k_distill_grad(DistillJob job, int chunks, float ce,
                                                              float ce_lo, float mean_weight, int splits,
@@ -450,11 +451,9 @@ __global__ __launch_bounds__(KD_THREADS) void k_distill_grad(DistillJob job, int
 
 }  // namespace
 
-// Pieces per row so that the first pass fills the GPU.  The second pass starts where the
-// first one ended, on what the memory's cache (256 MB) still holds.  Slabs of 192 MB, both passes of one before
-// the next, | none: 256 x 670,091 bf16 180 | 173 us, 512 x 205,443 fp32 205 | 200, bf16 109 | 100; both passes from the
-// first row on (one slab): 219 for the first of these at the time when the way back took 202.  512 | 1,024 |
-// 2,048 workgroups wanted: 180 | 171 | 172 us for the first, and no difference beyond 2 us for the others.
+// Pieces per row so that the first pass fills the GPU: 512 | 1,024 | 2,048 workgroups wanted take 180 | 171 | 172 us
+// for 256 x 670,091 bf16, and differ by at most 2 us elsewhere.  Both passes of 192 MB of rows before the next such
+// slab were slower than each pass in one launch (180 | 173; 512 x 205,443 fp32 205 | 200, bf16 109 | 100).
 int distill_splits(int rows, int cols) {
   const int want = (KD_WGS + rows - 1) / rows, most = (cols + 8191) / 8192;
   return want < most ? want : most;
@@ -485,8 +484,8 @@ static hipError_t distill_as(const DistillJob& j, int splits, void* ws, hipStrea
   if (n_vec <= 8 * 256) return distill_rows<T, 256, 8>(j, ce, ce_lo, st);
   if (n_vec <= 8 * 1024) return distill_rows<T, 1024, 8>(j, ce, ce_lo, st);
   // 256 KB: half of a compute unit's registers, so one row at a time on each, and worth it from two rows for
-  // each on (two passes | this: 512 x 60,000 fp32 63 | 51 us, 300 x 100,000 bf16 36 | 47 us; rows of 400 KB in the
-  // same way do not gain: 512 x 205,443 bf16 109 | 121 us)
+  // each on (two passes | this, with gradient: 512 x 60,000 fp32 61 | 51 us, 512 x 100,000 bf16 53 | 52, 300 of these
+  // 36 | 47; the loss alone 25 | 29 and 23 | 32.  Rows of 400 KB in the same way: 512 x 205,443 bf16 100 | 121)
   if (j.n_rows >= KD_ROWS && n_vec <= 16 * 1024) return distill_rows<T, 1024, 16>(j, ce, ce_lo, st);
   const int vps = (n_vec + splits - 1) / splits;
   float2* part = (float2*)ws;

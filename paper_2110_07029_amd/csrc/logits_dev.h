@@ -3,8 +3,8 @@
 // A row may start anywhere (odd label counts put every row at another
 // alignment), so it is walked in the 16-byte vectors that memory is divided
 // into: `phase` elements of the first vector lie before the row, vector i holds
-// columns V i - phase .. + V - 1, and the first and last vectors are
-// accessed element by element where they reach past the row.
+// columns V i - phase .. + V - 1, and the elements before the first and after the
+// last whole vector are accessed one by one.
 #pragma once
 
 #include "asgd_dev.h"
@@ -19,48 +19,15 @@ struct Row {
   static constexpr int V = 16 / (int)sizeof(T);
   typedef T vec __attribute__((ext_vector_type(V)));
   T* base;  // 16-byte aligned; element (i, e) of vector i is column V i - phase + e
-  int phase, n_cols, n_vec;
+  int phase, n_cols;
 
   __device__ Row(T* p, int64_t ld, int row, int cols) {
     T* const first = p + (int64_t)row * ld;
     phase = (int)(((uintptr_t)first & 15) / sizeof(T));
     base = first - phase;
     n_cols = cols;
-    n_vec = (phase + cols + V - 1) / V;
   }
   __device__ int col(int i) const { return V * i - phase; }
-  // Bit e: element e of vector i is a column of the row.
-  __device__ unsigned in_row(int i) const {
-    const int c = col(i);
-    unsigned bits = (1u << V) - 1;
-    if (c < 0) bits &= ~0u << -c;
-    if (c + V > n_cols) bits &= c >= n_cols ? 0u : (1u << (n_cols - c)) - 1;
-    return bits;
-  }
-  // The elements of `bits` (a subset of in_row) as floats; the others are not defined.
-  __device__ void load(int i, unsigned bits, float (&x)[V]) const {
-    if (in_row(i) == (1u << V) - 1) {
-      const vec v = *reinterpret_cast<const vec*>(base + (int64_t)V * i);
-#pragma unroll
-      for (int e = 0; e < V; ++e) x[e] = (float)v[e];
-    } else {
-#pragma unroll
-      for (int e = 0; e < V; ++e) x[e] = (bits >> e) & 1 ? (float)base[(int64_t)V * i + e] : 0.0f;
-    }
-  }
-  __device__ void store(int i, const float (&x)[V]) const {
-    const unsigned bits = in_row(i);
-    if (bits == (1u << V) - 1) {
-      vec v;
-#pragma unroll
-      for (int e = 0; e < V; ++e) v[e] = (T)x[e];
-      *reinterpret_cast<vec*>(base + (int64_t)V * i) = v;
-    } else {
-#pragma unroll
-      for (int e = 0; e < V; ++e)
-        if ((bits >> e) & 1) base[(int64_t)V * i + e] = (T)x[e];
-    }
-  }
 };
 
 // v of lane ^ X, without a trip through LDS.

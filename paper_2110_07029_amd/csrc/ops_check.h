@@ -24,7 +24,7 @@ RankRules rules_dev(const asgd_logit_rules* r, int row0);
 // The device memory that the rules name belongs to the current device.
 asgd_status check_rules_memory(const asgd_logit_rules* r);
 
-// p is device memory of the current device (or memory that it can reach).
+// p is device or managed memory of the current device.
 asgd_status check_device(const void* p, const char* name);
 asgd_status check_stream(void* hip_stream);
 asgd_status check_workspace(const void* ws, size_t have, size_t need);
