@@ -23,8 +23,10 @@
 // Measured: 1,024 x 670,091 fp32, k = 5, all rules, 551 us for 2.83 GB (5.1 TB/s: memory; the biases of rows that
 // start at odd places are not aligned: without biases 430, with aligned rows 478; aligned loads whose elements
 // neighbouring lanes pass on took 747, their branches end the loads' overlap); 256 x 205,443 bf16, k = 32, all
-// rules, 48 us, of which k_rank_join 4 (112 MB at 2.4 TB/s: vector work; without rules 41, without lse too 33, with
-// k = 1 besides 24); one row of 670,091 13 to 15 us in two launches of 8.6 and 4.8.
+// rules, 48 us, of which k_rank_join 4 (112 MB at 2.4 TB/s: vector units busy 68 % of k_rank; without rules 41, without lse too 33, with
+// k = 1 besides 24); one row of 670,091 13 to 15 us in two launches of 8.6 and 4.8 (no rules 7.2 and 4.9: listed labels
+// add 1.0, biases nothing; without lse 6.3 and 4.4, with k = 1 7.7 and 3.9).  Many distinct listed labels in one range
+// are slow: 256 x 670,091 fp32 with 40 in every row 122 us, with 900 | 3,000 in one of the rows 1,260 | 2,310.
 #include <math.h>
 
 #include <algorithm>

@@ -540,8 +540,10 @@ __global__ __launch_bounds__(256) void k_transpose_h(const bf16* __restrict__ H1
 // dW2 = dZ^T H1 for the 32 labels of one wave, rows as the product's inner index: lane (g, n)
 // reads label n of the rows that its group holds (whole 128-byte runs of a row of dZ per 32 lanes), rounds them
 // to the operand type, and the accumulator holds W2's own layout, hidden units across the
-// lanes.  b2's gradient is summed from the unrounded values, in row order per group.  Bound by reading dZ, and
-// W2 both ways: 256 x 670,091 bf16 operands, 1.37 GB, 396 us with the transposition (3.5 TB/s).
+// lanes.  b2's gradient is summed from the unrounded values, in row order per group.  256 x 670,091 bf16
+// operands: 1.37 GB (dZ once, W2 both ways; H1T comes from L2), 396 us with the transposition, 3.5 TB/s.  Bound by
+// waiting for memory with too little on its way: counters find 1.8 waves on a SIMD, which wait 80 % of their time
+// (vector units busy 17 %).
 constexpr int WG_THREADS = 256;
 template <bool BF16>
 __global__ __launch_bounds__(WG_THREADS) void k_stored_wgrad(float* __restrict__ W2, float* __restrict__ b2, int L,
