@@ -519,6 +519,87 @@ asgd_status asgd_distill_step(asgd_model* m, const asgd_csr* x, const int32_t* t
                               int32_t k, float temperature, float lr, float* loss_out);
 
 /* ------------------------------------------------------------------------ */
+/* A network of the caller's own under the label layer: dense layers,         */
+/* dropout and the label loss, with their gradients                           */
+/* ------------------------------------------------------------------------ */
+
+/* The conventions of the label-logits section hold here too: caller-owned
+ * matrices, streams and workspaces, nothing allocated, nothing waited for,
+ * every call can be captured.  A _workspace call takes the matrices that the
+ * call itself will get: rows that are not made of whole 16-byte pieces (data,
+ * ld and n_cols in bytes multiples of 16; ld at most 4 MiB) are laid out anew
+ * in it, the others are read in place.  It may give 0, then ws may be NULL.
+ * Products are summed in fp32, of fp32 operands too (no operand is rounded).
+ * An output may not share memory with an input or another output unless
+ * stated (EINVAL); columns of one buffer side by side share none.  Sums run in
+ * a fixed order: the same call gives the same bits. */
+
+enum { ASGD_ACT_NONE = 0, ASGD_ACT_RELU = 1, ASGD_ACT_GELU = 2, ASGD_ACT_SILU = 3 };
+
+/* What follows a product A = X W^T + bias:
+ *   Y = residual + drop(act(A))
+ * act: none, max(a, 0), a Phi(a) with the normal distribution function Phi,
+ * or a / (1 + e^-a).  drop as for asgd_dropout, on Y's rows and columns.  Zero-initialise the
+ * struct for the product alone. */
+typedef struct asgd_epilogue {
+  const float* bias;           /* device [n], or NULL */
+  int32_t act;                 /* ASGD_ACT_... */
+  double drop;                 /* probability in [0, 1), 0 for none */
+  uint64_t seed;
+  const asgd_matrix* residual; /* [m x n], any type, or NULL */
+} asgd_epilogue;
+
+/* A dense layer: x [m x k], w [n x k] of one type, y [m x n] of any type,
+ * which may be the residual itself.  pre (NULL, or [m x n] of any type)
+ * receives A for the backward pass; the activation is formed from A before
+ * it is rounded to pre's type.  ep may be NULL. */
+asgd_status asgd_dense_workspace(const asgd_matrix* x, const asgd_matrix* w, size_t* bytes);
+asgd_status asgd_dense(const asgd_matrix* x, const asgd_matrix* w, const asgd_epilogue* ep, const asgd_matrix* pre,
+                       const asgd_matrix* y, void* ws, size_t ws_bytes, void* hip_stream);
+
+/* Its gradients, given dy [m x n] of any type and the same ep (its bias and
+ * residual are not read; the residual's gradient is dy):
+ *   dA = act'(pre) drop(dy), rounded once to x's type for the products
+ *   dx = dA W, dw = dA^T X (any type), db [n] = column sums of dA in fp32
+ * Any of dx, dw, db may be NULL, not all.  pre may be NULL without activation.
+ * The slope of max(a, 0) at 0 is 0.  Dropped elements of dy are not read into
+ * any sum (a NaN there is lost). */
+asgd_status asgd_dense_backward_workspace(const asgd_matrix* x, const asgd_matrix* w, size_t* bytes);
+asgd_status asgd_dense_backward(const asgd_matrix* dy, const asgd_matrix* x, const asgd_matrix* w,
+                                const asgd_matrix* pre, const asgd_epilogue* ep, const asgd_matrix* dx,
+                                const asgd_matrix* dw, float* db, void* ws, size_t ws_bytes, void* hip_stream);
+
+/* y = residual + drop(x): an element stays, times fl32(1 / (1 - p)), where its
+ * 32 random bits are floor(p 2^32) or more, and is 0 elsewhere (infinities and
+ * NaN too).  The bits of (row i, column j) are half j % 2 (0: the low one) of
+ *   splitmix64(splitmix64(seed) ^ (i 2^22 + j / 2)),
+ * a function of seed and place alone: the mask is never stored, and the same call on
+ * dy is the backward pass.  x, residual (or NULL) and y are of one shape and
+ * any types; y may be x or the residual itself. */
+asgd_status asgd_dropout(const asgd_matrix* x, double p, uint64_t seed, const asgd_matrix* residual,
+                         const asgd_matrix* y, void* hip_stream);
+
+/* Softmax cross-entropy of rows h [B x D] against a label matrix w [L x D] of
+ * the same type (L below 2^22), without the logits in memory, and its gradients:
+ *   z_ij = h_i . w_j + bias_j, lse_i = ln sum_j e^z_ij, n_i = |y_i|
+ *   loss_i = lse_i - (1 / n_i) sum of z_ij over the entries j of y_i
+ *   dz_ij = weight_i (e^(z_ij - lse_i) - c_ij / n_i), c_ij = times that j stands in y_i
+ *   dh = dz W, dw = dz^T h, db_j = sum_i dz_ij   (the gradients of sum_i weight_i loss_i)
+ * y: lists per row (values ignored); ids outside [0, L) are skipped and not
+ * counted.  A row without counted entries has loss 0 and takes no part in any gradient, whatever
+ * it holds (its lse is written all the same).  bias: device float [L] or NULL; weights:
+ * device float [B] or NULL for 1 / B; loss_rows and lse (or NULL): device
+ * float [B]; dh, dw (any type) and db: each may be NULL.  All but loss_rows NULL: the loss alone, which
+ * asks for the workspace of gradients = 0, otherwise 1.
+ * In 16 bits dz is rounded once to h's type for its two products; db is
+ * formed before that.  A logit that is NaN or +inf makes its row's loss and gradients NaN, and dw and db with them; a
+ * label of logit -inf has probability 0. */
+asgd_status asgd_label_loss_workspace(const asgd_matrix* h, const asgd_matrix* w, int32_t gradients, size_t* bytes);
+asgd_status asgd_label_loss(const asgd_matrix* h, const asgd_matrix* w, const float* bias, const asgd_csr* y,
+                            const float* weights, float* loss_rows, float* lse, const asgd_matrix* dh,
+                            const asgd_matrix* dw, float* db, void* ws, size_t ws_bytes, void* hip_stream);
+
+/* ------------------------------------------------------------------------ */
 /* Kernel timing (HIP events on the model's stream)                          */
 /* ------------------------------------------------------------------------ */
 

@@ -19,5 +19,7 @@ from ._binding import (  # noqa: F401
     ASGD_F32, ASGD_BF16, ASGD_F16, asgd_matrix, asgd_fp4, asgd_logit_rules, asgd_fp4_quantize, asgd_fp4_dequantize,
     asgd_fp4_logits, asgd_logits_topk_workspace, asgd_logits_topk, asgd_distill_workspace, asgd_distill,
     asgd_model_fp4_labels, asgd_predict_rules_workspace, asgd_predict_topk_rules, asgd_distill_step,
+    ASGD_ACT_NONE, ASGD_ACT_RELU, ASGD_ACT_GELU, ASGD_ACT_SILU, asgd_epilogue, asgd_dense_workspace, asgd_dense,
+    asgd_dense_backward_workspace, asgd_dense_backward, asgd_dropout, asgd_label_loss_workspace, asgd_label_loss,
 )
-from .device_data import DeviceCSR, fp4_matrix, logit_rules, matrix  # noqa: F401
+from .device_data import DeviceCSR, dense_epilogue, fp4_matrix, logit_rules, matrix  # noqa: F401

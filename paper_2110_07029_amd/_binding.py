@@ -38,7 +38,10 @@ EXPORTS = (
     "asgd_fp4_quantize", "asgd_fp4_dequantize", "asgd_fp4_logits", "asgd_logits_topk_workspace",
     "asgd_logits_topk", "asgd_distill_workspace", "asgd_distill", "asgd_model_fp4_labels",
     "asgd_predict_rules_workspace", "asgd_predict_topk_rules", "asgd_distill_step",
+    "asgd_dense_workspace", "asgd_dense", "asgd_dense_backward_workspace", "asgd_dense_backward", "asgd_dropout",
+    "asgd_label_loss_workspace", "asgd_label_loss",
 )
+ASGD_ACT_NONE, ASGD_ACT_RELU, ASGD_ACT_GELU, ASGD_ACT_SILU = 0, 1, 2, 3
 ASGD_F32, ASGD_BF16, ASGD_F16 = 0, 1, 2
 ASGD_CLOCK_TIMED, ASGD_CLOCK_VIRTUAL = 0, 1
 
@@ -93,6 +96,13 @@ class asgd_logit_rules(ctypes.Structure):
     covers = None
 
 
+class asgd_epilogue(ctypes.Structure):
+    _fields_ = [("bias", c_void_p), ("act", c_int32), ("drop", c_double), ("seed", c_uint64),
+                ("residual", POINTER(asgd_matrix))]
+    # Elements of the tensor behind bias, where they are known.
+    n_bias = None
+
+
 class asgd_elastic_log(ctypes.Structure):
     _fields_ = [("n_dispatch", c_int32), ("max_dispatch", c_int32), ("replica", POINTER(c_int32)),
                 ("row0", POINTER(c_int32)), ("row1", POINTER(c_int32)), ("u", c_int32 * 16),
@@ -106,6 +116,7 @@ _lib = None
 
 def _declare(lib):
     P = c_void_p
+    M = POINTER(asgd_matrix)
     sig = {
         "asgd_model_init": (c_int32, [POINTER(c_void_p), POINTER(asgd_config), c_uint64, P]),
         "asgd_model_free": (c_int32, [P]),
@@ -153,6 +164,13 @@ def _declare(lib):
         "asgd_predict_topk_rules": (c_int32, [P, POINTER(asgd_csr), c_int32, POINTER(asgd_logit_rules),
                                               POINTER(asgd_fp4), P, P, P, P, c_size_t]),
         "asgd_distill_step": (c_int32, [P, POINTER(asgd_csr), P, P, c_int32, c_float, c_float, POINTER(c_float)]),
+        "asgd_dense_workspace": (c_int32, [M, M, POINTER(c_size_t)]),
+        "asgd_dense": (c_int32, [M, M, POINTER(asgd_epilogue), M, M, P, c_size_t, P]),
+        "asgd_dense_backward_workspace": (c_int32, [M, M, POINTER(c_size_t)]),
+        "asgd_dense_backward": (c_int32, [M, M, M, M, POINTER(asgd_epilogue), M, M, P, P, c_size_t, P]),
+        "asgd_dropout": (c_int32, [M, c_double, c_uint64, M, M, P]),
+        "asgd_label_loss_workspace": (c_int32, [M, M, c_int32, POINTER(c_size_t)]),
+        "asgd_label_loss": (c_int32, [M, M, P, POINTER(asgd_csr), P, P, P, M, M, P, P, c_size_t, P]),
     }
     for name, (res, args) in sig.items():
         f = getattr(lib, name)
@@ -504,3 +522,68 @@ def asgd_distill_step(m: int, x: asgd_csr, t_ids, t_logits, temperature: float, 
     _check(load().asgd_distill_step(m, byref(x), _ptr(t_ids), _ptr(t_logits), t_ids.shape[1] if k is None else k,
                                     temperature, lr, byref(v) if want_loss else None), "asgd_distill_step")
     return v.value if want_loss else None
+
+
+# ------------------------------------------------------------------ a network of the caller's own
+def _ref(a):
+    return None if a is None else byref(a)
+
+
+def _floats(t, n: int, name: str):
+    """Address of n floats given as a tensor (checked), an int or None."""
+    if t is None or isinstance(t, int):
+        return t
+    if str(t.dtype) != "torch.float32" or not t.is_contiguous() or t.numel() < n:
+        raise ValueError(f"{name} is a contiguous float32 tensor of at least {n} elements")
+    return t.data_ptr()
+
+
+def _check_bias(ep, n: int):
+    """The library sees an address only, so the size behind it is checked here."""
+    if ep is not None and ep.n_bias is not None and ep.n_bias < n:
+        raise ValueError(f"epilogue.bias has {ep.n_bias} elements, the layer {n} outputs")
+
+
+def asgd_dense_workspace(x: asgd_matrix, w: asgd_matrix) -> int:
+    v = c_size_t()
+    _check(load().asgd_dense_workspace(byref(x), byref(w), byref(v)), "asgd_dense_workspace")
+    return v.value
+
+
+def asgd_dense(x: asgd_matrix, w: asgd_matrix, y: asgd_matrix, epilogue=None, pre=None, workspace=None, stream=None):
+    _check_bias(epilogue, w.n_rows)
+    ws, n = _span(workspace)
+    _check(load().asgd_dense(byref(x), byref(w), _ref(epilogue), _ref(pre), byref(y), ws, n, _stream(stream)), "asgd_dense")
+
+
+def asgd_dense_backward_workspace(x: asgd_matrix, w: asgd_matrix) -> int:
+    v = c_size_t()
+    _check(load().asgd_dense_backward_workspace(byref(x), byref(w), byref(v)), "asgd_dense_backward_workspace")
+    return v.value
+
+
+def asgd_dense_backward(dy: asgd_matrix, x: asgd_matrix, w: asgd_matrix, pre=None, epilogue=None, dx=None, dw=None,
+                        db=None, workspace=None, stream=None):
+    ws, n = _span(workspace)
+    _check(load().asgd_dense_backward(byref(dy), byref(x), byref(w), _ref(pre), _ref(epilogue), _ref(dx), _ref(dw),
+                                      _floats(db, w.n_rows, "db"), ws, n, _stream(stream)), "asgd_dense_backward")
+
+
+def asgd_dropout(x: asgd_matrix, p: float, seed: int, y: asgd_matrix, residual=None, stream=None):
+    _check(load().asgd_dropout(byref(x), p, seed & (2 ** 64 - 1), _ref(residual), byref(y), _stream(stream)), "asgd_dropout")
+
+
+def asgd_label_loss_workspace(h: asgd_matrix, w: asgd_matrix, gradients: bool = True) -> int:
+    v = c_size_t()
+    _check(load().asgd_label_loss_workspace(byref(h), byref(w), 1 if gradients else 0, byref(v)),
+           "asgd_label_loss_workspace")
+    return v.value
+
+
+def asgd_label_loss(h: asgd_matrix, w: asgd_matrix, y: asgd_csr, loss_rows, bias=None, weights=None, lse=None, dh=None,
+                    dw=None, db=None, workspace=None, stream=None):
+    ws, n = _span(workspace)
+    B, L = h.n_rows, w.n_rows
+    _check(load().asgd_label_loss(byref(h), byref(w), _floats(bias, L, "bias"), _ref(y), _floats(weights, B, "weights"),
+                                  _floats(loss_rows, B, "loss_rows"), _floats(lse, B, "lse"), _ref(dh), _ref(dw),
+                                  _floats(db, L, "db"), ws, n, _stream(stream)), "asgd_label_loss")

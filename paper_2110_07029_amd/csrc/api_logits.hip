@@ -15,18 +15,11 @@ asgd_status set_error_named(asgd_status s, const char* name, const char* msg) {
   return set_error(s, buf);
 }
 
-namespace {
-
-constexpr int kMaxRows = 1 << 20;
-constexpr int kMaxLabels = 1 << 22;  // as for a model's n_labels
-
 asgd_status hip_failed(hipError_t e, const char* what) {
   char buf[200];
   snprintf(buf, sizeof buf, "%s: %s", what, hipGetErrorString(e));
   return set_error(ASGD_EHIP, buf);
 }
-
-int elem_bytes(int dtype) { return dtype == ASGD_F32 ? 4 : 2; }
 
 asgd_status check_list(const asgd_csr* a, const char* name, int rows, int cols, bool values) {
   if (!a) return ASGD_OK;
@@ -47,6 +40,13 @@ IdLists list_dev(const asgd_csr* a, int row0) {
   return IdLists{a->indptr, a->indptr + row0, a->indices, a->values, a->nnz};
 }
 
+namespace {
+
+constexpr int kMaxRows = 1 << 20;
+constexpr int kMaxLabels = 1 << 22;  // as for a model's n_labels
+
+int elem_bytes(int dtype) { return dtype == ASGD_F32 ? 4 : 2; }
+
 // One past the last byte of a matrix.
 uintptr_t end_of(const asgd_matrix* a) {
   return (uintptr_t)a->data + ((int64_t)(a->n_rows - 1) * a->ld + a->n_cols) * elem_bytes(a->dtype);
@@ -60,10 +60,11 @@ uintptr_t end_of(const asgd_matrix* a) {
     if (s_) return s_;        \
   } while (0)
 
-asgd_status check_matrix(const asgd_matrix* a, const char* name) {
+asgd_status check_matrix(const asgd_matrix* a, const char* name, bool label_rows) {
   if (!a) return set_error_named(ASGD_EINVAL, name, " is NULL");
   if (a->n_rows < 1 || a->n_cols < 1) return set_error_named(ASGD_EINVAL, name, ": n_rows and n_cols must be >= 1");
-  if (a->n_rows > kMaxRows) return set_error_named(ASGD_ERANGE, name, ": more than 2^20 rows");
+  if (label_rows ? a->n_rows >= kMaxLabels : a->n_rows > kMaxRows)
+    return set_error_named(ASGD_ERANGE, name, label_rows ? ": n_rows must be < 2^22" : ": more than 2^20 rows");
   if (a->n_cols >= kMaxLabels) return set_error_named(ASGD_ERANGE, name, ": n_cols must be < 2^22");
   if (a->dtype != ASGD_F32 && a->dtype != ASGD_BF16 && a->dtype != ASGD_F16)
     return set_error_named(ASGD_EINVAL, name, ": unknown element type");

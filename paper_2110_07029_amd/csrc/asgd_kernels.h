@@ -297,6 +297,64 @@ struct Fp4Rows {
 hipError_t launch_fp4_logits(const Fp4Rows& a, int B, const uint8_t* codes, const uint8_t* scales, const float* bias,
                              int L, int dtype, void* z, int64_t ldz, hipStream_t st);
 
+// ---- dense layers and dropout (k_layers.hip) ------------------------------------------
+// A matrix as the kernels see it; data null: none.  vec: rows and base aligned for 8 elements at a time.
+struct MatDev {
+  void* data;
+  int64_t ld;
+  int dtype, vec;
+};
+// Elements whose 32 random bits are below `below` are dropped (0: none), the others scaled.
+struct DropDev {
+  uint64_t key;
+  uint32_t below;
+  float scale;
+};
+struct DenseEpi {
+  const float* bias;
+  int act;  // 0 none, 1 ReLU, 2 GELU, 3 SiLU
+  DropDev drop;
+  MatDev res, pre, y;
+};
+// Y = res + drop(act(X W^T + bias)): x [m x k], w [n x k] of type `dtype`.
+struct DenseJob {
+  int dtype;
+  MatDev x, w;
+  int m, n, k;
+  DenseEpi epi;
+};
+size_t dense_ws_bytes(int dtype, const MatDev& x, const MatDev& w, int m, int n, int k);
+hipError_t launch_dense(const DenseJob& j, void* ws, hipStream_t st);
+// With dA = act'(pre) drop(dy): dx = dA W, dw = dA^T X, db = 1^T dA (each may be null).
+struct DenseGradJob {
+  int dtype;
+  MatDev dy, pre, x, w, dx, dw;
+  float* db;
+  int m, n, k, act;
+  DropDev drop;
+};
+size_t dense_grad_ws_bytes(int dtype, const MatDev& x, const MatDev& w, int m, int n, int k);
+hipError_t launch_dense_grad(const DenseGradJob& j, void* ws, hipStream_t st);
+// y = res + drop(x)
+hipError_t launch_dropout(const MatDev& x, const MatDev& res, const MatDev& y, const DropDev& d, int rows, int cols,
+                          hipStream_t st);
+
+// ---- label loss (k_label_loss.hip) ------------------------------------------------------
+// Cross entropy of rows h [n_rows x d] against labels w [n_labels x d], with its gradients (each may be null).
+struct LossJob {
+  int dtype;
+  MatDev h, w;
+  int n_rows, n_labels, d;
+  const float* bias;
+  IdLists y;
+  const float* weights;
+  float *loss_rows, *lse;
+  MatDev dh, dw;
+  float* db;
+};
+size_t label_loss_ws_bytes(int dtype, const MatDev& h, const MatDev& w, int n_rows, int n_labels, int d, bool grads);
+hipError_t launch_label_loss(const LossJob& j, void* ws, hipStream_t st);
+
 // ---- prediction ---------------------------------------------------------------
 // A prediction's launch shape: 32 nb rows per wave, nrb row blocks of 8 waves,
 // `splits` label splits of tps tiles each.

@@ -12,8 +12,14 @@ namespace asgd {
 asgd_status set_error(asgd_status s, const char* msg);
 asgd_status set_error_named(asgd_status s, const char* name, const char* msg);
 
-// Sizes, type, stride and alignment of a matrix.
-asgd_status check_matrix(const asgd_matrix* a, const char* name);
+asgd_status hip_failed(hipError_t e, const char* what);
+
+// Sizes, type, stride and alignment of a matrix (label_rows: it may have as many rows as a model labels).
+asgd_status check_matrix(const asgd_matrix* a, const char* name, bool label_rows = false);
+// Lists of ids (and values) per row, for rows x cols logits; NULL is fine.
+asgd_status check_list(const asgd_csr* a, const char* name, int rows, int cols, bool values);
+// The lists as the kernels take them, from row `row0` on.
+IdLists list_dev(const asgd_csr* a, int row0);
 // The same of an MXFP4 matrix.
 asgd_status check_fp4(const asgd_fp4* q, const char* name);
 // The rules for rows of `cols` labels, `rows` of them.

@@ -1,0 +1,167 @@
+// Launch shapes of the tiled products (tile_product.h), the epilogue that dense layers and stored
+// products share, and operands that are laid out anew where the caller's rows are out of line.
+#pragma once
+
+#include <atomic>
+
+#include "rows_dev.h"
+#include "tile_product.h"
+
+namespace asgd {
+
+using TpLarge = TpShape<256, 256, 2, 4, 2>;
+using TpMedium = TpShape<128, 128, 2, 2, 2>;
+using TpFew = TpShape<32, 128, 1, 4, 3>;
+
+enum { TP_LARGE = 0, TP_MEDIUM = 1, TP_FEW = 2 };
+
+struct TpPlan {
+  int shape;
+  TpJob job;
+};
+
+inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+inline int elem_size(int dtype) { return dtype == 0 ? 4 : 2; }
+
+// Shape and splits of a product of m x n over k; max_splits 1: the epilogue needs whole sums.
+inline TpPlan tp_plan(int dtype, int m, int n, int64_t k, int max_splits) {
+  TpPlan p{};
+  TpJob& j = p.job;
+  j.m = m;
+  j.n = n;
+  j.k = k;
+  const int64_t large = ceil_div(m, 256) * ceil_div(n, 256);
+  p.shape = m <= 32 ? TP_FEW : large >= 192 ? TP_LARGE : TP_MEDIUM;
+  const int bm = p.shape == TP_LARGE ? 256 : p.shape == TP_MEDIUM ? 128 : 32, bn = p.shape == TP_LARGE ? 256 : 128;
+  j.tiles_m = (int)ceil_div(m, bm);
+  j.tiles_n = (int)ceil_div(n, bn);
+  const int kb = TP_STEP / elem_size(dtype);
+  const int64_t steps = ceil_div(k, kb), tiles = (int64_t)j.tiles_m * j.tiles_n;
+  int64_t s = 1;
+  if (p.shape != TP_LARGE && tiles < 256) s = 512 / tiles;
+  s = s < steps / 2 ? s : steps / 2;
+  s = s < max_splits ? s : max_splits;
+  if (s < 1) s = 1;
+  const int64_t per = ceil_div(steps, s);
+  j.splits = (int)ceil_div(steps, per);
+  j.split_k = per * kb;
+  j.group = 8 < j.tiles_m ? 8 : j.tiles_m;
+  return p;
+}
+
+template <typename T, bool AK, bool BK, class S, class Epi>
+hipError_t tp_launch_shape(const TpJob& j, const typename Epi::Args& ea, hipStream_t st) {
+  constexpr int loop = S::NBUF * S::BUF, out = Epi::BLOCKS * S::WAVES * S::OUT;
+  constexpr int lds = (loop > out ? loop : out) + Epi::TAIL;
+  static_assert(lds <= 160 * 1024, "LDS of a compute unit");
+  const auto fn = k_tile_product<T, AK, BK, S, Epi>;
+  static std::atomic<uint64_t> done{0};  // a bit per device
+  int dev = 0;
+  hipError_t e = hipGetDevice(&dev);
+  if (e != hipSuccess) return e;
+  if (dev > 63 || !(done.load() >> dev & 1)) {
+    e = hipFuncSetAttribute((const void*)fn, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+    if (e != hipSuccess) return e;
+    if (dev < 64) done |= 1ull << dev;
+  }
+  hipLaunchKernelGGL(fn, dim3(tp_blocks(j)), dim3(S::THREADS), lds, st, j, ea);
+  return hipGetLastError();
+}
+
+template <typename T, bool AK, bool BK, template <class> class Epi>
+hipError_t tp_launch(const TpPlan& p, const typename Epi<TpLarge>::Args& ea, hipStream_t st) {
+  if (p.shape == TP_LARGE) return tp_launch_shape<T, AK, BK, TpLarge, Epi<TpLarge>>(p.job, ea, st);
+  if (p.shape == TP_MEDIUM) return tp_launch_shape<T, AK, BK, TpMedium, Epi<TpMedium>>(p.job, ea, st);
+  return tp_launch_shape<T, AK, BK, TpFew, Epi<TpFew>>(p.job, ea, st);
+}
+
+// The same plan for fewer columns.
+inline void tp_narrow(TpPlan* p, int n) {
+  p->job.n = n;
+  p->job.tiles_n = (int)ceil_div(n, p->shape == TP_LARGE ? 256 : 128);
+}
+
+// ---- operands in place or laid out anew ---------------------------------------------------
+// Rows can be read in place if they are made of whole 16-byte chunks and close enough for a tile's
+// offsets to fit 31 bits.
+inline bool tp_in_place(int dtype, const MatDev& a, int cols) {
+  const int es = elem_size(dtype);
+  return ((uintptr_t)a.data | (uint64_t)(a.ld * es)) % 16 == 0 && (int64_t)cols * es % 16 == 0 && a.ld * es <= (1 << 22);
+}
+inline int64_t tp_packed_cols(int dtype, int cols) { return ceil_div(cols, 16 / elem_size(dtype)) * (16 / elem_size(dtype)); }
+inline size_t round256(size_t n) { return (n + 255) / 256 * 256; }
+inline size_t tp_packed_bytes(int dtype, int64_t rows, int cols) {
+  return round256((size_t)(rows * tp_packed_cols(dtype, cols) * elem_size(dtype)));
+}
+inline TpOperand tp_operand(int dtype, const void* data, int64_t ld, int64_t rows, int64_t cols) {
+  const int es = elem_size(dtype);
+  return TpOperand{(const char*)data, ld * es, ((rows - 1) * ld + cols) * es};
+}
+// dst [rows x packed cols] = src, zeros behind its columns.
+hipError_t launch_pack(int dtype, const MatDev& src, int64_t rows, int cols, void* dst, hipStream_t st);
+
+// ---- the epilogue of dense layers and of stored products ---------------------------------
+// Sums of one split go to a slab of floats of their own (part, [splits][m x ldp]), added to what is
+// there with `add`; whole sums go out through dense_out8 (FULL) or scaled by alpha and *alpha_dev.
+struct StoreArgs {
+  DenseEpi epi;
+  float* part;
+  int64_t ldp, slab;
+  int add;
+  float alpha;
+  const float* alpha_dev;
+};
+
+template <class S, bool FULL>
+struct EpiStore {
+  using Args = StoreArgs;
+  static constexpr int BLOCKS = 1, TAIL = 0;
+  const StoreArgs& a;
+  int m, n;
+  float* part;
+  float alpha;
+  __device__ EpiStore(const StoreArgs& args, const TpJob& j, int, int, int split) : a(args), m(j.m), n(j.n) {
+    part = a.part ? a.part + split * a.slab : nullptr;
+    alpha = FULL ? 1.0f : a.alpha * (a.alpha_dev ? *a.alpha_dev : 1.0f);
+  }
+  __device__ void begin(char*) {}
+  __device__ void slab(int, int, int, int) {}
+  __device__ __forceinline__ void rows(int row, int, int col, float v[8], int, int) {
+    if (row >= m || col >= n) return;
+    if (part) {  // (ldp covers whole groups of 8 columns)
+      f32x4* p = reinterpret_cast<f32x4*>(part + row * a.ldp + col);
+      f32x4 lo{v[0], v[1], v[2], v[3]}, hi{v[4], v[5], v[6], v[7]};
+      if (a.add) {
+        lo += p[0];
+        hi += p[1];
+      }
+      p[0] = lo;
+      p[1] = hi;
+      return;
+    }
+    const int c = n - col < 8 ? n - col : 8;
+    if constexpr (FULL) {
+      dense_out8(a.epi, row, col, c, v);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] *= alpha;
+      store8(a.epi.y, row, col, c, v);
+    }
+  }
+  __device__ void end(int, int, int, int, int) {}
+};
+template <class S>
+using EpiDense = EpiStore<S, true>;
+template <class S>
+using EpiPlain = EpiStore<S, false>;
+
+// The product with the plain epilogue: a has k along its rows (a_krows) or across them, b across them.
+hipError_t launch_plain(int dtype, bool a_krows, const TpPlan& p, const StoreArgs& a, hipStream_t st);
+// Adds the slabs of a product and puts the sums out as the epilogue would; live (or null): rows whose
+// entry is 0 become zeros.
+hipError_t launch_join(const StoreArgs& a, int splits, int m, int n, bool full, const float* live, hipStream_t st);
+// y[j] = alpha *alpha_dev sum_i part[i][j], i < rows
+hipError_t launch_column_sums(const float* part, int rows, int64_t ld, int n, float alpha, const float* alpha_dev,
+                              float* y, hipStream_t st);
+
+}  // namespace asgd

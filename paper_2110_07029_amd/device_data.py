@@ -11,7 +11,7 @@ import ctypes
 
 import numpy as np
 
-from ._binding import ASGD_BF16, ASGD_F16, ASGD_F32, asgd_csr, asgd_fp4, asgd_logit_rules, asgd_matrix
+from ._binding import ASGD_BF16, ASGD_F16, ASGD_F32, asgd_csr, asgd_epilogue, asgd_fp4, asgd_logit_rules, asgd_matrix
 
 
 class DeviceCSR:
@@ -116,3 +116,17 @@ def logit_rules(bias=None, allowed=None, seen=None, repetition: float = 1.0, fre
     if cols != _ANY:
         r.covers = rows, cols
     return r
+
+
+_MATRIX = ctypes.POINTER(asgd_matrix)
+
+
+def dense_epilogue(bias=None, act: int = 0, drop: float = 0.0, seed: int = 0, residual=None) -> asgd_epilogue:
+    """What follows a dense layer's product: bias (a contiguous float32 tensor), activation (ASGD_ACT_...), dropout and a
+    residual (an asgd_matrix).  Tensors must outlive the epilogue's use."""
+    if bias is not None and (bias.dim() != 1 or not bias.is_contiguous() or not _FLOAT[bias.dtype]):
+        raise ValueError("epilogue.bias is a contiguous float32 tensor of one dimension")
+    e = asgd_epilogue(None if bias is None else bias.data_ptr(), act, drop, seed & (2 ** 64 - 1),
+                      None if residual is None else _MATRIX(residual))
+    e.n_bias = None if bias is None else bias.numel()
+    return e
