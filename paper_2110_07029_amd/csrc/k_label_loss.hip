@@ -31,6 +31,7 @@ namespace {
 
 constexpr int64_t PIECE_BYTES = 128ll << 20;  // of dz at a time
 constexpr int MAX_SLABS = 64;
+typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
 
 // Entries of row i that count: ids in [0, L).
 __device__ __forceinline__ int entry(const IdLists& y, int q, int L) {
@@ -45,6 +46,8 @@ __device__ __forceinline__ int entry(const IdLists& y, int q, int L) {
 template <typename T>
 __global__ __launch_bounds__(256) void k_loss_prep(MatDev h, IdLists y, int B, int L, int D, float* __restrict__ share,
                                                    T* __restrict__ hp, int64_t ldp) {
+  constexpr int V = 16 / (int)sizeof(T);
+  typedef T vec __attribute__((ext_vector_type(V)));
   const int lane = threadIdx.x & 63, i = blockIdx.x * 4 + (threadIdx.x >> 6);
   if (i >= B) return;
   int q0 = 0, q1 = 0, n = 0;
@@ -55,7 +58,18 @@ __global__ __launch_bounds__(256) void k_loss_prep(MatDev h, IdLists y, int B, i
   if (lane == 0) share[i] = n ? 1.0f / (float)n : 0.0f;
   if (!hp) return;
   const T* src = (const T*)h.data + (int64_t)i * h.ld;
-  for (int64_t c = lane; c < ldp; c += 64) hp[i * ldp + c] = n && c < D ? src[c] : (T)0.0f;
+  T* dst = hp + i * ldp;
+  for (int64_t c = V * lane; c < ldp; c += V * 64) {
+    vec v;
+    if (h.vec && c + V <= D) {
+      v = *reinterpret_cast<const vec*>(src + c);
+    } else {
+#pragma unroll
+      for (int k = 0; k < V; ++k) v[k] = c + k < D ? src[c + k] : (T)0.0f;
+    }
+    if (!n) v = vec{};
+    *reinterpret_cast<vec*>(dst + c) = v;
+  }
 }
 
 // ---- product 1 -------------------------------------------------------------------------------------
@@ -64,6 +78,21 @@ struct LseArgs {
   float2* part;  // [B][tiles_n]
 };
 
+// Biases of the columns that a lane's accumulators hold: col + 32 b + 8 q + i.
+template <class S>
+__device__ __forceinline__ void lane_bias(const float* bias, int col, int n, f32x4 (&v)[S::TN][4]) {
+#pragma unroll
+  for (int b = 0; b < S::TN; ++b)
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int c = col + 32 * b + 8 * q + i;
+        v[b][q][i] = bias && c < n ? bias[c] : 0.0f;
+      }
+}
+
+// All in the accumulators: a lane has half of a wave's columns of its row.
 template <class S>
 struct EpiLse {
   using Args = LseArgs;
@@ -71,28 +100,35 @@ struct EpiLse {
   const LseArgs& a;
   int m, n, row0, tile, tiles;
   float2* ms;  // [WN][BM]
-  __device__ EpiLse(const LseArgs& args, const TpJob& j, int r0, int c0, int)
-      : a(args), m(j.m), n(j.n), row0(r0), tile(c0 / S::BN), tiles(j.tiles_n) {}
+  f32x4 bias[S::TN][4];  // of the lane's columns
+  int col;
+  __device__ EpiLse(const LseArgs& args, const TpJob& j, int r0, int c0, int, int wave, int lane)
+      : a(args), m(j.m), n(j.n), row0(r0), tile(c0 / S::BN), tiles(j.tiles_n) {
+    col = c0 + wave % S::WN * S::WCOLS + 4 * (lane >> 5);
+    lane_bias<S>(a.bias, col, n, bias);
+  }
   __device__ void begin(char* tail) { ms = reinterpret_cast<float2*>(tail); }
-  __device__ void slab(int, int, int, int) {}
-  __device__ __forceinline__ void rows(int row, int, int col, float v[8], int wave, int lane) {
-    float top = -INFINITY;
+  __device__ __forceinline__ void block(const f32x16 (&acc)[S::TN], int r0, int, float*, int wave, int lane) {
+    float v[S::TN][16], top = -INFINITY;
+    const bool edge = col - 4 * (lane >> 5) + S::WCOLS > n;  // (the same for the whole wave)
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const bool in = col + i < n;
-      v[i] = in ? v[i] + (a.bias ? a.bias[col + i] : 0.0f) : -INFINITY;
-      top = fmaxf(top, v[i]);
-    }
-    constexpr int LPR = S::WCOLS / 8;
+    for (int b = 0; b < S::TN; ++b)
 #pragma unroll
-    for (int o = 1; o < LPR; o <<= 1) top = fmaxf(top, __shfl_xor(top, o));
+      for (int r = 0; r < 16; ++r) {
+        v[b][r] = acc[b][r] + bias[b][r >> 2][r & 3];
+        if (edge && col + 32 * b + 8 * (r >> 2) + (r & 3) >= n) v[b][r] = -INFINITY;
+        top = fmaxf(top, v[b][r]);
+      }
+    top = fmaxf(top, __builtin_bit_cast(float, lane_xor<32>(__builtin_bit_cast(unsigned, top), lane)));
     const float base = top == -INFINITY ? 0.0f : top;
-    float s = 0.0f;
+    float s[4] = {};
 #pragma unroll
-    for (int i = 0; i < 8; ++i) s += exp_fast(v[i] - base);
+    for (int b = 0; b < S::TN; ++b)
 #pragma unroll
-    for (int o = 1; o < LPR; o <<= 1) s += __shfl_xor(s, o);
-    if (lane % LPR == 0) ms[(wave % S::WN) * S::BM + row - row0] = make_float2(top, s);
+      for (int r = 0; r < 16; ++r) s[r & 3] += exp_fast(v[b][r] - base);
+    float t = (s[0] + s[1]) + (s[2] + s[3]);
+    t += __builtin_bit_cast(float, lane_xor<32>(__builtin_bit_cast(unsigned, t), lane));
+    if (lane < 32) ms[(wave % S::WN) * S::BM + r0 - row0 + lane] = make_float2(top, t);
   }
   __device__ void end(int, int, int, int, int tid) {
     __syncthreads();
@@ -110,14 +146,17 @@ struct EpiLse {
 };
 
 // ---- lse and loss --------------------------------------------------------------------------------
-// One workgroup per row.  Target logits are products of their own (a gather of n_i rows of W).  With `scale` one
-// workgroup more finds the gradients' scale: the largest finite |weight| of rows that have labels, 1 / B without weights.
+// One workgroup per row.  Target logits are products of their own, 16 lanes each (h and w as the products read them: whole
+// 16-byte pieces).  With `scale` one workgroup more finds the gradients' scale: the largest finite |weight| of rows
+// that have labels, 1 / B without weights.
 template <typename T>
-__global__ __launch_bounds__(256) void k_loss_rows(const float2* __restrict__ part, int tiles, MatDev h, MatDev w, int D,
-                                                   int L, const float* __restrict__ bias, IdLists y,
+__global__ __launch_bounds__(256) void k_loss_rows(const float2* __restrict__ part, int tiles, TpOperand h, TpOperand w,
+                                                   int D, int L, const float* __restrict__ bias, IdLists y,
                                                    const float* __restrict__ share, float* __restrict__ lse_ws,
                                                    float* __restrict__ lse_out, float* __restrict__ loss, int B,
                                                    const float* __restrict__ weights, float* __restrict__ scale) {
+  constexpr int V = 16 / (int)sizeof(T);
+  typedef T vec __attribute__((ext_vector_type(V)));
   const int i = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   __shared__ float sm[4], ss[4], st[4];
   if (i == B) {
@@ -136,35 +175,39 @@ __global__ __launch_bounds__(256) void k_loss_rows(const float2* __restrict__ pa
   const float2* p = part + (int64_t)i * tiles;
   float top = -INFINITY;
   for (int k = tid; k < tiles; k += 256) top = fmaxf(top, p[k].x);
+  float t = 0.0f;
+  const float sh = share[i];
+  if (sh > 0.0f) {
+    int q0, q1;
+    list_range(y, i, &q0, &q1);
+    const T* hr = (const T*)(h.base + i * h.ld);
+    const int l = tid & 15;
+    for (int q = q0 + (tid >> 4); q < q1; q += 16) {
+      const int id = entry(y, q, L);
+      if (id < 0) continue;
+      const T* wr = (const T*)(w.base + id * w.ld);
+      float d = 0.0f;
+      for (int c = V * l; c < D; c += V * 16) {
+        const vec a = *reinterpret_cast<const vec*>(hr + c), b = *reinterpret_cast<const vec*>(wr + c);
+#pragma unroll
+        for (int k = 0; k < V; ++k) d = fmaf((float)a[k], (float)b[k], d);
+      }
+      t += d + (bias && l == 0 ? bias[id] : 0.0f);
+    }
+  }
+  t = wave_sum(t);
   top = wave_max(top);
-  if (lane == 0) sm[wave] = top;
+  if (lane == 0) {
+    sm[wave] = top;
+    st[wave] = t;
+  }
   __syncthreads();
   top = fmaxf(fmaxf(sm[0], sm[1]), fmaxf(sm[2], sm[3]));
   const float base = top == -INFINITY ? 0.0f : top;
   float s = 0.0f;
   for (int k = tid; k < tiles; k += 256) s += p[k].y * exp_fast(p[k].x - base);
   s = wave_sum(s);
-
-  float t = 0.0f;
-  const float sh = share[i];
-  if (sh > 0.0f) {
-    int q0, q1;
-    list_range(y, i, &q0, &q1);
-    const T* hr = (const T*)h.data + (int64_t)i * h.ld;
-    for (int q = q0 + wave; q < q1; q += 4) {
-      const int id = entry(y, q, L);
-      if (id < 0) continue;
-      const T* wr = (const T*)w.data + (int64_t)id * w.ld;
-      float d = 0.0f;
-      for (int c = lane; c < D; c += 64) d = fmaf((float)hr[c], (float)wr[c], d);
-      d = wave_sum(d);
-      t += d + (bias ? bias[id] : 0.0f);
-    }
-  }
-  if (lane == 0) {
-    ss[wave] = s;
-    st[wave] = t;
-  }
+  if (lane == 0) ss[wave] = s;
   __syncthreads();
   if (tid == 0) {
     s = ss[0] + ss[1] + ss[2] + ss[3];
@@ -196,15 +239,20 @@ struct EpiDzT {
   using Args = DzArgs;
   static constexpr int HITS = 1023, BLOCKS = 2, TAIL = 4 * (HITS + 1);
   const DzArgs& a;
-  int m, n, row0, col0, tm;
+  int m, n, row0, col0, tm, col;
   int* hits;  // [0]: how many
   unsigned* counts;
-  bool any;
-  float sum[8];
-  __device__ EpiDzT(const DzArgs& args, const TpJob& j, int r0, int c0, int)
+  float scale;
+  f32x4 bias[S::TN][4], sum[S::TN][4];
+  __device__ EpiDzT(const DzArgs& args, const TpJob& j, int r0, int c0, int, int wave, int lane)
       : a(args), m(j.m), n(j.n), row0(r0), col0(c0), tm(r0 / S::BM) {
+    col = c0 + wave % S::WN * S::WCOLS + 4 * (lane >> 5);
+    lane_bias<S>(a.bias, col, n, bias);
+    scale = *a.scale;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) sum[i] = 0.0f;
+    for (int b = 0; b < S::TN; ++b)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) sum[b][q] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
   }
   __device__ void begin(char* tail) {
     hits = reinterpret_cast<int*>(tail);
@@ -226,13 +274,15 @@ struct EpiDzT {
       }
     }
   }
-  // (the loop's barriers lie between begin and here)
-  __device__ void slab(int r0, int c0, int wave, int lane) {
+  // Fills the wave's block of counts for rows r0 .. + 31, columns c0 .. ; false: none.
+  // (The loop's barriers lie between begin and here.)
+  __device__ bool targets(int r0, int c0, int wave, int lane) {
     const int total = hits[0];
-    counts = reinterpret_cast<unsigned*>(reinterpret_cast<char*>(hits) - a_out_offset()) + wave * (32 * S::OUT_LD);
+    if (total == 0) return false;
+    counts = reinterpret_cast<unsigned*>(reinterpret_cast<char*>(hits) - counts_offset()) + wave * (32 * S::OUT_LD);
     const int rl = r0 - row0, cl = c0 - col0;
-    any = total > HITS;
-    if (total && !any) {
+    bool any = total > HITS;
+    if (!any) {
       bool mine = false;
       for (int k = lane; k < total; k += 64) {
         const int h = hits[1 + k], r = (h >> 16) - rl, c = (h & 0xffff) - cl;
@@ -240,7 +290,7 @@ struct EpiDzT {
       }
       any = __ballot(mine) != 0;
     }
-    if (!any) return;
+    if (!any) return false;
     for (int k = lane; k < 32 * S::OUT_LD; k += 64) counts[k] = 0;
     __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "wavefront");
     if (total <= HITS) {
@@ -257,55 +307,79 @@ struct EpiDzT {
       }
     }
     __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "wavefront");
+    return true;
   }
-  // bytes from the blocks of counts to the tail
-  static __device__ constexpr int a_out_offset() {
+  // bytes from the output blocks to the tail, and from the blocks of counts
+  static __device__ constexpr int tail_offset() {
     constexpr int loop = S::NBUF * S::BUF, out = 2 * S::WAVES * S::OUT;
-    return (loop > out ? loop : out) - S::WAVES * S::OUT;
+    return loop > out ? loop : out;
   }
-  __device__ __forceinline__ void rows(int row, int r, int col, float v[8], int, int lane) {
-    if (row >= m || col >= n) return;
-    const float sh = a.share[row];
-    if (sh == 0.0f) {
-#pragma unroll
-      for (int i = 0; i < 8; ++i) v[i] = 0.0f;
-    } else {
+  static __device__ constexpr int counts_offset() { return tail_offset() - S::WAVES * S::OUT; }
+  // dz in the accumulators; 16 bits go through the wave's block as they will lie in memory.
+  __device__ __forceinline__ void block(const f32x16 (&acc)[S::TN], int r0, int colw, float* out, int wave, int lane) {
+    const int i = lane & 31, row = r0 + i;
+    const bool any = targets(r0, colw, wave, lane);
+    float sh = 0.0f, lse = 0.0f, f = 0.0f;
+    if (row < m) {
+      sh = a.share[row];
+      lse = a.lse[row];
       // (the weights are divided by the largest: 0 / 0 where all are 0)
-      const float lse = a.lse[row], top = *a.scale;
-      const float f = (a.weights ? top > 0.0f ? a.weights[row] / top : a.weights[row] : 1.0f) * a.up;
-      const int c0 = (col - col0) % S::WCOLS;
+      f = (a.weights ? scale > 0.0f ? a.weights[row] / scale : a.weights[row] : 1.0f) * a.up;
+    }
+    const bool live = sh > 0.0f;
+    constexpr int LD = S::OUT_LD * (4 / (int)sizeof(T));  // elements (16 bits: 8-byte writes of 16 lanes take every bank twice)
+    T* const block = reinterpret_cast<T*>(out);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        float p = exp_fast(v[i] + (a.bias && col + i < n ? a.bias[col + i] : 0.0f) - lse);
-        if (any) p -= (float)counts[r * S::OUT_LD + c0 + i] * sh;
-        v[i] = col + i < n ? p * f : 0.0f;
-        sum[i] += v[i];
+    for (int b = 0; b < S::TN; ++b)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        f32x4 v;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) v[k] = exp_fast(acc[b][4 * q + k] + bias[b][q][k] - lse);
+        if (any) {
+          const u32x4 c = *reinterpret_cast<const u32x4*>(counts + i * S::OUT_LD + 32 * b + 8 * q + 4 * (lane >> 5));
+#pragma unroll
+          for (int k = 0; k < 4; ++k) v[k] -= (float)c[k] * sh;
+        }
+        // rows without labels and columns past the last are zeros, whatever they hold
+#pragma unroll
+        for (int k = 0; k < 4; ++k) v[k] = live && col + 32 * b + 8 * q + k < n ? v[k] * f : 0.0f;
+        sum[b][q] += v;
+        typename TpMma<T>::frag4 o;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) o[k] = (T)v[k];
+        *reinterpret_cast<typename TpMma<T>::frag4*>(block + i * LD + 32 * b + 8 * q + 4 * (lane >> 5)) = o;
       }
-    }
-    if constexpr (sizeof(T) == 4) {
-      f32x4* q = reinterpret_cast<f32x4*>((T*)a.dz + row * a.ld + col);
-      q[0] = f32x4{v[0], v[1], v[2], v[3]};
-      q[1] = f32x4{v[4], v[5], v[6], v[7]};
-    } else {
-      typename TpMma<T>::frag8 o;
+    __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "wavefront");
+    constexpr int V = 16 / (int)sizeof(T), LPR = S::WCOLS / V, RPP = 64 / LPR;
+    typedef T vec __attribute__((ext_vector_type(V)));
+    const int c = V * (lane % LPR);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) o[i] = (T)v[i];
-      *reinterpret_cast<typename TpMma<T>::frag8*>((T*)a.dz + row * a.ld + col) = o;
+    for (int p = 0; p < 32 / RPP; ++p) {
+      const int r = p * RPP + lane / LPR;
+      const vec v = *reinterpret_cast<const vec*>(block + r * LD + c);
+      // (the matrix has whole groups of 64 columns)
+      if (r0 + r < m && colw + c < n) *reinterpret_cast<vec*>((T*)a.dz + (r0 + r) * a.ld + colw + c) = v;
     }
+    __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "wavefront");
   }
   __device__ void end(int wave, int wm, int wn, int lane, int tid) {
     if (!a.part) return;
-    constexpr int LPR = S::WCOLS / 8;
+    // a lane's sums are those of its row of each block: rows meet in LDS
+    float* const mine = reinterpret_cast<float*>(reinterpret_cast<char*>(hits) - tail_offset()) + wave * (32 * S::OUT_LD);
 #pragma unroll
-    for (int o = LPR; o < 64; o <<= 1)
+    for (int b = 0; b < S::TN; ++b)
 #pragma unroll
-      for (int i = 0; i < 8; ++i) sum[i] += __shfl_xor(sum[i], o);
+      for (int q = 0; q < 4; ++q)
+        *reinterpret_cast<f32x4*>(mine + (lane & 31) * S::OUT_LD + 32 * b + 8 * q + 4 * (lane >> 5)) = sum[b][q];
     __syncthreads();
     float* s = reinterpret_cast<float*>(hits);  // [WM][BN]
-    static_assert(S::WM * S::BN * 4 <= TAIL, "column sums");
-    if (lane < LPR) {
-#pragma unroll
-      for (int i = 0; i < 8; ++i) s[wm * S::BN + wn * S::WCOLS + 8 * lane + i] = sum[i];
+    static_assert(S::WM * S::BN * 4 <= TAIL && S::WCOLS <= 64, "column sums");
+    if (lane < S::WCOLS) {
+      float t = 0.0f;
+#pragma unroll 8
+      for (int r = 0; r < 32; ++r) t += mine[r * S::OUT_LD + lane];
+      s[wm * S::BN + wn * S::WCOLS + lane] = t;
     }
     __syncthreads();
     for (int c = tid; c < S::BN; c += S::THREADS) {
@@ -397,7 +471,7 @@ hipError_t run(const LossJob& j, char* ws, hipStream_t st) {
   s.fwd.job.a = h;
   s.fwd.job.b = w;
   if ((e = tp_launch<T, true, true, EpiLse>(s.fwd, LseArgs{j.bias, part}, st)) != hipSuccess) return e;
-  hipLaunchKernelGGL(k_loss_rows<T>, dim3(B + (scale ? 1 : 0)), dim3(256), 0, st, part, s.fwd.job.tiles_n, j.h, j.w, D, L, j.bias, j.y,
+  hipLaunchKernelGGL(k_loss_rows<T>, dim3(B + (scale ? 1 : 0)), dim3(256), 0, st, part, s.fwd.job.tiles_n, h, w, D, L, j.bias, j.y,
                      share, lse, j.lse, j.loss_rows, B, j.weights, scale);
   if ((e = hipGetLastError()) != hipSuccess) return e;
   if (!grads) return hipSuccess;

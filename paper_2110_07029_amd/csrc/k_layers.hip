@@ -60,7 +60,9 @@ __global__ __launch_bounds__(256) void k_join(StoreArgs a, int splits, int m, in
     }
     const int c = n - col < 8 ? n - col : 8;
     if constexpr (FULL) {
-      dense_out8(a.epi, row, col, c, v);
+      float b[8];
+      bias8(a.epi.bias, col, c, b);
+      dense_out8(a.epi, b, row, col, c, v);
     } else {
       const bool zero = live && live[row] == 0.0f;
 #pragma unroll
@@ -80,23 +82,30 @@ hipError_t launch_join(const StoreArgs& a, int splits, int m, int n, bool full, 
   return hipGetLastError();
 }
 
-// 64 columns per workgroup, four waves take every fourth row.
-__global__ __launch_bounds__(256) void k_column_sums(const float* __restrict__ part, int rows, int64_t ld, int n,
-                                                     float alpha, const float* alpha_dev, float* __restrict__ y) {
-  __shared__ float s[4][64];
+// 64 columns per workgroup, sixteen waves take every sixteenth row.
+__global__ __launch_bounds__(1024) void k_column_sums(const float* __restrict__ part, int rows, int64_t ld, int n,
+                                                      float alpha, const float* alpha_dev, float* __restrict__ y) {
+  __shared__ float s[16][64];
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
   const int64_t col = blockIdx.x * 64ll + lane;
   float v = 0.0f;
-  if (col < n)
-    for (int r = w; r < rows; r += 4) v += part[r * ld + col];
+  if (col < n) {
+#pragma unroll 4
+    for (int r = w; r < rows; r += 16) v += part[r * ld + col];
+  }
   s[w][lane] = v;
   __syncthreads();
-  if (w == 0 && col < n) y[col] = (s[0][lane] + s[1][lane] + s[2][lane] + s[3][lane]) * alpha * (alpha_dev ? *alpha_dev : 1.0f);
+  if (w == 0 && col < n) {
+    float t = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) t += s[i][lane];
+    y[col] = t * alpha * (alpha_dev ? *alpha_dev : 1.0f);
+  }
 }
 
 hipError_t launch_column_sums(const float* part, int rows, int64_t ld, int n, float alpha, const float* alpha_dev,
                               float* y, hipStream_t st) {
-  hipLaunchKernelGGL(k_column_sums, dim3((unsigned)ceil_div(n, 64)), dim3(256), 0, st, part, rows, ld, n, alpha, alpha_dev, y);
+  hipLaunchKernelGGL(k_column_sums, dim3((unsigned)ceil_div(n, 64)), dim3(1024), 0, st, part, rows, ld, n, alpha, alpha_dev, y);
   return hipGetLastError();
 }
 
@@ -241,7 +250,7 @@ __global__ __launch_bounds__(256) void k_dense_da(DaArgs a, T* __restrict__ da, 
 namespace {
 
 int da_rows_wg(int m) {
-  const int64_t r = ceil_div(m, 256);
+  const int64_t r = ceil_div(m, 128);
   return (int)(r < 32 ? 32 : r);
 }
 

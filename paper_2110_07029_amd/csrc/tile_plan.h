@@ -11,9 +11,11 @@ namespace asgd {
 
 using TpLarge = TpShape<256, 256, 2, 4, 2>;
 using TpMedium = TpShape<128, 128, 2, 2, 2>;
+using TpSmall = TpShape<64, 64, 2, 2, 3>;
 using TpFew = TpShape<32, 128, 1, 4, 3>;
 
-enum { TP_LARGE = 0, TP_MEDIUM = 1, TP_FEW = 2 };
+enum { TP_LARGE = 0, TP_MEDIUM = 1, TP_SMALL = 2, TP_FEW = 3 };
+constexpr int TP_BM[] = {256, 128, 64, 32}, TP_BN[] = {256, 128, 64, 128};
 
 struct TpPlan {
   int shape;
@@ -30,11 +32,10 @@ inline TpPlan tp_plan(int dtype, int m, int n, int64_t k, int max_splits) {
   j.m = m;
   j.n = n;
   j.k = k;
-  const int64_t large = ceil_div(m, 256) * ceil_div(n, 256);
-  p.shape = m <= 32 ? TP_FEW : large >= 192 ? TP_LARGE : TP_MEDIUM;
-  const int bm = p.shape == TP_LARGE ? 256 : p.shape == TP_MEDIUM ? 128 : 32, bn = p.shape == TP_LARGE ? 256 : 128;
-  j.tiles_m = (int)ceil_div(m, bm);
-  j.tiles_n = (int)ceil_div(n, bn);
+  const int64_t large = ceil_div(m, 256) * ceil_div(n, 256), medium = ceil_div(m, 128) * ceil_div(n, 128);
+  p.shape = m <= 32 ? TP_FEW : large >= 192 ? TP_LARGE : medium >= 192 ? TP_MEDIUM : TP_SMALL;
+  j.tiles_m = (int)ceil_div(m, TP_BM[p.shape]);
+  j.tiles_n = (int)ceil_div(n, TP_BN[p.shape]);
   const int kb = TP_STEP / elem_size(dtype);
   const int64_t steps = ceil_div(k, kb), tiles = (int64_t)j.tiles_m * j.tiles_n;
   int64_t s = 1;
@@ -71,6 +72,7 @@ hipError_t tp_launch_shape(const TpJob& j, const typename Epi::Args& ea, hipStre
 template <typename T, bool AK, bool BK, template <class> class Epi>
 hipError_t tp_launch(const TpPlan& p, const typename Epi<TpLarge>::Args& ea, hipStream_t st) {
   if (p.shape == TP_LARGE) return tp_launch_shape<T, AK, BK, TpLarge, Epi<TpLarge>>(p.job, ea, st);
+  if (p.shape == TP_SMALL) return tp_launch_shape<T, AK, BK, TpSmall, Epi<TpSmall>>(p.job, ea, st);
   if (p.shape == TP_MEDIUM) return tp_launch_shape<T, AK, BK, TpMedium, Epi<TpMedium>>(p.job, ea, st);
   return tp_launch_shape<T, AK, BK, TpFew, Epi<TpFew>>(p.job, ea, st);
 }
@@ -78,7 +80,7 @@ hipError_t tp_launch(const TpPlan& p, const typename Epi<TpLarge>::Args& ea, hip
 // The same plan for fewer columns.
 inline void tp_narrow(TpPlan* p, int n) {
   p->job.n = n;
-  p->job.tiles_n = (int)ceil_div(n, p->shape == TP_LARGE ? 256 : 128);
+  p->job.tiles_n = (int)ceil_div(n, TP_BN[p->shape]);
 }
 
 // ---- operands in place or laid out anew ---------------------------------------------------
@@ -116,18 +118,37 @@ template <class S, bool FULL>
 struct EpiStore {
   using Args = StoreArgs;
   static constexpr int BLOCKS = 1, TAIL = 0;
+  static constexpr int LPR = S::WCOLS / 8, RPP = 64 / LPR;  // lanes per row, rows per pass
   const StoreArgs& a;
-  int m, n;
+  int m, n, c;
   float* part;
   float alpha;
-  __device__ EpiStore(const StoreArgs& args, const TpJob& j, int, int, int split) : a(args), m(j.m), n(j.n) {
+  float b[FULL ? 8 : 1];
+  __device__ EpiStore(const StoreArgs& args, const TpJob& j, int, int col0, int split, int wave, int lane)
+      : a(args), m(j.m), n(j.n) {
     part = a.part ? a.part + split * a.slab : nullptr;
     alpha = FULL ? 1.0f : a.alpha * (a.alpha_dev ? *a.alpha_dev : 1.0f);
+    const int col = col0 + wave % S::WN * S::WCOLS + 8 * (lane % LPR);
+    c = n - col < 8 ? n - col : 8;
+    if constexpr (FULL) bias8(a.epi.bias, col, c, b);
   }
   __device__ void begin(char*) {}
-  __device__ void slab(int, int, int, int) {}
-  __device__ __forceinline__ void rows(int row, int, int col, float v[8], int, int) {
-    if (row >= m || col >= n) return;
+  __device__ __forceinline__ void block(const f32x16 (&acc)[S::TN], int row0, int colw, float* out, int, int lane) {
+    tp_stage<S>(acc, out, lane);
+    const int col = colw + 8 * (lane % LPR);
+    if (c > 0) {
+#pragma unroll 1  // (four copies of the epilogue's code are enough)
+      for (int p = 0; p < 32 / RPP; ++p) {
+        const int r = p * RPP + lane / LPR;
+        if (row0 + r >= m) break;
+        float v[8];
+        tp_staged8<S>(out, r, 8 * (lane % LPR), v);
+        put(row0 + r, col, v);
+      }
+    }
+    __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "wavefront");
+  }
+  __device__ __forceinline__ void put(int row, int col, float v[8]) {
     if (part) {  // (ldp covers whole groups of 8 columns)
       f32x4* p = reinterpret_cast<f32x4*>(part + row * a.ldp + col);
       f32x4 lo{v[0], v[1], v[2], v[3]}, hi{v[4], v[5], v[6], v[7]};
@@ -139,9 +160,8 @@ struct EpiStore {
       p[1] = hi;
       return;
     }
-    const int c = n - col < 8 ? n - col : 8;
     if constexpr (FULL) {
-      dense_out8(a.epi, row, col, c, v);
+      dense_out8(a.epi, b, row, col, c, v);
     } else {
 #pragma unroll
       for (int i = 0; i < 8; ++i) v[i] *= alpha;

@@ -16,9 +16,9 @@
 // NBUF buffers: the copies of step s + NBUF - 1 are issued once every wave has left step s - 1.
 //
 // The product is formed as B A^T: an accumulator's lane holds one row m and runs of four
-// columns n, which go through a block of LDS per wave ([32][32 TN + 4] floats, 16-byte writes and
-// reads without conflicts) so that the epilogue gets 8 consecutive columns of a row per lane and
-// memory gets whole lines.
+// columns n.  Epilogues that write rows take them through a block of LDS per wave ([32][32 TN + 4] floats,
+// 16-byte writes and reads without conflicts), 8 consecutive columns of a row per lane, so that memory gets
+// whole lines.
 #pragma once
 
 #include <type_traits>
@@ -217,9 +217,33 @@ __device__ __forceinline__ bool tp_place(const TpJob& j, int block, int* tm, int
 }
 inline int tp_blocks(const TpJob& j) { return 8 * ((j.tiles_m * j.tiles_n * j.splits + 7) / 8); }
 
+// A wave's block of 32 rows (accumulators of one row of blocks) in LDS, [32][OUT_LD] floats, private to the wave.
+template <class S>
+__device__ __forceinline__ void tp_stage(const f32x16 (&c)[S::TN], float* out, int lane) {
+  const int n = lane & 31, g = lane >> 5;
+#pragma unroll
+  for (int b = 0; b < S::TN; ++b)
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+      *reinterpret_cast<f32x4*>(out + n * S::OUT_LD + 32 * b + 8 * q + 4 * g) =
+          f32x4{c[b][4 * q], c[b][4 * q + 1], c[b][4 * q + 2], c[b][4 * q + 3]};
+  __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "wavefront");
+}
+// Eight consecutive columns of row r of it.
+template <class S>
+__device__ __forceinline__ void tp_staged8(const float* out, int r, int c, float v[8]) {
+  const f32x4 lo = *reinterpret_cast<const f32x4*>(out + r * S::OUT_LD + c);
+  const f32x4 hi = *reinterpret_cast<const f32x4*>(out + r * S::OUT_LD + c + 4);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) { v[i] = lo[i]; v[4 + i] = hi[i]; }
+}
+
 // Epi, the epilogue: begin(tail) while the first copies are on their way (Epi::TAIL bytes of LDS of its own behind
-// the buffers and Epi::BLOCKS output blocks per wave), slab() before and rows() for 8 columns of each row of a wave's
-// block, end() with the whole workgroup.
+// the buffers and Epi::BLOCKS output blocks per wave); block() with the accumulators of each 32 rows of a wave, where
+// lane (g, i) holds row i, columns 32 b + 8 q + 4 g + 0..3; end() with the whole workgroup.
+//
+// Fragments are read one chunk of k ahead of their products, over the barrier too: after it the first reads of
+// the new step go out, then the last products of the old one.  (4,096 x 32,001 x 2,048 in bf16: @@.)
 template <typename T, bool AK, bool BK, class S, class Epi>
 __global__ __launch_bounds__(S::THREADS) void k_tile_product(TpJob j, typename Epi::Args ea) {
   extern __shared__ __attribute__((aligned(16))) char smem[];
@@ -231,7 +255,7 @@ __global__ __launch_bounds__(S::THREADS) void k_tile_product(TpJob j, typename E
   constexpr int KB = TpMma<T>::KB, NB = S::NBUF;
   const int64_t k0 = split * j.split_k, k1 = min(j.k, k0 + j.split_k);
   const int steps = (int)((k1 - k0 + KB - 1) / KB);
-  Epi epi(ea, j, tm * S::BM, tn * S::BN, split);
+  Epi epi(ea, j, tm * S::BM, tn * S::BN, split, wave, lane);
 
   TpLoad<T, AK, S::BM, S> la;
   TpLoad<T, BK, S::BN, S> lb;
@@ -260,58 +284,50 @@ __global__ __launch_bounds__(S::THREADS) void k_tile_product(TpJob j, typename E
 #pragma unroll
       for (int r = 0; r < 16; ++r) acc[a][b][r] = 0.0f;
 
+  using Frag = decltype(tp_frag<T, AK, S::BM>(smem, 0, 0, 0));
+  Frag fa[2][S::TM], fb[2][S::TN];
+  auto read = [&](int s, int kk, int into) {
+    const char* pa = smem + (s % NB) * S::BUF;
+    const char* pb = pa + S::BM * TP_STEP;
+#pragma unroll
+    for (int b = 0; b < S::TN; ++b) fb[into][b] = tp_frag<T, BK, S::BN>(pb, 32 * (wn * S::TN + b), kk, lane);
+#pragma unroll
+    for (int a = 0; a < S::TM; ++a) fa[into][a] = tp_frag<T, AK, S::BM>(pa, 32 * (wm * S::TM + a), kk, lane);
+  };
+  auto multiply = [&](int from) {
+#pragma unroll
+    for (int a = 0; a < S::TM; ++a)
+#pragma unroll
+      for (int b = 0; b < S::TN; ++b) acc[a][b] = tp_mma(fb[from][b], fa[from][a], acc[a][b]);
+  };
   for (int s = 0; s < steps; ++s) {
-    // this step's copies have landed (those of later steps may be on their way), everywhere
+    // this step's copies have landed (those of later steps may be on their way), everywhere, and this wave has
+    // read all of the step before
     if (NB > 2 && s + NB - 2 < steps)
       tp_wait<(NB - 2) * COPIES>();
     else
       tp_wait<0>();
     __builtin_amdgcn_s_barrier();
+    read(s, 0, 0);
     if (s + NB - 1 < steps) issue(s + NB - 1);
-    const char* pa = smem + (s % NB) * S::BUF;
-    const char* pb = pa + S::BM * TP_STEP;
+    __builtin_amdgcn_sched_barrier(0);
+    if (s > 0) multiply(1);
+    __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-    for (int kk = 0; kk < 4; ++kk) {
-      decltype(tp_frag<T, AK, S::BM>(pa, 0, 0, 0)) fa[S::TM], fb[S::TN];
-#pragma unroll
-      for (int a = 0; a < S::TM; ++a) fa[a] = tp_frag<T, AK, S::BM>(pa, 32 * (wm * S::TM + a), kk, lane);
-#pragma unroll
-      for (int b = 0; b < S::TN; ++b) fb[b] = tp_frag<T, BK, S::BN>(pb, 32 * (wn * S::TN + b), kk, lane);
-#pragma unroll
-      for (int a = 0; a < S::TM; ++a)
-#pragma unroll
-        for (int b = 0; b < S::TN; ++b) acc[a][b] = tp_mma(fb[b], fa[a], acc[a][b]);
+    for (int kk = 1; kk < 4; ++kk) {
+      read(s, kk, kk & 1);
+      __builtin_amdgcn_sched_barrier(0);
+      multiply((kk - 1) & 1);
+      __builtin_amdgcn_sched_barrier(0);
     }
   }
+  if (steps > 0) multiply(1);
   __syncthreads();  // the buffers are free for the epilogue
 
   float* const out = reinterpret_cast<float*>(smem + wave * S::OUT);
-  const int n = lane & 31, g = lane >> 5;
-  constexpr int LPR = S::WCOLS / 8, RPP = 64 / LPR;  // lanes per row, rows per pass
-  const int col = tn * S::BN + wn * S::WCOLS + 8 * (lane % LPR);
 #pragma unroll
-  for (int a = 0; a < S::TM; ++a) {
-    const int row0 = tm * S::BM + 32 * (wm * S::TM + a);
-#pragma unroll
-    for (int b = 0; b < S::TN; ++b)
-#pragma unroll
-      for (int q = 0; q < 4; ++q)
-        *reinterpret_cast<f32x4*>(out + n * S::OUT_LD + 32 * b + 8 * q + 4 * g) =
-            f32x4{acc[a][b][4 * q], acc[a][b][4 * q + 1], acc[a][b][4 * q + 2], acc[a][b][4 * q + 3]};
-    __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "wavefront");
-    epi.slab(row0, col - 8 * (lane % LPR), wave, lane);
-#pragma unroll 1  // (the accumulators' loop around it must unroll)
-    for (int p = 0; p < 32 / RPP; ++p) {
-      const int r = p * RPP + lane / LPR;
-      float v[8];
-      const f32x4 lo = *reinterpret_cast<const f32x4*>(out + r * S::OUT_LD + 8 * (lane % LPR));
-      const f32x4 hi = *reinterpret_cast<const f32x4*>(out + r * S::OUT_LD + 8 * (lane % LPR) + 4);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) { v[i] = lo[i]; v[4 + i] = hi[i]; }
-      epi.rows(row0 + r, r, col, v, wave, lane);
-    }
-    __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "wavefront");
-  }
+  for (int a = 0; a < S::TM; ++a)
+    epi.block(acc[a], tm * S::BM + 32 * (wm * S::TM + a), tn * S::BN + wn * S::WCOLS, out, wave, lane);
   epi.end(wave, wm, wn, lane, tid);
 }
 

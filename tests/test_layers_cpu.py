@@ -188,7 +188,7 @@ def test_workspaces(dtype):
 def test_reference_of_the_random_bits():
     # splitmix64 as published: the first outputs of the generator that starts at 0
     with open(os.path.join(os.path.dirname(__file__), "golden", "splitmix64_seed0.txt")) as f:
-        first = [int(x, 0) for x in f if not x.startswith("#")][0]
+        first = [int(x.split()[1], 0) for x in f if not x.startswith("#")][0]  # of state 0
 
     def mix(v):
         v = (v + 0x9E3779B97F4A7C15) % 2 ** 64
