@@ -78,46 +78,45 @@ struct LseArgs {
   float2* part;  // [B][tiles_n]
 };
 
-// Biases of the columns that a lane's accumulators hold: col + 32 b + 8 q + i.
+// The tile's biases in LDS (zeros without, and past the last column): a lane's accumulators hold columns
+// 32 b + 8 q + 4 g + 0..3 of its wave's.
 template <class S>
-__device__ __forceinline__ void lane_bias(const float* bias, int col, int n, f32x4 (&v)[S::TN][4]) {
-#pragma unroll
-  for (int b = 0; b < S::TN; ++b)
-#pragma unroll
-    for (int q = 0; q < 4; ++q)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int c = col + 32 * b + 8 * q + i;
-        v[b][q][i] = bias && c < n ? bias[c] : 0.0f;
-      }
+__device__ __forceinline__ void tile_bias(const float* bias, int c0, int n, float* to) {
+  for (int c = threadIdx.x; c < S::BN; c += S::THREADS) to[c] = bias && c0 + c < n ? bias[c0 + c] : 0.0f;
 }
 
 // All in the accumulators: a lane has half of a wave's columns of its row.
 template <class S>
 struct EpiLse {
   using Args = LseArgs;
-  static constexpr int BLOCKS = 1, TAIL = S::WN * S::BM * 8;
+  static constexpr int BLOCKS = 1, TAIL = S::WN * S::BM * 8 + S::BN * 4;
   const LseArgs& a;
-  int m, n, row0, tile, tiles;
-  float2* ms;  // [WN][BM]
-  f32x4 bias[S::TN][4];  // of the lane's columns
-  int col;
+  int m, n, row0, col0, tile, tiles;
+  float2* ms;   // [WN][BM]
+  float* bias;  // [BN]
   __device__ EpiLse(const LseArgs& args, const TpJob& j, int r0, int c0, int, int wave, int lane)
-      : a(args), m(j.m), n(j.n), row0(r0), tile(c0 / S::BN), tiles(j.tiles_n) {
-    col = c0 + wave % S::WN * S::WCOLS + 4 * (lane >> 5);
-    lane_bias<S>(a.bias, col, n, bias);
+      : a(args), m(j.m), n(j.n), row0(r0), col0(c0), tile(c0 / S::BN), tiles(j.tiles_n) {}
+  __device__ void begin(char* tail) {
+    ms = reinterpret_cast<float2*>(tail);
+    bias = reinterpret_cast<float*>(tail + S::WN * S::BM * 8);
+    tile_bias<S>(a.bias, col0, n, bias);  // (the loop's barriers lie between)
   }
-  __device__ void begin(char* tail) { ms = reinterpret_cast<float2*>(tail); }
-  __device__ __forceinline__ void block(const f32x16 (&acc)[S::TN], int r0, int, float*, int wave, int lane) {
+  __device__ __forceinline__ void block(const f32x16 (&acc)[S::TN], int r0, int colw, float*, int wave, int lane) {
     float v[S::TN][16], top = -INFINITY;
-    const bool edge = col - 4 * (lane >> 5) + S::WCOLS > n;  // (the same for the whole wave)
+    const bool edge = colw + S::WCOLS > n;  // (the same for the whole wave)
+    const int g = lane >> 5;
 #pragma unroll
     for (int b = 0; b < S::TN; ++b)
 #pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        v[b][r] = acc[b][r] + bias[b][r >> 2][r & 3];
-        if (edge && col + 32 * b + 8 * (r >> 2) + (r & 3) >= n) v[b][r] = -INFINITY;
-        top = fmaxf(top, v[b][r]);
+      for (int q = 0; q < 4; ++q) {
+        const f32x4 t = *reinterpret_cast<const f32x4*>(bias + colw - col0 + 32 * b + 8 * q + 4 * g);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          float& x = v[b][4 * q + i];
+          x = acc[b][4 * q + i] + t[i];
+          if (edge && colw + 32 * b + 8 * q + 4 * g + i >= n) x = -INFINITY;
+          top = fmaxf(top, x);
+        }
       }
     top = fmaxf(top, __builtin_bit_cast(float, lane_xor<32>(__builtin_bit_cast(unsigned, top), lane)));
     const float base = top == -INFINITY ? 0.0f : top;
@@ -237,17 +236,16 @@ struct DzArgs {
 template <typename T, class S>
 struct EpiDzT {
   using Args = DzArgs;
-  static constexpr int HITS = 1023, BLOCKS = 2, TAIL = 4 * (HITS + 1);
+  static constexpr int HITS = 1023, BLOCKS = 2, TAIL = 4 * (HITS + 1) + 4 * S::BN;
   const DzArgs& a;
-  int m, n, row0, col0, tm, col;
-  int* hits;  // [0]: how many
+  int m, n, row0, col0, tm;
+  int* hits;    // [0]: how many
+  float* bias;  // [BN]
   unsigned* counts;
   float scale;
-  f32x4 bias[S::TN][4], sum[S::TN][4];
+  f32x4 sum[S::TN][4];
   __device__ EpiDzT(const DzArgs& args, const TpJob& j, int r0, int c0, int, int wave, int lane)
       : a(args), m(j.m), n(j.n), row0(r0), col0(c0), tm(r0 / S::BM) {
-    col = c0 + wave % S::WN * S::WCOLS + 4 * (lane >> 5);
-    lane_bias<S>(a.bias, col, n, bias);
     scale = *a.scale;
 #pragma unroll
     for (int b = 0; b < S::TN; ++b)
@@ -256,6 +254,8 @@ struct EpiDzT {
   }
   __device__ void begin(char* tail) {
     hits = reinterpret_cast<int*>(tail);
+    bias = reinterpret_cast<float*>(tail + 4 * (HITS + 1));
+    tile_bias<S>(a.bias, col0, n, bias);
     if (threadIdx.x == 0) hits[0] = 0;
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     __builtin_amdgcn_s_barrier();
@@ -333,22 +333,24 @@ struct EpiDzT {
     for (int b = 0; b < S::TN; ++b)
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
+        const int c = 32 * b + 8 * q + 4 * (lane >> 5);
+        const f32x4 t = *reinterpret_cast<const f32x4*>(bias + colw - col0 + c);
         f32x4 v;
 #pragma unroll
-        for (int k = 0; k < 4; ++k) v[k] = exp_fast(acc[b][4 * q + k] + bias[b][q][k] - lse);
+        for (int k = 0; k < 4; ++k) v[k] = exp_fast(acc[b][4 * q + k] + t[k] - lse);
         if (any) {
-          const u32x4 c = *reinterpret_cast<const u32x4*>(counts + i * S::OUT_LD + 32 * b + 8 * q + 4 * (lane >> 5));
+          const u32x4 times = *reinterpret_cast<const u32x4*>(counts + i * S::OUT_LD + c);
 #pragma unroll
-          for (int k = 0; k < 4; ++k) v[k] -= (float)c[k] * sh;
+          for (int k = 0; k < 4; ++k) v[k] -= (float)times[k] * sh;
         }
         // rows without labels and columns past the last are zeros, whatever they hold
 #pragma unroll
-        for (int k = 0; k < 4; ++k) v[k] = live && col + 32 * b + 8 * q + k < n ? v[k] * f : 0.0f;
+        for (int k = 0; k < 4; ++k) v[k] = live && colw + c + k < n ? v[k] * f : 0.0f;
         sum[b][q] += v;
         typename TpMma<T>::frag4 o;
 #pragma unroll
         for (int k = 0; k < 4; ++k) o[k] = (T)v[k];
-        *reinterpret_cast<typename TpMma<T>::frag4*>(block + i * LD + 32 * b + 8 * q + 4 * (lane >> 5)) = o;
+        *reinterpret_cast<typename TpMma<T>::frag4*>(block + i * LD + c) = o;
       }
     __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "wavefront");
     constexpr int V = 16 / (int)sizeof(T), LPR = S::WCOLS / V, RPP = 64 / LPR;
@@ -374,12 +376,12 @@ struct EpiDzT {
         *reinterpret_cast<f32x4*>(mine + (lane & 31) * S::OUT_LD + 32 * b + 8 * q + 4 * (lane >> 5)) = sum[b][q];
     __syncthreads();
     float* s = reinterpret_cast<float*>(hits);  // [WM][BN]
-    static_assert(S::WM * S::BN * 4 <= TAIL && S::WCOLS <= 64, "column sums");
-    if (lane < S::WCOLS) {
+    static_assert(S::WM * S::BN * 4 <= TAIL, "column sums");
+    for (int c = lane; c < S::WCOLS; c += 64) {
       float t = 0.0f;
 #pragma unroll 8
-      for (int r = 0; r < 32; ++r) t += mine[r * S::OUT_LD + lane];
-      s[wm * S::BN + wn * S::WCOLS + lane] = t;
+      for (int r = 0; r < 32; ++r) t += mine[r * S::OUT_LD + c];
+      s[wm * S::BN + wn * S::WCOLS + c] = t;
     }
     __syncthreads();
     for (int c = tid; c < S::BN; c += S::THREADS) {

@@ -102,21 +102,22 @@ struct TpLoad {
   }
   __device__ __forceinline__ void init(const TpOperand& o, int64_t r0, int64_t k0, int tid) {
     const int row = tid / CPR, pos = tid % CPR;
-    unsigned v;
+    kchunk = pos ^ ((row >> 1) & 7);
+    static_assert(!KROWS || ROWS_IT % 16 == 0, "a lane keeps its chunk");
+#pragma unroll
+    for (int i = 0; i < ITS; ++i) {
+      const int r = row + i * ROWS_IT;
+      const unsigned chunk = KROWS ? kchunk : ((pos / UNIT) ^ swz(r)) * UNIT + pos % UNIT;
+      voff[i] = (unsigned)(r * o.ld) + 16 * chunk;
+    }
     if constexpr (KROWS) {
-      kchunk = pos ^ ((row >> 1) & 7);
-      v = (unsigned)(row * o.ld) + 16 * kchunk;
       at = o.base + r0 * o.ld + k0 * (int64_t)sizeof(T);
       step = TP_STEP;
     } else {
-      kchunk = 0;
-      v = (unsigned)(row * o.ld) + 16 * (((pos / UNIT) ^ swz(row)) * UNIT + pos % UNIT);
       at = o.base + k0 * o.ld + r0 * (int64_t)sizeof(T);
       step = TpMma<T>::KB * o.ld;
     }
     left = o.end - (at - o.base);
-#pragma unroll
-    for (int i = 0; i < ITS; ++i) voff[i] = v + (unsigned)(i * ROWS_IT * o.ld);
   }
   // Copies the next step into the buffer at LDS byte `lds` (of this wave's first lane: + 1024 wave);
   // kleft: bytes of k left in the rows (K rows), TP_STEP or more except in the last step.
@@ -326,8 +327,10 @@ __global__ __launch_bounds__(S::THREADS) void k_tile_product(TpJob j, typename E
 
   float* const out = reinterpret_cast<float*>(smem + wave * S::OUT);
 #pragma unroll
-  for (int a = 0; a < S::TM; ++a)
+  for (int a = 0; a < S::TM; ++a) {
+    __builtin_amdgcn_sched_barrier(0);  // (one row of blocks at a time: all at once do not fit the registers)
     epi.block(acc[a], tm * S::BM + 32 * (wm * S::TM + a), tn * S::BN + wn * S::WCOLS, out, wave, lane);
+  }
   epi.end(wave, wm, wn, lane, tid);
 }
 
