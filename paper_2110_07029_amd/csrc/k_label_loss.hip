@@ -22,8 +22,7 @@
 // largest weight, so that probabilities down to 2^-29 stay normal.
 #include <math.h>
 
-#include "logits_dev.h"
-#include "tile_plan.h"
+#include "label_loss_dev.h"
 
 namespace asgd {
 
@@ -51,7 +50,7 @@ __global__ __launch_bounds__(256) void k_loss_prep(MatDev h, IdLists y, int B, i
   const int lane = threadIdx.x & 63, i = blockIdx.x * 4 + (threadIdx.x >> 6);
   if (i >= B) return;
   int q0 = 0, q1 = 0, n = 0;
-  if (y.indptr) list_range(y, i, &q0, &q1);
+  if (y.indptr) label_range(y, i, &q0, &q1);
   for (int q = q0 + lane; q < q1; q += 64) n += entry(y, q, L) >= 0;
 #pragma unroll
   for (int o = 32; o; o >>= 1) n += __shfl_xor(n, o);
@@ -178,7 +177,7 @@ __global__ __launch_bounds__(256) void k_loss_rows(const float2* __restrict__ pa
   const float sh = share[i];
   if (sh > 0.0f) {
     int q0, q1;
-    list_range(y, i, &q0, &q1);
+    label_range(y, i, &q0, &q1);
     const T* hr = (const T*)(h.base + i * h.ld);
     const int l = tid & 15;
     for (int q = q0 + (tid >> 4); q < q1; q += 16) {
@@ -219,17 +218,6 @@ __global__ __launch_bounds__(256) void k_loss_rows(const float2* __restrict__ pa
 }
 
 // ---- product 2 -------------------------------------------------------------------------------------
-struct DzArgs {
-  const float* bias;   // of the piece's first label
-  const float *lse, *share, *weights, *scale;
-  float up;            // 2^15 for fp16
-  void* dz;            // [B x ld]
-  int64_t ld;
-  float* part;         // [tiles_m x ld] column sums, or null
-  IdLists y;
-  int label0, n_labels;
-};
-
 // Targets of a tile: every thread looks through a share of one row's list while the first copies
 // are on their way; what falls into the tile is listed in LDS.  A wave's block of 32 rows that has any gets a
 // block of counts beside its output block.  A tile with more than HITS looks through the lists again per block.
@@ -263,7 +251,7 @@ struct EpiDzT {
     const int r = threadIdx.x / PER, row = row0 + r;
     if (row < m && a.y.indptr) {
       int q0, q1;
-      list_range(a.y, row, &q0, &q1);
+      label_range(a.y, row, &q0, &q1);
       for (int q = q0 + (int)threadIdx.x % PER; q < q1; q += PER) {
         const int id = a.y.indices[q];
         const int c = id - a.label0 - col0;
@@ -300,7 +288,7 @@ struct EpiDzT {
       }
     } else if (r0 + (lane >> 1) < m) {
       int q0, q1;
-      list_range(a.y, r0 + (lane >> 1), &q0, &q1);
+      label_range(a.y, r0 + (lane >> 1), &q0, &q1);
       for (int q = q0 + (lane & 1); q < q1; q += 2) {
         const int id = a.y.indices[q], c = id - a.label0 - c0;
         if (c >= 0 && c < S::WCOLS && id < a.n_labels) atomicAdd(counts + (lane >> 1) * S::OUT_LD + c, 1u);
@@ -405,6 +393,9 @@ namespace {
 struct Sizes {
   int piece;  // labels of a piece (a multiple of 64 unless it is all)
   int64_t ldz;
+  NarrowPlan nl, ng;
+  bool narrow, narrow_grad;
+  int parts;  // of a row's log-sum-exp
   TpPlan fwd, dz, dh;
   size_t hp, hq, wp, share, lse, scale, part, dzb, dbp, slabs, total;
 };
@@ -412,22 +403,32 @@ struct Sizes {
 Sizes sizes(int dtype, const MatDev& h, const MatDev& w, int B, int L, int D, bool grads) {
   Sizes s{};
   const int es = elem_size(dtype);
+  s.narrow = narrow_takes(dtype, D);
+  s.narrow_grad = grads && narrow_grad_takes(dtype, B, D);
+  s.nl = narrow_lse_plan(B, L);
   s.fwd = tp_plan(dtype, B, L, D, 1);
+  s.parts = s.narrow ? s.nl.ranges : s.fwd.job.tiles_n;
   s.share = round256((size_t)B * 4);
   s.lse = round256((size_t)B * 4);
-  s.part = round256((size_t)B * s.fwd.job.tiles_n * 8);
+  s.part = round256((size_t)B * s.parts * 8);
   s.wp = tp_in_place(dtype, w, D) ? 0 : tp_packed_bytes(dtype, L, D);
   s.hq = tp_in_place(dtype, h, D) ? 0 : tp_packed_bytes(dtype, B, D);
   s.hp = grads ? tp_packed_bytes(dtype, B, D) : 0;
   s.total = s.share + s.lse + s.part + s.wp + s.hp + s.hq;
   if (!grads) return s;
+  s.scale = 256;
+  if (s.narrow_grad) {
+    s.ng = narrow_grad_plan(L);
+    s.slabs = narrow_slab_bytes(s.ng, B);
+    s.total += s.scale + s.slabs;
+    return s;
+  }
   const int64_t fit = PIECE_BYTES / ((int64_t)B * es) / 256 * 256;
   s.piece = (int)(fit < 256 ? 256 : fit);
   if (s.piece > L) s.piece = L;
   s.ldz = ceil_div(s.piece, 64) * 64;
   s.dz = tp_plan(dtype, B, s.piece, D, 1);
   s.dh = tp_plan(dtype, B, D, s.piece, MAX_SLABS);
-  s.scale = 256;
   s.dzb = round256((size_t)B * s.ldz * es);
   s.dbp = round256((size_t)s.dz.job.tiles_m * s.ldz * 4);
   s.slabs = round256((size_t)s.dh.job.splits * B * ceil_div(D, 8) * 8 * 4);
@@ -472,23 +473,35 @@ hipError_t run(const LossJob& j, char* ws, hipStream_t st) {
   }
   s.fwd.job.a = h;
   s.fwd.job.b = w;
-  if ((e = tp_launch<T, true, true, EpiLse>(s.fwd, LseArgs{j.bias, part}, st)) != hipSuccess) return e;
-  hipLaunchKernelGGL(k_loss_rows<T>, dim3(B + (scale ? 1 : 0)), dim3(256), 0, st, part, s.fwd.job.tiles_n, h, w, D, L, j.bias, j.y,
+  e = s.narrow ? launch_narrow_lse(dt, s.nl, h, w, j.bias, B, L, D, part, st)
+               : tp_launch<T, true, true, EpiLse>(s.fwd, LseArgs{j.bias, part}, st);
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL(k_loss_rows<T>, dim3(B + (scale ? 1 : 0)), dim3(256), 0, st, part, s.parts, h, w, D, L, j.bias, j.y,
                      share, lse, j.lse, j.loss_rows, B, j.weights, scale);
   if ((e = hipGetLastError()) != hipSuccess) return e;
   if (!grads) return hipSuccess;
 
-  char* dz = take(s.dzb);
-  float* dbp = (float*)take(s.dbp);
-  float* slabs = (float*)take(s.slabs);
   const float up = dt == 2 ? 32768.0f : 1.0f;
   StoreArgs da{};
   da.epi.y = j.dh;
+  da.alpha = 1.0f / up;
+  da.alpha_dev = scale;
+  if (s.narrow_grad) {
+    float* slabs = j.dh.data ? (float*)take(s.slabs) : nullptr;
+    const DzArgs za{j.bias, lse, share, j.weights, scale, up, nullptr, 0, nullptr, j.y, 0, L};
+    e = launch_narrow_grad(dt, s.ng, hz, w, za, B, D, 1.0f / up, j.dw, j.db, slabs, st);
+    if (e != hipSuccess || !slabs) return e;
+    da.part = slabs;
+    da.ldp = 128;
+    da.slab = 128ll * B;
+    return launch_join(da, s.ng.ranges, B, D, false, share, st);
+  }
+  char* dz = take(s.dzb);
+  float* dbp = (float*)take(s.dbp);
+  float* slabs = (float*)take(s.slabs);
   da.part = slabs;
   da.ldp = ceil_div(D, 8) * 8;
   da.slab = da.ldp * B;
-  da.alpha = 1.0f / up;
-  da.alpha_dev = scale;
   int splits = 0;
   for (int64_t l0 = 0; l0 < L; l0 += s.piece) {
     const int n = (int)(L - l0 < s.piece ? L - l0 : s.piece);

@@ -1,0 +1,450 @@
+// The label loss over rows of at most 128 columns of 16 bits: a tile of labels then needs no loop over k, and
+// what bounds the general kernels (k_label_loss.hip) is what surrounds it: an epilogue per two steps of k,
+// and dz, which is larger than the label matrix itself at such widths, written to memory and read twice.
+//
+//   k_narrow_lse   256 rows in registers (a wave has 32), labels pass by in tiles of 64 through LDS; maximum and
+//                  sum of exponentials per lane until the end
+//   k_narrow_grad  up to 256 rows.  Per tile of 64 labels: z, dz in registers; dz W onto the rows' gradient, which stays in
+//                  registers (dz is fed to the matrix cores as the accumulators hold it, the tile of W read with the k order
+//                  that this gives); dz through LDS, turned around, times h: the tile's rows of dw
+//
+// LDS rows of W and h are 256 bytes; chunk c (16 bytes) of row r lies at place c ^ (4 (r % 4) + r / 4 % 4), which makes both
+// row reads (16 lanes of consecutive rows, the same c) and transposing reads (four rows, 64 bytes each) free of
+// conflicts.  dz rows are 128 bytes (64 labels), in slots of 8: slot s of row r at s ^ (8 (r / 2 % 2) + r / 4 % 8), for
+// transposing reads of four rows and writes of 32.
+#include "label_loss_dev.h"
+
+namespace asgd {
+
+namespace {
+
+constexpr int NW_THREADS = 512, NW_ROWS = 256, NW_TILE = 64, NW_COLS = 128;
+constexpr int NW_WBUF = NW_TILE * 256, NW_BIAS = 8 * 256;  // bytes of a tile; of its biases, a copy per wave
+
+__device__ __forceinline__ int nw_turn(int r) { return 4 * (r & 3) + ((r >> 2) & 3); }
+
+// The copies of tiles of W (two per wave) and their biases (one).
+struct NwLoad {
+  const char* base;
+  int64_t ld, end;
+  const float* bias;
+  int n;
+  unsigned voff[2];
+  __device__ NwLoad(const TpOperand& w, const float* b, int n_labels, int d_bytes, int tid)
+      : base(w.base), ld(w.ld), end(w.end), bias(b), n(n_labels) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int r = (tid >> 4) + 32 * i, c = (tid & 15) ^ nw_turn(r);
+      voff[i] = 16 * c < d_bytes ? (unsigned)(r * ld) + 16 * c : 0x80000000u;
+    }
+  }
+  // tile t into LDS byte `to` (the buffer) and `to_bias` (this wave's copy)
+  __device__ __forceinline__ void copy(int t, unsigned to, unsigned to_bias, int wave, int lane) const {
+    const int64_t l0 = (int64_t)t * NW_TILE;
+    const i32x4 rs = tp_rsrc(base + l0 * ld, end - l0 * ld);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) tp_copy16(rs, voff[i], to + 8192 * i + 1024 * wave);
+    const i32x4 rb = tp_rsrc((const char*)(bias + (bias ? l0 : 0)), bias ? (n - l0) * 4 : 0);  // (zeros without)
+    tp_copy4(rb, 4u * lane, to_bias);
+  }
+};
+constexpr int NW_COPIES = 3;
+
+// Row r's chunk pair kk (32 bytes of k) of a tile in LDS.
+template <typename T>
+__device__ __forceinline__ typename TpMma<T>::frag8 nw_row_frag(const char* p, int r, int kk, int g) {
+  return *reinterpret_cast<const typename TpMma<T>::frag8*>(p + 256 * r + 16 * ((2 * kk + g) ^ nw_turn(r)));
+}
+// Byte of a transposing read's source lane: row r (of this lane), columns 32 u + 16 (G % 2) + 4 a .. + 3.
+__device__ __forceinline__ int nw_turned_at(int r, int u, int G, int a) {
+  return 256 * r + 16 * ((4 * u + 2 * (G & 1) + (a >> 1)) ^ nw_turn(r)) + 8 * (a & 1);
+}
+template <typename T>
+__device__ __forceinline__ typename TpMma<T>::frag8 nw_join(typename TpMma<T>::frag4 lo, typename TpMma<T>::frag4 hi) {
+  return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+}
+
+// A row of h as fragments (zeros past B and d).
+template <typename T>
+__device__ __forceinline__ void nw_rows(const TpOperand& h, int row, int B, int d_bytes, int g,
+                                        typename TpMma<T>::frag8 (&f)[8]) {
+#pragma unroll
+  for (int kk = 0; kk < 8; ++kk) {
+    f[kk] = typename TpMma<T>::frag8{};
+    if (row < B && 32 * kk + 16 * g < d_bytes)
+      f[kk] = *reinterpret_cast<const typename TpMma<T>::frag8*>(h.base + row * h.ld + 32 * kk + 16 * g);
+  }
+}
+
+// z + bias of tile rows 32 b + 8 q + 4 g + i (labels) for this lane's row.
+template <typename T>
+__device__ __forceinline__ void nw_logits(const char* w, const char* bias, const typename TpMma<T>::frag8 (&hf)[8], int lane,
+                                          f32x16 (&z)[2]) {
+  const int n = lane & 31, g = lane >> 5;
+#pragma unroll
+  for (int b = 0; b < 2; ++b)
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const f32x4 t = *reinterpret_cast<const f32x4*>(bias + 4 * (32 * b + 8 * q + 4 * g));
+#pragma unroll
+      for (int i = 0; i < 4; ++i) z[b][4 * q + i] = t[i];
+    }
+#pragma unroll
+  for (int kk = 0; kk < 8; ++kk)
+#pragma unroll
+    for (int b = 0; b < 2; ++b) z[b] = tp_mma(nw_row_frag<T>(w, 32 * b + n, kk, g), hf[kk], z[b]);
+}
+
+}  // namespace
+
+// ---- log-sum-exp ---------------------------------------------------------------------------------
+// Workgroup = (256 rows, a range of tiles); the row blocks of a range sit on one XCD, whose L2 then has its labels.
+// Four tiles are on their way.
+constexpr int NWF_BUFS = 4;
+constexpr int NWF_LDS = NWF_BUFS * (NW_WBUF + NW_BIAS);
+
+template <typename T>
+__global__ __launch_bounds__(NW_THREADS) void k_narrow_lse(TpOperand h, TpOperand w, const float* bias, int B, int L,
+                                                          int d_bytes, int row_blocks, int ranges, int per, int tiles,
+                                                          float2* __restrict__ part) {
+  extern __shared__ __attribute__((aligned(16))) char smem[];
+  const int tid = threadIdx.x, lane = tid & 63, g = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int set = (int)blockIdx.x / (8 * row_blocks), in = (int)blockIdx.x % (8 * row_blocks);
+  const int range = 8 * set + in % 8;
+  if (range >= ranges) return;
+  const int row = (in / 8) * NW_ROWS + 32 * wave + (lane & 31);
+  const int t0 = range * per, t1 = min(tiles, t0 + per);
+  const NwLoad load(w, bias, L, d_bytes, tid);
+  const unsigned lds0 = __builtin_amdgcn_readfirstlane((unsigned)(uintptr_t)(__attribute__((address_space(3))) char*)smem);
+  auto issue = [&](int t) {
+    const unsigned at = lds0 + (unsigned)((t - t0) % NWF_BUFS) * (NW_WBUF + NW_BIAS);
+    load.copy(t, at, at + NW_WBUF + 256 * wave, wave, lane);
+  };
+  typename TpMma<T>::frag8 hf[8];
+  nw_rows<T>(h, row, B, d_bytes, g, hf);
+#pragma unroll
+  for (int k = 0; k < NWF_BUFS - 1; ++k)
+    if (t0 + k < t1) issue(t0 + k);
+  float m = -INFINITY, s = 0.0f;
+  for (int t = t0; t < t1; ++t) {
+    if (t + NWF_BUFS - 2 < t1) tp_wait<(NWF_BUFS - 2) * NW_COPIES>();
+    else tp_wait<0>();
+    __builtin_amdgcn_s_barrier();
+    if (t + NWF_BUFS - 1 < t1) issue(t + NWF_BUFS - 1);
+    const char* p = smem + (t - t0) % NWF_BUFS * (NW_WBUF + NW_BIAS);
+    f32x16 z[2];
+    nw_logits<T>(p, p + NW_WBUF + 256 * wave, hf, lane, z);
+    if ((t + 1) * NW_TILE > L) {
+#pragma unroll
+      for (int b = 0; b < 2; ++b)
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+          if (t * NW_TILE + 32 * b + 8 * (r >> 2) + 4 * g + (r & 3) >= L) z[b][r] = -INFINITY;
+    }
+    float top[2] = {m, m};
+#pragma unroll
+    for (int b = 0; b < 2; ++b)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) top[b] = fmaxf(top[b], z[b][r]);
+    const float mm = fmaxf(top[0], top[1]);
+    // base 2; the maximum's rounding is of the size of the result's own
+    const float base = mm == -INFINITY ? 0.0f : mm * LOG2E;
+    float e[4] = {s * __builtin_amdgcn_exp2f(fmaf(m, LOG2E, -base)), 0.0f, 0.0f, 0.0f};
+    if (m == -INFINITY) e[0] = s;  // (0, or NaN)
+#pragma unroll
+    for (int b = 0; b < 2; ++b)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) e[r & 3] += __builtin_amdgcn_exp2f(fmaf(z[b][r], LOG2E, -base));
+    s = (e[0] + e[1]) + (e[2] + e[3]);
+    m = mm;
+  }
+  const float m2 = __builtin_bit_cast(float, lane_xor<32>(__builtin_bit_cast(unsigned, m), lane));
+  const float s2 = __builtin_bit_cast(float, lane_xor<32>(__builtin_bit_cast(unsigned, s), lane));
+  const float mm = fmaxf(m, m2), base = mm == -INFINITY ? 0.0f : mm;
+  if (row < B && g == 0) part[(int64_t)row * ranges + range] = make_float2(mm, s * exp_fast(m - base) + s2 * exp_fast(m2 - base));
+}
+
+// ---- gradients ---------------------------------------------------------------------------------------
+constexpr int NWG_BUFS = 2, NWG_HITS = 1023;
+constexpr int NWG_H = 0, NWG_DZ = NWG_H + NW_ROWS * 256, NWG_W = NWG_DZ + NW_ROWS * 128;
+constexpr int NWG_HIT = NWG_W + NWG_BUFS * (NW_WBUF + NW_BIAS), NWG_SUM = NWG_HIT + 4 * (NWG_HITS + 1);
+constexpr int NWG_LDS = NWG_SUM + 8 * NW_TILE * 4;
+static_assert(NWG_LDS <= 160 * 1024, "LDS of a compute unit");
+
+// LDS byte of labels 4 s .. + 3 of row r in the tile of dz.
+__device__ __forceinline__ int nw_dz(int r, int s) { return 128 * r + 8 * (s ^ (8 * ((r >> 1) & 1) + ((r >> 2) & 7))); }
+
+// v[k] summed over the 32 lanes of each half; lane i keeps label (k index) i.  Halves of the values change sides at every step.
+__device__ __forceinline__ float nw_sum_lanes(float (&v)[32], int lane) {
+#pragma unroll
+  for (int k = 0; k < 16; ++k) {
+    const auto s = __builtin_amdgcn_permlane16_swap(__builtin_bit_cast(unsigned, v[k]), __builtin_bit_cast(unsigned, v[k + 16]),
+                                                    false, false);
+    v[k] = __builtin_bit_cast(float, (unsigned)s[0]) + __builtin_bit_cast(float, (unsigned)s[1]);
+  }
+  auto halve = [&](int half, bool up, auto other) {
+    for (int k = 0; k < half; ++k) {
+      const float keep = up ? v[k + half] : v[k], give = up ? v[k] : v[k + half];
+      v[k] = keep + __builtin_bit_cast(float, other(__builtin_bit_cast(unsigned, give)));
+    }
+  };
+#pragma unroll
+  for (int k = 0; k < 1; ++k) {
+    halve(8, lane & 8, [&](unsigned x) { return lane_xor<8>(x, lane); });
+    halve(4, lane & 4, [&](unsigned x) { return lane_xor<4>(x, lane); });
+    halve(2, lane & 2, [&](unsigned x) { return lane_xor<2>(x, lane); });
+    halve(1, lane & 1, [&](unsigned x) { return lane_xor<1>(x, lane); });
+  }
+  return v[0];
+}
+
+template <typename T>
+__global__ __launch_bounds__(NW_THREADS) void k_narrow_grad(TpOperand h, TpOperand w, DzArgs a, int B, int d, int ranges,
+                                                           int per, int tiles, float alpha, MatDev dw, float* __restrict__ db,
+                                                           float* __restrict__ slabs) {
+  typedef typename TpMma<T>::frag8 Frag;
+  typedef typename TpMma<T>::frag4 Half;
+  extern __shared__ __attribute__((aligned(16))) char smem[];
+  const int tid = threadIdx.x, lane = tid & 63, g = lane >> 5, n = lane & 31;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int G = lane >> 4, ti = (lane >> 2) & 3, ta = lane & 3;  // of a transposing read's address
+  const int range = blockIdx.x, L = a.n_labels, d_bytes = d * 2;
+  const int t0 = range * per, t1 = min(tiles, t0 + per);
+  const NwLoad load(w, a.bias, L, d_bytes, tid);
+  const unsigned lds0 = __builtin_amdgcn_readfirstlane((unsigned)(uintptr_t)(__attribute__((address_space(3))) char*)smem);
+  auto issue = [&](int t) {
+    const unsigned at = lds0 + NWG_W + (unsigned)((t - t0) % NWG_BUFS) * (NW_WBUF + NW_BIAS);
+    load.copy(t, at, at + NW_WBUF + 256 * wave, wave, lane);
+  };
+  // the rows: all of them in LDS, a wave's own in registers too
+  {
+    const i32x4 rs = tp_rsrc(h.base, h.end);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int r = (tid >> 4) + 32 * i, c = (tid & 15) ^ nw_turn(r);
+      tp_copy16(rs, 16 * c < d_bytes && r < B ? (unsigned)(r * h.ld) + 16 * c : 0x80000000u, lds0 + NWG_H + 8192 * i + 1024 * wave);
+    }
+  }
+  if (t0 < t1) issue(t0);
+  const int row = 32 * wave + n;
+  Frag hf[8];
+  nw_rows<T>(h, row, B, d_bytes, g, hf);
+  const float scale = *a.scale;
+  float sh = 0.0f, lse = 0.0f, f = 0.0f;
+  if (row < B) {
+    sh = a.share[row];
+    lse = a.lse[row];
+    f = (a.weights ? scale > 0.0f ? a.weights[row] / scale : a.weights[row] : 1.0f) * a.up;
+  }
+  const bool live = sh > 0.0f;
+  const float out = alpha * scale;
+  // targets among this workgroup's labels, listed once
+  int* const hits = reinterpret_cast<int*>(smem + NWG_HIT);
+  if (tid == 0) hits[0] = 0;
+  asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+  __builtin_amdgcn_s_barrier();
+  const int l0 = t0 * NW_TILE, l1 = min(L, t1 * NW_TILE);
+  if ((tid >> 1) < B && a.y.indptr) {
+    int q0, q1;
+    label_range(a.y, tid >> 1, &q0, &q1);
+    for (int q = q0 + (tid & 1); q < q1; q += 2) {
+      const int id = a.y.indices[q];
+      if (id >= l0 && id < l1) {
+        const int at = atomicAdd(hits, 1);
+        if (at < NWG_HITS) hits[1 + at] = (tid >> 1) << 23 | (id - l0);
+      }
+    }
+  }
+  f32x16 dh[4];
+#pragma unroll
+  for (int u = 0; u < 4; ++u)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) dh[u][r] = 0.0f;
+  char* const dzt = smem + NWG_DZ;
+  // addresses of the transposing reads: rows that differ by multiples of 16 differ by a constant
+  int wat[2][4], hat[2], zat[2][2];
+  const int lb = wave >> 2, wu = wave & 3;  // this wave's block of dw: labels 32 lb .., columns 32 wu ..
+#pragma unroll
+  for (int hi = 0; hi < 2; ++hi) {
+#pragma unroll
+    for (int u = 0; u < 4; ++u) wat[hi][u] = nw_turned_at(8 * hi + 4 * (G >> 1) + ti, u, G, ta);
+    hat[hi] = nw_turned_at(8 * (G >> 1) + 4 * hi + ti, wu, G, ta);
+#pragma unroll
+    for (int c = 0; c < 2; ++c) zat[hi][c] = nw_dz(16 * c + 8 * (G >> 1) + 4 * hi + ti, 8 * lb + 4 * (G & 1) + ta);
+  }
+  // stores of dw that are sure to follow a tile's copies
+  const bool stores = dw.data && 32 * wu + 32 <= d;
+  float* const sums = reinterpret_cast<float*>(smem + NWG_SUM);
+
+  for (int t = t0; t < t1; ++t) {
+    // (vmcnt counts stores too: the four or more of the last tile's dw came after the copies and need not be waited for)
+    if (stores && t > t0) tp_wait<4>();
+    else tp_wait<0>();
+    __builtin_amdgcn_s_barrier();  // the tile is here, and nobody reads dz or the other tile any more
+    if (t + 1 < t1) issue(t + 1);
+    const char* p = smem + NWG_W + (t - t0) % NWG_BUFS * (NW_WBUF + NW_BIAS);
+    // how often this tile's labels stand in the wave's rows: 16-bit counts where dz will lie
+    const int total = hits[0], c0 = (t - t0) * NW_TILE;
+    bool any = total > NWG_HITS;
+    if (total && !any) {
+      bool mine = false;
+      for (int k = lane; k < total; k += 64) {
+        const int hit = hits[1 + k], c = (hit & 0x7fffff) - c0;
+        mine |= (int)((unsigned)hit >> 28) == wave && c >= 0 && c < NW_TILE;
+      }
+      any = __ballot(mine) != 0;
+    }
+    if (any) {
+      auto add = [&](int r, int c) {  // row of the wave, label of the tile
+        const int at = nw_dz(32 * wave + r, c >> 2) + 2 * (c & 3);
+        atomicAdd(reinterpret_cast<unsigned*>(dzt + (at & ~3)), at & 2 ? 0x10000u : 1u);
+      };
+#pragma unroll
+      for (int k = 0; k < 8; ++k) *reinterpret_cast<uint64_t*>(dzt + 4096 * wave + 512 * k + 8 * lane) = 0;
+      __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "wavefront");
+      if (total <= NWG_HITS) {
+        for (int k = lane; k < total; k += 64) {
+          const int hit = hits[1 + k], c = (hit & 0x7fffff) - c0;
+          if ((int)((unsigned)hit >> 28) == wave && c >= 0 && c < NW_TILE) add(((unsigned)hit >> 23) & 31, c);
+        }
+      } else if (32 * wave + (lane >> 1) < B) {
+        int q0, q1;
+        label_range(a.y, 32 * wave + (lane >> 1), &q0, &q1);
+        for (int q = q0 + (lane & 1); q < q1; q += 2) {
+          const int id = a.y.indices[q], c = id - t * NW_TILE;
+          if (c >= 0 && c < NW_TILE && id < L) add(lane >> 1, c);
+        }
+      }
+      __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "wavefront");
+    }
+    f32x16 z[2];
+    nw_logits<T>(p, p + NW_WBUF + 256 * wave, hf, lane, z);
+    const bool edge = (t + 1) * NW_TILE > L;
+    Frag df[2][2];
+#pragma unroll
+    for (int b = 0; b < 2; ++b)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        char* const at = dzt + nw_dz(row, 8 * b + 2 * q + g);
+        float v[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) v[k] = exp_fast(z[b][4 * q + k] - lse);
+        if (any) {
+          const uint64_t times = *reinterpret_cast<const uint64_t*>(at);
+#pragma unroll
+          for (int k = 0; k < 4; ++k) v[k] -= (float)((times >> (16 * k)) & 0xffff) * sh;
+        }
+        Half o;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          // rows without labels and labels past the last are zeros, whatever they hold
+          v[k] = live && !(edge && t * NW_TILE + 32 * b + 8 * q + 4 * g + k >= L) ? v[k] * f : 0.0f;
+          z[b][4 * q + k] = v[k];
+          o[k] = (T)v[k];
+          df[b][q >> 1][4 * (q & 1) + k] = o[k];
+        }
+        *reinterpret_cast<Half*>(at) = o;
+      }
+    if (db) {
+      float v[32];
+#pragma unroll
+      for (int k = 0; k < 32; ++k) v[k] = z[k >> 4][k & 15];
+      // lane i of half g keeps accumulator register i: label 32 (i / 16) + 8 (i / 4 % 4) + 4 g + i % 4
+      sums[wave * NW_TILE + 32 * (n >> 4) + 8 * ((n >> 2) & 3) + 4 * g + (n & 3)] = nw_sum_lanes(v, lane);
+    }
+    // dz W: k are the labels in the accumulators' order, 16 c + 8 hi + 4 g + 0..3 of a block
+#pragma unroll
+    for (int b = 0; b < 2; ++b)
+#pragma unroll
+      for (int c = 0; c < 2; ++c)
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+          const char* q = p + 256 * (32 * b + 16 * c);
+          dh[u] = tp_mma(nw_join<T>(tp_turned<T>(q + wat[0][u]), tp_turned<T>(q + wat[1][u])), df[b][c], dh[u]);
+        }
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    __builtin_amdgcn_s_barrier();  // dz of all rows is here
+    if (db && tid < NW_TILE && t * NW_TILE + tid < L) {
+      float v = 0.0f;
+#pragma unroll
+      for (int k = 0; k < 8; ++k) v += sums[k * NW_TILE + tid];
+      db[t * NW_TILE + tid] = v * out;
+    }
+    if (dw.data) {
+      f32x16 acc;
+#pragma unroll
+      for (int r = 0; r < 16; ++r) acc[r] = 0.0f;
+#pragma unroll
+      for (int c = 0; c < NW_ROWS / 16; ++c) {
+        const char *zp = dzt + 4096 * (c >> 1), *hp = smem + NWG_H + 4096 * c;
+        acc = tp_mma(nw_join<T>(tp_turned<T>(hp + hat[0]), tp_turned<T>(hp + hat[1])),
+                     nw_join<T>(tp_turned<T>(zp + zat[0][c & 1]), tp_turned<T>(zp + zat[1][c & 1])), acc);
+      }
+      const int label = t * NW_TILE + 32 * lb + n;
+      if (label < L) {
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const int col = 32 * wu + 8 * q + 4 * g;
+          const float v[4] = {acc[4 * q] * out, acc[4 * q + 1] * out, acc[4 * q + 2] * out, acc[4 * q + 3] * out};
+          store4(dw, label, col, d - col, v);
+        }
+      }
+    }
+  }
+  if (slabs && row < B) {
+    float* o = slabs + ((int64_t)range * B + row) * NW_COLS + 4 * g;
+#pragma unroll
+    for (int u = 0; u < 4; ++u)
+#pragma unroll
+      for (int q = 0; q < 4; ++q)
+        *reinterpret_cast<f32x4*>(o + 32 * u + 8 * q) = f32x4{dh[u][4 * q], dh[u][4 * q + 1], dh[u][4 * q + 2], dh[u][4 * q + 3]};
+  }
+}
+
+// ---- launches ----------------------------------------------------------------------------------------
+bool narrow_takes(int dtype, int d) { return dtype != 0 && d <= NW_COLS; }
+bool narrow_grad_takes(int dtype, int n_rows, int d) { return narrow_takes(dtype, d) && n_rows <= NW_ROWS; }
+
+// Two workgroups of the log-sum-exp share a compute unit, so that one's exponentials meet the other's products.
+NarrowPlan narrow_lse_plan(int n_rows, int n_labels) {
+  NarrowPlan p;
+  p.row_blocks = (int)ceil_div(n_rows, NW_ROWS);
+  p.tiles = (int)ceil_div(n_labels, NW_TILE);
+  int64_t want = ceil_div(512, p.row_blocks);
+  p.per = (int)ceil_div(p.tiles, want);
+  p.ranges = (int)ceil_div(p.tiles, p.per);
+  return p;
+}
+NarrowPlan narrow_grad_plan(int n_labels) {
+  NarrowPlan p;
+  p.row_blocks = 1;
+  p.tiles = (int)ceil_div(n_labels, NW_TILE);
+  p.per = (int)ceil_div(p.tiles, 256);
+  p.ranges = (int)ceil_div(p.tiles, p.per);
+  return p;
+}
+size_t narrow_slab_bytes(const NarrowPlan& p, int n_rows) { return round256((size_t)p.ranges * n_rows * NW_COLS * 4); }
+
+hipError_t launch_narrow_lse(int dtype, const NarrowPlan& p, const TpOperand& h, const TpOperand& w, const float* bias,
+                             int n_rows, int n_labels, int d, float2* part, hipStream_t st) {
+  const unsigned blocks = (unsigned)(ceil_div(p.ranges, 8) * 8 * p.row_blocks);
+  const auto fn = dtype == 1 ? k_narrow_lse<bf16> : k_narrow_lse<f16>;
+  const hipError_t e = tp_allow_lds((const void*)fn, NWF_LDS);
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL(fn, dim3(blocks), dim3(NW_THREADS), NWF_LDS, st, h, w, bias, n_rows, n_labels, 2 * d, p.row_blocks,
+                     p.ranges, p.per, p.tiles, part);
+  return hipGetLastError();
+}
+
+hipError_t launch_narrow_grad(int dtype, const NarrowPlan& p, const TpOperand& h, const TpOperand& w, const DzArgs& a,
+                              int n_rows, int d, float alpha, const MatDev& dw, float* db, float* slabs, hipStream_t st) {
+  const auto fn = dtype == 1 ? k_narrow_grad<bf16> : k_narrow_grad<f16>;
+  const hipError_t e = tp_allow_lds((const void*)fn, NWG_LDS);
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL(fn, dim3(p.ranges), dim3(NW_THREADS), NWG_LDS, st, h, w, a, n_rows, d, p.ranges, p.per, p.tiles, alpha,
+                     dw, db, slabs);
+  return hipGetLastError();
+}
+
+}  // namespace asgd

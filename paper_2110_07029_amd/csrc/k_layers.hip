@@ -11,9 +11,28 @@
 // meet in k_join.
 #include <math.h>
 
+#include <mutex>
+#include <set>
+
 #include "tile_plan.h"
 
 namespace asgd {
+
+hipError_t tp_allow_lds(const void* fn, int lds) {
+  static std::mutex lock;
+  static std::set<std::pair<const void*, int>> done;  // (kernel, device)
+  int dev = 0;
+  hipError_t e = hipGetDevice(&dev);
+  if (e != hipSuccess) return e;
+  try {
+    const std::lock_guard<std::mutex> hold(lock);
+    if (done.count({fn, dev})) return hipSuccess;
+    e = hipFuncSetAttribute(fn, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+    if (e == hipSuccess) done.insert({fn, dev});
+  } catch (...) {  // (no memory for the note: set it again the next time)
+  }
+  return e;
+}
 
 // ---- rows out of line -----------------------------------------------------------------
 template <typename T>
@@ -44,20 +63,41 @@ hipError_t launch_pack(int dtype, const MatDev& src, int64_t rows, int cols, voi
 }
 
 // ---- slabs --------------------------------------------------------------------------------
-template <bool FULL>
+// 256 / P groups of 8 columns per workgroup, P threads each, which take every P-th slab and meet in LDS (many slabs of few
+// sums: 256 slabs of 256 x 128 take 25 us with one thread per group).
+template <bool FULL, int P>
 __global__ __launch_bounds__(256) void k_join(StoreArgs a, int splits, int m, int n, const float* __restrict__ live) {
+  constexpr int GROUPS = 256 / P;
+  __shared__ f32x4 meet[P > 1 ? 512 : 1];
   const int64_t per_row = (n + 7) / 8, total = m * per_row;
   const float alpha = FULL ? 1.0f : a.alpha * (a.alpha_dev ? *a.alpha_dev : 1.0f);
-  for (int64_t e = blockIdx.x * 256ll + threadIdx.x; e < total; e += 256ll * gridDim.x) {
-    const int64_t row = e / per_row;
+  const int which = threadIdx.x % GROUPS, part = threadIdx.x / GROUPS;
+  for (int64_t e0 = blockIdx.x * (int64_t)GROUPS; e0 < total; e0 += (int64_t)GROUPS * gridDim.x) {
+    const int64_t e = e0 + which, row = e / per_row;
     const int col = (int)(e % per_row) * 8;
-    float v[8] = {};
-    const float* p = a.part + row * a.ldp + col;
-    for (int s = 0; s < splits; ++s, p += a.slab) {
-      const f32x4 lo = *reinterpret_cast<const f32x4*>(p), hi = *reinterpret_cast<const f32x4*>(p + 4);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) { v[i] += lo[i]; v[4 + i] += hi[i]; }
+    f32x4 lo{0.0f, 0.0f, 0.0f, 0.0f}, hi = lo;
+    if (e < total) {
+      const float* p = a.part + row * a.ldp + col + part * a.slab;
+#pragma unroll 4
+      for (int s = part; s < splits; s += P, p += P * a.slab) {
+        lo += *reinterpret_cast<const f32x4*>(p);
+        hi += *reinterpret_cast<const f32x4*>(p + 4);
+      }
     }
+    if constexpr (P > 1) {
+      __syncthreads();
+      meet[threadIdx.x] = lo;
+      meet[256 + threadIdx.x] = hi;
+      __syncthreads();
+      if (part) continue;
+#pragma unroll
+      for (int k = 1; k < P; ++k) {
+        lo += meet[k * GROUPS + which];
+        hi += meet[256 + k * GROUPS + which];
+      }
+    }
+    if (e >= total) continue;
+    float v[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
     const int c = n - col < 8 ? n - col : 8;
     if constexpr (FULL) {
       float b[8];
@@ -73,12 +113,12 @@ __global__ __launch_bounds__(256) void k_join(StoreArgs a, int splits, int m, in
 }
 
 hipError_t launch_join(const StoreArgs& a, int splits, int m, int n, bool full, const float* live, hipStream_t st) {
-  const int64_t want = ceil_div((int64_t)m * ((n + 7) / 8), 256);
+  const int p = splits >= 32 ? 16 : splits >= 8 ? 4 : 1;
+  const int64_t want = ceil_div((int64_t)m * ((n + 7) / 8), 256 / p);
   const dim3 grid((unsigned)(want < 8192 ? want : 8192));
-  if (full)
-    hipLaunchKernelGGL(k_join<true>, grid, dim3(256), 0, st, a, splits, m, n, live);
-  else
-    hipLaunchKernelGGL(k_join<false>, grid, dim3(256), 0, st, a, splits, m, n, live);
+  auto go = [&](auto fn) { hipLaunchKernelGGL(fn, grid, dim3(256), 0, st, a, splits, m, n, live); };
+  if (full) p == 16 ? go(k_join<true, 16>) : p == 4 ? go(k_join<true, 4>) : go(k_join<true, 1>);
+  else p == 16 ? go(k_join<false, 16>) : p == 4 ? go(k_join<false, 4>) : go(k_join<false, 1>);
   return hipGetLastError();
 }
 

@@ -69,6 +69,29 @@ __device__ __forceinline__ void store8(const MatDev& m, int64_t row, int col, in
     }
 }
 
+// Element (row, col + i) = v[i], i < min(n, 4).
+__device__ __forceinline__ void store4(const MatDev& m, int64_t row, int col, int n, const float v[4]) {
+  const int64_t at = row * m.ld + col;
+  if (m.vec && n >= 4) {
+    if (m.dtype == 0) {
+      *reinterpret_cast<f32x4*>((float*)m.data + at) = f32x4{v[0], v[1], v[2], v[3]};
+    } else if (m.dtype == 1) {
+      *reinterpret_cast<bf16x4*>((bf16*)m.data + at) = bf16x4{(bf16)v[0], (bf16)v[1], (bf16)v[2], (bf16)v[3]};
+    } else {
+      typedef f16 f16x4v __attribute__((ext_vector_type(4)));
+      *reinterpret_cast<f16x4v*>((f16*)m.data + at) = f16x4v{(f16)v[0], (f16)v[1], (f16)v[2], (f16)v[3]};
+    }
+    return;
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    if (i < n) {
+      if (m.dtype == 0) ((float*)m.data)[at + i] = v[i];
+      else if (m.dtype == 1) ((bf16*)m.data)[at + i] = (bf16)v[i];
+      else ((f16*)m.data)[at + i] = (f16)v[i];
+    }
+}
+
 // ---- activations ------------------------------------------------------------------
 // The normal distribution function Phi(a) and its density, from e^(-a^2/2) and a polynomial in
 // 1 / (1 + p |a| / sqrt 2) (Abramowitz and Stegun 7.1.26, off by 0.75e-7 at most, one and a quarter steps of fp32 at 1):

@@ -2,8 +2,6 @@
 // products share, and operands that are laid out anew where the caller's rows are out of line.
 #pragma once
 
-#include <atomic>
-
 #include "rows_dev.h"
 #include "tile_product.h"
 
@@ -33,13 +31,16 @@ inline TpPlan tp_plan(int dtype, int m, int n, int64_t k, int max_splits) {
   j.n = n;
   j.k = k;
   const int64_t large = ceil_div(m, 256) * ceil_div(n, 256), medium = ceil_div(m, 128) * ceil_div(n, 128);
-  p.shape = m <= 32 ? TP_FEW : large >= 192 ? TP_LARGE : medium >= 192 ? TP_MEDIUM : TP_SMALL;
+  // (large tiles, too, where few of them have so long a k that their slabs cost less than they gain)
+  const bool split_large = large >= 48 && large < 192 && max_splits > 1 && k * large >= 8192ll * 256;
+  p.shape = m <= 32 ? TP_FEW : large >= 192 || split_large ? TP_LARGE : medium >= 192 ? TP_MEDIUM : TP_SMALL;
   j.tiles_m = (int)ceil_div(m, TP_BM[p.shape]);
   j.tiles_n = (int)ceil_div(n, TP_BN[p.shape]);
   const int kb = TP_STEP / elem_size(dtype);
   const int64_t steps = ceil_div(k, kb), tiles = (int64_t)j.tiles_m * j.tiles_n;
   int64_t s = 1;
-  if (p.shape != TP_LARGE && tiles < 256) s = 512 / tiles;
+  if (split_large) s = 256 / tiles;
+  else if (p.shape != TP_LARGE && tiles <= 256) s = 512 / tiles;
   s = s < steps / 2 ? s : steps / 2;
   s = s < max_splits ? s : max_splits;
   if (s < 1) s = 1;
@@ -50,21 +51,17 @@ inline TpPlan tp_plan(int dtype, int m, int n, int64_t k, int max_splits) {
   return p;
 }
 
+// Lets a kernel have `lds` bytes of dynamic LDS on the current device.
+hipError_t tp_allow_lds(const void* fn, int lds);
+
 template <typename T, bool AK, bool BK, class S, class Epi>
 hipError_t tp_launch_shape(const TpJob& j, const typename Epi::Args& ea, hipStream_t st) {
   constexpr int loop = S::NBUF * S::BUF, out = Epi::BLOCKS * S::WAVES * S::OUT;
   constexpr int lds = (loop > out ? loop : out) + Epi::TAIL;
   static_assert(lds <= 160 * 1024, "LDS of a compute unit");
   const auto fn = k_tile_product<T, AK, BK, S, Epi>;
-  static std::atomic<uint64_t> done{0};  // a bit per device
-  int dev = 0;
-  hipError_t e = hipGetDevice(&dev);
+  const hipError_t e = tp_allow_lds((const void*)fn, lds);
   if (e != hipSuccess) return e;
-  if (dev > 63 || !(done.load() >> dev & 1)) {
-    e = hipFuncSetAttribute((const void*)fn, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
-    if (e != hipSuccess) return e;
-    if (dev < 64) done |= 1ull << dev;
-  }
   hipLaunchKernelGGL(fn, dim3(tp_blocks(j)), dim3(S::THREADS), lds, st, j, ea);
   return hipGetLastError();
 }

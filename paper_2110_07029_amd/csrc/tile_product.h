@@ -69,6 +69,11 @@ __device__ __forceinline__ void tp_copy16(i32x4 rsrc, unsigned voff, unsigned ld
   asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds" ::"v"(voff), "s"(rsrc), "s"(lds)
                : "memory");
 }
+// The same with 4 bytes a lane.
+__device__ __forceinline__ void tp_copy4(i32x4 rsrc, unsigned voff, unsigned lds) {
+  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tbuffer_load_dword %0, %1, 0 offen lds" ::"v"(voff), "s"(rsrc), "s"(lds)
+               : "memory");
+}
 template <int N>
 __device__ __forceinline__ void tp_wait() {
   asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(N) : "memory");
@@ -137,7 +142,11 @@ struct TpLoad {
 };
 
 // ---- fragments -----------------------------------------------------------------------
-typedef __attribute__((address_space(3))) f16x4 lds_f16x4;
+// A transposing read of 16-bit elements (lds_read_tr16).
+template <typename T>
+__device__ __forceinline__ typename TpMma<T>::frag4 tp_turned(const char* p) {
+  return __builtin_bit_cast(typename TpMma<T>::frag4, lds_read_tr16(reinterpret_cast<const bf16*>(p)));
+}
 
 // Fragment of block row-base r0 (a multiple of 32), k chunk kk (of four) of the tile at `p`.
 template <typename T, bool KROWS, int R>
@@ -159,15 +168,9 @@ __device__ __forceinline__ typename std::conditional<sizeof(T) == 2, typename Tp
       const int k = 16 * kk + 8 * (G >> 1) + 4 * hi + i;
       const int u = (r0 >> 5) ^ (i & (R / 32 - 1));
       const char* q = p + k * (R * 2) + u * 64 + 32 * (G & 1) + 8 * a;
-      if constexpr (std::is_same<T, bf16>::value) {
-        const bf16x4 v = lds_read_tr16(reinterpret_cast<const bf16*>(q));
+      const typename TpMma<T>::frag4 v = tp_turned<T>(q);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) f[4 * hi + j] = v[j];
-      } else {
-        const f16x4 v = __builtin_bit_cast(f16x4, lds_read_tr16(reinterpret_cast<const bf16*>(q)));
-#pragma unroll
-        for (int j = 0; j < 4; ++j) f[4 * hi + j] = v[j];
-      }
+      for (int j = 0; j < 4; ++j) f[4 * hi + j] = v[j];
     }
     return f;
   } else {
