@@ -6,16 +6,14 @@
 //   dz_ij = weight_i (e^(z_ij - lse_i) - c_ij / n_i), c_ij how often j stands in the list
 //   dh = dz W ; dw = dz^T h ; db = 1^T dz
 //
-//   k_loss_prep   n_i; for gradients a copy of h in which rows without labels are zeros (what they hold
-//                 must not reach dw)
 //   product 1     z in tiles; per row and tile the maximum and the sum of exponentials
-//   k_loss_rows   lse; the target logits as products of their own; loss; the largest |weight|
+//   k_loss_rows   n_i; lse; the target logits as products of their own; loss; for gradients the largest |weight| and a
+//                 copy of h in which rows without labels are zeros (what they hold must not reach dw)
 //   per piece of labels:
 //     product 2   z again, dz formed in fp32 from it, the targets taken off in place; its column sums
 //                 for db in fp32; dz rounded to the operands' type in the workspace
-//     product 3   dz W onto slabs of dh
-//     product 4   dz^T h: the piece's rows of dw
-//   k_join, k_column_sums   dh and db
+//     products 3, 4   dz W onto slabs of dh, dz^T h: the piece's rows of dw; column sums for db
+//   k_join        dh
 //
 // Forming z twice costs 2 B L D operations of 8; a piece's dz stays near the last caches.  dz in 16 bits is
 // rounded once, with the target in it (p and the target may nearly cancel); fp16 holds it times 2^15 over the
@@ -39,37 +37,6 @@ __device__ __forceinline__ int entry(const IdLists& y, int q, int L) {
 }
 
 }  // namespace
-
-// ---- rows before the products ------------------------------------------------------------------
-// One wave per row: share[i] = 1 / n_i, 0 without entries; hp: the row, or zeros.
-template <typename T>
-__global__ __launch_bounds__(256) void k_loss_prep(MatDev h, IdLists y, int B, int L, int D, float* __restrict__ share,
-                                                   T* __restrict__ hp, int64_t ldp) {
-  constexpr int V = 16 / (int)sizeof(T);
-  typedef T vec __attribute__((ext_vector_type(V)));
-  const int lane = threadIdx.x & 63, i = blockIdx.x * 4 + (threadIdx.x >> 6);
-  if (i >= B) return;
-  int q0 = 0, q1 = 0, n = 0;
-  if (y.indptr) label_range(y, i, &q0, &q1);
-  for (int q = q0 + lane; q < q1; q += 64) n += entry(y, q, L) >= 0;
-#pragma unroll
-  for (int o = 32; o; o >>= 1) n += __shfl_xor(n, o);
-  if (lane == 0) share[i] = n ? 1.0f / (float)n : 0.0f;
-  if (!hp) return;
-  const T* src = (const T*)h.data + (int64_t)i * h.ld;
-  T* dst = hp + i * ldp;
-  for (int64_t c = V * lane; c < ldp; c += V * 64) {
-    vec v;
-    if (h.vec && c + V <= D) {
-      v = *reinterpret_cast<const vec*>(src + c);
-    } else {
-#pragma unroll
-      for (int k = 0; k < V; ++k) v[k] = c + k < D ? src[c + k] : (T)0.0f;
-    }
-    if (!n) v = vec{};
-    *reinterpret_cast<vec*>(dst + c) = v;
-  }
-}
 
 // ---- product 1 -------------------------------------------------------------------------------------
 struct LseArgs {
@@ -150,19 +117,25 @@ struct EpiLse {
 template <typename T>
 __global__ __launch_bounds__(256) void k_loss_rows(const float2* __restrict__ part, int tiles, TpOperand h, TpOperand w,
                                                    int D, int L, const float* __restrict__ bias, IdLists y,
-                                                   const float* __restrict__ share, float* __restrict__ lse_ws,
+                                                   float* __restrict__ share, float* __restrict__ lse_ws,
                                                    float* __restrict__ lse_out, float* __restrict__ loss, int B,
-                                                   const float* __restrict__ weights, float* __restrict__ scale) {
+                                                   const float* __restrict__ weights, float* __restrict__ scale,
+                                                   T* __restrict__ hp, int64_t ldp) {
   constexpr int V = 16 / (int)sizeof(T);
   typedef T vec __attribute__((ext_vector_type(V)));
   const int i = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   __shared__ float sm[4], ss[4], st[4];
+  __shared__ int sn[4];
   if (i == B) {
     float v = 0.0f;
     if (weights)
       for (int r = tid; r < B; r += 256) {
         const float a = fabsf(weights[r]);
-        if (share[r] > 0.0f && a < INFINITY) v = fmaxf(v, a);
+        if (!(a < INFINITY) || !y.indptr) continue;
+        int q0, q1;
+        label_range(y, r, &q0, &q1);
+        while (q0 < q1 && entry(y, q0, L) < 0) ++q0;
+        if (q0 < q1) v = fmaxf(v, a);
       }
     v = wave_max(v);
     if (lane == 0) sm[wave] = v;
@@ -174,15 +147,16 @@ __global__ __launch_bounds__(256) void k_loss_rows(const float2* __restrict__ pa
   float top = -INFINITY;
   for (int k = tid; k < tiles; k += 256) top = fmaxf(top, p[k].x);
   float t = 0.0f;
-  const float sh = share[i];
-  if (sh > 0.0f) {
+  int n = 0;
+  const T* hr = (const T*)(h.base + i * h.ld);
+  if (y.indptr) {
     int q0, q1;
     label_range(y, i, &q0, &q1);
-    const T* hr = (const T*)(h.base + i * h.ld);
     const int l = tid & 15;
     for (int q = q0 + (tid >> 4); q < q1; q += 16) {
       const int id = entry(y, q, L);
       if (id < 0) continue;
+      n += l == 0;
       const T* wr = (const T*)(w.base + id * w.ld);
       float d = 0.0f;
       for (int c = V * l; c < D; c += V * 16) {
@@ -195,11 +169,18 @@ __global__ __launch_bounds__(256) void k_loss_rows(const float2* __restrict__ pa
   }
   t = wave_sum(t);
   top = wave_max(top);
+#pragma unroll
+  for (int o = 32; o; o >>= 1) n += __shfl_xor(n, o);
   if (lane == 0) {
     sm[wave] = top;
     st[wave] = t;
+    sn[wave] = n;
   }
   __syncthreads();
+  n = sn[0] + sn[1] + sn[2] + sn[3];
+  if (hp)
+    for (int64_t c = V * tid; c < ldp; c += V * 256)
+      *reinterpret_cast<vec*>(hp + i * ldp + c) = n ? *reinterpret_cast<const vec*>(hr + c) : vec{};
   top = fmaxf(fmaxf(sm[0], sm[1]), fmaxf(sm[2], sm[3]));
   const float base = top == -INFINITY ? 0.0f : top;
   float s = 0.0f;
@@ -210,10 +191,11 @@ __global__ __launch_bounds__(256) void k_loss_rows(const float2* __restrict__ pa
   if (tid == 0) {
     s = ss[0] + ss[1] + ss[2] + ss[3];
     t = st[0] + st[1] + st[2] + st[3];
-    const float lse = top + logf(s);
+    const float lse = top + logf(s), sh = n ? 1.0f / (float)n : 0.0f;
+    share[i] = sh;
     lse_ws[i] = lse;
     if (lse_out) lse_out[i] = lse;
-    loss[i] = sh > 0.0f ? lse - t * sh : 0.0f;
+    loss[i] = n ? lse - t * sh : 0.0f;
   }
 }
 
@@ -365,7 +347,7 @@ struct EpiDzT {
     __syncthreads();
     float* s = reinterpret_cast<float*>(hits);  // [WM][BN]
     static_assert(S::WM * S::BN * 4 <= TAIL, "column sums");
-    for (int c = lane; c < S::WCOLS; c += 64) {
+    for (int c = lane; c < S::WCOLS && wave < S::WM * S::WN; c += 64) {
       float t = 0.0f;
 #pragma unroll 8
       for (int r = 0; r < 32; ++r) t += mine[r * S::OUT_LD + c];
@@ -454,30 +436,30 @@ hipError_t run(const LossJob& j, char* ws, hipStream_t st) {
   float* scale = grads ? (float*)take(s.scale) : nullptr;
   const int64_t ldp = tp_packed_cols(dt, D);
   hipError_t e;
-  hipLaunchKernelGGL(k_loss_prep<T>, dim3((unsigned)ceil_div(B, 4)), dim3(256), 0, st, j.h, j.y, B, L, D, share,
-                     s.hp ? (T*)hp : (T*)nullptr, ldp);
-  if ((e = hipGetLastError()) != hipSuccess) return e;
-  TpOperand h = tp_operand(dt, j.h.data, j.h.ld, B, D);
+  // operands in place, or laid out anew
+  TpOperand h = tp_operand(dt, j.h.data, j.h.ld, B, D), w = tp_operand(dt, j.w.data, j.w.ld, L, D);
   const TpOperand hz = tp_operand(dt, hp, ldp, B, ldp);  // (zeros in rows without labels: for the gradients alone)
+  int64_t ldw = j.w.ld;
+  PackJob jobs[2];
+  int packs = 0;
   if (s.hq) {
     char* hq = take(s.hq);
-    if ((e = launch_pack(dt, j.h, B, D, hq, st)) != hipSuccess) return e;
     h = tp_operand(dt, hq, ldp, B, ldp);
+    jobs[packs++] = PackJob{j.h.data, j.h.ld, B, D, hq};
   }
-  TpOperand w = tp_operand(dt, j.w.data, j.w.ld, L, D);
-  int64_t ldw = j.w.ld;
   if (s.wp) {
-    if ((e = launch_pack(dt, j.w, L, D, wp, st)) != hipSuccess) return e;
     w = tp_operand(dt, wp, ldp, L, ldp);
     ldw = ldp;
+    jobs[packs++] = PackJob{j.w.data, j.w.ld, L, D, wp};
   }
+  if (packs && (e = launch_pack(dt, jobs, packs, st)) != hipSuccess) return e;
   s.fwd.job.a = h;
   s.fwd.job.b = w;
   e = s.narrow ? launch_narrow_lse(dt, s.nl, h, w, j.bias, B, L, D, part, st)
                : tp_launch<T, true, true, EpiLse>(s.fwd, LseArgs{j.bias, part}, st);
   if (e != hipSuccess) return e;
   hipLaunchKernelGGL(k_loss_rows<T>, dim3(B + (scale ? 1 : 0)), dim3(256), 0, st, part, s.parts, h, w, D, L, j.bias, j.y,
-                     share, lse, j.lse, j.loss_rows, B, j.weights, scale);
+                     share, lse, j.lse, j.loss_rows, B, j.weights, scale, s.hp ? (T*)hp : (T*)nullptr, ldp);
   if ((e = hipGetLastError()) != hipSuccess) return e;
   if (!grads) return hipSuccess;
 
@@ -486,6 +468,7 @@ hipError_t run(const LossJob& j, char* ws, hipStream_t st) {
   da.epi.y = j.dh;
   da.alpha = 1.0f / up;
   da.alpha_dev = scale;
+  da.live = share;
   if (s.narrow_grad) {
     float* slabs = j.dh.data ? (float*)take(s.slabs) : nullptr;
     const DzArgs za{j.bias, lse, share, j.weights, scale, up, nullptr, 0, nullptr, j.y, 0, L};
@@ -494,7 +477,7 @@ hipError_t run(const LossJob& j, char* ws, hipStream_t st) {
     da.part = slabs;
     da.ldp = 128;
     da.slab = 128ll * B;
-    return launch_join(da, s.ng.ranges, B, D, false, share, st);
+    return launch_join(da, s.ng.ranges, B, D, false, st);
   }
   char* dz = take(s.dzb);
   float* dbp = (float*)take(s.dbp);
@@ -502,6 +485,8 @@ hipError_t run(const LossJob& j, char* ws, hipStream_t st) {
   da.part = slabs;
   da.ldp = ceil_div(D, 8) * 8;
   da.slab = da.ldp * B;
+  // One piece and one split: whole sums, straight into dh (rows without labels are zeros in dz).
+  if (s.piece >= L && s.dh.job.splits == 1) da.part = nullptr;
   int splits = 0;
   for (int64_t l0 = 0; l0 < L; l0 += s.piece) {
     const int n = (int)(L - l0 < s.piece ? L - l0 : s.piece);
@@ -513,31 +498,33 @@ hipError_t run(const LossJob& j, char* ws, hipStream_t st) {
     const DzArgs za{j.bias ? j.bias + l0 : nullptr, lse, share, j.weights, scale, up, dz, s.ldz, j.db ? dbp : nullptr, j.y,
                     (int)l0, L};
     if ((e = tp_launch<T, true, true, EpiDz>(p, za, st)) != hipSuccess) return e;
-    if (j.db && (e = launch_column_sums(dbp, p.job.tiles_m, s.ldz, n, 1.0f / up, scale, j.db + l0, st)) != hipSuccess) return e;
+    PairJob pair{};
+    if (j.db) pair.sums = SumJob{dbp, p.job.tiles_m, s.ldz, n, 1.0f / up, scale, j.db + l0};
     if (j.dh.data) {
-      TpPlan q = s.dh;
-      q.job.k = n;
-      q.job.a = tp_operand(dt, dz, s.ldz, B, ceil_div(n, 8) * 8);
-      q.job.b = wl;
-      da.add = l0 > 0;
+      pair.x = s.dh;
+      TpJob& q = pair.x.job;
+      q.k = n;
+      q.a = tp_operand(dt, dz, s.ldz, B, ceil_div(n, 8) * 8);
+      q.b = wl;
       // (the first piece is the longest, so every slab of it is written)
-      q.job.splits = (int)ceil_div(n, q.job.split_k);
-      if (!splits) splits = q.job.splits;
-      if ((e = launch_plain(dt, true, q, da, st)) != hipSuccess) return e;
+      q.splits = (int)ceil_div(n, q.split_k);
+      if (!splits) splits = q.splits;
+      da.add = l0 > 0;
+      da.keep = 1;
+      pair.ax = da;
     }
     if (j.dw.data) {
-      TpPlan q = tp_plan(dt, n, D, B, 1);
-      q.job.a = tp_operand(dt, dz, s.ldz, B, ceil_div(n, 8) * 8);
-      q.job.b = hz;
-      StoreArgs wa{};
-      wa.epi.y = j.dw;
-      wa.epi.y.data = (char*)j.dw.data + l0 * j.dw.ld * elem_size(j.dw.dtype);
-      wa.alpha = 1.0f / up;
-      wa.alpha_dev = scale;
-      if ((e = launch_plain(dt, false, q, wa, st)) != hipSuccess) return e;
+      pair.y = tp_plan(dt, n, D, B, 1);
+      pair.y.job.a = tp_operand(dt, dz, s.ldz, B, ceil_div(n, 8) * 8);
+      pair.y.job.b = hz;
+      pair.ay.epi.y = j.dw;
+      pair.ay.epi.y.data = (char*)j.dw.data + l0 * j.dw.ld * elem_size(j.dw.dtype);
+      pair.ay.alpha = 1.0f / up;
+      pair.ay.alpha_dev = scale;
     }
+    if ((e = launch_pair(dt, pair, st)) != hipSuccess) return e;
   }
-  if (j.dh.data) return launch_join(da, splits, B, D, false, share, st);
+  if (da.part && j.dh.data) return launch_join(da, splits, B, D, false, st);
   return hipSuccess;
 }
 

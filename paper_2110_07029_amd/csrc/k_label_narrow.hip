@@ -234,7 +234,7 @@ __global__ __launch_bounds__(NW_THREADS) void k_narrow_grad(TpOperand h, TpOpera
   float sh = 0.0f, lse = 0.0f, f = 0.0f;
   if (row < B) {
     sh = a.share[row];
-    lse = a.lse[row];
+    lse = a.lse[row] * LOG2E;  // base 2; its rounding is of the size of lse's own
     f = (a.weights ? scale > 0.0f ? a.weights[row] / scale : a.weights[row] : 1.0f) * a.up;
   }
   const bool live = sh > 0.0f;
@@ -329,7 +329,7 @@ __global__ __launch_bounds__(NW_THREADS) void k_narrow_grad(TpOperand h, TpOpera
         char* const at = dzt + nw_dz(row, 8 * b + 2 * q + g);
         float v[4];
 #pragma unroll
-        for (int k = 0; k < 4; ++k) v[k] = exp_fast(z[b][4 * q + k] - lse);
+        for (int k = 0; k < 4; ++k) v[k] = __builtin_amdgcn_exp2f(fmaf(z[b][4 * q + k], LOG2E, -lse));
         if (any) {
           const uint64_t times = *reinterpret_cast<const uint64_t*>(at);
 #pragma unroll

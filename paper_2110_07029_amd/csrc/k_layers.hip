@@ -35,30 +35,44 @@ hipError_t tp_allow_lds(const void* fn, int lds) {
 }
 
 // ---- rows out of line -----------------------------------------------------------------
+struct PackJobs {
+  PackJob j[2];
+};
+// One or two matrices, side by side in the grid's y.
 template <typename T>
-__global__ __launch_bounds__(256) void k_pack(const T* __restrict__ src, int64_t ld, int64_t rows, int cols,
-                                              T* __restrict__ dst, int64_t ldp) {
+__global__ __launch_bounds__(256) void k_pack(PackJobs jobs) {
   constexpr int V = 16 / (int)sizeof(T);
   typedef T vec __attribute__((ext_vector_type(V)));
-  const int64_t per_row = ldp / V, total = rows * per_row;
+  const PackJob& j = jobs.j[blockIdx.y];
+  const int64_t per_row = (j.cols + V - 1) / V, total = j.rows * per_row;
   for (int64_t e = blockIdx.x * 256ll + threadIdx.x; e < total; e += 256ll * gridDim.x) {
     const int64_t r = e / per_row;
     const int c = (int)(e % per_row) * V;
+    const T* src = (const T*)j.src + r * j.ld + c;
     vec v;
+    if (c + V <= j.cols && ((uintptr_t)src & 15) == 0) {
+      v = *reinterpret_cast<const vec*>(src);
+    } else {
 #pragma unroll
-    for (int i = 0; i < V; ++i) v[i] = c + i < cols ? src[r * ld + c + i] : (T)0.0f;
-    *reinterpret_cast<vec*>(dst + r * ldp + c) = v;
+      for (int i = 0; i < V; ++i) v[i] = c + i < j.cols ? src[i] : (T)0.0f;
+    }
+    reinterpret_cast<vec*>(j.dst)[e] = v;
   }
 }
 
-hipError_t launch_pack(int dtype, const MatDev& src, int64_t rows, int cols, void* dst, hipStream_t st) {
-  const int64_t ldp = tp_packed_cols(dtype, cols), chunks = rows * ldp * elem_size(dtype) / 16;
-  const int64_t want = ceil_div(chunks, 256);
-  const dim3 grid((unsigned)(want < 4096 ? want : 4096));
+hipError_t launch_pack(int dtype, const PackJob* jobs, int n, hipStream_t st) {
+  PackJobs p{};
+  int64_t want = 1;
+  for (int i = 0; i < n; ++i) {
+    p.j[i] = jobs[i];
+    const int64_t w = ceil_div(jobs[i].rows * tp_packed_cols(dtype, jobs[i].cols) * elem_size(dtype) / 16, 256);
+    if (w > want) want = w;
+  }
+  const dim3 grid((unsigned)(want < 4096 ? want : 4096), n);
   if (dtype == 0)
-    hipLaunchKernelGGL(k_pack<float>, grid, dim3(256), 0, st, (const float*)src.data, src.ld, rows, cols, (float*)dst, ldp);
+    hipLaunchKernelGGL(k_pack<float>, grid, dim3(256), 0, st, p);
   else  // (16 bits are 16 bits)
-    hipLaunchKernelGGL(k_pack<f16>, grid, dim3(256), 0, st, (const f16*)src.data, src.ld, rows, cols, (f16*)dst, ldp);
+    hipLaunchKernelGGL(k_pack<f16>, grid, dim3(256), 0, st, p);
   return hipGetLastError();
 }
 
@@ -66,7 +80,7 @@ hipError_t launch_pack(int dtype, const MatDev& src, int64_t rows, int cols, voi
 // 256 / P groups of 8 columns per workgroup, P threads each, which take every P-th slab and meet in LDS (many slabs of few
 // sums: 256 slabs of 256 x 128 take 25 us with one thread per group).
 template <bool FULL, int P>
-__global__ __launch_bounds__(256) void k_join(StoreArgs a, int splits, int m, int n, const float* __restrict__ live) {
+__global__ __launch_bounds__(256) void k_join(StoreArgs a, int splits, int m, int n) {
   constexpr int GROUPS = 256 / P;
   __shared__ f32x4 meet[P > 1 ? 512 : 1];
   const int64_t per_row = (n + 7) / 8, total = m * per_row;
@@ -104,7 +118,7 @@ __global__ __launch_bounds__(256) void k_join(StoreArgs a, int splits, int m, in
       bias8(a.epi.bias, col, c, b);
       dense_out8(a.epi, b, row, col, c, v);
     } else {
-      const bool zero = live && live[row] == 0.0f;
+      const bool zero = a.live && a.live[row] == 0.0f;
 #pragma unroll
       for (int i = 0; i < 8; ++i) v[i] = zero ? 0.0f : v[i] * alpha;
       store8(a.epi.y, row, col, c, v);
@@ -112,41 +126,95 @@ __global__ __launch_bounds__(256) void k_join(StoreArgs a, int splits, int m, in
   }
 }
 
-hipError_t launch_join(const StoreArgs& a, int splits, int m, int n, bool full, const float* live, hipStream_t st) {
+hipError_t launch_join(const StoreArgs& a, int splits, int m, int n, bool full, hipStream_t st) {
   const int p = splits >= 32 ? 16 : splits >= 8 ? 4 : 1;
   const int64_t want = ceil_div((int64_t)m * ((n + 7) / 8), 256 / p);
   const dim3 grid((unsigned)(want < 8192 ? want : 8192));
-  auto go = [&](auto fn) { hipLaunchKernelGGL(fn, grid, dim3(256), 0, st, a, splits, m, n, live); };
+  auto go = [&](auto fn) { hipLaunchKernelGGL(fn, grid, dim3(256), 0, st, a, splits, m, n); };
   if (full) p == 16 ? go(k_join<true, 16>) : p == 4 ? go(k_join<true, 4>) : go(k_join<true, 1>);
   else p == 16 ? go(k_join<false, 16>) : p == 4 ? go(k_join<false, 4>) : go(k_join<false, 1>);
   return hipGetLastError();
 }
 
-// 64 columns per workgroup, sixteen waves take every sixteenth row.
-__global__ __launch_bounds__(1024) void k_column_sums(const float* __restrict__ part, int rows, int64_t ld, int n,
-                                                      float alpha, const float* alpha_dev, float* __restrict__ y) {
-  __shared__ float s[16][64];
-  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-  const int64_t col = blockIdx.x * 64ll + lane;
+// 64 columns per workgroup of 256 or more threads, whose waves take turns at the rows.
+__device__ __forceinline__ void column_sums(const SumJob& j, int block, float* s) {
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, waves = blockDim.x >> 6;
+  const int64_t col = block * 64ll + lane;
   float v = 0.0f;
-  if (col < n) {
+  if (col < j.n) {
 #pragma unroll 4
-    for (int r = w; r < rows; r += 16) v += part[r * ld + col];
+    for (int r = w; r < j.rows; r += waves) v += j.part[r * j.ld + col];
   }
-  s[w][lane] = v;
+  s[threadIdx.x] = v;
   __syncthreads();
-  if (w == 0 && col < n) {
+  if (w == 0 && col < j.n) {
     float t = 0.0f;
-#pragma unroll
-    for (int i = 0; i < 16; ++i) t += s[i][lane];
-    y[col] = t * alpha * (alpha_dev ? *alpha_dev : 1.0f);
+    for (int i = 0; i < waves; ++i) t += s[64 * i + lane];
+    j.y[col] = t * j.alpha * (j.alpha_dev ? *j.alpha_dev : 1.0f);
   }
 }
+__global__ __launch_bounds__(1024) void k_column_sums(SumJob j) {
+  __shared__ float s[1024];
+  column_sums(j, blockIdx.x, s);
+}
 
-hipError_t launch_column_sums(const float* part, int rows, int64_t ld, int n, float alpha, const float* alpha_dev,
-                              float* y, hipStream_t st) {
-  hipLaunchKernelGGL(k_column_sums, dim3((unsigned)ceil_div(n, 64)), dim3(1024), 0, st, part, rows, ld, n, alpha, alpha_dev, y);
+hipError_t launch_column_sums(const SumJob& j, hipStream_t st) {
+  if (!j.y) return hipSuccess;
+  hipLaunchKernelGGL(k_column_sums, dim3((unsigned)ceil_div(j.n, 64)), dim3(1024), 0, st, j);
   return hipGetLastError();
+}
+
+// Both products and the sums in one launch: small ones are a few microseconds each, most of it the launch.
+template <typename T, class S>
+__global__ __launch_bounds__(S::THREADS) void k_pair(TpJob jx, StoreArgs ax, int nx, TpJob jy, StoreArgs ay, int ny, SumJob sums) {
+  extern __shared__ __attribute__((aligned(16))) char smem[];
+  const int b = blockIdx.x;
+  if (b < nx)
+    tp_tile<T, true, false, S, EpiPlain<S>>(jx, ax, b, smem);
+  else if (b < nx + ny)
+    tp_tile<T, false, false, S, EpiPlain<S>>(jy, ay, b - nx, smem);
+  else
+    column_sums(sums, b - nx - ny, reinterpret_cast<float*>(smem));
+}
+
+template <typename T, class S>
+static hipError_t pair_launch(const PairJob& p, hipStream_t st) {
+  const auto fn = k_pair<T, S>;
+  constexpr int loop = S::NBUF * S::BUF, out = S::WAVES * S::OUT, lds = loop > out ? loop : out;
+  const hipError_t e = tp_allow_lds((const void*)fn, lds);
+  if (e != hipSuccess) return e;
+  const int nx = p.x.job.a.base ? tp_blocks(p.x.job) : 0, ny = p.y.job.a.base ? tp_blocks(p.y.job) : 0;
+  const int ns = p.sums.y ? (int)ceil_div(p.sums.n, 64) : 0;
+  hipLaunchKernelGGL(fn, dim3(nx + ny + ns), dim3(S::THREADS), lds, st, p.x.job, p.ax, nx, p.y.job, p.ay, ny, p.sums);
+  return hipGetLastError();
+}
+template <class S>
+static hipError_t pair_type(int dtype, const PairJob& p, hipStream_t st) {
+  if (dtype == 0) return pair_launch<float, S>(p, st);
+  if (dtype == 1) return pair_launch<bf16, S>(p, st);
+  return pair_launch<f16, S>(p, st);
+}
+
+hipError_t launch_pair(int dtype, const PairJob& p, hipStream_t st) {
+  const bool x = p.x.job.a.base, y = p.y.job.a.base;
+  hipError_t e = hipSuccess;
+  if (x + y + (p.sums.y != nullptr) > 1 && (!x || !y || p.x.shape == p.y.shape) &&
+      (x ? p.x : p.y).shape == TP_TINY) {
+    e = pair_type<TpTiny>(dtype, p, st);
+  } else if (x + y + (p.sums.y != nullptr) > 1 && (!x || !y || p.x.shape == p.y.shape) &&
+             (x ? p.x : p.y).shape == TP_SMALL) {
+    e = pair_type<TpSmall>(dtype, p, st);
+  } else {
+    e = launch_column_sums(p.sums, st);
+    if (e == hipSuccess && x) e = launch_plain(dtype, true, p.x, p.ax, st);
+    if (e == hipSuccess && y) e = launch_plain(dtype, false, p.y, p.ay, st);
+  }
+  // (slabs that were added to are joined by the caller when all of them are there)
+  if (e == hipSuccess && x && p.ax.part && !p.ax.keep)
+    e = launch_join(p.ax, p.x.job.splits, p.x.job.m, p.x.job.n, false, st);
+  if (e == hipSuccess && y && p.ay.part && !p.ay.keep)
+    e = launch_join(p.ay, p.y.job.splits, p.y.job.m, p.y.job.n, false, st);
+  return e;
 }
 
 // ---- forward ------------------------------------------------------------------------------
@@ -167,16 +235,22 @@ struct Carve {  // places in the workspace, in order
   }
 };
 
-// `a` in place, or laid out anew in the workspace.
-hipError_t operand(int dtype, const MatDev& a, int64_t rows, int cols, Carve* c, hipStream_t st, TpOperand* out) {
-  if (tp_in_place(dtype, a, cols)) {
-    *out = tp_operand(dtype, a.data, a.ld, rows, cols);
-    return hipSuccess;
+// Operands in place, or laid out anew in the workspace (both in one launch).
+hipError_t operands(int dtype, const MatDev* const* a, const int64_t* rows, int cols, int n, Carve* c, TpOperand* out,
+                    hipStream_t st) {
+  PackJob jobs[2];
+  int packs = 0;
+  for (int i = 0; i < n; ++i) {
+    if (tp_in_place(dtype, *a[i], cols)) {
+      out[i] = tp_operand(dtype, a[i]->data, a[i]->ld, rows[i], cols);
+      continue;
+    }
+    void* p = c->take(tp_packed_bytes(dtype, rows[i], cols));
+    const int64_t ldp = tp_packed_cols(dtype, cols);
+    out[i] = tp_operand(dtype, p, ldp, rows[i], ldp);
+    jobs[packs++] = PackJob{a[i]->data, a[i]->ld, rows[i], cols, p};
   }
-  void* p = c->take(tp_packed_bytes(dtype, rows, cols));
-  const int64_t ldp = tp_packed_cols(dtype, cols);
-  *out = tp_operand(dtype, p, ldp, rows, ldp);
-  return launch_pack(dtype, a, rows, cols, p, st);
+  return packs ? launch_pack(dtype, jobs, packs, st) : hipSuccess;
 }
 size_t operand_bytes(int dtype, const MatDev& a, int64_t rows, int cols) {
   return tp_in_place(dtype, a, cols) ? 0 : tp_packed_bytes(dtype, rows, cols);
@@ -189,22 +263,12 @@ hipError_t any_type(int dtype, const TpPlan& p, const StoreArgs& a, hipStream_t 
   return tp_launch<f16, AK, BK, Epi>(p, a, st);
 }
 
-// C = A B^T through the epilogue, by way of slabs where k is split.
-enum { DENSE, KROWS, KCOLS };
-hipError_t product(int dtype, int kind, TpPlan p, const TpOperand& x, const TpOperand& y, StoreArgs a, Carve c,
-                   hipStream_t st) {
-  p.job.a = x;
-  p.job.b = y;
-  a.part = nullptr;
-  if (p.job.splits > 1) {
-    a.ldp = ceil_div(p.job.n, 8) * 8;
-    a.slab = a.ldp * p.job.m;
-    a.part = (float*)c.take(slab_bytes(p));
-  }
-  const hipError_t e =
-      kind == DENSE ? any_type<EpiDense, true, true>(dtype, p, a, st) : launch_plain(dtype, kind == KROWS, p, a, st);
-  if (e != hipSuccess || p.job.splits == 1) return e;
-  return launch_join(a, p.job.splits, p.job.m, p.job.n, kind == DENSE, nullptr, st);
+// Slabs for the splits of a product.
+void take_slabs(const TpPlan& p, StoreArgs* a, Carve* c) {
+  if (p.job.splits < 2) return;
+  a->ldp = ceil_div(p.job.n, 8) * 8;
+  a->slab = a->ldp * p.job.m;
+  a->part = (float*)c->take(slab_bytes(p));
 }
 
 }  // namespace
@@ -219,13 +283,20 @@ size_t dense_ws_bytes(int dtype, const MatDev& x, const MatDev& w, int m, int n,
 
 hipError_t launch_dense(const DenseJob& j, void* ws, hipStream_t st) {
   Carve c{(char*)ws};
-  TpOperand x, w;
-  hipError_t e = operand(j.dtype, j.x, j.m, j.k, &c, st, &x);
-  if (e == hipSuccess) e = operand(j.dtype, j.w, j.n, j.k, &c, st, &w);
+  const MatDev* const mats[] = {&j.x, &j.w};
+  const int64_t rows[] = {j.m, j.n};
+  TpOperand o[2];
+  hipError_t e = operands(j.dtype, mats, rows, j.k, 2, &c, o, st);
   if (e != hipSuccess) return e;
   StoreArgs a{};
   a.epi = j.epi;
-  return product(j.dtype, DENSE, tp_plan(j.dtype, j.m, j.n, j.k, MAX_SPLITS), x, w, a, c, st);
+  TpPlan p = tp_plan(j.dtype, j.m, j.n, j.k, MAX_SPLITS);
+  p.job.a = o[0];
+  p.job.b = o[1];
+  take_slabs(p, &a, &c);
+  e = any_type<EpiDense, true, true>(j.dtype, p, a, st);
+  if (e != hipSuccess || !a.part) return e;
+  return launch_join(a, p.job.splits, j.m, j.n, true, st);
 }
 
 // ---- backward ------------------------------------------------------------------------------
@@ -289,22 +360,25 @@ __global__ __launch_bounds__(256) void k_dense_da(DaArgs a, T* __restrict__ da, 
 
 namespace {
 
-int da_rows_wg(int m) {
-  const int64_t r = ceil_div(m, 128);
-  return (int)(r < 32 ? 32 : r);
+// Rows per workgroup: some 1,024 workgroups, sums of 512 row blocks at most.
+int da_rows_wg(int m, int n) {
+  const int64_t cols = ceil_div(n, 512), blocks = ceil_div(1024, cols) < 512 ? ceil_div(1024, cols) : 512;
+  const int64_t r = ceil_div(m, blocks);
+  return (int)(r < 16 ? 16 : r);
 }
 
 }  // namespace
 
 size_t dense_grad_ws_bytes(int dtype, const MatDev& x, const MatDev& w, int m, int n, int k) {
-  const size_t da = tp_packed_bytes(dtype, m, n), part = round256(ceil_div(m, da_rows_wg(m)) * (size_t)n * 4);
+  const size_t da = tp_packed_bytes(dtype, m, n), part = round256(ceil_div(m, da_rows_wg(m, n)) * (size_t)n * 4);
   const size_t dx = slab_bytes(tp_plan(dtype, m, k, n, MAX_SPLITS)), dw = slab_bytes(tp_plan(dtype, n, k, m, MAX_SPLITS));
-  return da + part + operand_bytes(dtype, x, m, k) + operand_bytes(dtype, w, n, k) + (dx > dw ? dx : dw);
+  return da + part + operand_bytes(dtype, x, m, k) + operand_bytes(dtype, w, n, k) + dx + dw;
 }
 
 hipError_t launch_dense_grad(const DenseGradJob& j, void* ws, hipStream_t st) {
   Carve c{(char*)ws};
   hipError_t e;
+  PairJob p{};
   const int64_t ldd = tp_packed_cols(j.dtype, j.n);
   const bool products = j.dx.data || j.dw.data;
   const bool same = !j.act && !j.drop.below && j.dy.dtype == j.dtype && tp_in_place(j.dtype, j.dy, j.n);
@@ -315,7 +389,7 @@ hipError_t launch_dense_grad(const DenseGradJob& j, void* ws, hipStream_t st) {
     da = tp_operand(j.dtype, dst, ldd, j.m, ldd);
   }
   if (dst || j.db) {
-    DaArgs a{j.dy, j.pre, j.act, j.drop, j.m, j.n, da_rows_wg(j.m), 64, ldd};
+    DaArgs a{j.dy, j.pre, j.act, j.drop, j.m, j.n, da_rows_wg(j.m, j.n), 64, ldd};
     while (a.lpr > 8 && a.lpr * 4 >= j.n) a.lpr /= 2;
     const int blocks = (int)ceil_div(j.m, a.rows_wg);
     float* part = j.db ? (float*)c.take((size_t)blocks * j.n * 4) : nullptr;
@@ -326,30 +400,33 @@ hipError_t launch_dense_grad(const DenseGradJob& j, void* ws, hipStream_t st) {
       hipLaunchKernelGGL(k_dense_da<bf16>, grid, dim3(256), 0, st, a, (bf16*)dst, part);
     else
       hipLaunchKernelGGL(k_dense_da<f16>, grid, dim3(256), 0, st, a, (f16*)dst, part);
-    e = hipGetLastError();
-    if (e == hipSuccess && j.db) e = launch_column_sums(part, blocks, j.n, j.n, 1.0f, nullptr, j.db, st);
-    if (e != hipSuccess) return e;
+    if ((e = hipGetLastError()) != hipSuccess) return e;
+    if (j.db) p.sums = SumJob{part, blocks, j.n, j.n, 1.0f, nullptr, j.db};
   }
-  StoreArgs a{};
-  a.alpha = 1.0f;
+  // x is needed for dw, w for dx
+  const MatDev* mats[2];
+  int64_t rows[2];
+  int n = 0;
+  if (j.dx.data) { mats[n] = &j.w; rows[n++] = j.n; }
+  if (j.dw.data) { mats[n] = &j.x; rows[n++] = j.m; }
+  TpOperand o[2];
+  if ((e = operands(j.dtype, mats, rows, j.k, n, &c, o, st)) != hipSuccess) return e;
+  p.ax.alpha = p.ay.alpha = 1.0f;
   if (j.dx.data) {
-    TpOperand w;
-    Carve d = c;
-    e = operand(j.dtype, j.w, j.n, j.k, &d, st, &w);
-    if (e != hipSuccess) return e;
-    a.epi.y = j.dx;
-    e = product(j.dtype, KROWS, tp_plan(j.dtype, j.m, j.k, j.n, MAX_SPLITS), da, w, a, d, st);
-    if (e != hipSuccess) return e;
+    p.x = tp_plan(j.dtype, j.m, j.k, j.n, MAX_SPLITS);
+    p.x.job.a = da;
+    p.x.job.b = o[0];
+    p.ax.epi.y = j.dx;
+    take_slabs(p.x, &p.ax, &c);
   }
   if (j.dw.data) {
-    TpOperand x;
-    Carve d = c;
-    e = operand(j.dtype, j.x, j.m, j.k, &d, st, &x);
-    if (e != hipSuccess) return e;
-    a.epi.y = j.dw;
-    return product(j.dtype, KCOLS, tp_plan(j.dtype, j.n, j.k, j.m, MAX_SPLITS), da, x, a, d, st);
+    p.y = tp_plan(j.dtype, j.n, j.k, j.m, MAX_SPLITS);
+    p.y.job.a = da;
+    p.y.job.b = o[n - 1];
+    p.ay.epi.y = j.dw;
+    take_slabs(p.y, &p.ay, &c);
   }
-  return hipSuccess;
+  return launch_pair(j.dtype, p, st);
 }
 
 // ---- dropout -----------------------------------------------------------------------------

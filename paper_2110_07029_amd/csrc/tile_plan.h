@@ -11,9 +11,10 @@ using TpLarge = TpShape<256, 256, 2, 4, 2>;
 using TpMedium = TpShape<128, 128, 2, 2, 2>;
 using TpSmall = TpShape<64, 64, 2, 2, 3>;
 using TpFew = TpShape<32, 128, 1, 4, 3>;
+using TpTiny = TpShape<32, 32, 1, 1, 8, 4>;
 
-enum { TP_LARGE = 0, TP_MEDIUM = 1, TP_SMALL = 2, TP_FEW = 3 };
-constexpr int TP_BM[] = {256, 128, 64, 32}, TP_BN[] = {256, 128, 64, 128};
+enum { TP_LARGE = 0, TP_MEDIUM = 1, TP_SMALL = 2, TP_FEW = 3, TP_TINY = 4 };
+constexpr int TP_BM[] = {256, 128, 64, 32, 32}, TP_BN[] = {256, 128, 64, 128, 32};
 
 struct TpPlan {
   int shape;
@@ -33,15 +34,21 @@ inline TpPlan tp_plan(int dtype, int m, int n, int64_t k, int max_splits) {
   const int64_t large = ceil_div(m, 256) * ceil_div(n, 256), medium = ceil_div(m, 128) * ceil_div(n, 128);
   // (large tiles, too, where few of them have so long a k that their slabs cost less than they gain)
   const bool split_large = large >= 48 && large < 192 && max_splits > 1 && k * large >= 8192ll * 256;
-  p.shape = m <= 32 ? TP_FEW : large >= 192 || split_large ? TP_LARGE : medium >= 192 ? TP_MEDIUM : TP_SMALL;
+  const int64_t small = ceil_div(m, 64) * ceil_div(n, 64);
+  p.shape = m <= 32             ? (n > 192 * 128 ? TP_FEW : TP_TINY)
+            : large >= 192 || split_large ? TP_LARGE
+            : medium >= 192     ? TP_MEDIUM
+            : small >= 128      ? TP_SMALL
+                                : TP_TINY;
   j.tiles_m = (int)ceil_div(m, TP_BM[p.shape]);
   j.tiles_n = (int)ceil_div(n, TP_BN[p.shape]);
   const int kb = TP_STEP / elem_size(dtype);
   const int64_t steps = ceil_div(k, kb), tiles = (int64_t)j.tiles_m * j.tiles_n;
+  // Splits of k cost a launch that joins them: long k of few tiles alone.
   int64_t s = 1;
   if (split_large) s = 256 / tiles;
-  else if (p.shape != TP_LARGE && tiles <= 256) s = 512 / tiles;
-  s = s < steps / 2 ? s : steps / 2;
+  else if (p.shape != TP_LARGE && tiles <= 256 && steps >= 64) s = 512 / tiles;
+  s = s < steps / 16 ? s : steps / 16;
   s = s < max_splits ? s : max_splits;
   if (s < 1) s = 1;
   const int64_t per = ceil_div(steps, s);
@@ -71,6 +78,7 @@ hipError_t tp_launch(const TpPlan& p, const typename Epi<TpLarge>::Args& ea, hip
   if (p.shape == TP_LARGE) return tp_launch_shape<T, AK, BK, TpLarge, Epi<TpLarge>>(p.job, ea, st);
   if (p.shape == TP_SMALL) return tp_launch_shape<T, AK, BK, TpSmall, Epi<TpSmall>>(p.job, ea, st);
   if (p.shape == TP_MEDIUM) return tp_launch_shape<T, AK, BK, TpMedium, Epi<TpMedium>>(p.job, ea, st);
+  if (p.shape == TP_TINY) return tp_launch_shape<T, AK, BK, TpTiny, Epi<TpTiny>>(p.job, ea, st);
   return tp_launch_shape<T, AK, BK, TpFew, Epi<TpFew>>(p.job, ea, st);
 }
 
@@ -97,7 +105,13 @@ inline TpOperand tp_operand(int dtype, const void* data, int64_t ld, int64_t row
   return TpOperand{(const char*)data, ld * es, ((rows - 1) * ld + cols) * es};
 }
 // dst [rows x packed cols] = src, zeros behind its columns.
-hipError_t launch_pack(int dtype, const MatDev& src, int64_t rows, int cols, void* dst, hipStream_t st);
+struct PackJob {
+  const void* src;
+  int64_t ld, rows;
+  int cols;
+  void* dst;
+};
+hipError_t launch_pack(int dtype, const PackJob* jobs, int n, hipStream_t st);  // n <= 2
 
 // ---- the epilogue of dense layers and of stored products ---------------------------------
 // Sums of one split go to a slab of floats of their own (part, [splits][m x ldp]), added to what is
@@ -106,9 +120,10 @@ struct StoreArgs {
   DenseEpi epi;
   float* part;
   int64_t ldp, slab;
-  int add;
+  int add, keep;  // keep: the slabs are joined by the caller
   float alpha;
   const float* alpha_dev;
+  const float* live;  // or null: rows whose entry is 0 become zeros
 };
 
 template <class S, bool FULL>
@@ -161,7 +176,7 @@ struct EpiStore {
       dense_out8(a.epi, b, row, col, c, v);
     } else {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) v[i] *= alpha;
+      for (int i = 0; i < 8; ++i) v[i] = a.live && a.live[row] == 0.0f ? 0.0f : v[i] * alpha;
       store8(a.epi.y, row, col, c, v);
     }
   }
@@ -174,11 +189,26 @@ using EpiPlain = EpiStore<S, false>;
 
 // The product with the plain epilogue: a has k along its rows (a_krows) or across them, b across them.
 hipError_t launch_plain(int dtype, bool a_krows, const TpPlan& p, const StoreArgs& a, hipStream_t st);
-// Adds the slabs of a product and puts the sums out as the epilogue would; live (or null): rows whose
-// entry is 0 become zeros.
-hipError_t launch_join(const StoreArgs& a, int splits, int m, int n, bool full, const float* live, hipStream_t st);
-// y[j] = alpha *alpha_dev sum_i part[i][j], i < rows
-hipError_t launch_column_sums(const float* part, int rows, int64_t ld, int n, float alpha, const float* alpha_dev,
-                              float* y, hipStream_t st);
+// Adds the slabs of a product and puts the sums out as the epilogue would.
+hipError_t launch_join(const StoreArgs& a, int splits, int m, int n, bool full, hipStream_t st);
+// y[j] = alpha *alpha_dev sum_i part[i][j], i < rows; y null: nothing.
+struct SumJob {
+  const float* part;
+  int rows;
+  int64_t ld;
+  int n;
+  float alpha;
+  const float* alpha_dev;
+  float* y;
+};
+hipError_t launch_column_sums(const SumJob& s, hipStream_t st);
+// What both gradients of a product take: a x (k along a's rows) and a^T y (k across), either with its operands null
+// for none, and sums; in one launch where the products are small.  Products that split k are joined.
+struct PairJob {
+  TpPlan x, y;
+  StoreArgs ax, ay;
+  SumJob sums;
+};
+hipError_t launch_pair(int dtype, const PairJob& p, hipStream_t st);
 
 }  // namespace asgd

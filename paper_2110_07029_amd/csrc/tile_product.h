@@ -42,15 +42,17 @@ struct TpMma {
 };
 
 // ---- tile shapes ----------------------------------------------------------------
-template <int BM_, int BN_, int WM_, int WN_, int NBUF_>
+template <int BM_, int BN_, int WM_, int WN_, int NBUF_, int WK_ = 1>
 struct TpShape {
-  static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, NBUF = NBUF_;
-  static constexpr int WAVES = WM * WN, THREADS = 64 * WAVES;
+  static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, NBUF = NBUF_, WK = WK_;
+  static constexpr int WAVES = WM * WN * WK, THREADS = 64 * WAVES;
   static constexpr int TM = BM / WM / 32, TN = BN / WN / 32;  // 32 x 32 blocks of a wave
   static constexpr int BUF = (BM + BN) * TP_STEP;             // bytes of a buffer
   static constexpr int WCOLS = 32 * TN;                       // columns of a wave
   static constexpr int OUT_LD = WCOLS + 4;                    // floats, a wave's output block
   static constexpr int OUT = 32 * OUT_LD * 4;                 // bytes of it
+  // WK > 1: that many waves share a block and take turns along k; the first of them has the sums in the end
+  static_assert(WK == 1 || (WK == 4 && TM == 1 && TN == 1), "one wave per chunk of a step");
   static_assert(BM % (32 * WM) == 0 && BN % (32 * WN) == 0, "whole blocks");
 };
 
@@ -249,13 +251,12 @@ __device__ __forceinline__ void tp_staged8(const float* out, int r, int c, float
 // Fragments are read one chunk of k ahead of their products, over the barrier too: after it the first reads of
 // the new step go out, then the last products of the old one.  (4,096 x 32,001 x 2,048 in bf16: @@.)
 template <typename T, bool AK, bool BK, class S, class Epi>
-__global__ __launch_bounds__(S::THREADS) void k_tile_product(TpJob j, typename Epi::Args ea) {
-  extern __shared__ __attribute__((aligned(16))) char smem[];
+__device__ __forceinline__ void tp_tile(const TpJob& j, const typename Epi::Args& ea, int block, char* smem) {
   int tm, tn, split;
-  if (!tp_place(j, blockIdx.x, &tm, &tn, &split)) return;
+  if (!tp_place(j, block, &tm, &tn, &split)) return;
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int wm = wave / S::WN, wn = wave % S::WN;
+  const int wk = wave / (S::WM * S::WN), wm = wave / S::WN % S::WM, wn = wave % S::WN;
   constexpr int KB = TpMma<T>::KB, NB = S::NBUF;
   const int64_t k0 = split * j.split_k, k1 = min(j.k, k0 + j.split_k);
   const int steps = (int)((k1 - k0 + KB - 1) / KB);
@@ -312,6 +313,12 @@ __global__ __launch_bounds__(S::THREADS) void k_tile_product(TpJob j, typename E
     else
       tp_wait<0>();
     __builtin_amdgcn_s_barrier();
+    if constexpr (S::WK > 1) {
+      if (s + NB - 1 < steps) issue(s + NB - 1);
+      read(s, wk, 0);
+      multiply(0);
+      continue;
+    }
     read(s, 0, 0);
     if (s + NB - 1 < steps) issue(s + NB - 1);
     __builtin_amdgcn_sched_barrier(0);
@@ -325,16 +332,41 @@ __global__ __launch_bounds__(S::THREADS) void k_tile_product(TpJob j, typename E
       __builtin_amdgcn_sched_barrier(0);
     }
   }
-  if (steps > 0) multiply(1);
+  if (S::WK == 1 && steps > 0) multiply(1);
   __syncthreads();  // the buffers are free for the epilogue
 
   float* const out = reinterpret_cast<float*>(smem + wave * S::OUT);
+  if constexpr (S::WK > 1) {
+    tp_stage<S>(acc[0], out, lane);
+    __syncthreads();
+    if (wk == 0) {
+#pragma unroll
+      for (int k = 1; k < S::WK; ++k)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const f32x4 v = *reinterpret_cast<const f32x4*>(out + k * S::WM * S::WN * (S::OUT / 4) + (lane & 31) * S::OUT_LD + 8 * q +
+                                                          4 * (lane >> 5));
+#pragma unroll
+          for (int i = 0; i < 4; ++i) acc[0][0][4 * q + i] += v[i];
+        }
+    }
+    __syncthreads();  // (the other waves' blocks are theirs again)
+    if (wk == 0) epi.block(acc[0], tm * S::BM + 32 * wm, tn * S::BN + 32 * wn, out, wave, lane);
+    epi.end(wave, wm, wn, lane, tid);
+    return;
+  }
 #pragma unroll
   for (int a = 0; a < S::TM; ++a) {
     __builtin_amdgcn_sched_barrier(0);  // (one row of blocks at a time: all at once do not fit the registers)
     epi.block(acc[a], tm * S::BM + 32 * (wm * S::TM + a), tn * S::BN + wn * S::WCOLS, out, wave, lane);
   }
   epi.end(wave, wm, wn, lane, tid);
+}
+
+template <typename T, bool AK, bool BK, class S, class Epi>
+__global__ __launch_bounds__(S::THREADS) void k_tile_product(TpJob j, typename Epi::Args ea) {
+  extern __shared__ __attribute__((aligned(16))) char smem[];
+  tp_tile<T, AK, BK, S, Epi>(j, ea, blockIdx.x, smem);
 }
 
 }  // namespace asgd
