@@ -41,7 +41,7 @@ def sources() -> list:
 # the W2 update reads dW2 without first copying them out of accumulation registers
 # (a kernel with the whole register file would otherwise get the accumulation form;
 # the operands pinned to accumulation registers stay there).
-FILE_FLAGS = {"k_out_bwd.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"]}
+FILE_FLAGS = {f: ["-mllvm", "-amdgpu-mfma-vgpr-form"] for f in ("k_out_bwd.hip", "k_label_narrow.hip")}
 
 
 def _compile(src: str, extra: list, verbose: bool) -> str:

@@ -18,23 +18,27 @@ namespace asgd {
 
 namespace {
 
+typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
+typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
 constexpr int NW_THREADS = 512, NW_ROWS = 256, NW_TILE = 64, NW_COLS = 128;
 constexpr int NW_WBUF = NW_TILE * 256, NW_BIAS = 8 * 256;  // bytes of a tile; of its biases, a copy per wave
 
 __device__ __forceinline__ int nw_turn(int r) { return 4 * (r & 3) + ((r >> 2) & 3); }
 
-// The copies of tiles of W (two per wave) and their biases (one).
+// The copies of tiles of W and their biases by a workgroup of THREADS.
+template <int THREADS>
 struct NwLoad {
+  static constexpr int ITS = 1024 / THREADS, COPIES = ITS + 1;
   const char* base;
   int64_t ld, end;
   const float* bias;
   int n;
-  unsigned voff[2];
+  unsigned voff[ITS];
   __device__ NwLoad(const TpOperand& w, const float* b, int n_labels, int d_bytes, int tid)
       : base(w.base), ld(w.ld), end(w.end), bias(b), n(n_labels) {
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const int r = (tid >> 4) + 32 * i, c = (tid & 15) ^ nw_turn(r);
+    for (int i = 0; i < ITS; ++i) {
+      const int r = (tid >> 4) + THREADS / 16 * i, c = (tid & 15) ^ nw_turn(r);
       voff[i] = 16 * c < d_bytes ? (unsigned)(r * ld) + 16 * c : 0x80000000u;
     }
   }
@@ -43,12 +47,11 @@ struct NwLoad {
     const int64_t l0 = (int64_t)t * NW_TILE;
     const i32x4 rs = tp_rsrc(base + l0 * ld, end - l0 * ld);
 #pragma unroll
-    for (int i = 0; i < 2; ++i) tp_copy16(rs, voff[i], to + 8192 * i + 1024 * wave);
+    for (int i = 0; i < ITS; ++i) tp_copy16(rs, voff[i], to + 16 * THREADS * i + 1024 * wave);
     const i32x4 rb = tp_rsrc((const char*)(bias + (bias ? l0 : 0)), bias ? (n - l0) * 4 : 0);  // (zeros without)
     tp_copy4(rb, 4u * lane, to_bias);
   }
 };
-constexpr int NW_COPIES = 3;
 
 // Row r's chunk pair kk (32 bytes of k) of a tile in LDS.
 template <typename T>
@@ -76,11 +79,8 @@ __device__ __forceinline__ void nw_rows(const TpOperand& h, int row, int B, int 
   }
 }
 
-// z + bias of tile rows 32 b + 8 q + 4 g + i (labels) for this lane's row.
-template <typename T>
-__device__ __forceinline__ void nw_logits(const char* w, const char* bias, const typename TpMma<T>::frag8 (&hf)[8], int lane,
-                                          f32x16 (&z)[2]) {
-  const int n = lane & 31, g = lane >> 5;
+// z = bias for labels 32 b + 8 q + 4 g + i of a tile; then 32 bytes kk of k after the other.
+__device__ __forceinline__ void nw_bias(const char* bias, int g, f32x16 (&z)[2]) {
 #pragma unroll
   for (int b = 0; b < 2; ++b)
 #pragma unroll
@@ -89,6 +89,12 @@ __device__ __forceinline__ void nw_logits(const char* w, const char* bias, const
 #pragma unroll
       for (int i = 0; i < 4; ++i) z[b][4 * q + i] = t[i];
     }
+}
+template <typename T>
+__device__ __forceinline__ void nw_logits(const char* w, const char* bias, const typename TpMma<T>::frag8 (&hf)[8], int lane,
+                                          f32x16 (&z)[2]) {
+  const int n = lane & 31, g = lane >> 5;
+  nw_bias(bias, g, z);
 #pragma unroll
   for (int kk = 0; kk < 8; ++kk)
 #pragma unroll
@@ -99,70 +105,90 @@ __device__ __forceinline__ void nw_logits(const char* w, const char* bias, const
 
 // ---- log-sum-exp ---------------------------------------------------------------------------------
 // Workgroup = (256 rows, a range of tiles); the row blocks of a range sit on one XCD, whose L2 then has its labels.
-// Four tiles are on their way.
-constexpr int NWF_BUFS = 4;
-constexpr int NWF_LDS = NWF_BUFS * (NW_WBUF + NW_BIAS);
+// Four waves with 64 rows each: what a wave reads of a tile serves two products.  Two workgroups share a compute unit, so
+// that one's exponentials meet the other's products.
+constexpr int NWF_THREADS = 256, NWF_BUFS = 2;
+constexpr int NWF_LDS = NWF_BUFS * (NW_WBUF + 4 * 256);
 
 template <typename T>
-__global__ __launch_bounds__(NW_THREADS) void k_narrow_lse(TpOperand h, TpOperand w, const float* bias, int B, int L,
-                                                          int d_bytes, int row_blocks, int ranges, int per, int tiles,
-                                                          float2* __restrict__ part) {
+__global__ __launch_bounds__(NWF_THREADS, 2) void k_narrow_lse(TpOperand h, TpOperand w, const float* bias, int B, int L,
+                                                           int d_bytes, int row_blocks, int ranges, int per, int tiles,
+                                                           float2* __restrict__ part) {
   extern __shared__ __attribute__((aligned(16))) char smem[];
-  const int tid = threadIdx.x, lane = tid & 63, g = lane >> 5;
+  constexpr int BUF = NW_WBUF + 4 * 256;
+  const int tid = threadIdx.x, lane = tid & 63, g = lane >> 5, n = lane & 31;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int set = (int)blockIdx.x / (8 * row_blocks), in = (int)blockIdx.x % (8 * row_blocks);
   const int range = 8 * set + in % 8;
   if (range >= ranges) return;
-  const int row = (in / 8) * NW_ROWS + 32 * wave + (lane & 31);
+  const int row = (in / 8) * NW_ROWS + 64 * wave + n;
   const int t0 = range * per, t1 = min(tiles, t0 + per);
-  const NwLoad load(w, bias, L, d_bytes, tid);
+  const NwLoad<NWF_THREADS> load(w, bias, L, d_bytes, tid);
   const unsigned lds0 = __builtin_amdgcn_readfirstlane((unsigned)(uintptr_t)(__attribute__((address_space(3))) char*)smem);
   auto issue = [&](int t) {
-    const unsigned at = lds0 + (unsigned)((t - t0) % NWF_BUFS) * (NW_WBUF + NW_BIAS);
+    const unsigned at = lds0 + (unsigned)((t - t0) % NWF_BUFS) * BUF;
     load.copy(t, at, at + NW_WBUF + 256 * wave, wave, lane);
   };
-  typename TpMma<T>::frag8 hf[8];
-  nw_rows<T>(h, row, B, d_bytes, g, hf);
+  typename TpMma<T>::frag8 hf[2][8];
+  nw_rows<T>(h, row, B, d_bytes, g, hf[0]);
+  nw_rows<T>(h, row + 32, B, d_bytes, g, hf[1]);
 #pragma unroll
   for (int k = 0; k < NWF_BUFS - 1; ++k)
     if (t0 + k < t1) issue(t0 + k);
-  float m = -INFINITY, s = 0.0f;
+  float m[2] = {-INFINITY, -INFINITY}, s[2] = {0.0f, 0.0f};
   for (int t = t0; t < t1; ++t) {
-    if (t + NWF_BUFS - 2 < t1) tp_wait<(NWF_BUFS - 2) * NW_COPIES>();
+    if (t + NWF_BUFS - 2 < t1) tp_wait<(NWF_BUFS - 2) * NwLoad<NWF_THREADS>::COPIES>();
     else tp_wait<0>();
-    __builtin_amdgcn_s_barrier();
+    __builtin_amdgcn_s_barrier();  // the tile is here, and nobody reads the one before
     if (t + NWF_BUFS - 1 < t1) issue(t + NWF_BUFS - 1);
-    const char* p = smem + (t - t0) % NWF_BUFS * (NW_WBUF + NW_BIAS);
-    f32x16 z[2];
-    nw_logits<T>(p, p + NW_WBUF + 256 * wave, hf, lane, z);
-    if ((t + 1) * NW_TILE > L) {
+    const char* p = smem + (t - t0) % NWF_BUFS * BUF;
+    f32x16 z[2][2];
+    nw_bias(p + NW_WBUF + 256 * wave, g, z[0]);
+    z[1][0] = z[0][0];
+    z[1][1] = z[0][1];
+#pragma unroll
+    for (int kk = 0; kk < 8; ++kk)
+#pragma unroll
+      for (int b = 0; b < 2; ++b) {
+        const auto f = nw_row_frag<T>(p, 32 * b + n, kk, g);
+        z[0][b] = tp_mma(f, hf[0][kk], z[0][b]);
+        z[1][b] = tp_mma(f, hf[1][kk], z[1][b]);
+      }
+    const bool edge = (t + 1) * NW_TILE > L;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      if (edge) {
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+          for (int r = 0; r < 16; ++r)
+            if (t * NW_TILE + 32 * b + 8 * (r >> 2) + 4 * g + (r & 3) >= L) z[i][b][r] = -INFINITY;
+      }
+      float top[2] = {m[i], m[i]};
 #pragma unroll
       for (int b = 0; b < 2; ++b)
 #pragma unroll
-        for (int r = 0; r < 16; ++r)
-          if (t * NW_TILE + 32 * b + 8 * (r >> 2) + 4 * g + (r & 3) >= L) z[b][r] = -INFINITY;
+        for (int r = 0; r < 16; ++r) top[b] = fmaxf(top[b], z[i][b][r]);
+      const float mm = fmaxf(top[0], top[1]);
+      // base 2; the maximum's rounding is of the size of the result's own
+      const float base = mm == -INFINITY ? 0.0f : mm * LOG2E;
+      float e[4] = {m[i] == -INFINITY ? s[i] : s[i] * __builtin_amdgcn_exp2f(fmaf(m[i], LOG2E, -base)), 0.0f, 0.0f, 0.0f};
+#pragma unroll
+      for (int b = 0; b < 2; ++b)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) e[r & 3] += __builtin_amdgcn_exp2f(fmaf(z[i][b][r], LOG2E, -base));
+      s[i] = (e[0] + e[1]) + (e[2] + e[3]);
+      m[i] = mm;
     }
-    float top[2] = {m, m};
-#pragma unroll
-    for (int b = 0; b < 2; ++b)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) top[b] = fmaxf(top[b], z[b][r]);
-    const float mm = fmaxf(top[0], top[1]);
-    // base 2; the maximum's rounding is of the size of the result's own
-    const float base = mm == -INFINITY ? 0.0f : mm * LOG2E;
-    float e[4] = {s * __builtin_amdgcn_exp2f(fmaf(m, LOG2E, -base)), 0.0f, 0.0f, 0.0f};
-    if (m == -INFINITY) e[0] = s;  // (0, or NaN)
-#pragma unroll
-    for (int b = 0; b < 2; ++b)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) e[r & 3] += __builtin_amdgcn_exp2f(fmaf(z[b][r], LOG2E, -base));
-    s = (e[0] + e[1]) + (e[2] + e[3]);
-    m = mm;
   }
-  const float m2 = __builtin_bit_cast(float, lane_xor<32>(__builtin_bit_cast(unsigned, m), lane));
-  const float s2 = __builtin_bit_cast(float, lane_xor<32>(__builtin_bit_cast(unsigned, s), lane));
-  const float mm = fmaxf(m, m2), base = mm == -INFINITY ? 0.0f : mm;
-  if (row < B && g == 0) part[(int64_t)row * ranges + range] = make_float2(mm, s * exp_fast(m - base) + s2 * exp_fast(m2 - base));
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const float m2 = __builtin_bit_cast(float, lane_xor<32>(__builtin_bit_cast(unsigned, m[i]), lane));
+    const float s2 = __builtin_bit_cast(float, lane_xor<32>(__builtin_bit_cast(unsigned, s[i]), lane));
+    const float mm = fmaxf(m[i], m2), base = mm == -INFINITY ? 0.0f : mm;
+    if (row + 32 * i < B && g == 0)
+      part[(int64_t)(row + 32 * i) * ranges + range] = make_float2(mm, s[i] * exp_fast(m[i] - base) + s2 * exp_fast(m2 - base));
+  }
 }
 
 // ---- gradients ---------------------------------------------------------------------------------------
@@ -211,7 +237,7 @@ __global__ __launch_bounds__(NW_THREADS) void k_narrow_grad(TpOperand h, TpOpera
   const int G = lane >> 4, ti = (lane >> 2) & 3, ta = lane & 3;  // of a transposing read's address
   const int range = blockIdx.x, L = a.n_labels, d_bytes = d * 2;
   const int t0 = range * per, t1 = min(tiles, t0 + per);
-  const NwLoad load(w, a.bias, L, d_bytes, tid);
+  const NwLoad<NW_THREADS> load(w, a.bias, L, d_bytes, tid);
   const unsigned lds0 = __builtin_amdgcn_readfirstlane((unsigned)(uintptr_t)(__attribute__((address_space(3))) char*)smem);
   auto issue = [&](int t) {
     const unsigned at = lds0 + NWG_W + (unsigned)((t - t0) % NWG_BUFS) * (NW_WBUF + NW_BIAS);
@@ -273,13 +299,13 @@ __global__ __launch_bounds__(NW_THREADS) void k_narrow_grad(TpOperand h, TpOpera
 #pragma unroll
     for (int c = 0; c < 2; ++c) zat[hi][c] = nw_dz(16 * c + 8 * (G >> 1) + 4 * hi + ti, 8 * lb + 4 * (G & 1) + ta);
   }
-  // stores of dw that are sure to follow a tile's copies
-  const bool stores = dw.data && 32 * wu + 32 <= d;
+  // whole 16-byte pieces of dw in the operands' type: two stores, which are sure to follow a tile's copies
+  const bool wide = dw.data && dw.vec && dw.dtype == (std::is_same<T, bf16>::value ? 1 : 2) && 32 * wu + 32 <= d;
   float* const sums = reinterpret_cast<float*>(smem + NWG_SUM);
 
   for (int t = t0; t < t1; ++t) {
-    // (vmcnt counts stores too: the four or more of the last tile's dw came after the copies and need not be waited for)
-    if (stores && t > t0) tp_wait<4>();
+    // (vmcnt counts stores too: the two of the last tile's dw came after the copies and need not be waited for)
+    if (wide && t > t0) tp_wait<2>();
     else tp_wait<0>();
     __builtin_amdgcn_s_barrier();  // the tile is here, and nobody reads dz or the other tile any more
     if (t + 1 < t1) issue(t + 1);
@@ -322,30 +348,35 @@ __global__ __launch_bounds__(NW_THREADS) void k_narrow_grad(TpOperand h, TpOpera
     nw_logits<T>(p, p + NW_WBUF + 256 * wave, hf, lane, z);
     const bool edge = (t + 1) * NW_TILE > L;
     Frag df[2][2];
+    // dz, to LDS and as fragments; checked: with targets, or past the last label
+    auto form = [&](auto checked) {
 #pragma unroll
-    for (int b = 0; b < 2; ++b)
+      for (int b = 0; b < 2; ++b)
 #pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        char* const at = dzt + nw_dz(row, 8 * b + 2 * q + g);
-        float v[4];
+        for (int q = 0; q < 4; ++q) {
+          char* const at = dzt + nw_dz(row, 8 * b + 2 * q + g);
+          Half o;
+          uint64_t times = 0;
+          if (checked) times = any ? *reinterpret_cast<const uint64_t*>(at) : 0;
 #pragma unroll
-        for (int k = 0; k < 4; ++k) v[k] = __builtin_amdgcn_exp2f(fmaf(z[b][4 * q + k], LOG2E, -lse));
-        if (any) {
-          const uint64_t times = *reinterpret_cast<const uint64_t*>(at);
-#pragma unroll
-          for (int k = 0; k < 4; ++k) v[k] -= (float)((times >> (16 * k)) & 0xffff) * sh;
+          for (int k = 0; k < 4; ++k) {
+            float v = z[b][4 * q + k];
+            v = __builtin_amdgcn_exp2f(fmaf(v, LOG2E, -lse));
+            bool in = live;  // (rows without labels and labels past the last are zeros, whatever they hold)
+            if (checked) {
+              v -= (float)((times >> (16 * k)) & 0xffff) * sh;
+              in = live && t * NW_TILE + 32 * b + 8 * q + 4 * g + k < L;
+            }
+            v = in ? v * f : 0.0f;
+            z[b][4 * q + k] = v;
+            o[k] = (T)v;
+            df[b][q >> 1][4 * (q & 1) + k] = o[k];
+          }
+          *reinterpret_cast<Half*>(at) = o;
         }
-        Half o;
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          // rows without labels and labels past the last are zeros, whatever they hold
-          v[k] = live && !(edge && t * NW_TILE + 32 * b + 8 * q + 4 * g + k >= L) ? v[k] * f : 0.0f;
-          z[b][4 * q + k] = v[k];
-          o[k] = (T)v[k];
-          df[b][q >> 1][4 * (q & 1) + k] = o[k];
-        }
-        *reinterpret_cast<Half*>(at) = o;
-      }
+    };
+    if (any || edge) form(std::true_type());
+    else form(std::false_type());
     if (db) {
       float v[32];
 #pragma unroll
@@ -382,7 +413,26 @@ __global__ __launch_bounds__(NW_THREADS) void k_narrow_grad(TpOperand h, TpOpera
                      nw_join<T>(tp_turned<T>(zp + zat[0][c & 1]), tp_turned<T>(zp + zat[1][c & 1])), acc);
       }
       const int label = t * NW_TILE + 32 * lb + n;
-      if (label < L) {
+      if (wide) {
+        // lanes n and n + 32 hold columns 8 q .. + 3 and + 4 .. + 7 of label n: with a change of sides between q and q + 1
+        // each has 8 columns
+#pragma unroll
+        for (int q = 0; q < 4; q += 2) {
+          u32x2 v[2];
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            Half o;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) o[k] = (T)(acc[4 * (q + i) + k] * out);
+            v[i] = __builtin_bit_cast(u32x2, o);
+          }
+          const auto lo = __builtin_amdgcn_permlane32_swap(v[0][0], v[1][0], false, false);
+          const auto hi = __builtin_amdgcn_permlane32_swap(v[0][1], v[1][1], false, false);
+          const u32x4 o{(unsigned)lo[0], (unsigned)hi[0], (unsigned)lo[1], (unsigned)hi[1]};
+          if (label < L)
+            *reinterpret_cast<u32x4*>((T*)dw.data + label * dw.ld + 32 * wu + 8 * (q + g)) = o;
+        }
+      } else if (label < L) {
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
           const int col = 32 * wu + 8 * q + 4 * g;
@@ -406,7 +456,6 @@ __global__ __launch_bounds__(NW_THREADS) void k_narrow_grad(TpOperand h, TpOpera
 bool narrow_takes(int dtype, int d) { return dtype != 0 && d <= NW_COLS; }
 bool narrow_grad_takes(int dtype, int n_rows, int d) { return narrow_takes(dtype, d) && n_rows <= NW_ROWS; }
 
-// Two workgroups of the log-sum-exp share a compute unit, so that one's exponentials meet the other's products.
 NarrowPlan narrow_lse_plan(int n_rows, int n_labels) {
   NarrowPlan p;
   p.row_blocks = (int)ceil_div(n_rows, NW_ROWS);
@@ -432,7 +481,7 @@ hipError_t launch_narrow_lse(int dtype, const NarrowPlan& p, const TpOperand& h,
   const auto fn = dtype == 1 ? k_narrow_lse<bf16> : k_narrow_lse<f16>;
   const hipError_t e = tp_allow_lds((const void*)fn, NWF_LDS);
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL(fn, dim3(blocks), dim3(NW_THREADS), NWF_LDS, st, h, w, bias, n_rows, n_labels, 2 * d, p.row_blocks,
+  hipLaunchKernelGGL(fn, dim3(blocks), dim3(NWF_THREADS), NWF_LDS, st, h, w, bias, n_rows, n_labels, 2 * d, p.row_blocks,
                      p.ranges, p.per, p.tiles, part);
   return hipGetLastError();
 }
