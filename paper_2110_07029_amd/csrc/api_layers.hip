@@ -25,8 +25,7 @@ int elem_bytes(int dtype) { return dtype == ASGD_F32 ? 4 : 2; }
 
 MatDev mat_dev(const asgd_matrix* a) {
   if (!a) return MatDev{};
-  const int es = elem_bytes(a->dtype);
-  return MatDev{a->data, a->ld, a->dtype, ((uintptr_t)a->data | (uint64_t)(a->ld * es)) % 16 == 0};
+  return MatDev{a->data, a->ld, a->dtype};
 }
 
 // Bytes that an argument spans: rows of `width` bytes, `step` apart.
@@ -101,9 +100,16 @@ asgd_status check_rows(const asgd_matrix* h, const asgd_matrix* w) {
   return ASGD_OK;
 }
 
-asgd_status check_mat_device(const asgd_matrix* a, const char* name) {
-  return a ? check_device(a->data, name) : ASGD_OK;
-}
+// The current device, which everything has to be on.
+struct Device {
+  int id = -1;
+  asgd_status find() {
+    const hipError_t e = hipGetDevice(&id);
+    return e == hipSuccess ? ASGD_OK : hip_failed(e, "hipGetDevice");
+  }
+  asgd_status has(const void* p, const char* name) const { return p ? check_device_is(id, p, name) : ASGD_OK; }
+  asgd_status has(const asgd_matrix* a, const char* name) const { return a ? has((const void*)a->data, name) : ASGD_OK; }
+};
 
 }  // namespace
 
@@ -131,13 +137,15 @@ asgd_status asgd_dense(const asgd_matrix* x, const asgd_matrix* w, const asgd_ep
   if (pre && (meet(pre, x) || meet(pre, w) || meet(pre, y) || meet(pre, res) || meet(span_of(pre), bias)))
     return set_error(ASGD_EINVAL, "pre overlaps another matrix");
   TRY(check_workspace(ws, ws_bytes, dense_ws_bytes(x->dtype, mat_dev(x), mat_dev(w), m, n, x->n_cols)));
+  Device dev;
+  TRY(dev.find());
   TRY(check_stream(hip_stream));
-  TRY(check_mat_device(x, "x.data"));
-  TRY(check_mat_device(w, "w.data"));
-  TRY(check_mat_device(y, "y.data"));
-  TRY(check_mat_device(pre, "pre.data"));
-  TRY(check_mat_device(res, "epilogue.residual.data"));
-  if (ep && ep->bias) TRY(check_device(ep->bias, "epilogue.bias"));
+  TRY(dev.has(x, "x.data"));
+  TRY(dev.has(w, "w.data"));
+  TRY(dev.has(y, "y.data"));
+  TRY(dev.has(pre, "pre.data"));
+  TRY(dev.has(res, "epilogue.residual.data"));
+  TRY(dev.has(ep ? ep->bias : nullptr, "epilogue.bias"));
   DenseJob j{x->dtype, mat_dev(x), mat_dev(w), m, n, x->n_cols, {}};
   if (ep) {
     j.epi.bias = ep->bias;
@@ -178,14 +186,16 @@ asgd_status asgd_dense_backward(const asgd_matrix* dy, const asgd_matrix* x, con
   if (meet(dx, dw) || (dx && meet(span_of(dx), dbs)) || (dw && meet(span_of(dw), dbs)))
     return set_error(ASGD_EINVAL, "gradients overlap");
   TRY(check_workspace(ws, ws_bytes, dense_grad_ws_bytes(x->dtype, mat_dev(x), mat_dev(w), m, n, k)));
+  Device dev;
+  TRY(dev.find());
   TRY(check_stream(hip_stream));
-  TRY(check_mat_device(dy, "dy.data"));
-  TRY(check_mat_device(x, "x.data"));
-  TRY(check_mat_device(w, "w.data"));
-  TRY(check_mat_device(pre, "pre.data"));
-  TRY(check_mat_device(dx, "dx.data"));
-  TRY(check_mat_device(dw, "dw.data"));
-  if (db) TRY(check_device(db, "db"));
+  TRY(dev.has(dy, "dy.data"));
+  TRY(dev.has(x, "x.data"));
+  TRY(dev.has(w, "w.data"));
+  TRY(dev.has(pre, "pre.data"));
+  TRY(dev.has(dx, "dx.data"));
+  TRY(dev.has(dw, "dw.data"));
+  TRY(dev.has(db, "db"));
   const DenseGradJob j{x->dtype, mat_dev(dy), mat_dev(pre), mat_dev(x), mat_dev(w), mat_dev(dx), mat_dev(dw), db, m, n, k,
                        act, ep ? drop_dev(ep->drop, ep->seed) : DropDev{}};
   LAUNCH(launch_dense_grad(j, ws, (hipStream_t)hip_stream));
@@ -200,10 +210,12 @@ asgd_status asgd_dropout(const asgd_matrix* x, double p, uint64_t seed, const as
   if (residual) TRY(check_shape(residual, "residual", x->n_rows, x->n_cols));
   if (meet_partly(y, x) || meet_partly(y, residual))
     return set_error(ASGD_EINVAL, "y overlaps an input without being it");
+  Device dev;
+  TRY(dev.find());
   TRY(check_stream(hip_stream));
-  TRY(check_mat_device(x, "x.data"));
-  TRY(check_mat_device(y, "y.data"));
-  TRY(check_mat_device(residual, "residual.data"));
+  TRY(dev.has(x, "x.data"));
+  TRY(dev.has(y, "y.data"));
+  TRY(dev.has(residual, "residual.data"));
   LAUNCH(launch_dropout(mat_dev(x), mat_dev(residual), mat_dev(y), drop_dev(p, seed), x->n_rows, x->n_cols,
                         (hipStream_t)hip_stream));
   return ASGD_OK;
@@ -243,18 +255,20 @@ asgd_status asgd_label_loss(const asgd_matrix* h, const asgd_matrix* w, const fl
   }
   const bool grads = dh || dw || db;
   TRY(check_workspace(ws, ws_bytes, label_loss_ws_bytes(h->dtype, mat_dev(h), mat_dev(w), B, L, D, grads)));
+  Device dev;
+  TRY(dev.find());
   TRY(check_stream(hip_stream));
-  TRY(check_mat_device(h, "h.data"));
-  TRY(check_mat_device(w, "w.data"));
-  TRY(check_device(y->indptr, "y.indptr"));
-  if (y->nnz) TRY(check_device(y->indices, "y.indices"));
-  if (bias) TRY(check_device(bias, "bias"));
-  if (weights) TRY(check_device(weights, "weights"));
-  TRY(check_device(loss_rows, "loss_rows"));
-  if (lse) TRY(check_device(lse, "lse"));
-  if (db) TRY(check_device(db, "db"));
-  TRY(check_mat_device(dh, "dh.data"));
-  TRY(check_mat_device(dw, "dw.data"));
+  TRY(dev.has(h, "h.data"));
+  TRY(dev.has(w, "w.data"));
+  TRY(dev.has(y->indptr, "y.indptr"));
+  TRY(dev.has(y->nnz ? y->indices : nullptr, "y.indices"));
+  TRY(dev.has(bias, "bias"));
+  TRY(dev.has(weights, "weights"));
+  TRY(dev.has(loss_rows, "loss_rows"));
+  TRY(dev.has(lse, "lse"));
+  TRY(dev.has(db, "db"));
+  TRY(dev.has(dh, "dh.data"));
+  TRY(dev.has(dw, "dw.data"));
   const LossJob j{h->dtype, mat_dev(h), mat_dev(w), B, L, D, bias, list_dev(y, 0), weights, loss_rows, lse, mat_dev(dh),
                   mat_dev(dw), db};
   LAUNCH(launch_label_loss(j, ws, (hipStream_t)hip_stream));

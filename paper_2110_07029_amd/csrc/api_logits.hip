@@ -144,8 +144,12 @@ asgd_status check_device(const void* p, const char* name) {
   int dev = 0;
   hipError_t e = hipGetDevice(&dev);
   if (e != hipSuccess) return hip_failed(e, "hipGetDevice");
+  return check_device_is(dev, p, name);
+}
+
+asgd_status check_device_is(int dev, const void* p, const char* name) {
   hipPointerAttribute_t a{};
-  e = hipPointerGetAttributes(&a, p);
+  hipError_t e = hipPointerGetAttributes(&a, p);
   if (e != hipSuccess) (void)hipGetLastError();  // (an unknown address leaves an error behind)
   if (e != hipSuccess || (a.type != hipMemoryTypeDevice && a.type != hipMemoryTypeManaged))
     return set_error_named(ASGD_EINVAL, name, " is not device memory");

@@ -298,11 +298,11 @@ hipError_t launch_fp4_logits(const Fp4Rows& a, int B, const uint8_t* codes, cons
                              int L, int dtype, void* z, int64_t ldz, hipStream_t st);
 
 // ---- dense layers and dropout (k_layers.hip) ------------------------------------------
-// A matrix as the kernels see it; data null: none.  vec: rows and base aligned for 8 elements at a time.
+// A matrix as the kernels see it; data null: none.
 struct MatDev {
   void* data;
   int64_t ld;
-  int dtype, vec;
+  int dtype;
 };
 // Elements whose 32 random bits are below `below` are dropped (0: none), the others scaled.
 struct DropDev {

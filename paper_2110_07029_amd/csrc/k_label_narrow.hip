@@ -20,6 +20,7 @@ namespace {
 
 typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
 typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
+typedef unsigned u32x4u __attribute__((ext_vector_type(4), aligned(2)));
 constexpr int NW_THREADS = 512, NW_ROWS = 256, NW_TILE = 64, NW_COLS = 128;
 constexpr int NW_WBUF = NW_TILE * 256, NW_BIAS = 8 * 256;  // bytes of a tile; of its biases, a copy per wave
 
@@ -300,7 +301,7 @@ __global__ __launch_bounds__(NW_THREADS) void k_narrow_grad(TpOperand h, TpOpera
     for (int c = 0; c < 2; ++c) zat[hi][c] = nw_dz(16 * c + 8 * (G >> 1) + 4 * hi + ti, 8 * lb + 4 * (G & 1) + ta);
   }
   // whole 16-byte pieces of dw in the operands' type: two stores, which are sure to follow a tile's copies
-  const bool wide = dw.data && dw.vec && dw.dtype == (std::is_same<T, bf16>::value ? 1 : 2) && 32 * wu + 32 <= d;
+  const bool wide = dw.data && dw.dtype == (std::is_same<T, bf16>::value ? 1 : 2) && 32 * wu + 32 <= d;
   float* const sums = reinterpret_cast<float*>(smem + NWG_SUM);
 
   for (int t = t0; t < t1; ++t) {
@@ -430,7 +431,7 @@ __global__ __launch_bounds__(NW_THREADS) void k_narrow_grad(TpOperand h, TpOpera
           const auto hi = __builtin_amdgcn_permlane32_swap(v[0][1], v[1][1], false, false);
           const u32x4 o{(unsigned)lo[0], (unsigned)hi[0], (unsigned)lo[1], (unsigned)hi[1]};
           if (label < L)
-            *reinterpret_cast<u32x4*>((T*)dw.data + label * dw.ld + 32 * wu + 8 * (q + g)) = o;
+            *reinterpret_cast<u32x4u*>((T*)dw.data + label * dw.ld + 32 * wu + 8 * (q + g)) = o;
         }
       } else if (label < L) {
 #pragma unroll

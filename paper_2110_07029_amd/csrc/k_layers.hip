@@ -198,11 +198,11 @@ static hipError_t pair_type(int dtype, const PairJob& p, hipStream_t st) {
 hipError_t launch_pair(int dtype, const PairJob& p, hipStream_t st) {
   const bool x = p.x.job.a.base, y = p.y.job.a.base;
   hipError_t e = hipSuccess;
-  if (x + y + (p.sums.y != nullptr) > 1 && (!x || !y || p.x.shape == p.y.shape) &&
-      (x ? p.x : p.y).shape == TP_TINY) {
+  const bool several = x + y + (p.sums.y != nullptr) > 1 && (x || y);
+  const int shape = !several ? TP_LARGE : x && y && p.x.shape != p.y.shape ? TP_LARGE : (x ? p.x : p.y).shape;
+  if (shape == TP_TINY) {
     e = pair_type<TpTiny>(dtype, p, st);
-  } else if (x + y + (p.sums.y != nullptr) > 1 && (!x || !y || p.x.shape == p.y.shape) &&
-             (x ? p.x : p.y).shape == TP_SMALL) {
+  } else if (shape == TP_SMALL) {
     e = pair_type<TpSmall>(dtype, p, st);
   } else {
     e = launch_column_sums(p.sums, st);

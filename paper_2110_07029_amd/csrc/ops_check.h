@@ -32,6 +32,8 @@ asgd_status check_rules_memory(const asgd_logit_rules* r);
 
 // p is device or managed memory of the current device.
 asgd_status check_device(const void* p, const char* name);
+// The same for a device that the caller has looked up.
+asgd_status check_device_is(int dev, const void* p, const char* name);
 asgd_status check_stream(void* hip_stream);
 asgd_status check_workspace(const void* ws, size_t have, size_t need);
 

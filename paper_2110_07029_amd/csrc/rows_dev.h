@@ -10,21 +10,29 @@ namespace asgd {
 typedef _Float16 f16;
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 
+// Vectors at any element's address (the hardware takes them; eight accesses of 2 bytes instead cost a layer of
+// 777 x 1,001 x 515 out of line @@ us).
+typedef float f32x4u __attribute__((ext_vector_type(4), aligned(4)));
+typedef __bf16 bf16x8u __attribute__((ext_vector_type(8), aligned(2)));
+typedef _Float16 f16x8u __attribute__((ext_vector_type(8), aligned(2)));
+typedef __bf16 bf16x4u __attribute__((ext_vector_type(4), aligned(2)));
+typedef _Float16 f16x4u __attribute__((ext_vector_type(4), aligned(2)));
+
 // v[i] = element (row, col + i), i < n <= 8; zeros from n on.
 __device__ __forceinline__ void load8(const MatDev& m, int64_t row, int col, int n, float v[8]) {
   const int64_t at = row * m.ld + col;
-  if (m.vec && n == 8) {
+  if (n == 8) {
     if (m.dtype == 0) {
-      const f32x4* p = reinterpret_cast<const f32x4*>((const float*)m.data + at);
+      const f32x4u* p = reinterpret_cast<const f32x4u*>((const float*)m.data + at);
       const f32x4 a = p[0], b = p[1];
 #pragma unroll
       for (int i = 0; i < 4; ++i) { v[i] = a[i]; v[4 + i] = b[i]; }
     } else if (m.dtype == 1) {
-      const bf16x8 a = *reinterpret_cast<const bf16x8*>((const bf16*)m.data + at);
+      const bf16x8 a = *reinterpret_cast<const bf16x8u*>((const bf16*)m.data + at);
 #pragma unroll
       for (int i = 0; i < 8; ++i) v[i] = (float)a[i];
     } else {
-      const f16x8 a = *reinterpret_cast<const f16x8*>((const f16*)m.data + at);
+      const f16x8 a = *reinterpret_cast<const f16x8u*>((const f16*)m.data + at);
 #pragma unroll
       for (int i = 0; i < 8; ++i) v[i] = (float)a[i];
     }
@@ -42,21 +50,21 @@ __device__ __forceinline__ void load8(const MatDev& m, int64_t row, int col, int
 // Element (row, col + i) = v[i], i < n <= 8, rounded to nearest.
 __device__ __forceinline__ void store8(const MatDev& m, int64_t row, int col, int n, const float v[8]) {
   const int64_t at = row * m.ld + col;
-  if (m.vec && n == 8) {
+  if (n == 8) {
     if (m.dtype == 0) {
-      f32x4* p = reinterpret_cast<f32x4*>((float*)m.data + at);
+      f32x4u* p = reinterpret_cast<f32x4u*>((float*)m.data + at);
       p[0] = f32x4{v[0], v[1], v[2], v[3]};
       p[1] = f32x4{v[4], v[5], v[6], v[7]};
     } else if (m.dtype == 1) {
       bf16x8 a;
 #pragma unroll
       for (int i = 0; i < 8; ++i) a[i] = (bf16)v[i];
-      *reinterpret_cast<bf16x8*>((bf16*)m.data + at) = a;
+      *reinterpret_cast<bf16x8u*>((bf16*)m.data + at) = a;
     } else {
       f16x8 a;
 #pragma unroll
       for (int i = 0; i < 8; ++i) a[i] = (f16)v[i];
-      *reinterpret_cast<f16x8*>((f16*)m.data + at) = a;
+      *reinterpret_cast<f16x8u*>((f16*)m.data + at) = a;
     }
     return;
   }
@@ -72,14 +80,13 @@ __device__ __forceinline__ void store8(const MatDev& m, int64_t row, int col, in
 // Element (row, col + i) = v[i], i < min(n, 4).
 __device__ __forceinline__ void store4(const MatDev& m, int64_t row, int col, int n, const float v[4]) {
   const int64_t at = row * m.ld + col;
-  if (m.vec && n >= 4) {
+  if (n >= 4) {
     if (m.dtype == 0) {
-      *reinterpret_cast<f32x4*>((float*)m.data + at) = f32x4{v[0], v[1], v[2], v[3]};
+      *reinterpret_cast<f32x4u*>((float*)m.data + at) = f32x4{v[0], v[1], v[2], v[3]};
     } else if (m.dtype == 1) {
-      *reinterpret_cast<bf16x4*>((bf16*)m.data + at) = bf16x4{(bf16)v[0], (bf16)v[1], (bf16)v[2], (bf16)v[3]};
+      *reinterpret_cast<bf16x4u*>((bf16*)m.data + at) = bf16x4{(bf16)v[0], (bf16)v[1], (bf16)v[2], (bf16)v[3]};
     } else {
-      typedef f16 f16x4v __attribute__((ext_vector_type(4)));
-      *reinterpret_cast<f16x4v*>((f16*)m.data + at) = f16x4v{(f16)v[0], (f16)v[1], (f16)v[2], (f16)v[3]};
+      *reinterpret_cast<f16x4u*>((f16*)m.data + at) = f16x4u{(f16)v[0], (f16)v[1], (f16)v[2], (f16)v[3]};
     }
     return;
   }

@@ -47,8 +47,8 @@ inline TpPlan tp_plan(int dtype, int m, int n, int64_t k, int max_splits) {
   // Splits of k cost a launch that joins them: long k of few tiles alone.
   int64_t s = 1;
   if (split_large) s = 256 / tiles;
-  else if (p.shape != TP_LARGE && tiles <= 256 && steps >= 64) s = 512 / tiles;
-  s = s < steps / 16 ? s : steps / 16;
+  else if (p.shape != TP_LARGE && tiles <= 256 && steps >= 24) s = 512 / tiles;
+  s = s < steps / 8 ? s : steps / 8;
   s = s < max_splits ? s : max_splits;
   if (s < 1) s = 1;
   const int64_t per = ceil_div(steps, s);
