@@ -96,10 +96,22 @@ __device__ __forceinline__ void nw_logits(const char* w, const char* bias, const
                                           f32x16 (&z)[2]) {
   const int n = lane & 31, g = lane >> 5;
   nw_bias(bias, g, z);
+  // (what a product reads from LDS is on its way while the ones before run)
+  typename TpMma<T>::frag8 f[3][2];
+  auto read = [&](int kk) {
 #pragma unroll
-  for (int kk = 0; kk < 8; ++kk)
+    for (int b = 0; b < 2; ++b) f[kk % 3][b] = nw_row_frag<T>(w, 32 * b + n, kk, g);
+  };
+  read(0);
+  read(1);
 #pragma unroll
-    for (int b = 0; b < 2; ++b) z[b] = tp_mma(nw_row_frag<T>(w, 32 * b + n, kk, g), hf[kk], z[b]);
+  for (int kk = 0; kk < 8; ++kk) {
+    if (kk + 2 < 8) read(kk + 2);
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int b = 0; b < 2; ++b) z[b] = tp_mma(f[kk % 3][b], hf[kk], z[b]);
+    __builtin_amdgcn_sched_barrier(0);
+  }
 }
 
 }  // namespace
@@ -386,15 +398,20 @@ __global__ __launch_bounds__(NW_THREADS) void k_narrow_grad(TpOperand h, TpOpera
       sums[wave * NW_TILE + 32 * (n >> 4) + 8 * ((n >> 2) & 3) + 4 * g + (n & 3)] = nw_sum_lanes(v, lane);
     }
     // dz W: k are the labels in the accumulators' order, 16 c + 8 hi + 4 g + 0..3 of a block
+    Frag uf[4];
+    auto w_read = [&](int k) {  // k = 8 b + 4 c + u
+      const char* const q = p + 256 * (16 * (k >> 2));
+      uf[k & 3] = nw_join<T>(tp_turned<T>(q + wat[0][k & 3]), tp_turned<T>(q + wat[1][k & 3]));
+    };
 #pragma unroll
-    for (int b = 0; b < 2; ++b)
+    for (int k = 0; k < 3; ++k) w_read(k);
 #pragma unroll
-      for (int c = 0; c < 2; ++c)
-#pragma unroll
-        for (int u = 0; u < 4; ++u) {
-          const char* q = p + 256 * (32 * b + 16 * c);
-          dh[u] = tp_mma(nw_join<T>(tp_turned<T>(q + wat[0][u]), tp_turned<T>(q + wat[1][u])), df[b][c], dh[u]);
-        }
+    for (int k = 0; k < 16; ++k) {
+      if (k + 3 < 16) w_read(k + 3);
+      __builtin_amdgcn_sched_barrier(0);
+      dh[k & 3] = tp_mma(uf[k & 3], df[k >> 3][(k >> 2) & 1], dh[k & 3]);
+      __builtin_amdgcn_sched_barrier(0);
+    }
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     __builtin_amdgcn_s_barrier();  // dz of all rows is here
     if (db && tid < NW_TILE && t * NW_TILE + tid < L) {
@@ -407,11 +424,20 @@ __global__ __launch_bounds__(NW_THREADS) void k_narrow_grad(TpOperand h, TpOpera
       f32x16 acc;
 #pragma unroll
       for (int r = 0; r < 16; ++r) acc[r] = 0.0f;
+      // (what a product reads from LDS is on its way while the one before runs)
+      Frag hd[2], zd[2];
+      auto read = [&](int c) {
+        const char *zp = dzt + 4096 * (c >> 1), *hp = smem + NWG_H + 4096 * c;
+        hd[c & 1] = nw_join<T>(tp_turned<T>(hp + hat[0]), tp_turned<T>(hp + hat[1]));
+        zd[c & 1] = nw_join<T>(tp_turned<T>(zp + zat[0][c & 1]), tp_turned<T>(zp + zat[1][c & 1]));
+      };
+      read(0);
 #pragma unroll
       for (int c = 0; c < NW_ROWS / 16; ++c) {
-        const char *zp = dzt + 4096 * (c >> 1), *hp = smem + NWG_H + 4096 * c;
-        acc = tp_mma(nw_join<T>(tp_turned<T>(hp + hat[0]), tp_turned<T>(hp + hat[1])),
-                     nw_join<T>(tp_turned<T>(zp + zat[0][c & 1]), tp_turned<T>(zp + zat[1][c & 1])), acc);
+        if (c + 1 < NW_ROWS / 16) read(c + 1);
+        __builtin_amdgcn_sched_barrier(0);
+        acc = tp_mma(hd[c & 1], zd[c & 1], acc);
+        __builtin_amdgcn_sched_barrier(0);
       }
       const int label = t * NW_TILE + 32 * lb + n;
       if (wide) {

@@ -118,23 +118,44 @@ __device__ __forceinline__ Normal normal_of(float a) {
 __device__ __forceinline__ float logistic(float a) {
   return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-LOG2E * a));
 }
-__device__ __forceinline__ float act_value(int act, float a) {
-  if (act == 1) return a > 0.0f ? a : a == a ? 0.0f : a;  // (NaN stays)
-  if (act == 2) return a == -INFINITY ? 0.0f : a * normal_of(a).cdf;
-  if (act == 3) return a == -INFINITY ? 0.0f : a * logistic(a);
-  return a;
+__device__ __forceinline__ float relu_value(float a) { return a > 0.0f ? a : a == a ? 0.0f : a; }  // (NaN stays)
+__device__ __forceinline__ float gelu_value(float a) { return a == -INFINITY ? 0.0f : a * normal_of(a).cdf; }
+__device__ __forceinline__ float silu_value(float a) { return a == -INFINITY ? 0.0f : a * logistic(a); }
+__device__ __forceinline__ float relu_slope(float a) { return a > 0.0f ? 1.0f : a == a ? 0.0f : a; }
+__device__ __forceinline__ float gelu_slope(float a) {
+  const Normal n = normal_of(a);
+  return n.cdf + (n.density == 0.0f ? 0.0f : a * n.density);  // (0, not infinity times 0, at infinity)
 }
-__device__ __forceinline__ float act_slope(int act, float a) {
-  if (act == 1) return a > 0.0f ? 1.0f : a == a ? 0.0f : a;
-  if (act == 2) {
-    const Normal n = normal_of(a);
-    return n.cdf + (n.density == 0.0f ? 0.0f : a * n.density);  // (0, not infinity times 0, at infinity)
+__device__ __forceinline__ float silu_slope(float a) {
+  const float g = logistic(a), r = 1.0f - g;
+  return g + (g == 0.0f || r == 0.0f ? 0.0f : a * g * r);
+}
+// Eight at a time, so that their chains of dependent steps run side by side (one element per branch: a layer's gradients
+// of 8,192 x 4,096 @@ us).
+__device__ __forceinline__ void act8(int act, float v[8]) {
+  if (act == 1) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = relu_value(v[i]);
+  } else if (act == 2) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = gelu_value(v[i]);
+  } else if (act == 3) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = silu_value(v[i]);
   }
-  if (act == 3) {
-    const float g = logistic(a), r = 1.0f - g;
-    return g + (g == 0.0f || r == 0.0f ? 0.0f : a * g * r);
+}
+// v[i] *= act'(a[i])
+__device__ __forceinline__ void slope8(int act, const float a[8], float v[8]) {
+  if (act == 1) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] *= relu_slope(a[i]);
+  } else if (act == 2) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] *= gelu_slope(a[i]);
+  } else if (act == 3) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] *= silu_slope(a[i]);
   }
-  return 1.0f;
 }
 
 // ---- dropout -----------------------------------------------------------------------
@@ -167,10 +188,7 @@ __device__ __forceinline__ void dense_out8(const DenseEpi& e, const float b[8], 
 #pragma unroll
   for (int i = 0; i < 8; ++i) v[i] += b[i];
   if (e.pre.data) store8(e.pre, row, col, n, v);
-  if (e.act) {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = act_value(e.act, v[i]);
-  }
+  act8(e.act, v);
   if (e.drop.below) drop8(e.drop, row, col, v);
   if (e.res.data) {
     float r[8];
