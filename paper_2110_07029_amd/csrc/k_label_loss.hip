@@ -246,16 +246,13 @@ struct EpiDzT {
     constexpr int PER = S::THREADS / S::BM;
     const int r = threadIdx.x / PER, row = row0 + r;
     if (row < m && a.y.indptr) {
-      int q0, q1;
-      label_range(a.y, row, &q0, &q1);
-      for (int q = q0 + (int)threadIdx.x % PER; q < q1; q += PER) {
-        const int id = a.y.indices[q];
+      each_label(a.y, row, (int)threadIdx.x % PER, PER, [&](int id) {
         const int c = id - a.label0 - col0;
-        if (c >= 0 && c < S::BN && id < a.n_labels) {
+        if (id >= 0 && c >= 0 && c < S::BN && id < a.n_labels) {
           const int at = atomicAdd(hits, 1);
           if (at < HITS) hits[1 + at] = r << 16 | c;
         }
-      }
+      });
     }
   }
   // Fills the wave's block of counts for rows r0 .. + 31, columns c0 .. ; false: none.
@@ -283,12 +280,10 @@ struct EpiDzT {
         if (r >= 0 && r < 32 && c >= 0 && c < S::WCOLS) atomicAdd(counts + r * S::OUT_LD + c, 1u);
       }
     } else if (r0 + (lane >> 1) < m) {
-      int q0, q1;
-      label_range(a.y, r0 + (lane >> 1), &q0, &q1);
-      for (int q = q0 + (lane & 1); q < q1; q += 2) {
-        const int id = a.y.indices[q], c = id - a.label0 - c0;
-        if (c >= 0 && c < S::WCOLS && id < a.n_labels) atomicAdd(counts + (lane >> 1) * S::OUT_LD + c, 1u);
-      }
+      each_label(a.y, r0 + (lane >> 1), lane & 1, 2, [&](int id) {
+        const int c = id - a.label0 - c0;
+        if (id >= 0 && c >= 0 && c < S::WCOLS && id < a.n_labels) atomicAdd(counts + (lane >> 1) * S::OUT_LD + c, 1u);
+      });
     }
     __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "wavefront");
     return true;

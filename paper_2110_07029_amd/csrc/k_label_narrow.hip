@@ -285,15 +285,12 @@ __global__ __launch_bounds__(NW_THREADS) void k_narrow_grad(TpOperand h, TpOpera
   __builtin_amdgcn_s_barrier();
   const int l0 = t0 * NW_TILE, l1 = min(L, t1 * NW_TILE);
   if ((tid >> 1) < B && a.y.indptr) {
-    int q0, q1;
-    label_range(a.y, tid >> 1, &q0, &q1);
-    for (int q = q0 + (tid & 1); q < q1; q += 2) {
-      const int id = a.y.indices[q];
+    each_label(a.y, tid >> 1, tid & 1, 2, [&](int id) {
       if (id >= l0 && id < l1) {
         const int at = atomicAdd(hits, 1);
         if (at < NWG_HITS) hits[1 + at] = (tid >> 1) << 23 | (id - l0);
       }
-    }
+    });
   }
   f32x16 dh[4];
 #pragma unroll
@@ -348,12 +345,10 @@ __global__ __launch_bounds__(NW_THREADS) void k_narrow_grad(TpOperand h, TpOpera
           if ((int)((unsigned)hit >> 28) == wave && c >= 0 && c < NW_TILE) add(((unsigned)hit >> 23) & 31, c);
         }
       } else if (32 * wave + (lane >> 1) < B) {
-        int q0, q1;
-        label_range(a.y, 32 * wave + (lane >> 1), &q0, &q1);
-        for (int q = q0 + (lane & 1); q < q1; q += 2) {
-          const int id = a.y.indices[q], c = id - t * NW_TILE;
-          if (c >= 0 && c < NW_TILE && id < L) add(lane >> 1, c);
-        }
+        each_label(a.y, 32 * wave + (lane >> 1), lane & 1, 2, [&](int id) {
+          const int c = id - t * NW_TILE;
+          if (id >= 0 && c >= 0 && c < NW_TILE && id < L) add(lane >> 1, c);
+        });
       }
       __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "wavefront");
     }

@@ -12,6 +12,21 @@ __device__ __forceinline__ void label_range(const IdLists& y, int i, int* q0, in
   *q1 = min(*q1, *q0 + 65535);
 }
 
+// Calls take(id) for every `step`-th entry of row i from `first` on, eight loads at a time (one at a time, lists of 75 ids cost
+// more than a tile's products).
+template <class F>
+__device__ __forceinline__ void each_label(const IdLists& y, int i, int first, int step, F take) {
+  int q0, q1;
+  label_range(y, i, &q0, &q1);
+  for (int q = q0 + first; q < q1; q += 8 * step) {
+    int id[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) id[k] = q + k * step < q1 ? y.indices[q + k * step] : -1;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) take(id[k]);
+  }
+}
+
 // How dz is formed from z.
 struct DzArgs {
   const float* bias;   // of the piece's first label

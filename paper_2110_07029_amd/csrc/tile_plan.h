@@ -16,6 +16,10 @@ using TpTiny = TpShape<32, 32, 1, 1, 8, 4>;
 enum { TP_LARGE = 0, TP_MEDIUM = 1, TP_SMALL = 2, TP_FEW = 3, TP_TINY = 4 };
 constexpr int TP_BM[] = {256, 128, 64, 32, 32}, TP_BN[] = {256, 128, 64, 128, 32};
 
+// Up to so many steps of k large tiles spend too much of their time around the loop: gradients of 732 rows, 26,436
+// labels, width 763 (12 steps) 333 us with them, 264 without; a layer of 8,192 x 4,096 with 16 steps 120, 124 without.
+constexpr int SHORT_K = 12;
+
 struct TpPlan {
   int shape;
   TpJob job;
@@ -25,31 +29,38 @@ inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 inline int elem_size(int dtype) { return dtype == 0 ? 4 : 2; }
 
 // Shape and splits of a product of m x n over k; max_splits 1: the epilogue needs whole sums.
+//   large tiles   where they fill the chip and k is long enough that what surrounds the loop (1 workgroup per CU) is
+//                 little; also where few of them with a long k are worth their slabs
+//   medium, small where they fill it, with k split if that takes a long k and (medium) enough work to pay for the slabs
+//   few           up to 32 rows of many columns; tiny: everything else, latency counts
+// (The label loss of 326 rows, 82,407 labels, width 538, whose dz W has 326 x 538 sums over 82,407: 548 us with tiny tiles
+// for them, 354 with medium ones.)
 inline TpPlan tp_plan(int dtype, int m, int n, int64_t k, int max_splits) {
   TpPlan p{};
   TpJob& j = p.job;
   j.m = m;
   j.n = n;
   j.k = k;
+  const int kb = TP_STEP / elem_size(dtype);
   const int64_t large = ceil_div(m, 256) * ceil_div(n, 256), medium = ceil_div(m, 128) * ceil_div(n, 128);
-  // (large tiles, too, where few of them have so long a k that their slabs cost less than they gain)
+  const int64_t small = ceil_div(m, 64) * ceil_div(n, 64), steps = ceil_div(k, kb);
+  int64_t most = steps / 8 < max_splits ? steps / 8 : max_splits;
+  if (most < 1 || steps < 24) most = 1;
   const bool split_large = large >= 48 && large < 192 && max_splits > 1 && k * large >= 8192ll * 256;
-  const int64_t small = ceil_div(m, 64) * ceil_div(n, 64);
-  p.shape = m <= 32             ? (n > 192 * 128 ? TP_FEW : TP_TINY)
-            : large >= 192 || split_large ? TP_LARGE
-            : medium >= 192     ? TP_MEDIUM
-            : small >= 128      ? TP_SMALL
-                                : TP_TINY;
+  const bool much = (double)m * n * k >= 1e10;
+  p.shape = m <= 32                                           ? (n > 192 * 128 ? TP_FEW : TP_TINY)
+            : (large >= 192 && steps > SHORT_K) || split_large ? TP_LARGE
+            : medium >= 192 || (much && medium * most >= 256)  ? TP_MEDIUM
+            : small * most >= 128                              ? TP_SMALL
+                                                               : TP_TINY;
   j.tiles_m = (int)ceil_div(m, TP_BM[p.shape]);
   j.tiles_n = (int)ceil_div(n, TP_BN[p.shape]);
-  const int kb = TP_STEP / elem_size(dtype);
-  const int64_t steps = ceil_div(k, kb), tiles = (int64_t)j.tiles_m * j.tiles_n;
-  // Splits of k cost a launch that joins them: long k of few tiles alone.
+  const int64_t tiles = (int64_t)j.tiles_m * j.tiles_n;
+  // splits of k cost a launch that joins them: long k of few tiles alone
   int64_t s = 1;
   if (split_large) s = 256 / tiles;
-  else if (p.shape != TP_LARGE && tiles <= 256 && steps >= 24) s = 512 / tiles;
-  s = s < steps / 8 ? s : steps / 8;
-  s = s < max_splits ? s : max_splits;
+  else if (p.shape != TP_LARGE && tiles <= 256) s = 512 / tiles;
+  s = s < most ? s : most;
   if (s < 1) s = 1;
   const int64_t per = ceil_div(steps, s);
   j.splits = (int)ceil_div(steps, per);
