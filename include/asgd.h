@@ -539,8 +539,8 @@ enum { ASGD_ACT_NONE = 0, ASGD_ACT_RELU = 1, ASGD_ACT_GELU = 2, ASGD_ACT_SILU = 
 /* What follows a product A = X W^T + bias:
  *   Y = residual + drop(act(A))
  * act: none, max(a, 0), a Phi(a) with the normal distribution function Phi,
- * or a / (1 + e^-a).  drop as for asgd_dropout, on Y's rows and columns.  Zero-initialise the
- * struct for the product alone. */
+ * or a / (1 + e^-a).  drop as for asgd_dropout, on Y's rows and columns.
+ * Zero-initialise the struct for the product alone. */
 typedef struct asgd_epilogue {
   const float* bias;           /* device [n], or NULL */
   int32_t act;                 /* ASGD_ACT_... */
@@ -549,8 +549,8 @@ typedef struct asgd_epilogue {
   const asgd_matrix* residual; /* [m x n], any type, or NULL */
 } asgd_epilogue;
 
-/* A dense layer: x [m x k], w [n x k] of one type, y [m x n] of any type,
- * which may be the residual itself.  pre (NULL, or [m x n] of any type)
+/* A dense layer: x [m x k], w [n x k] of one type with k at most 2^20 (ERANGE),
+ * y [m x n] of any type, which may be the residual itself.  pre (NULL, or [m x n] of any type)
  * receives A for the backward pass; the activation is formed from A before
  * it is rounded to pre's type.  ep may be NULL. */
 asgd_status asgd_dense_workspace(const asgd_matrix* x, const asgd_matrix* w, size_t* bytes);
@@ -573,27 +573,29 @@ asgd_status asgd_dense_backward(const asgd_matrix* dy, const asgd_matrix* x, con
  * 32 random bits are floor(p 2^32) or more, and is 0 elsewhere (infinities and
  * NaN too).  The bits of (row i, column j) are half j % 2 (0: the low one) of
  *   splitmix64(splitmix64(seed) ^ (i 2^22 + j / 2)),
- * a function of seed and place alone: the mask is never stored, and the same call on
- * dy is the backward pass.  x, residual (or NULL) and y are of one shape and
+ * a function of seed and place alone: the mask is never stored, and the same
+ * call on dy is the backward pass.  x, residual (or NULL) and y are of one shape and
  * any types; y may be x or the residual itself. */
 asgd_status asgd_dropout(const asgd_matrix* x, double p, uint64_t seed, const asgd_matrix* residual,
                          const asgd_matrix* y, void* hip_stream);
 
 /* Softmax cross-entropy of rows h [B x D] against a label matrix w [L x D] of
- * the same type (L below 2^22), without the logits in memory, and its gradients:
+ * the same type (L below 2^22, D at most 2^20), without the logits in memory, and its gradients:
  *   z_ij = h_i . w_j + bias_j, lse_i = ln sum_j e^z_ij, n_i = |y_i|
  *   loss_i = lse_i - (1 / n_i) sum of z_ij over the entries j of y_i
  *   dz_ij = weight_i (e^(z_ij - lse_i) - c_ij / n_i), c_ij = times that j stands in y_i
  *   dh = dz W, dw = dz^T h, db_j = sum_i dz_ij   (the gradients of sum_i weight_i loss_i)
- * y: lists per row (values ignored); ids outside [0, L) are skipped and not
- * counted.  A row without counted entries has loss 0 and takes no part in any gradient, whatever
- * it holds (its lse is written all the same).  bias: device float [L] or NULL; weights:
- * device float [B] or NULL for 1 / B; loss_rows and lse (or NULL): device
- * float [B]; dh, dw (any type) and db: each may be NULL.  All but loss_rows NULL: the loss alone, which
- * asks for the workspace of gradients = 0, otherwise 1.
+ * y: lists per row (values ignored), of which the first 65,535 entries of a row
+ * are taken; ids outside [0, L) are skipped and not counted.  A row without
+ * counted entries has loss 0 and takes no part in any gradient, whatever it
+ * holds (its lse is written all the same).  bias: device float [L] or NULL;
+ * weights: device float [B] or NULL for 1 / B; loss_rows and lse (or NULL):
+ * device float [B]; dh, dw (any type) and db: each may be NULL.  Without any of
+ * the three the workspace of gradients = 0 is enough, otherwise it is that of 1.
  * In 16 bits dz is rounded once to h's type for its two products; db is
- * formed before that.  A logit that is NaN or +inf makes its row's loss and gradients NaN, and dw and db with them; a
- * label of logit -inf has probability 0. */
+ * formed before that.  A logit that is NaN or +inf makes its row's loss and
+ * gradients NaN, and dw and db with them; a label of logit -inf has
+ * probability 0. */
 asgd_status asgd_label_loss_workspace(const asgd_matrix* h, const asgd_matrix* w, int32_t gradients, size_t* bytes);
 asgd_status asgd_label_loss(const asgd_matrix* h, const asgd_matrix* w, const float* bias, const asgd_csr* y,
                             const float* weights, float* loss_rows, float* lse, const asgd_matrix* dh,

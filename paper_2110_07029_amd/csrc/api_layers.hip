@@ -76,13 +76,19 @@ DropDev drop_dev(double p, uint64_t seed) {
   return DropDev{splitmix(seed), (uint32_t)floor(p * 4294967296.0), (float)(1.0 / (1.0 - p))};
 }
 
+// Columns that a product is summed over: the offsets of a tile's copies are 32 bits, which its 256 rows of 4 MiB fill.
+asgd_status check_sum(const asgd_matrix* a, const char* name) {
+  if (a->n_cols > 1 << 20) return set_error_named(ASGD_ERANGE, name, ": more than 2^20 columns");
+  return ASGD_OK;
+}
+
 // x [m x k] and w [n x k] of a layer.
 asgd_status check_layer(const asgd_matrix* x, const asgd_matrix* w) {
   TRY(check_matrix(x, "x"));
   TRY(check_matrix(w, "w"));
   if (x->n_cols != w->n_cols) return set_error(ASGD_EINVAL, "x and w differ in columns");
   if (x->dtype != w->dtype) return set_error(ASGD_EINVAL, "x and w differ in type");
-  return ASGD_OK;
+  return check_sum(x, "x");
 }
 
 asgd_status check_epilogue(const asgd_epilogue* e) {
@@ -97,7 +103,7 @@ asgd_status check_rows(const asgd_matrix* h, const asgd_matrix* w) {
   TRY(check_matrix(w, "w", true));
   if (h->n_cols != w->n_cols) return set_error(ASGD_EINVAL, "h and w differ in columns");
   if (h->dtype != w->dtype) return set_error(ASGD_EINVAL, "h and w differ in type");
-  return ASGD_OK;
+  return check_sum(h, "h");
 }
 
 // The current device, which everything has to be on.

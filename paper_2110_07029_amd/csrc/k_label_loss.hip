@@ -154,12 +154,12 @@ __global__ __launch_bounds__(256) void k_loss_rows(const float2* __restrict__ pa
     label_range(y, i, &q0, &q1);
     const int l = tid & 15;
     constexpr int E = 4;  // entries on their way at once (75 of them in 1,024 rows: 13 us one at a time)
-    for (int q = q0 + (tid >> 4); q < q1; q += 16 * E) {
+    for (int o = tid >> 4; o < q1 - q0; o += 16 * E) {
       int id[E];
       float d[E];
 #pragma unroll
       for (int e = 0; e < E; ++e) {
-        id[e] = q + 16 * e < q1 ? entry(y, q + 16 * e, L) : -1;
+        id[e] = o + 16 * e < q1 - q0 ? entry(y, q0 + o + 16 * e, L) : -1;
         d[e] = 0.0f;
       }
       for (int c = V * l; c < D; c += V * 16) {
@@ -248,7 +248,7 @@ struct EpiDzT {
     if (row < m && a.y.indptr) {
       each_label(a.y, row, (int)threadIdx.x % PER, PER, [&](int id) {
         const int c = id - a.label0 - col0;
-        if (id >= 0 && c >= 0 && c < S::BN && id < a.n_labels) {
+        if (c >= 0 && c < S::BN && id < a.n_labels) {
           const int at = atomicAdd(hits, 1);
           if (at < HITS) hits[1 + at] = r << 16 | c;
         }
@@ -282,7 +282,7 @@ struct EpiDzT {
     } else if (r0 + (lane >> 1) < m) {
       each_label(a.y, r0 + (lane >> 1), lane & 1, 2, [&](int id) {
         const int c = id - a.label0 - c0;
-        if (id >= 0 && c >= 0 && c < S::WCOLS && id < a.n_labels) atomicAdd(counts + (lane >> 1) * S::OUT_LD + c, 1u);
+        if (c >= 0 && c < S::WCOLS && id < a.n_labels) atomicAdd(counts + (lane >> 1) * S::OUT_LD + c, 1u);
       });
     }
     __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "wavefront");

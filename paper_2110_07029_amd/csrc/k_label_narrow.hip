@@ -347,7 +347,7 @@ __global__ __launch_bounds__(NW_THREADS) void k_narrow_grad(TpOperand h, TpOpera
       } else if (32 * wave + (lane >> 1) < B) {
         each_label(a.y, 32 * wave + (lane >> 1), lane & 1, 2, [&](int id) {
           const int c = id - t * NW_TILE;
-          if (id >= 0 && c >= 0 && c < NW_TILE && id < L) add(lane >> 1, c);
+          if (c >= 0 && c < NW_TILE && id < L) add(lane >> 1, c);
         });
       }
       __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "wavefront");

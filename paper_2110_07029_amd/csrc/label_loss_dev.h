@@ -9,21 +9,24 @@ namespace asgd {
 // Entries of row i: the first 65,535 of them (counts of a label in a row then fit 16 bits).
 __device__ __forceinline__ void label_range(const IdLists& y, int i, int* q0, int* q1) {
   list_range(y, i, q0, q1);
-  *q1 = min(*q1, *q0 + 65535);
+  if (*q1 - *q0 > 65535) *q1 = *q0 + 65535;
 }
 
-// Calls take(id) for every `step`-th entry of row i from `first` on, eight loads at a time (one at a time, lists of 75 ids cost
-// more than a tile's products).
+// Calls take(id) for every `step`-th entry of row i from `first` on that is not negative, eight loads at a time (one at a
+// time, lists of 75 ids cost more than a tile's products).
 template <class F>
 __device__ __forceinline__ void each_label(const IdLists& y, int i, int first, int step, F take) {
   int q0, q1;
   label_range(y, i, &q0, &q1);
-  for (int q = q0 + first; q < q1; q += 8 * step) {
+  const int32_t* const list = y.indices + q0;
+  const int n = q1 - q0;
+  for (int q = first; q < n; q += 8 * step) {
     int id[8];
 #pragma unroll
-    for (int k = 0; k < 8; ++k) id[k] = q + k * step < q1 ? y.indices[q + k * step] : -1;
+    for (int k = 0; k < 8; ++k) id[k] = q + k * step < n ? list[q + k * step] : -1;
 #pragma unroll
-    for (int k = 0; k < 8; ++k) take(id[k]);
+    for (int k = 0; k < 8; ++k)
+      if (id[k] >= 0) take(id[k]);
   }
 }
 

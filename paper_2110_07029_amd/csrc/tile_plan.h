@@ -80,8 +80,17 @@ hipError_t tp_launch_shape(const TpJob& j, const typename Epi::Args& ea, hipStre
   const auto fn = k_tile_product<T, AK, BK, S, Epi>;
   const hipError_t e = tp_allow_lds((const void*)fn, lds);
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL(fn, dim3(tp_blocks(j)), dim3(S::THREADS), lds, st, j, ea);
-  return hipGetLastError();
+  // (a launch has less than 2^32 threads)
+  constexpr int MOST = 1 << 22;
+  TpJob part = j;
+  for (int64_t b = 0; b < tp_blocks(j); b += MOST) {
+    part.block0 = (int)b;
+    const int64_t n = tp_blocks(j) - b < MOST ? tp_blocks(j) - b : MOST;
+    hipLaunchKernelGGL(fn, dim3((unsigned)n), dim3(S::THREADS), lds, st, part, ea);
+    const hipError_t r = hipGetLastError();
+    if (r != hipSuccess) return r;
+  }
+  return hipSuccess;
 }
 
 template <typename T, bool AK, bool BK, template <class> class Epi>

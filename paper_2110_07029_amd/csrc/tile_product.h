@@ -204,6 +204,7 @@ struct TpJob {
   int tiles_m, tiles_n, splits;
   int64_t split_k;   // k per split, a multiple of the step's
   int group;         // tiles of m that share their tiles of n in a row of the launch order
+  int block0;        // this launch's first workgroup
 };
 
 // Launch order: workgroups go to the 8 XCDs in turn, so XCD x takes every 8th; consecutive tiles of one
@@ -249,7 +250,9 @@ __device__ __forceinline__ void tp_staged8(const float* out, int r, int c, float
 // lane (g, i) holds row i, columns 32 b + 8 q + 4 g + 0..3; end() with the whole workgroup.
 //
 // Fragments are read one chunk of k ahead of their products, over the barrier too: after it the first reads of
-// the new step go out, then the last products of the old one.  (4,096 x 32,001 x 2,048 in bf16: @@.)
+// the new step go out, then the last products of the old one (log-sum-exp of 4,096 x 32,001 over 2,048 in bf16: 544 us without, 484 with.
+// Also measured: steps of 64 bytes in four buffers 531, four waves of 128 x 128 each 532, lines touched ahead of their
+// copies 2,200 for the whole loss against 2,063; the products alone, without a copy or a read, take 380).
 template <typename T, bool AK, bool BK, class S, class Epi>
 __device__ __forceinline__ void tp_tile(const TpJob& j, const typename Epi::Args& ea, int block, char* smem) {
   int tm, tn, split;
@@ -366,7 +369,7 @@ __device__ __forceinline__ void tp_tile(const TpJob& j, const typename Epi::Args
 template <typename T, bool AK, bool BK, class S, class Epi>
 __global__ __launch_bounds__(S::THREADS) void k_tile_product(TpJob j, typename Epi::Args ea) {
   extern __shared__ __attribute__((aligned(16))) char smem[];
-  tp_tile<T, AK, BK, S, Epi>(j, ea, blockIdx.x, smem);
+  tp_tile<T, AK, BK, S, Epi>(j, ea, j.block0 + (int)blockIdx.x, smem);
 }
 
 }  // namespace asgd

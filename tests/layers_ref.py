@@ -17,7 +17,7 @@ ACTS = {"none": asgd.ASGD_ACT_NONE, "relu": asgd.ASGD_ACT_RELU, "gelu": asgd.ASG
 
 
 def kept(rows, cols, p, seed):
-    """bool [rows, cols] (numpy): which elements stay, from the documented bits."""
+    """bool [rows, cols] (numpy): which elements stay, from the documented bits; rows: their number or some of them."""
     u = np.uint64
 
     def mix(v):
@@ -27,7 +27,7 @@ def kept(rows, cols, p, seed):
         return v ^ (v >> u(31))
 
     with np.errstate(over="ignore"):
-        i, j = np.arange(rows, dtype=u)[:, None], np.arange(cols, dtype=u)
+        i, j = np.array(range(rows) if isinstance(rows, int) else rows, dtype=u)[:, None], np.arange(cols, dtype=u)
         word = mix(mix(np.array([seed], u)) ^ (i * u(2 ** 22) + j // u(2)))
     return ((word >> (u(32) * (j % u(2)))) & u(2 ** 32 - 1)) >= u(math.floor(p * 2.0 ** 32))
 

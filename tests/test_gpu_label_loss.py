@@ -318,3 +318,51 @@ def test_layers_under_the_label_loss_as_they_are_used():
         want = v[k].grad
         # sums of up to 1,500 fp32 products in a chain of five: some 5 sqrt(1500) 2^-24 of the norm, 1.2e-5; twice that
         assert float((t.cpu().double() - want).norm()) <= 2.4e-5 * float(want.norm()), k
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_very_long_lists_and_many_targets_in_a_tile(dtype):
+    # row 0 names one label 70,000 times and another 5 times behind them: the first 65,535 entries count; the other rows
+    # name so many labels that every tile has more targets than it lists
+    B, L, D = 200, 260, 40
+    h, w = placed(normal(1, B, D), dtype), placed(normal(2, L, D, scale=0.3), dtype)
+    lists = [[7] * 70000 + [9] * 5] + [list(range(i % 3, L, 2)) for i in range(1, B)]
+    c = Call(h, w, lists, normal(4, L), dtype=dtype).run()
+    c.check([[7] * 65535] + lists[1:], dtype)
+
+
+def test_more_tiles_than_a_launch_has_threads():
+    # 65,536 rows against 2^22 - 1 labels of width 136: 16.8 million tiles.  Some rows' log-sum-exp in 64 bits.
+    B, L, D = 65536, (1 << 22) - 1, 136
+    g = torch.Generator(device="cuda").manual_seed(1)
+    h = torch.randn(B, D, generator=g, device="cuda").bfloat16()
+    w = (torch.randn(L, D, generator=g, device="cuda") * 0.1).bfloat16()
+    y = torch.arange(B + 1, dtype=torch.int32, device="cuda")
+    ids = torch.randint(0, L, (B,), generator=g, device="cuda").int()
+    loss, lse = torch.full((B,), NAN, device="cuda"), torch.full((B,), NAN, device="cuda")
+    ws = torch.empty(asgd.asgd_label_loss_workspace(asgd.matrix(h), asgd.matrix(w), False), dtype=torch.uint8, device="cuda")
+    asgd.asgd_label_loss(asgd.matrix(h), asgd.matrix(w), asgd.asgd_csr(B, L, B, y.data_ptr(), ids.data_ptr(), None), loss,
+                         lse=lse, workspace=ws, stream=torch.cuda.current_stream())
+    assert bool(lse.isfinite().all()) and bool(loss.isfinite().all())
+    for i in (0, 1, 12345, 65535):
+        z = w.double() @ h[i].double()
+        want = torch.logsumexp(z, 0)
+        ez = (D + 2) * ref.U * float((w.double().abs() @ h[i].double().abs()).max())
+        # (bounds as in the reference)
+        tol = 2 * ez + (200 + 2 * L / 32768 + 4 * np.log(L)) * ref.U + 4 * ref.U * float(want)
+        assert abs(float(lse[i]) - float(want)) <= tol, (i, float(lse[i]), float(want), tol)
+        assert abs(float(loss[i]) - float(want - z[ids[i].long()])) <= 2 * tol, i
+    del w, h, ws
+    torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("B,L,D,mean,dtype", [
+    (3600, 3700, 1000, 2, "bf16"), (3600, 3700, 1000, 2, "f16"),  # large tiles of long rows
+    (256, 300, 128, 75, "bf16"), (256, 300, 128, 75, "f16"),      # narrow rows: more targets than a workgroup lists
+    (256, 20000, 120, 3, "bf16"), (255, 4097, 64, 3, "f16"),      # narrow rows: the most whose gradients take one pass, and about
+    (300, 70000, 520, 3, "bf16"), (300, 70000, 520, 3, "f16"),    # medium tiles, the sum over labels split
+    (5, 30000, 200, 3, "bf16"), (32, 30000, 200, 3, "f32")])      # few rows
+def test_sizes_behind_each_choice_of_tiles(B, L, D, mean, dtype):
+    h, w = placed(normal(1, B, D), dtype), placed(normal(2, L, D, scale=2 * D ** -0.5), dtype)
+    lists = random_lists(3, B, L, mean)
+    Call(h, w, lists, normal(4, L), dtype=dtype).run().check(lists, dtype)

@@ -326,3 +326,63 @@ def test_captured_layer_and_its_gradients():
         torch.cuda.synchronize()
         for a, b in zip(replayed, outs):
             assert torch.equal(a, b), i
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+def test_large_tiles_of_long_rows(dtype):
+    m, n, k = 3590, 3601, 1000
+    x, w, bias = placed(normal(7, m, k), dtype), placed(normal(8, n, k, scale=k ** -0.5), dtype), normal(9, n)
+    y, clean = room(m, n, dtype, 0, 7)
+    pre, clean_pre = room(m, n, "f32")
+    forward(x, w, y, pre, bias=bias, act="gelu", drop=0.1, seed=5)
+    a, ea, want, ey = ref.dense(x, w, bias, "gelu", 0.1, 5)
+    ref.near(pre, a, ea, "f32", "pre")
+    ref.near(y, want, ey, dtype, "y")
+    clean()
+    clean_pre()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_the_longest_rows(dtype):
+    # 2^20 columns, in rows of 4 MiB for floats; 300 rows of x make tiles of more than one row block
+    m, n, k = 300, 33, 1 << 20
+    g = torch.Generator(device="cuda").manual_seed(1)
+    x, w = ((torch.randn(r, k, generator=g, device="cuda") * s).to(ref.DTYPES[dtype]) for r, s in ((m, 1.0), (n, 2.0 ** -10)))
+    y, clean = room(m, n, "f32")
+    forward(x, w, y)
+    a, ea, _, _ = ref.dense(x, w)
+    ref.near(y, a, ea, "f32", "y")
+    clean()
+
+
+def test_outputs_beyond_31_bits_and_the_sums_over_their_rows():
+    # 2^20 rows of 2,100: 2.2 billion elements.  Some rows and columns against 64 bits.
+    m, n, k = 1 << 20, 2100, 16
+    g = torch.Generator(device="cuda").manual_seed(2)
+    x, w = ((torch.randn(r, k, generator=g, device="cuda")).bfloat16() for r in (m, n))
+    y = torch.full((m, n), NAN, dtype=torch.bfloat16, device="cuda")
+    forward(x, w, y, drop=0.5, seed=3)
+    rows = [0, 1, 12345, m // 2, m - 2, m - 1]
+    keep = torch.from_numpy(ref.kept(rows, n, 0.5, 3)).cuda()
+    a, ea, _, _ = ref.dense(x[rows], w)
+    ref.near(y[rows], a * keep * 2, ea * keep * 2, "bf16", "y")
+    # dw and db of a gradient of that size; a sum over 2^20 rows, so the gradient is exact in few bits: 2^-10 or 0
+    dy = y
+    for r0 in range(0, m, 1 << 16):
+        dy[r0:r0 + (1 << 16)] = ((torch.arange(r0, r0 + (1 << 16), device="cuda")[:, None]
+                                 + torch.arange(n, device="cuda")) % 5 == 0).bfloat16() * 2.0 ** -10
+    dw, db = torch.full((n, k), NAN, device="cuda"), torch.full((n,), NAN, device="cuda")
+    mx, mw = asgd.matrix(x), asgd.matrix(w)
+    asgd.asgd_dense_backward(asgd.matrix(dy), mx, mw, dw=asgd.matrix(dw), db=db,
+                             workspace=scratch(asgd.asgd_dense_backward_workspace(mx, mw)), stream=torch.cuda.current_stream())
+    at = torch.arange(m, device="cuda")
+    for j in range(5):  # (columns of equal j % 5 are alike)
+        part = x[(at + j) % 5 == 0].double()
+        want, size = part.sum(0) * 2.0 ** -10, part.abs().sum(0) * 2.0 ** -10
+        some = list(range(j, n, 5))
+        ref.near(dw[some], want.expand(len(some), k), (m + 2) * ref.U * size.expand(len(some), k), "f32", "dw")
+        assert bool((db[some] == part.shape[0] * 2.0 ** -10).all())  # (counts below 2^24: exact)
+    # and the dropout of all of it, in place
+    want = dy[rows].double()
+    asgd.asgd_dropout(asgd.matrix(dy), 0.5, 3, asgd.matrix(dy), stream=torch.cuda.current_stream())
+    assert torch.equal(dy[rows].double(), want * keep * 2)

@@ -94,6 +94,21 @@ def test_dense_layers_are_checked():
     assert lib.asgd_dense_backward_workspace(a["x"], a["w"], None) == E
 
 
+def test_sums_over_more_than_two_to_the_twenty_columns_are_refused():
+    k = 1 << 20
+    long = dict(x=mat(4, k + 1, data=at(1)), w=mat(6, k + 1, data=at(2)))
+    refused(R, "2^20 columns", dense, **long)
+    refused(R, "2^20 columns", backward, **long)
+    refused(R, "2^20 columns", asgd.asgd_dense_workspace, *long.values())
+    refused(R, "2^20 columns", asgd.asgd_dense_backward_workspace, *long.values())
+    refused(R, "2^20 columns", loss, h=long["x"], w=mat(100, k + 1, data=at(2)))
+    refused(R, "2^20 columns", asgd.asgd_label_loss_workspace, *long.values(), False)
+    refused(R, "workspace", dense, x=mat(4, k, data=at(1)), w=mat(6, k, data=at(2)), workspace=Ws(0))
+    asgd.asgd_label_loss_workspace(mat(4, k), mat(6, k), True)
+    # (a dropout of that width sums nothing)
+    refused(E, "overlaps", asgd.asgd_dropout, mat(4, k + 1), 0.1, 0, mat(4, k + 1, data=A + 4))
+
+
 def test_outputs_that_share_memory_are_refused():
     refused(E, "overlaps", dense, y=mat(4, 6, data=at(1) + 32))
     refused(E, "overlaps", dense, y=mat(4, 6, data=at(2)))
