@@ -366,3 +366,20 @@ def test_sizes_behind_each_choice_of_tiles(B, L, D, mean, dtype):
     h, w = placed(normal(1, B, D), dtype), placed(normal(2, L, D, scale=2 * D ** -0.5), dtype)
     lists = random_lists(3, B, L, mean)
     Call(h, w, lists, normal(4, L), dtype=dtype).run().check(lists, dtype)
+
+
+@pytest.mark.parametrize("B", [33000, 70000, 131073])
+def test_narrow_rows_in_many_blocks(B):
+    # each choice of ranges of labels; rows of integers in few bits, whose logits are exact
+    L, D = 700, 24
+    g = torch.Generator().manual_seed(B)
+    h, w = (torch.randint(-2, 3, s, generator=g).to(torch.bfloat16).cuda() for s in ((B, D), (L, D)))
+    ids = torch.randint(0, L, (B,), generator=g)
+    c = Call(h, w, [[i] for i in ids.tolist()], dtype="bf16", grads=()).run()
+    z = h.double() @ w.double().T
+    want = torch.logsumexp(z, 1)
+    # exponentials as in the reference; the logits are exact
+    tol = (200 + 2 * L / 32768 + 4 * np.log(L)) * ref.U + 4 * ref.U * want.abs()
+    assert bool(((c.lse[:B].double() - want).abs() <= tol).all())
+    target = z[torch.arange(B), ids.cuda()]
+    assert bool(((c.loss[:B].double() - (want - target)).abs() <= tol + 12 * ref.U * (want.abs() + target.abs())).all())
