@@ -40,7 +40,8 @@ def sources() -> list:
 # ordinary vector registers, so that the exponentials read the recomputed logits and
 # the W2 update reads dW2 without first copying them out of accumulation registers
 # (a kernel with the whole register file would otherwise get the accumulation form;
-# the operands pinned to accumulation registers stay there).
+# the operands pinned to accumulation registers stay there).  k_label_narrow.hip: the
+# same for its logits, which the softmax reads at once.
 FILE_FLAGS = {f: ["-mllvm", "-amdgpu-mfma-vgpr-form"] for f in ("k_out_bwd.hip", "k_label_narrow.hip")}
 
 

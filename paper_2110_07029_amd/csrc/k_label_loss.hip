@@ -15,7 +15,13 @@
 //     products 3, 4   dz W onto slabs of dh, dz^T h: the piece's rows of dw; column sums for db
 //   k_join        dh
 //
-// Forming z twice costs 2 B L D operations of 8; a piece's dz stays near the last caches.  dz in 16 bits is
+// Rows of 16 bits up to 128 wide take other kernels for product 1, and up to 256 of them for the gradients
+// (k_label_narrow.hip).
+//
+// 4,096 rows, 32,001 labels, width 2,048 in bf16: 1,930 to 2,090 us for four products of 537 GFLOP, 1.03 to 1.11 PFLOP/s
+// (the library's product of 8,192 cubed reaches 1.39 with k along both operands' rows, 1.21 and 1.08 in the forms that the
+// gradients' products have).  Forming z twice is the fourth product; storing dz of all labels would take 262 MB, and a loss
+// that is only read needs no dz at all.  dz in 16 bits is
 // rounded once, with the target in it (p and the target may nearly cancel); fp16 holds it times 2^15 over the
 // largest weight, so that probabilities down to 2^-29 stay normal.
 #include <math.h>
@@ -26,7 +32,9 @@ namespace asgd {
 
 namespace {
 
-constexpr int64_t PIECE_BYTES = 128ll << 20;  // of dz at a time
+// Of dz at a time: the products read it from the last cache (256 MB), and pieces are large enough to fill the chip (4,096 rows,
+// 32,001 labels, width 2,048: 2,151 us with 64 MiB, 2,078 with 128, 2,079 with 512).
+constexpr int64_t PIECE_BYTES = 128ll << 20;
 constexpr int MAX_SLABS = 64;
 typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
 
@@ -112,7 +120,7 @@ struct EpiLse {
 
 // ---- lse and loss --------------------------------------------------------------------------------
 // One workgroup per row.  Target logits are products of their own, 16 lanes each (h and w as the products read them: whole
-// 16-byte pieces).  With `scale` one workgroup more finds the gradients' scale: the largest finite |weight| of rows
+// 16-byte pieces).  With `scale` one workgroup more, the first, finds the gradients' scale: the largest finite |weight| of rows
 // that have labels, 1 / B without weights.
 template <typename T>
 __global__ __launch_bounds__(256) void k_loss_rows(const float2* __restrict__ part, int tiles, TpOperand h, TpOperand w,
@@ -123,19 +131,19 @@ __global__ __launch_bounds__(256) void k_loss_rows(const float2* __restrict__ pa
                                                    T* __restrict__ hp, int64_t ldp) {
   constexpr int V = 16 / (int)sizeof(T);
   typedef T vec __attribute__((ext_vector_type(V)));
-  const int i = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int i = (int)blockIdx.x - (scale ? 1 : 0), tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   __shared__ float sm[4], ss[4], st[4];
   __shared__ int sn[4];
-  if (i == B) {
+  if (i < 0) {
     float v = 0.0f;
     if (weights)
       for (int r = tid; r < B; r += 256) {
         const float a = fabsf(weights[r]);
-        if (!(a < INFINITY) || !y.indptr) continue;
+        if (!(a > v) || !(a < INFINITY) || !y.indptr) continue;  // (few lists are looked at)
         int q0, q1;
         label_range(y, r, &q0, &q1);
         while (q0 < q1 && entry(y, q0, L) < 0) ++q0;
-        if (q0 < q1) v = fmaxf(v, a);
+        if (q0 < q1) v = a;
       }
     v = wave_max(v);
     if (lane == 0) sm[wave] = v;

