@@ -125,8 +125,8 @@ struct EpiLse {
 template <typename T>
 __global__ __launch_bounds__(256) void k_loss_rows(const float2* __restrict__ part, int tiles, TpOperand h, TpOperand w,
                                                    int D, int L, const float* __restrict__ bias, IdLists y,
-                                                   float* __restrict__ share, float* __restrict__ lse_ws,
-                                                   float* __restrict__ lse_out, float* __restrict__ loss, int B,
+                                                   float* __restrict__ share, float* __restrict__ top_ws,
+                                                   float* __restrict__ inv, float* __restrict__ lse_out, float* __restrict__ loss, int B,
                                                    const float* __restrict__ weights, float* __restrict__ scale,
                                                    T* __restrict__ hp, int64_t ldp) {
   constexpr int V = 16 / (int)sizeof(T);
@@ -215,7 +215,8 @@ __global__ __launch_bounds__(256) void k_loss_rows(const float2* __restrict__ pa
     t = st[0] + st[1] + st[2] + st[3];
     const float lse = top + logf(s), sh = n ? 1.0f / (float)n : 0.0f;
     share[i] = sh;
-    lse_ws[i] = lse;
+    top_ws[i] = top;
+    inv[i] = 1.0f / s;
     if (lse_out) lse_out[i] = lse;
     loss[i] = n ? lse - t * sh : 0.0f;
   }
@@ -306,14 +307,16 @@ struct EpiDzT {
   __device__ __forceinline__ void block(const f32x16 (&acc)[S::TN], int r0, int colw, float* out, int wave, int lane) {
     const int i = lane & 31, row = r0 + i;
     const bool any = targets(r0, colw, wave, lane);
-    float sh = 0.0f, lse = 0.0f, f = 0.0f;
+    float sh = 0.0f, top = 0.0f, f = 0.0f, fp = 0.0f;
     if (row < m) {
       sh = a.share[row];
-      lse = a.lse[row];
+      top = a.top[row];
       // (the weights are divided by the largest: 0 / 0 where all are 0)
       f = (a.weights ? scale > 0.0f ? a.weights[row] / scale : a.weights[row] : 1.0f) * a.up;
+      fp = f * a.inv[row];
     }
     const bool live = sh > 0.0f;
+    const float fs = f * sh;
     constexpr int LD = S::OUT_LD * (4 / (int)sizeof(T));  // elements (16 bits: 8-byte writes of 16 lanes take every bank twice)
     T* const block = reinterpret_cast<T*>(out);
 #pragma unroll
@@ -324,15 +327,15 @@ struct EpiDzT {
         const f32x4 t = *reinterpret_cast<const f32x4*>(bias + colw - col0 + c);
         f32x4 v;
 #pragma unroll
-        for (int k = 0; k < 4; ++k) v[k] = exp_fast(acc[b][4 * q + k] + t[k] - lse);
+        for (int k = 0; k < 4; ++k) v[k] = exp_fast(acc[b][4 * q + k] + t[k] - top) * fp;
         if (any) {
           const u32x4 times = *reinterpret_cast<const u32x4*>(counts + i * S::OUT_LD + c);
 #pragma unroll
-          for (int k = 0; k < 4; ++k) v[k] -= (float)times[k] * sh;
+          for (int k = 0; k < 4; ++k) v[k] -= (float)times[k] * fs;
         }
         // rows without labels and columns past the last are zeros, whatever they hold
 #pragma unroll
-        for (int k = 0; k < 4; ++k) v[k] = live && colw + c + k < n ? v[k] * f : 0.0f;
+        for (int k = 0; k < 4; ++k) v[k] = live && colw + c + k < n ? v[k] : 0.0f;
         sum[b][q] += v;
         typename TpMma<T>::frag4 o;
 #pragma unroll
@@ -396,7 +399,7 @@ struct Sizes {
   bool narrow, narrow_grad;
   int parts;  // of a row's log-sum-exp
   TpPlan fwd, dz, dh;
-  size_t hp, hq, wp, share, lse, scale, part, dzb, dbp, slabs, total;
+  size_t hp, hq, wp, share, top, inv, scale, part, dzb, dbp, slabs, total;
 };
 
 Sizes sizes(int dtype, const MatDev& h, const MatDev& w, int B, int L, int D, bool grads) {
@@ -408,12 +411,12 @@ Sizes sizes(int dtype, const MatDev& h, const MatDev& w, int B, int L, int D, bo
   s.fwd = tp_plan(dtype, B, L, D, 1);
   s.parts = s.narrow ? s.nl.ranges : s.fwd.job.tiles_n;
   s.share = round256((size_t)B * 4);
-  s.lse = round256((size_t)B * 4);
+  s.top = s.inv = s.share;
   s.part = round256((size_t)B * s.parts * 8);
   s.wp = tp_in_place(dtype, w, D) ? 0 : tp_packed_bytes(dtype, L, D);
   s.hq = tp_in_place(dtype, h, D) ? 0 : tp_packed_bytes(dtype, B, D);
   s.hp = grads ? tp_packed_bytes(dtype, B, D) : 0;
-  s.total = s.share + s.lse + s.part + s.wp + s.hp + s.hq;
+  s.total = s.share + s.top + s.inv + s.part + s.wp + s.hp + s.hq;
   if (!grads) return s;
   s.scale = 256;
   if (s.narrow_grad) {
@@ -446,7 +449,8 @@ hipError_t run(const LossJob& j, char* ws, hipStream_t st) {
     return p;
   };
   float* share = (float*)take(s.share);
-  float* lse = (float*)take(s.lse);
+  float* top = (float*)take(s.top);
+  float* inv = (float*)take(s.inv);
   float2* part = (float2*)take(s.part);
   char* wp = take(s.wp);
   char* hp = take(s.hp);
@@ -476,7 +480,7 @@ hipError_t run(const LossJob& j, char* ws, hipStream_t st) {
                : tp_launch<T, true, true, EpiLse>(s.fwd, LseArgs{j.bias, part}, st);
   if (e != hipSuccess) return e;
   hipLaunchKernelGGL(k_loss_rows<T>, dim3(B + (scale ? 1 : 0)), dim3(256), 0, st, part, s.parts, h, w, D, L, j.bias, j.y,
-                     share, lse, j.lse, j.loss_rows, B, j.weights, scale, s.hp ? (T*)hp : (T*)nullptr, ldp);
+                     share, top, inv, j.lse, j.loss_rows, B, j.weights, scale, s.hp ? (T*)hp : (T*)nullptr, ldp);
   if ((e = hipGetLastError()) != hipSuccess) return e;
   if (!grads) return hipSuccess;
 
@@ -488,7 +492,7 @@ hipError_t run(const LossJob& j, char* ws, hipStream_t st) {
   da.live = share;
   if (s.narrow_grad) {
     float* slabs = j.dh.data ? (float*)take(s.slabs) : nullptr;
-    const DzArgs za{j.bias, lse, share, j.weights, scale, up, nullptr, 0, nullptr, j.y, 0, L};
+    const DzArgs za{j.bias, top, inv, share, j.weights, scale, up, nullptr, 0, nullptr, j.y, 0, L};
     e = launch_narrow_grad(dt, s.ng, hz, w, za, B, D, 1.0f / up, j.dw, j.db, slabs, st);
     if (e != hipSuccess || !slabs) return e;
     da.part = slabs;
@@ -512,7 +516,7 @@ hipError_t run(const LossJob& j, char* ws, hipStream_t st) {
     tp_narrow(&p, n);
     p.job.a = hz;
     p.job.b = wl;
-    const DzArgs za{j.bias ? j.bias + l0 : nullptr, lse, share, j.weights, scale, up, dz, s.ldz, j.db ? dbp : nullptr, j.y,
+    const DzArgs za{j.bias ? j.bias + l0 : nullptr, top, inv, share, j.weights, scale, up, dz, s.ldz, j.db ? dbp : nullptr, j.y,
                     (int)l0, L};
     if ((e = tp_launch<T, true, true, EpiDz>(p, za, st)) != hipSuccess) return e;
     PairJob pair{};

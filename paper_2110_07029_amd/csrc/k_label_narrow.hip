@@ -119,6 +119,9 @@ __device__ __forceinline__ void nw_logits(const char* w, const char* bias, const
 
 }  // namespace
 
+// The whole power of two that exponentials of logits up to `top` are taken relative to.
+__device__ __forceinline__ float nw_base(float top) { return top == -INFINITY ? 0.0f : __builtin_ceilf(top * LOG2E); }
+
 // ---- log-sum-exp ---------------------------------------------------------------------------------
 // Workgroup = (256 rows, a range of tiles); the row blocks of a range follow each other on one XCD, whose L2 then has its
 // labels (and all 8 XCDs have work where there are fewer ranges: 65,536 rows, 5,000 labels 441 us on one, 202 on
@@ -154,7 +157,7 @@ __global__ __launch_bounds__(NWF_THREADS, 2) void k_narrow_lse(TpOperand h, TpOp
 #pragma unroll
   for (int k = 0; k < NWF_BUFS - 1; ++k)
     if (t0 + k < t1) issue(t0 + k);
-  float m[2] = {-INFINITY, -INFINITY}, s[2] = {0.0f, 0.0f};
+  float m[2] = {-INFINITY, -INFINITY}, s[2] = {0.0f, 0.0f}, base[2] = {0.0f, 0.0f};
   for (int t = t0; t < t1; ++t) {
     if (t + NWF_BUFS - 2 < t1) tp_wait<(NWF_BUFS - 2) * NwLoad<NWF_THREADS>::COPIES>();
     else tp_wait<0>();
@@ -189,24 +192,28 @@ __global__ __launch_bounds__(NWF_THREADS, 2) void k_narrow_lse(TpOperand h, TpOp
 #pragma unroll
         for (int r = 0; r < 16; ++r) top[b] = fmaxf(top[b], z[i][b][r]);
       const float mm = fmaxf(top[0], top[1]);
-      // base 2; the maximum's rounding is of the size of the result's own
-      const float base = mm == -INFINITY ? 0.0f : mm * LOG2E;
-      float e[4] = {m[i] == -INFINITY ? s[i] : s[i] * __builtin_amdgcn_exp2f(fmaf(m[i], LOG2E, -base)), 0.0f, 0.0f, 0.0f};
+      // base 2, relative to a whole number: it rounds nothing, and sums change their base exactly
+      const float b2 = nw_base(mm);
+      float e[4] = {m[i] == -INFINITY ? s[i] : s[i] * __builtin_amdgcn_exp2f(base[i] - b2), 0.0f, 0.0f, 0.0f};
 #pragma unroll
       for (int b = 0; b < 2; ++b)
 #pragma unroll
-        for (int r = 0; r < 16; ++r) e[r & 3] += __builtin_amdgcn_exp2f(fmaf(z[i][b][r], LOG2E, -base));
+        for (int r = 0; r < 16; ++r) e[r & 3] += __builtin_amdgcn_exp2f(fmaf(z[i][b][r], LOG2E, -b2));
       s[i] = (e[0] + e[1]) + (e[2] + e[3]);
       m[i] = mm;
+      base[i] = b2;
     }
   }
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
     const float m2 = __builtin_bit_cast(float, lane_xor<32>(__builtin_bit_cast(unsigned, m[i]), lane));
     const float s2 = __builtin_bit_cast(float, lane_xor<32>(__builtin_bit_cast(unsigned, s[i]), lane));
-    const float mm = fmaxf(m[i], m2), base = mm == -INFINITY ? 0.0f : mm;
+    const float b2 = __builtin_bit_cast(float, lane_xor<32>(__builtin_bit_cast(unsigned, base[i]), lane));
+    const float mm = fmaxf(m[i], m2), top = mm == -INFINITY ? 0.0f : mm;
     if (row + 32 * i < B && g == 0)
-      part[(int64_t)(row + 32 * i) * ranges + range] = make_float2(mm, s[i] * exp_fast(m[i] - base) + s2 * exp_fast(m2 - base));
+      part[(int64_t)(row + 32 * i) * ranges + range] =  // (relative to the maximum from here on)
+          make_float2(mm, (m[i] == -INFINITY ? s[i] : s[i] * __builtin_amdgcn_exp2f(fmaf(-top, LOG2E, base[i]))) +
+                              (m2 == -INFINITY ? s2 : s2 * __builtin_amdgcn_exp2f(fmaf(-top, LOG2E, b2))));
   }
 }
 
@@ -281,14 +288,16 @@ __global__ __launch_bounds__(NW_THREADS) void k_narrow_grad(TpOperand h, TpOpera
   Frag hf[8];
   nw_rows<T>(h, row, B, d_bytes, g, hf);
   const float scale = *a.scale;
-  float sh = 0.0f, lse = 0.0f, f = 0.0f;
+  float sh = 0.0f, b2 = 0.0f, f = 0.0f, fp = 0.0f;
   if (row < B) {
     sh = a.share[row];
-    lse = a.lse[row] * LOG2E;  // base 2; its rounding is of the size of lse's own
+    const float top = a.top[row];
+    b2 = nw_base(top);
     f = (a.weights ? scale > 0.0f ? a.weights[row] / scale : a.weights[row] : 1.0f) * a.up;
+    fp = f * a.inv[row] * __builtin_amdgcn_exp2f(fmaf(-(top == -INFINITY ? 0.0f : top), LOG2E, b2));
   }
   const bool live = sh > 0.0f;
-  const float out = alpha * scale;
+  const float out = alpha * scale, fs = f * sh;
   // targets among this workgroup's labels, listed once
   int* const hits = reinterpret_cast<int*>(smem + NWG_HIT);
   if (tid == 0) hits[0] = 0;
@@ -380,13 +389,13 @@ __global__ __launch_bounds__(NW_THREADS) void k_narrow_grad(TpOperand h, TpOpera
 #pragma unroll
           for (int k = 0; k < 4; ++k) {
             float v = z[b][4 * q + k];
-            v = __builtin_amdgcn_exp2f(fmaf(v, LOG2E, -lse));
+            v = __builtin_amdgcn_exp2f(fmaf(v, LOG2E, -b2)) * fp;
             bool in = live;  // (rows without labels and labels past the last are zeros, whatever they hold)
             if (checked) {
-              v -= (float)((times >> (16 * k)) & 0xffff) * sh;
+              v -= (float)((times >> (16 * k)) & 0xffff) * fs;
               in = live && t * NW_TILE + 32 * b + 8 * q + 4 * g + k < L;
             }
-            v = in ? v * f : 0.0f;
+            v = in ? v : 0.0f;
             z[b][4 * q + k] = v;
             o[k] = (T)v;
             df[b][q >> 1][4 * (q & 1) + k] = o[k];

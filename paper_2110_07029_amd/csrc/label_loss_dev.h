@@ -33,7 +33,8 @@ __device__ __forceinline__ void each_label(const IdLists& y, int i, int first, i
 // How dz is formed from z.
 struct DzArgs {
   const float* bias;   // of the piece's first label
-  const float *lse, *share, *weights, *scale;
+  // p_ij = e^(z_ij - top_i) inv_i: the rounding of a log-sum-exp would be in all of a row's probabilities alike
+  const float *top, *inv, *share, *weights, *scale;
   float up;            // 2^15 for fp16
   void* dz;            // [B x ld]
   int64_t ld;
