@@ -15,8 +15,8 @@
 //     products 3, 4   dz W onto slabs of dh, dz^T h: the piece's rows of dw; column sums for db
 //   k_join        dh
 //
-// Rows of 16 bits up to 128 wide take other kernels for product 1, and up to 256 of them for the gradients
-// (k_label_narrow.hip).
+// Rows of 16 bits up to 128 wide take other kernels for product 1, and for the gradients where there are up to 256 of them or
+// many labels (k_label_narrow.hip).
 //
 // 4,096 rows, 32,001 labels, width 2,048 in bf16: 1,930 to 2,090 us for four products of 537 GFLOP, 1.03 to 1.11 PFLOP/s
 // (the library's product of 8,192 cubed reaches 1.39 with k along both operands' rows, 1.21 and 1.08 in the forms that the
@@ -396,10 +396,10 @@ struct Sizes {
   int piece;  // labels of a piece (a multiple of 64 unless it is all)
   int64_t ldz;
   NarrowPlan nl, ng;
-  bool narrow, narrow_grad;
+  bool narrow, narrow_grad, sides;
   int parts;  // of a row's log-sum-exp
   TpPlan fwd, dz, dh;
-  size_t hp, hq, wp, share, top, inv, scale, part, dzb, dbp, slabs, total;
+  size_t hp, hq, wp, share, top, inv, scale, part, dzb, dbp, slabs, side_slabs, total;
 };
 
 Sizes sizes(int dtype, const MatDev& h, const MatDev& w, int B, int L, int D, bool grads) {
@@ -419,11 +419,14 @@ Sizes sizes(int dtype, const MatDev& h, const MatDev& w, int B, int L, int D, bo
   s.total = s.share + s.top + s.inv + s.part + s.wp + s.hp + s.hq;
   if (!grads) return s;
   s.scale = 256;
-  if (s.narrow_grad) {
-    s.ng = narrow_grad_plan(L);
-    s.slabs = narrow_slab_bytes(s.ng, B);
-    s.total += s.scale + s.slabs;
-    return s;
+  s.sides = narrow_sides_take(dtype, B, L, D);
+  if (s.narrow_grad || s.sides) {
+    s.ng = s.sides ? narrow_rows_plan(B, L) : narrow_grad_plan(L);
+    s.side_slabs = narrow_slab_bytes(s.ng, B);
+    if (s.narrow_grad) {
+      s.total += s.scale + s.side_slabs;
+      return s;
+    }
   }
   const int64_t fit = PIECE_BYTES / ((int64_t)B * es) / 256 * 256;
   s.piece = (int)(fit < 256 ? 256 : fit);
@@ -434,7 +437,9 @@ Sizes sizes(int dtype, const MatDev& h, const MatDev& w, int B, int L, int D, bo
   s.dzb = round256((size_t)B * s.ldz * es);
   s.dbp = round256((size_t)s.dz.job.tiles_m * s.ldz * 4);
   s.slabs = round256((size_t)s.dh.job.splits * B * ceil_div(D, 8) * 8 * 4);
-  s.total += s.scale + s.dzb + s.dbp + s.slabs;
+  // (the lists decide between the two, and they are not known here)
+  const size_t general = s.dzb + s.dbp + s.slabs;
+  s.total += s.scale + (general > s.side_slabs ? general : s.side_slabs);
   return s;
 }
 
@@ -490,10 +495,11 @@ hipError_t run(const LossJob& j, char* ws, hipStream_t st) {
   da.alpha = 1.0f / up;
   da.alpha_dev = scale;
   da.live = share;
-  if (s.narrow_grad) {
-    float* slabs = j.dh.data ? (float*)take(s.slabs) : nullptr;
+  if (s.sides && !narrow_sides_worth(B, L, j.y.nnz)) s.sides = false;
+  if (s.narrow_grad || s.sides) {
+    float* slabs = j.dh.data ? (float*)take(s.side_slabs) : nullptr;
     const DzArgs za{j.bias, top, inv, share, j.weights, scale, up, nullptr, 0, nullptr, j.y, 0, L};
-    e = launch_narrow_grad(dt, s.ng, hz, w, za, B, D, 1.0f / up, j.dw, j.db, slabs, st);
+    e = (s.sides ? launch_narrow_sides : launch_narrow_grad)(dt, s.ng, hz, w, za, B, D, 1.0f / up, j.dw, j.db, slabs, st);
     if (e != hipSuccess || !slabs) return e;
     da.part = slabs;
     da.ldp = 128;

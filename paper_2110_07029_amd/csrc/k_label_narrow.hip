@@ -4,6 +4,7 @@
 //
 //   k_narrow_lse   256 rows in registers (a wave has 64), labels pass by in tiles of 64 through LDS; maximum and
 //                  sum of exponentials per lane until the end
+//   k_narrow_side  more rows: one kernel for dh and one for dw and db, each of which forms dz again
 //   k_narrow_grad  up to 256 rows.  Per tile of 64 labels: z, dz in registers; dz W onto the rows' gradient, which stays in
 //                  registers (dz is fed to the matrix cores as the accumulators hold it, the tile of W read with the k order
 //                  that this gives); dz through LDS, turned around, times h: the tile's rows of dw
@@ -23,6 +24,7 @@ namespace {
 
 typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
 typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
+typedef int i32x4u __attribute__((ext_vector_type(4), aligned(4)));
 typedef unsigned u32x4u __attribute__((ext_vector_type(4), aligned(2)));
 constexpr int NW_THREADS = 512, NW_ROWS = 256, NW_TILE = 64, NW_COLS = 128;
 constexpr int NW_WBUF = NW_TILE * 256, NW_BIAS = 8 * 256;  // bytes of a tile; of its biases, a copy per wave
@@ -95,10 +97,8 @@ __device__ __forceinline__ void nw_bias(const char* bias, int g, f32x16 (&z)[2])
     }
 }
 template <typename T>
-__device__ __forceinline__ void nw_logits(const char* w, const char* bias, const typename TpMma<T>::frag8 (&hf)[8], int lane,
-                                          f32x16 (&z)[2]) {
+__device__ __forceinline__ void nw_logits(const char* w, const typename TpMma<T>::frag8 (&hf)[8], int lane, f32x16 (&z)[2]) {
   const int n = lane & 31, g = lane >> 5;
-  nw_bias(bias, g, z);
   // (what a product reads from LDS is on its way while the ones before run)
   typename TpMma<T>::frag8 f[3][2];
   auto read = [&](int kk) {
@@ -256,6 +256,28 @@ __device__ __forceinline__ float nw_sum_lanes(float (&v)[32], int lane) {
   return v[0];
 }
 
+// Columns col .. + 31 of a label's row of dw in two 16-byte stores: lanes n and n + 32 hold columns 8 q .. + 3 and + 4 .. + 7,
+// and with a change of sides between q and q + 1 each has 8.
+template <typename T>
+__device__ __forceinline__ void nw_store32(const MatDev& dw, int label, int col, int g, const f32x16& acc, float out, bool in) {
+  typedef typename TpMma<T>::frag4 Half;
+#pragma unroll
+  for (int q = 0; q < 4; q += 2) {
+    u32x2 v[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      Half o;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) o[k] = (T)(acc[4 * (q + i) + k] * out);
+      v[i] = __builtin_bit_cast(u32x2, o);
+    }
+    const auto lo = __builtin_amdgcn_permlane32_swap(v[0][0], v[1][0], false, false);
+    const auto hi = __builtin_amdgcn_permlane32_swap(v[0][1], v[1][1], false, false);
+    const u32x4 o{(unsigned)lo[0], (unsigned)hi[0], (unsigned)lo[1], (unsigned)hi[1]};
+    if (in) *reinterpret_cast<u32x4u*>((T*)dw.data + label * dw.ld + col + 8 * (q + g)) = o;
+  }
+}
+
 template <typename T>
 __global__ __launch_bounds__(NW_THREADS) void k_narrow_grad(TpOperand h, TpOperand w, DzArgs a, int B, int d, int ranges,
                                                            int per, int tiles, float alpha, MatDev dw, float* __restrict__ db,
@@ -373,7 +395,8 @@ __global__ __launch_bounds__(NW_THREADS) void k_narrow_grad(TpOperand h, TpOpera
       __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "wavefront");
     }
     f32x16 z[2];
-    nw_logits<T>(p, p + NW_WBUF + 256 * wave, hf, lane, z);
+    nw_bias(p + NW_WBUF + 256 * wave, g, z);
+    nw_logits<T>(p, hf, lane, z);
     const bool edge = (t + 1) * NW_TILE > L;
     Frag df[2][2];
     // dz, to LDS and as fragments; checked: with targets, or past the last label
@@ -456,24 +479,7 @@ __global__ __launch_bounds__(NW_THREADS) void k_narrow_grad(TpOperand h, TpOpera
       }
       const int label = t * NW_TILE + 32 * lb + n;
       if (wide) {
-        // lanes n and n + 32 hold columns 8 q .. + 3 and + 4 .. + 7 of label n: with a change of sides between q and q + 1
-        // each has 8 columns
-#pragma unroll
-        for (int q = 0; q < 4; q += 2) {
-          u32x2 v[2];
-#pragma unroll
-          for (int i = 0; i < 2; ++i) {
-            Half o;
-#pragma unroll
-            for (int k = 0; k < 4; ++k) o[k] = (T)(acc[4 * (q + i) + k] * out);
-            v[i] = __builtin_bit_cast(u32x2, o);
-          }
-          const auto lo = __builtin_amdgcn_permlane32_swap(v[0][0], v[1][0], false, false);
-          const auto hi = __builtin_amdgcn_permlane32_swap(v[0][1], v[1][1], false, false);
-          const u32x4 o{(unsigned)lo[0], (unsigned)hi[0], (unsigned)lo[1], (unsigned)hi[1]};
-          if (label < L)
-            *reinterpret_cast<u32x4u*>((T*)dw.data + label * dw.ld + 32 * wu + 8 * (q + g)) = o;
-        }
+        nw_store32<T>(dw, label, 32 * wu, g, acc, out, label < L);
       } else if (label < L) {
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
@@ -494,9 +500,377 @@ __global__ __launch_bounds__(NW_THREADS) void k_narrow_grad(TpOperand h, TpOpera
   }
 }
 
+// ---- gradients of more rows ----------------------------------------------------------------------------
+// One side of the product in registers, 32 per wave, with the sums of its gradient; the other passes by in tiles of 64
+// through LDS.  Rows in registers give dh, labels dw and db: z is formed once more for each (and its exponentials), but dz
+// leaves its registers for neither.  Four waves, two workgroups per compute unit, one barrier per tile.  406 rows, 225,682
+// labels, width 128 in bf16: dh 70 us, dw and db 94 (the general kernels' dz, 183 MB written and read twice, and its products
+// 245); the whole call 304 -> 198.  For up to 256 rows k_narrow_grad, which forms z once for both, is faster.
+constexpr int NWS_THREADS = 256, NWS_OWN = 128, NWS_HITS = 2047;
+constexpr int NWS_BUF = NW_WBUF + 4 * 256, NWS_COUNT = 2 * NWS_BUF, NWS_ROW = NWS_COUNT + NWS_OWN * 128;
+constexpr int NWS_HIT = NWS_ROW + 4 * 3 * 256, NWS_SORT = NWS_HIT + 4 * (NWS_HITS + 1), NWS_START = NWS_SORT + 4 * (NWS_HITS + 1);
+constexpr int NWS_AT = NWS_START + 4 * 260, NWS_LDS = NWS_AT + 4 * 256;
+static_assert(2 * NWS_LDS <= 160 * 1024, "two workgroups per compute unit");
+
+// What turns a logit of row i into dz: v = 2^(z log2 e - base) fp - times fs.  A row without labels gets zeros, and NaN where
+// its logit (a bias, since its h is zeros) is NaN or +infinity: its dh is made zeros when the slabs are joined, and in dw and db every other
+// row gives NaN there too (no other row: zeros at the end).
+struct NwRow {
+  float base, fp, fs;
+};
+__device__ __forceinline__ NwRow nw_row(const DzArgs& a, float top, float inv, float share, float weight, float scale) {
+  if (!(share > 0.0f)) return NwRow{3e38f, 0.0f, 0.0f};
+  const float f = (a.weights ? scale > 0.0f ? weight / scale : weight : 1.0f) * a.up, b = nw_base(top);
+  return NwRow{b, f * inv * __builtin_amdgcn_exp2f(fmaf(-(top == -INFINITY ? 0.0f : top), LOG2E, b)), f * share};
+}
+
+// ROWS: own = rows of h, 128 of them, and tiles t0 .. of labels; else own = labels, `per` blocks of 128 after each other,
+// and all tiles of rows.
+template <typename T, bool ROWS>
+__global__ __launch_bounds__(NWS_THREADS, 2) void k_narrow_side(TpOperand own, TpOperand other, DzArgs a, int n_own, int n_other,
+                                                                int d, int blocks, int ranges, int per, int tiles, float alpha,
+                                                                MatDev dw, float* __restrict__ db, float* __restrict__ slabs) {
+  typedef typename TpMma<T>::frag8 Frag;
+  typedef typename TpMma<T>::frag4 Half;
+  extern __shared__ __attribute__((aligned(16))) char smem[];
+  const int tid = threadIdx.x, lane = tid & 63, g = lane >> 5, n = lane & 31;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int G = lane >> 4, ti = (lane >> 2) & 3, ta = lane & 3;  // of a transposing read's address
+  const int all = ROWS ? ranges * blocks : ranges, share = (all + 7) >> 3;
+  const int at = (int)(blockIdx.x & 7) * share + (int)(blockIdx.x >> 3);
+  if (at >= all || (int)(blockIdx.x >> 3) >= share) return;
+  const int range = ROWS ? at / blocks : at;
+  const int b0 = ROWS ? at % blocks : range * per, b1 = ROWS ? b0 + 1 : min(blocks, b0 + per);
+  const int t0 = ROWS ? range * per : 0, t1 = ROWS ? min(tiles, t0 + per) : tiles;
+  const int d_bytes = 2 * d, B = ROWS ? n_own : n_other;
+  const NwLoad<NWS_THREADS> load(other, ROWS ? a.bias : nullptr, n_other, d_bytes, tid);
+  const unsigned lds0 = __builtin_amdgcn_readfirstlane((unsigned)(uintptr_t)(__attribute__((address_space(3))) char*)smem);
+  const float scale = *a.scale, out = alpha * scale;
+  auto issue = [&](int t, int buf) {
+    const unsigned to = lds0 + (unsigned)buf * NWS_BUF;
+    load.copy(t, to, to + NW_WBUF + 256 * wave, wave, lane);
+  };
+  // (tiles of rows) this wave's copy of what belongs to the tile's rows, a lane per row, loaded a tile ahead
+  float* const rows = reinterpret_cast<float*>(smem + NWS_ROW + 768 * wave);  // [3][64]
+  float r_top = 0.0f, r_inv = 0.0f, r_share = 0.0f, r_weight = 0.0f;
+  auto fetch_row = [&](int t) {
+    const int r = t * NW_TILE + lane;
+    const bool in = r < B;
+    r_top = in ? a.top[r] : 0.0f;
+    r_inv = in ? a.inv[r] : 0.0f;
+    r_share = in ? a.share[r] : 0.0f;
+    r_weight = in && a.weights ? a.weights[r] : 0.0f;
+  };
+  issue(t0, 0);
+  if (!ROWS) fetch_row(t0);
+  // targets between own and what passes by, listed once: own within the workgroup's, other; then in the order of the tiles
+  // (or of up to 256 groups of them), so that a tile looks at its own alone
+  unsigned* const hits = reinterpret_cast<unsigned*>(smem + NWS_HIT);
+  unsigned* const sorted = reinterpret_cast<unsigned*>(smem + NWS_SORT);
+  int* const start = reinterpret_cast<int*>(smem + NWS_START);  // [257]
+  int* const next = reinterpret_cast<int*>(smem + NWS_AT);
+  constexpr int SHIFT = ROWS ? 24 : 18;
+  int group = 0;  // tiles of one: 2^group
+  while ((t1 - t0) >> group > 255) ++group;
+  start[tid] = 0;
+  if (tid == 0) hits[0] = start[256] = 0;
+  asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+  __builtin_amdgcn_s_barrier();
+  const int own0 = b0 * NWS_OWN, own1 = min(n_own, b1 * NWS_OWN);
+  if constexpr (ROWS) {
+    const int l0 = t0 * NW_TILE, l1 = min(n_other, t1 * NW_TILE);
+    if (own0 + (tid >> 1) < B && a.y.indptr)
+      each_label(a.y, own0 + (tid >> 1), tid & 1, 2, [&](int id) {
+        if (id >= l0 && id < l1) {
+          const unsigned k = atomicAdd(hits, 1u);
+          if (k < NWS_HITS) hits[1 + k] = (unsigned)(tid >> 1) << SHIFT | (unsigned)id;
+        }
+      });
+  } else if (a.y.indptr) {
+    // the lists as one: entries whose label is here, then their rows by bisection
+    const int64_t first = *a.y.first;
+    const int32_t* const ids = a.y.indices + first;
+    const int nnz = a.y.nnz;
+    auto take = [&](int id, int q) {
+      if (id < own0 || id >= own1) return;
+      const unsigned h = atomicAdd(hits, 1u);
+      if (h < NWS_HITS) hits[1 + h] = (unsigned)q;
+    };
+    const int whole = nnz & ~(16 * NWS_THREADS - 1);  // (16 ids a thread on their way at once)
+    for (int q = 4 * tid; q < whole; q += 16 * NWS_THREADS) {
+      i32x4 id[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) id[k] = *reinterpret_cast<const i32x4u*>(ids + q + 4 * NWS_THREADS * k);
+#pragma unroll
+      for (int k = 0; k < 16; ++k) take(id[k >> 2][k & 3], q + 4 * NWS_THREADS * (k >> 2) + (k & 3));
+    }
+    for (int q = whole + tid; q < nnz; q += 8 * NWS_THREADS) {
+      int id[8];
+#pragma unroll
+      for (int k = 0; k < 8; ++k) id[k] = q + k * NWS_THREADS < nnz ? ids[q + k * NWS_THREADS] : -1;
+#pragma unroll
+      for (int k = 0; k < 8; ++k) take(id[k], q + k * NWS_THREADS);
+    }
+    __syncthreads();
+    const int total = min((int)hits[0], NWS_HITS);
+    for (int h = tid; h < total; h += NWS_THREADS) {
+      const int64_t q = first + hits[1 + h];
+      int lo = 0, hi = B;  // the last row that does not begin behind q
+      while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (a.y.indptr[mid] <= q) lo = mid;
+        else hi = mid;
+      }
+      int q0, q1;
+      label_range(a.y, lo, &q0, &q1);
+      hits[1 + h] = q >= q0 && q < q1 ? (unsigned)(a.y.indices[q] - own0) << SHIFT | (unsigned)lo : ~0u;
+    }
+  }
+  __syncthreads();
+  const int total = (int)hits[0];
+  if (total && total <= NWS_HITS) {
+    auto group_of = [&](unsigned hit) { return (int)((((hit & ((1u << SHIFT) - 1)) >> 6) - t0) >> group); };
+    for (int h = tid; h < total; h += NWS_THREADS)
+      if (hits[1 + h] != ~0u) atomicAdd(start + 1 + group_of(hits[1 + h]), 1);
+    __syncthreads();
+    for (int o = 1; o < 256; o <<= 1) {
+      const int v = tid >= o ? start[1 + tid - o] : 0;
+      __syncthreads();
+      start[1 + tid] += v;
+      __syncthreads();
+    }
+    next[tid] = start[tid];
+    __syncthreads();
+    for (int h = tid; h < total; h += NWS_THREADS)
+      if (hits[1 + h] != ~0u) sorted[atomicAdd(next + group_of(hits[1 + h]), 1)] = hits[1 + h];
+    __syncthreads();
+  }
+  char* const counts = smem + NWS_COUNT;
+  // LDS addresses, of which the parts of kk, u, hi, b and q flip bits: formed where they are used (as loop invariants they
+  // would take the registers that the sums need)
+  int row_at = 256 * n + 16 * (g ^ nw_turn(n)), turned_at = nw_turned_at(4 * (G >> 1) + ti, 0, G, ta);
+  int count_at = nw_dz(32 * wave + n, g);
+  int buf = 0;
+  for (int blk = b0; blk < b1; ++blk) {
+    const int me = blk * NWS_OWN + 32 * wave + n;
+    Frag of[8];
+    nw_rows<T>(own, me, n_own, d_bytes, g, of);
+    const float own_bias = !ROWS && a.bias && me < n_own ? a.bias[me] : 0.0f;
+    NwRow mine{3e38f, 0.0f, 0.0f};
+    if (ROWS && me < B) mine = nw_row(a, a.top[me], a.inv[me], a.share[me], a.weights ? a.weights[me] : 0.0f, scale);
+    f32x16 acc[4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) acc[u][r] = 0.0f;
+    float sums = 0.0f;
+    bool live = ROWS;
+    for (int t = t0; t < t1; ++t) {
+      tp_wait<0>();
+      __builtin_amdgcn_s_barrier();  // the tile is here, and nobody reads the one before
+      asm volatile("" : "+v"(row_at), "+v"(turned_at), "+v"(count_at));
+      const char* const p = smem + buf * NWS_BUF;
+      buf ^= 1;
+      if (t + 1 < t1) issue(t + 1, buf);
+      else if (blk + 1 < b1) issue(t0, buf);
+      bool masked = false;  // labels past the last
+      if constexpr (ROWS) {
+        masked = (t + 1) * NW_TILE > n_other;
+      } else {
+        const NwRow r = nw_row(a, r_top, r_inv, r_share, r_weight, scale);
+        rows[lane] = r.base;
+        rows[64 + lane] = r.fp;
+        rows[128 + lane] = r.fs;
+        live |= __ballot(r_share > 0.0f) != 0;
+        fetch_row(t + 1 < t1 ? t + 1 : t0);
+      }
+      // how often a label stands in a row's list: 16-bit counts per own
+      bool any = total > NWS_HITS;
+      const int first = t * NW_TILE, from = (blk - b0) * NWS_OWN + 32 * wave;
+      auto place = [&](unsigned hit, int* o, int* c) {
+        *o = (int)(hit >> SHIFT) - from;
+        *c = (int)(hit & ((1u << SHIFT) - 1)) - first;
+        return *o >= 0 && *o < 32 && *c >= 0 && *c < NW_TILE;
+      };
+      int h0 = 0, h1 = 0;
+      if (total && !any) {
+        h0 = start[(t - t0) >> group];
+        h1 = start[((t - t0) >> group) + 1];
+        bool here = false;
+        int o, c;
+        for (int k = h0 + lane; k < h1; k += 64) here |= place(sorted[k], &o, &c);
+        any = __ballot(here) != 0;
+      }
+      if (any) {
+        auto add = [&](int o, int c) {
+          const int to = nw_dz(32 * wave + o, c >> 2) + 2 * (c & 3);
+          atomicAdd(reinterpret_cast<unsigned*>(counts + (to & ~3)), to & 2 ? 0x10000u : 1u);
+        };
+#pragma unroll
+        for (int k = 0; k < 8; ++k) *reinterpret_cast<uint64_t*>(counts + 4096 * wave + 512 * k + 8 * lane) = 0;
+        __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "wavefront");
+        if (total <= NWS_HITS) {
+          int o, c;
+          for (int k = h0 + lane; k < h1; k += 64)
+            if (place(sorted[k], &o, &c)) add(o, c);
+        } else if constexpr (ROWS) {
+          if (own0 + 32 * wave + (lane >> 1) < B)
+            each_label(a.y, own0 + 32 * wave + (lane >> 1), lane & 1, 2, [&](int id) {
+              const int c = id - first;
+              if (c >= 0 && c < NW_TILE && id < n_other) add(lane >> 1, c);
+            });
+        } else if (first + lane < B) {
+          each_label(a.y, first + lane, 0, 1, [&](int id) {
+            const int o = id - own0 - from;
+            if (o >= 0 && o < 32 && id < n_own) add(o, lane);
+          });
+        }
+      }
+      __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "wavefront");
+      f32x16 z[2];
+      if constexpr (ROWS) {
+        nw_bias(p + NW_WBUF + 256 * wave, g, z);
+      } else {
+#pragma unroll
+        for (int r = 0; r < 16; ++r) z[0][r] = z[1][r] = own_bias;
+      }
+      Frag f[2][2];
+      auto read = [&](int kk) {
+#pragma unroll
+        for (int b = 0; b < 2; ++b) f[kk & 1][b] = *reinterpret_cast<const Frag*>(p + (row_at ^ (32 * kk)) + 8192 * b);
+      };
+      read(0);
+#pragma unroll
+      for (int kk = 0; kk < 8; ++kk) {
+        if (kk + 1 < 8) read(kk + 1);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int b = 0; b < 2; ++b) z[b] = tp_mma(f[kk & 1][b], of[kk], z[b]);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      Frag df[2][2];
+      auto form = [&](auto checked) {
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+          for (int q = 0; q < 4; ++q) {
+            const int c = 32 * b + 8 * q + 4 * g;
+            f32x4 base, fp, fs;
+            if constexpr (!ROWS) {
+              base = *reinterpret_cast<const f32x4*>(rows + c);
+              fp = *reinterpret_cast<const f32x4*>(rows + 64 + c);
+              if (checked) fs = *reinterpret_cast<const f32x4*>(rows + 128 + c);
+            }
+            uint64_t times = 0;
+            if (checked) times = any ? *reinterpret_cast<const uint64_t*>(counts + (count_at ^ (64 * b) ^ (16 * q))) : 0;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+              const float bk = ROWS ? mine.base : base[k];
+              float v = __builtin_amdgcn_exp2f(fmaf(z[b][4 * q + k], LOG2E, -bk)) * (ROWS ? mine.fp : fp[k]);
+              if (checked) {
+                v -= (float)((times >> (16 * k)) & 0xffff) * (ROWS ? mine.fs : fs[k]);
+                if (ROWS && first + c + k >= n_other) v = 0.0f;
+              }
+              if constexpr (!ROWS) sums += v;
+              df[b][q >> 1][4 * (q & 1) + k] = (T)v;
+            }
+            __builtin_amdgcn_sched_barrier(0);
+          }
+      };
+      if (any || masked) form(std::true_type());
+      else form(std::false_type());
+      // dz times what passes by: k in the accumulators' order, 16 c + 8 hi + 4 g + 0..3 of a block
+      Frag uf[4];
+      auto turned = [&](int k) {  // k = 8 b + 4 c + u
+        const char* const q = p + 4096 * (k >> 2);
+        const int to = turned_at ^ (64 * (k & 3));
+        uf[k & 3] = nw_join<T>(tp_turned<T>(q + to), tp_turned<T>(q + (to ^ 32) + 2048));
+      };
+#pragma unroll
+      for (int k = 0; k < 3; ++k) turned(k);
+#pragma unroll
+      for (int k = 0; k < 16; ++k) {
+        if (k + 3 < 16) turned(k + 3);
+        __builtin_amdgcn_sched_barrier(0);
+        acc[k & 3] = tp_mma(uf[k & 3], df[k >> 3][(k >> 2) & 1], acc[k & 3]);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    }
+    if constexpr (ROWS) {
+      if (me < B) {
+        float* o = slabs + ((int64_t)range * B + me) * NW_COLS + 4 * g;
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+#pragma unroll
+          for (int q = 0; q < 4; ++q)
+            *reinterpret_cast<f32x4*>(o + 32 * u + 8 * q) =
+                f32x4{acc[u][4 * q], acc[u][4 * q + 1], acc[u][4 * q + 2], acc[u][4 * q + 3]};
+      }
+    } else {
+      sums += __builtin_bit_cast(float, lane_xor<32>(__builtin_bit_cast(unsigned, sums), lane));
+      if (db && g == 0 && me < n_own) db[me] = live ? sums * out : 0.0f;
+      if (dw.data) {
+        // 32 columns at a time through the wave's block of counts, chunk c of label r at place c ^ (r % 8)
+        float* const block = reinterpret_cast<float*>(counts + 4096 * wave);
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+#pragma unroll
+          for (int q = 0; q < 4; ++q)
+            *reinterpret_cast<f32x4*>(block + 32 * n + 4 * ((2 * q + g) ^ (n & 7))) =
+                f32x4{acc[u][4 * q] * out, acc[u][4 * q + 1] * out, acc[u][4 * q + 2] * out, acc[u][4 * q + 3] * out};
+          __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "wavefront");
+#pragma unroll 1
+          for (int r = lane >> 2; r < 32; r += 16) {
+            const int c = 2 * (lane & 3), label = me - n + r, col = 32 * u + 4 * c;
+            const f32x4 lo = *reinterpret_cast<const f32x4*>(block + 32 * r + 4 * (c ^ (r & 7)));
+            const f32x4 hi = *reinterpret_cast<const f32x4*>(block + 32 * r + 4 * ((c + 1) ^ (r & 7)));
+            float v[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+            if (!live)
+#pragma unroll
+              for (int i = 0; i < 8; ++i) v[i] = 0.0f;
+            if (label < n_own && col < d) store8(dw, label, col, min(8, d - col), v);
+          }
+          __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "wavefront");
+        }
+      }
+    }
+  }
+}
+
 // ---- launches ----------------------------------------------------------------------------------------
 bool narrow_takes(int dtype, int d) { return dtype != 0 && d <= NW_COLS; }
 bool narrow_grad_takes(int dtype, int n_rows, int d) { return narrow_takes(dtype, d) && n_rows <= NW_ROWS; }
+
+// Labels that give most of the chip's 512 places a block (loss and gradients in bf16, general kernels and these: 4,096 rows,
+// 48,000 labels 503 and 384 us; 1,584 rows, 17,219 labels, 75 a row 140 and 205; 278 rows, 16,698 labels 58 and 83).
+bool narrow_sides_take(int dtype, int n_rows, int n_labels, int d) {
+  return narrow_takes(dtype, d) && n_rows > NW_ROWS && n_rows <= 1 << 18 && n_labels >= 40000;
+}
+// Whether the lists are short enough that a workgroup's share of labels holds its targets (evenly spread: three quarters of
+// what it lists; more, and every tile goes through its rows' lists: 4,096 rows of 75 labels out of 16,400 316 us with the
+// general kernels, 1,190 with these).
+bool narrow_sides_worth(int n_rows, int n_labels, int nnz) {
+  const int64_t labels = NWS_OWN * ceil_div(ceil_div(n_labels, NWS_OWN), 512);
+  return (int64_t)nnz * labels <= (int64_t)(NWS_HITS * 3 / 4) * n_labels;
+}
+// Rows in registers: about 512 workgroups.
+NarrowPlan narrow_rows_plan(int n_rows, int n_labels) {
+  NarrowPlan p;
+  p.row_blocks = (int)ceil_div(n_rows, NWS_OWN);
+  p.tiles = (int)ceil_div(n_labels, NW_TILE);
+  p.per = (int)ceil_div(p.tiles, p.row_blocks < 512 ? 512 / p.row_blocks : 1);
+  p.ranges = (int)ceil_div(p.tiles, p.per);
+  return p;
+}
+// Labels in registers: up to 512 workgroups.
+static NarrowPlan narrow_labels_plan(int n_rows, int n_labels) {
+  NarrowPlan p;
+  p.row_blocks = (int)ceil_div(n_labels, NWS_OWN);
+  p.tiles = (int)ceil_div(n_rows, NW_TILE);
+  p.per = (int)ceil_div(p.row_blocks, 512);
+  p.ranges = (int)ceil_div(p.row_blocks, p.per);
+  return p;
+}
 
 NarrowPlan narrow_lse_plan(int n_rows, int n_labels) {
   NarrowPlan p;
@@ -541,6 +915,34 @@ hipError_t launch_narrow_grad(int dtype, const NarrowPlan& p, const TpOperand& h
   hipLaunchKernelGGL(fn, dim3(p.ranges), dim3(NW_THREADS), NWG_LDS, st, h, w, a, n_rows, d, p.ranges, p.per, p.tiles, alpha,
                      dw, db, slabs);
   return hipGetLastError();
+}
+
+template <typename T>
+static hipError_t sides(const NarrowPlan& p, const TpOperand& h, const TpOperand& w, const DzArgs& a, int n_rows, int d,
+                        float alpha, const MatDev& dw, float* db, float* slabs, hipStream_t st) {
+  hipError_t e = hipSuccess;
+  const int L = a.n_labels;
+  if (slabs) {
+    const auto fn = k_narrow_side<T, true>;
+    if ((e = tp_allow_lds((const void*)fn, NWS_LDS)) != hipSuccess) return e;
+    hipLaunchKernelGGL(fn, dim3((unsigned)(8 * ceil_div((int64_t)p.ranges * p.row_blocks, 8))), dim3(NWS_THREADS), NWS_LDS, st, h,
+                       w, a, n_rows, L, d, p.row_blocks, p.ranges, p.per, p.tiles, alpha, MatDev{}, (float*)nullptr, slabs);
+    if ((e = hipGetLastError()) != hipSuccess) return e;
+  }
+  if (dw.data || db) {
+    const NarrowPlan q = narrow_labels_plan(n_rows, L);
+    const auto fn = k_narrow_side<T, false>;
+    if ((e = tp_allow_lds((const void*)fn, NWS_LDS)) != hipSuccess) return e;
+    hipLaunchKernelGGL(fn, dim3((unsigned)(8 * ceil_div(q.ranges, 8))), dim3(NWS_THREADS), NWS_LDS, st, w, h, a, L, n_rows, d,
+                       q.row_blocks, q.ranges, q.per, q.tiles, alpha, dw, db, (float*)nullptr);
+    e = hipGetLastError();
+  }
+  return e;
+}
+hipError_t launch_narrow_sides(int dtype, const NarrowPlan& p, const TpOperand& h, const TpOperand& w, const DzArgs& a,
+                               int n_rows, int d, float alpha, const MatDev& dw, float* db, float* slabs, hipStream_t st) {
+  return dtype == 1 ? sides<bf16>(p, h, w, a, n_rows, d, alpha, dw, db, slabs, st)
+                    : sides<f16>(p, h, w, a, n_rows, d, alpha, dw, db, slabs, st);
 }
 
 }  // namespace asgd

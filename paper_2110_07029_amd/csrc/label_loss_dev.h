@@ -49,6 +49,9 @@ struct NarrowPlan {
 };
 bool narrow_takes(int dtype, int d);
 bool narrow_grad_takes(int dtype, int n_rows, int d);
+bool narrow_sides_take(int dtype, int n_rows, int n_labels, int d);
+bool narrow_sides_worth(int n_rows, int n_labels, int nnz);
+NarrowPlan narrow_rows_plan(int n_rows, int n_labels);
 NarrowPlan narrow_lse_plan(int n_rows, int n_labels);
 NarrowPlan narrow_grad_plan(int n_labels);
 size_t narrow_slab_bytes(const NarrowPlan& p, int n_rows);
@@ -58,5 +61,8 @@ hipError_t launch_narrow_lse(int dtype, const NarrowPlan& p, const TpOperand& h,
 // dw, db complete (scaled by alpha *a.scale); slabs [ranges][n_rows][128]: sums for dh, not scaled.
 hipError_t launch_narrow_grad(int dtype, const NarrowPlan& p, const TpOperand& h, const TpOperand& w, const DzArgs& a,
                               int n_rows, int d, float alpha, const MatDev& dw, float* db, float* slabs, hipStream_t st);
+// The same, for any number of rows.
+hipError_t launch_narrow_sides(int dtype, const NarrowPlan& p, const TpOperand& h, const TpOperand& w, const DzArgs& a,
+                               int n_rows, int d, float alpha, const MatDev& dw, float* db, float* slabs, hipStream_t st);
 
 }  // namespace asgd

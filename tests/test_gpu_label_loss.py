@@ -398,3 +398,75 @@ def test_weights_whose_largest_has_no_labels(dtype):
         c = Call(h, w, lists, normal(4, L), weights, dtype=dtype).run()
         weights[1] = weights[599] = 0.0  # (rows without labels: the reference needs finite ones)
         c.check(lists, dtype)
+
+
+@pytest.mark.parametrize("B,L,D,mean,shift,pad,dtype", [
+    (300, 41000, 128, 3, 0, 0, "bf16"), (257, 40000, 64, 75, 0, 8, "f16"), (1000, 40500, 120, 5, 0, 0, "f16"),
+    (700, 66000, 61, 1, 1, 5, "bf16"), (2000, 40960, 8, 2, 0, 0, "bf16"), (1100, 41000, 128, 300, 0, 0, "bf16"),
+    (300, 140000, 128, 3, 0, 0, "f16")])
+def test_gradients_of_many_narrow_rows(B, L, D, mean, shift, pad, dtype):
+    h, w = placed(normal(1, B, D), dtype, shift, pad), placed(normal(2, L, D, scale=2 * D ** -0.5), dtype, shift, pad)
+    lists = random_lists(3, B, L, mean)
+    lists[1], lists[2], lists[130] = [L - 1, L, -1, L - 1], [], [7] * 3
+    weights = torch.rand(B, generator=torch.Generator().manual_seed(1)).cuda() * 3e-3
+    weights[::7] = 0.0
+    h[2] = NAN  # (a row without labels)
+    c = Call(h, w, lists, normal(4, L), weights, dtype, shift=shift, pad=pad, before=9).run()
+    bits = {k: v.clone() for k, v in c.outputs().items()}
+    c.run()
+    for k, v in c.outputs().items():
+        assert torch.equal(v.nan_to_num(5.0), bits[k].nan_to_num(5.0)), k
+    assert bool(c.lse[2].isnan()) and float(c.loss[2]) == 0.0
+    c.lse[2] = 0.0
+    h[2] = 0.0
+    want = ref.label_loss(h, w, lists, c.bias, weights, dtype)
+    for k, got in c.outputs().items():
+        if k == "lse":
+            got[2] = want["lse"][0][2]
+        ref.near(got, *want[k], c.types[k], k)
+    c.clean_h()
+    c.clean_w()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+def test_a_label_of_every_row_and_parts_of_the_outputs(dtype):
+    # more targets in a workgroup's share than it lists
+    B, L, D = 4200, 40000, 32
+    h, w = placed(normal(1, B, D), dtype), placed(normal(2, L, D, scale=0.4), dtype)
+    lists = [[5, 6 + i % 90, 5] for i in range(B)]
+    c = Call(h, w, lists, normal(4, L), dtype=dtype, out="f32").run()
+    c.check(lists, dtype)
+    whole = {k: v.clone() for k, v in c.outputs().items()}
+    for grads in (("dh",), ("dw",), ("db",)):
+        part = Call(h, w, lists, normal(4, L), dtype=dtype, out="f32", grads=grads).run().outputs()
+        assert set(part) == {"loss", "lse", *grads}
+        for k, v in part.items():
+            assert torch.equal(v, whole[k]), k
+
+
+def test_many_narrow_rows_without_labels():
+    # zeros, whatever the rows and the biases hold
+    B, L, D = 300, 40000, 128
+    h, w, bias = placed(normal(1, B, D), "bf16"), placed(normal(2, L, D), "bf16"), normal(4, L)
+    h[3], bias[7], bias[8] = NAN, NAN, INF
+    for weights in (None, torch.ones(B, device="cuda")):
+        for lists in ([[] for _ in range(B)], [[-1, L] for _ in range(B)]):
+            c = Call(h, w, lists, bias, weights, "bf16").run()
+            for k, v in c.outputs().items():
+                assert k == "lse" or bool((v == 0).all()), k
+
+
+def test_many_narrow_rows_whose_logits_are_not_finite():
+    B, L, D = 300, 40000, 64
+    h, w, bias = placed(normal(1, B, D), "f16"), placed(normal(2, L, D, scale=0.3), "f16"), normal(4, L)
+    lists = [[i] for i in range(B)]
+    h[5] = NAN
+    c = Call(h, w, lists, bias, dtype="f16").run()
+    assert bool(c.loss[5].isnan()) and bool(c.dh[5].isnan().all()) and bool(c.dw.isnan().all()) and bool(c.db[:L].isnan().all())
+    rest = [i for i in range(B) if i != 5]
+    assert bool(c.loss[rest].isfinite().all()) and bool(c.dh[rest].isfinite().all())
+    # labels of bias -inf have no probability
+    h[5], bias[1000:1200] = 0.0, -INF
+    c = Call(h, w, lists, bias, dtype="f16").run()
+    c.check(lists, "f16")
+    assert bool((c.dw[1000:1200] == 0).all()) and bool((c.db[1000:1200] == 0).all())
