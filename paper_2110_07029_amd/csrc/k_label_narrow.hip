@@ -749,6 +749,7 @@ __global__ __launch_bounds__(NWS_THREADS, 2) void k_narrow_side(TpOperand own, T
         __builtin_amdgcn_sched_barrier(0);
       }
       Frag df[2][2];
+      float part[4] = {};  // (one sum over thousands of rows would round as often)
       auto form = [&](auto checked) {
 #pragma unroll
         for (int b = 0; b < 2; ++b)
@@ -771,7 +772,7 @@ __global__ __launch_bounds__(NWS_THREADS, 2) void k_narrow_side(TpOperand own, T
                 v -= (float)((times >> (16 * k)) & 0xffff) * (ROWS ? mine.fs : fs[k]);
                 if (ROWS && first + c + k >= n_other) v = 0.0f;
               }
-              if constexpr (!ROWS) sums += v;
+              if constexpr (!ROWS) part[k] += v;
               df[b][q >> 1][4 * (q & 1) + k] = (T)v;
             }
             __builtin_amdgcn_sched_barrier(0);
@@ -779,6 +780,7 @@ __global__ __launch_bounds__(NWS_THREADS, 2) void k_narrow_side(TpOperand own, T
       };
       if (any || masked) form(std::true_type());
       else form(std::false_type());
+      if constexpr (!ROWS) sums += (part[0] + part[1]) + (part[2] + part[3]);
       // dz times what passes by: k in the accumulators' order, 16 c + 8 hi + 4 g + 0..3 of a block
       Frag uf[4];
       auto turned = [&](int k) {  // k = 8 b + 4 c + u
