@@ -47,7 +47,10 @@ inline TpPlan tp_plan(int dtype, int m, int n, int64_t k, int max_splits) {
   int64_t most = steps / 8 < max_splits ? steps / 8 : max_splits;
   if (most < 1 || steps < 24) most = 1;
   const bool split_large = large >= 48 && large < 192 && max_splits > 1 && k * large >= 8192ll * 256;
-  const bool much = (double)m * n * k >= 1e10;
+  // (fp32 takes longer for the same slabs; tiles that would be a quarter emptier than small ones stay small.  The label loss in
+  // fp32 of 995 rows, 6,929 labels, width 1,208: 803 us from 1e10 on, 676 from 5e9; of 556 rows, 253,146 labels, width 128
+  // 2,116, and 2,262 from 1e9.)
+  const bool much = (double)m * n * k >= (dtype == 0 ? 5e9 : 1e10) && 16 * medium <= 5 * small;
   p.shape = m <= 32                                           ? (n > 192 * 128 ? TP_FEW : TP_TINY)
             : (large >= 192 && steps > SHORT_K) || split_large ? TP_LARGE
             : medium >= 192 || (much && medium * most >= 256)  ? TP_MEDIUM

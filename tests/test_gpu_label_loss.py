@@ -470,3 +470,11 @@ def test_many_narrow_rows_whose_logits_are_not_finite():
     c = Call(h, w, lists, bias, dtype="f16").run()
     c.check(lists, "f16")
     assert bool((c.dw[1000:1200] == 0).all()) and bool((c.db[1000:1200] == 0).all())
+
+
+def test_medium_tiles_in_single_precision():
+    # dz W in medium tiles with the labels split
+    B, L, D = 995, 5000, 1208
+    h, w = placed(normal(1, B, D), "f32"), placed(normal(2, L, D, scale=2 * D ** -0.5), "f32")
+    lists = random_lists(3, B, L, 2)
+    Call(h, w, lists, normal(4, L), dtype="f32").run().check(lists, "f32")
