@@ -351,14 +351,14 @@ __global__ __launch_bounds__(NW_THREADS) void k_narrow_grad(TpOperand h, TpOpera
 #pragma unroll
     for (int c = 0; c < 2; ++c) zat[hi][c] = nw_dz(16 * c + 8 * (G >> 1) + 4 * hi + ti, 8 * lb + 4 * (G & 1) + ta);
   }
-  // whole 16-byte pieces of dw in the operands' type: two stores, which are sure to follow a tile's copies
+  // whole 16-byte pieces of dw in the operands' type
   const bool wide = dw.data && dw.dtype == (std::is_same<T, bf16>::value ? 1 : 2) && 32 * wu + 32 <= d;
   float* const sums = reinterpret_cast<float*>(smem + NWG_SUM);
 
+  tp_wait<0>();
   for (int t = t0; t < t1; ++t) {
-    // (vmcnt counts stores too: the two of the last tile's dw came after the copies and need not be waited for)
-    if (wide && t > t0) tp_wait<2>();
-    else tp_wait<0>();
+    // (the wait for this tile's copies stands before the last tile's stores of dw)
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     __builtin_amdgcn_s_barrier();  // the tile is here, and nobody reads dz or the other tile any more
     if (t + 1 < t1) issue(t + 1);
     const char* p = smem + NWG_W + (t - t0) % NWG_BUFS * (NW_WBUF + NW_BIAS);
@@ -458,8 +458,8 @@ __global__ __launch_bounds__(NW_THREADS) void k_narrow_grad(TpOperand h, TpOpera
       for (int k = 0; k < 8; ++k) v += sums[k * NW_TILE + tid];
       db[t * NW_TILE + tid] = v * out;
     }
+    f32x16 acc;
     if (dw.data) {
-      f32x16 acc;
 #pragma unroll
       for (int r = 0; r < 16; ++r) acc[r] = 0.0f;
       // (what a product reads from LDS is on its way while the one before runs)
@@ -477,6 +477,11 @@ __global__ __launch_bounds__(NW_THREADS) void k_narrow_grad(TpOperand h, TpOpera
         acc = tp_mma(hd[c & 1], zd[c & 1], acc);
         __builtin_amdgcn_sched_barrier(0);
       }
+    }
+    // The next tile's copies, of which the whole of this tile's work lies behind, before any store: nothing then goes by
+    // how many stores follow them, or by the order in which loads and stores end.
+    tp_wait<0>();
+    if (dw.data) {
       const int label = t * NW_TILE + 32 * lb + n;
       if (wide) {
         nw_store32<T>(dw, label, 32 * wu, g, acc, out, label < L);
