@@ -119,9 +119,6 @@ __device__ __forceinline__ void nw_logits(const char* w, const typename TpMma<T>
 
 }  // namespace
 
-// The whole power of two that exponentials of logits up to `top` are taken relative to.
-__device__ __forceinline__ float nw_base(float top) { return top == -INFINITY ? 0.0f : __builtin_ceilf(top * LOG2E); }
-
 // ---- log-sum-exp ---------------------------------------------------------------------------------
 // Workgroup = (256 rows, a range of tiles); the row blocks of a range follow each other on one XCD, whose L2 then has its
 // labels (and all 8 XCDs have work where there are fewer ranges: 65,536 rows, 5,000 labels 441 us on one, 202 on
@@ -157,7 +154,7 @@ __global__ __launch_bounds__(NWF_THREADS, 2) void k_narrow_lse(TpOperand h, TpOp
 #pragma unroll
   for (int k = 0; k < NWF_BUFS - 1; ++k)
     if (t0 + k < t1) issue(t0 + k);
-  float m[2] = {-INFINITY, -INFINITY}, s[2] = {0.0f, 0.0f}, base[2] = {0.0f, 0.0f};
+  float m[2] = {-INFINITY, -INFINITY}, s[2] = {0.0f, 0.0f};
   for (int t = t0; t < t1; ++t) {
     if (t + NWF_BUFS - 2 < t1) tp_wait<(NWF_BUFS - 2) * NwLoad<NWF_THREADS>::COPIES>();
     else tp_wait<0>();
@@ -192,28 +189,26 @@ __global__ __launch_bounds__(NWF_THREADS, 2) void k_narrow_lse(TpOperand h, TpOp
 #pragma unroll
         for (int r = 0; r < 16; ++r) top[b] = fmaxf(top[b], z[i][b][r]);
       const float mm = fmaxf(top[0], top[1]);
-      // base 2, relative to a whole number: it rounds nothing, and sums change their base exactly
-      const float b2 = nw_base(mm);
-      float e[4] = {m[i] == -INFINITY ? s[i] : s[i] * __builtin_amdgcn_exp2f(base[i] - b2), 0.0f, 0.0f, 0.0f};
+      // Relative to the maximum, which is taken off first: masks may be of any size (the lowest value times log2 e is
+      // -infinity, and from 10^10 on that product rounds by more than an exponent holds).
+      const float base = mm == -INFINITY ? 0.0f : mm;
+      float e[4] = {s[i] * exp_fast(m[i] - base), 0.0f, 0.0f, 0.0f};
 #pragma unroll
       for (int b = 0; b < 2; ++b)
 #pragma unroll
-        for (int r = 0; r < 16; ++r) e[r & 3] += __builtin_amdgcn_exp2f(fmaf(z[i][b][r], LOG2E, -b2));
+        for (int r = 0; r < 16; ++r) e[r & 3] += exp_fast(z[i][b][r] - base);
       s[i] = (e[0] + e[1]) + (e[2] + e[3]);
       m[i] = mm;
-      base[i] = b2;
     }
   }
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
     const float m2 = __builtin_bit_cast(float, lane_xor<32>(__builtin_bit_cast(unsigned, m[i]), lane));
     const float s2 = __builtin_bit_cast(float, lane_xor<32>(__builtin_bit_cast(unsigned, s[i]), lane));
-    const float b2 = __builtin_bit_cast(float, lane_xor<32>(__builtin_bit_cast(unsigned, base[i]), lane));
-    const float mm = fmaxf(m[i], m2), top = mm == -INFINITY ? 0.0f : mm;
+    const float mm = fmaxf(m[i], m2), base = mm == -INFINITY ? 0.0f : mm;
     if (row + 32 * i < B && g == 0)
-      part[(int64_t)(row + 32 * i) * ranges + range] =  // (relative to the maximum from here on)
-          make_float2(mm, (m[i] == -INFINITY ? s[i] : s[i] * __builtin_amdgcn_exp2f(fmaf(-top, LOG2E, base[i]))) +
-                              (m2 == -INFINITY ? s2 : s2 * __builtin_amdgcn_exp2f(fmaf(-top, LOG2E, b2))));
+      part[(int64_t)(row + 32 * i) * ranges + range] =
+          make_float2(mm, s[i] * exp_fast(m[i] - base) + s2 * exp_fast(m2 - base));
   }
 }
 
@@ -310,13 +305,12 @@ __global__ __launch_bounds__(NW_THREADS) void k_narrow_grad(TpOperand h, TpOpera
   Frag hf[8];
   nw_rows<T>(h, row, B, d_bytes, g, hf);
   const float scale = *a.scale;
-  float sh = 0.0f, b2 = 0.0f, f = 0.0f, fp = 0.0f;
+  float sh = 0.0f, top = 0.0f, f = 0.0f, fp = 0.0f;
   if (row < B) {
     sh = a.share[row];
-    const float top = a.top[row];
-    b2 = nw_base(top);
+    top = a.top[row];
     f = (a.weights ? scale > 0.0f ? a.weights[row] / scale : a.weights[row] : 1.0f) * a.up;
-    fp = f * a.inv[row] * __builtin_amdgcn_exp2f(fmaf(-(top == -INFINITY ? 0.0f : top), LOG2E, b2));
+    fp = f * a.inv[row];
   }
   const bool live = sh > 0.0f;
   const float out = alpha * scale, fs = f * sh;
@@ -412,7 +406,7 @@ __global__ __launch_bounds__(NW_THREADS) void k_narrow_grad(TpOperand h, TpOpera
 #pragma unroll
           for (int k = 0; k < 4; ++k) {
             float v = z[b][4 * q + k];
-            v = __builtin_amdgcn_exp2f(fmaf(v, LOG2E, -b2)) * fp;
+            v = exp_fast(v - top) * fp;  // (a row's best label gets 1 / sum exactly, so one that is certain 1)
             bool in = live;  // (rows without labels and labels past the last are zeros, whatever they hold)
             if (checked) {
               v -= (float)((times >> (16 * k)) & 0xffff) * fs;
@@ -517,16 +511,16 @@ constexpr int NWS_HIT = NWS_ROW + 4 * 3 * 256, NWS_SORT = NWS_HIT + 4 * (NWS_HIT
 constexpr int NWS_AT = NWS_START + 4 * 260, NWS_LDS = NWS_AT + 4 * 256;
 static_assert(2 * NWS_LDS <= 160 * 1024, "two workgroups per compute unit");
 
-// What turns a logit of row i into dz: v = 2^(z log2 e - base) fp - times fs.  A row without labels gets zeros, and NaN where
+// What turns a logit of row i into dz: v = e^(z - top) fp - times fs.  A row without labels gets zeros, and NaN where
 // its logit (a bias, since its h is zeros) is NaN or +infinity: its dh is made zeros when the slabs are joined, and in dw and db every other
 // row gives NaN there too (no other row: zeros at the end).
 struct NwRow {
-  float base, fp, fs;
+  float top, fp, fs;
 };
 __device__ __forceinline__ NwRow nw_row(const DzArgs& a, float top, float inv, float share, float weight, float scale) {
-  if (!(share > 0.0f)) return NwRow{3e38f, 0.0f, 0.0f};
-  const float f = (a.weights ? scale > 0.0f ? weight / scale : weight : 1.0f) * a.up, b = nw_base(top);
-  return NwRow{b, f * inv * __builtin_amdgcn_exp2f(fmaf(-(top == -INFINITY ? 0.0f : top), LOG2E, b)), f * share};
+  if (!(share > 0.0f)) return NwRow{INFINITY, 0.0f, 0.0f};
+  const float f = (a.weights ? scale > 0.0f ? weight / scale : weight : 1.0f) * a.up;
+  return NwRow{top, f * inv, f * share};
 }
 
 // ROWS: own = rows of h, 128 of them, and tiles t0 .. of labels; else own = labels, `per` blocks of 128 after each other,
@@ -661,7 +655,7 @@ __global__ __launch_bounds__(NWS_THREADS, 2) void k_narrow_side(TpOperand own, T
     Frag of[8];
     nw_rows<T>(own, me, n_own, d_bytes, g, of);
     const float own_bias = !ROWS && a.bias && me < n_own ? a.bias[me] : 0.0f;
-    NwRow mine{3e38f, 0.0f, 0.0f};
+    NwRow mine{INFINITY, 0.0f, 0.0f};
     if (ROWS && me < B) mine = nw_row(a, a.top[me], a.inv[me], a.share[me], a.weights ? a.weights[me] : 0.0f, scale);
     f32x16 acc[4];
 #pragma unroll
@@ -683,7 +677,7 @@ __global__ __launch_bounds__(NWS_THREADS, 2) void k_narrow_side(TpOperand own, T
         masked = (t + 1) * NW_TILE > n_other;
       } else {
         const NwRow r = nw_row(a, r_top, r_inv, r_share, r_weight, scale);
-        rows[lane] = r.base;
+        rows[lane] = r.top;
         rows[64 + lane] = r.fp;
         rows[128 + lane] = r.fs;
         live |= __ballot(r_share > 0.0f) != 0;
@@ -761,9 +755,9 @@ __global__ __launch_bounds__(NWS_THREADS, 2) void k_narrow_side(TpOperand own, T
 #pragma unroll
           for (int q = 0; q < 4; ++q) {
             const int c = 32 * b + 8 * q + 4 * g;
-            f32x4 base, fp, fs;
+            f32x4 top, fp, fs;
             if constexpr (!ROWS) {
-              base = *reinterpret_cast<const f32x4*>(rows + c);
+              top = *reinterpret_cast<const f32x4*>(rows + c);
               fp = *reinterpret_cast<const f32x4*>(rows + 64 + c);
               if (checked) fs = *reinterpret_cast<const f32x4*>(rows + 128 + c);
             }
@@ -771,8 +765,7 @@ __global__ __launch_bounds__(NWS_THREADS, 2) void k_narrow_side(TpOperand own, T
             if (checked) times = any ? *reinterpret_cast<const uint64_t*>(counts + (count_at ^ (64 * b) ^ (16 * q))) : 0;
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
-              const float bk = ROWS ? mine.base : base[k];
-              float v = __builtin_amdgcn_exp2f(fmaf(z[b][4 * q + k], LOG2E, -bk)) * (ROWS ? mine.fp : fp[k]);
+              float v = exp_fast(z[b][4 * q + k] - (ROWS ? mine.top : top[k])) * (ROWS ? mine.fp : fp[k]);
               if (checked) {
                 v -= (float)((times >> (16 * k)) & 0xffff) * (ROWS ? mine.fs : fs[k]);
                 if (ROWS && first + c + k >= n_other) v = 0.0f;

@@ -59,3 +59,69 @@ def test_bias_gradient_of_many_tiles_a_workgroup(scale, dtype):
         c.run()
         for k, v in c.outputs().items():
             assert torch.equal(v, first[k]), k
+
+
+LOWEST = torch.finfo(torch.float32).min
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("low", [LOWEST, -1e30, -1e10, -1e9])
+@pytest.mark.parametrize("B,L,D", [(100, 70_000, 128), (300, 70_000, 128), (300, 45_000, 61), (40, 3_000, 64)])
+def test_labels_masked_by_very_low_biases(B, L, D, low, dtype):
+    # whole tiles of them: the first of each range of tiles, runs, and all but one label
+    h, w = placed(normal(1, B, D), dtype), placed(normal(2, L, D, scale=2 * D ** -0.5), dtype)
+    lane = torch.arange(L, device="cuda") // 64
+    for masked in (lane % 3 == 0, lane % 3 != 0, lane > 0, lane < L // 64):
+        bias = torch.where(masked, low, normal(4, L))
+        free = (~masked).nonzero()[:, 0].tolist()
+        lists = [[free[(7 * i) % len(free)], free[(11 * i + 1) % len(free)]] for i in range(B)]
+        lists[3] = []
+        Call(h, w, lists, bias, dtype=dtype).run().check(lists, dtype)
+        alone = Call(h, w, lists, bias, dtype=dtype, grads=()).run()
+        alone.check(lists, dtype)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("low", [LOWEST, -1e10, -300.0, -INF])
+@pytest.mark.parametrize("B,L", [(100, 70_000), (300, 70_000), (256, 20_001)])
+def test_one_label_that_is_certain(B, L, low, dtype):
+    # p is 1 and 0 exactly, so nothing is left of the gradients
+    h, w = placed(normal(1, B, 128), dtype), placed(normal(2, L, 128, scale=0.1), dtype)
+    for one in (0, 12_345, L - 1):
+        bias = torch.full((L,), low, device="cuda")
+        bias[one] = 0.5
+        c = Call(h, w, [[one]] * B, bias, dtype=dtype).run()
+        c.check([[one]] * B, dtype)
+        for k in ("dh", "dw", "db"):
+            assert bool((c.outputs()[k] == 0).all()), k
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("B,L", [(100, 70_000), (300, 70_000)])
+def test_all_labels_masked_alike(B, L, dtype):
+    # logits of the lowest value whatever h and w are: as likely as each other
+    h, w = placed(normal(1, B, 128), dtype), placed(normal(2, L, 128, scale=0.1), dtype)
+    lists = [[i, 2 * i + 500] for i in range(B)]
+    c = Call(h, w, lists, torch.full((L,), LOWEST, device="cuda"), dtype=dtype).run()
+    assert bool((c.lse[:B] == LOWEST).all())
+    want = torch.full((L,), 1.0 / L, dtype=torch.float64, device="cuda")
+    ids = torch.tensor(lists, device="cuda").flatten()
+    want.index_add_(0, ids, torch.full_like(ids, -0.5 / B, dtype=torch.float64))
+    # sums of B equal terms that are good to 8 steps
+    assert bool(((c.db[:L].double() - want).abs() <= (B + 8) * ref.U * (1.0 / L + want.abs())).all())
+    assert all(bool(c.outputs()[k].isfinite().all()) for k in ("dh", "dw", "db"))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("B,L", [(100, 70_000), (300, 45_000), (40, 3_000)])
+def test_logits_far_from_zero(B, L, dtype):
+    # a bias that all labels share moves the log-sum-exp and nothing else; 2^14 leaves logits of few bits exact
+    g = torch.Generator().manual_seed(1)
+    h, w = (torch.randint(-2, 3, s, generator=g).float() for s in ((B, 128), (L, 128)))
+    h, w = placed(h.cuda(), dtype), placed((w / 8).cuda(), dtype)
+    lists = random_lists(3, B, L, 3)
+    near = Call(h, w, lists, torch.zeros(L, device="cuda"), dtype=dtype).run().outputs()
+    for shift in (-16384.0, 16384.0, -131072.0):
+        far = Call(h, w, lists, torch.full((L,), shift, device="cuda"), dtype=dtype).run().outputs()
+        for k in ("dh", "dw", "db"):
+            assert torch.equal(far[k], near[k]), (shift, k)
