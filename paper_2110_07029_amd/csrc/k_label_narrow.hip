@@ -511,9 +511,8 @@ constexpr int NWS_HIT = NWS_ROW + 4 * 3 * 256, NWS_SORT = NWS_HIT + 4 * (NWS_HIT
 constexpr int NWS_AT = NWS_START + 4 * 260, NWS_LDS = NWS_AT + 4 * 256;
 static_assert(2 * NWS_LDS <= 160 * 1024, "two workgroups per compute unit");
 
-// What turns a logit of row i into dz: v = e^(z - top) fp - times fs.  A row without labels gets zeros, and NaN where
-// its logit (a bias, since its h is zeros) is NaN or +infinity: its dh is made zeros when the slabs are joined, and in dw and db every other
-// row gives NaN there too (no other row: zeros at the end).
+// What turns a logit of row i into dz: v = e^(z - top) fp - times fs.  A row without labels gets zeros from
+// any finite logit; one that is not (its h is zeros, but w or the bias of a label may hold anything) is made one before.
 struct NwRow {
   float top, fp, fs;
 };
@@ -663,7 +662,15 @@ __global__ __launch_bounds__(NWS_THREADS, 2) void k_narrow_side(TpOperand own, T
 #pragma unroll
       for (int r = 0; r < 16; ++r) acc[u][r] = 0.0f;
     float sums = 0.0f;
-    bool live = ROWS;
+    bool odd = false;  // some label of the wave holds a value that is not finite (0 times the others sum to 0)
+    if constexpr (!ROWS) {
+      float zero = own_bias * 0.0f;
+#pragma unroll
+      for (int kk = 0; kk < 8; ++kk)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) zero = fmaf((float)of[kk][i], 0.0f, zero);
+      odd = __ballot(!(zero == 0.0f)) != 0;
+    }
     for (int t = t0; t < t1; ++t) {
       tp_wait<0>();
       __builtin_amdgcn_s_barrier();  // the tile is here, and nobody reads the one before
@@ -680,7 +687,6 @@ __global__ __launch_bounds__(NWS_THREADS, 2) void k_narrow_side(TpOperand own, T
         rows[lane] = r.top;
         rows[64 + lane] = r.fp;
         rows[128 + lane] = r.fs;
-        live |= __ballot(r_share > 0.0f) != 0;
         fetch_row(t + 1 < t1 ? t + 1 : t0);
       }
       // how often a label stands in a row's list: 16-bit counts per own
@@ -747,6 +753,18 @@ __global__ __launch_bounds__(NWS_THREADS, 2) void k_narrow_side(TpOperand own, T
         for (int b = 0; b < 2; ++b) z[b] = tp_mma(f[kk & 1][b], of[kk], z[b]);
         __builtin_amdgcn_sched_barrier(0);
       }
+      if constexpr (!ROWS) {
+        if (odd) {  // (in dh such rows are made zeros when the slabs are joined)
+#pragma unroll
+          for (int b = 0; b < 2; ++b)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+              const f32x4 top = *reinterpret_cast<const f32x4*>(rows + 32 * b + 8 * q + 4 * g);
+#pragma unroll
+              for (int k = 0; k < 4; ++k) z[b][4 * q + k] = top[k] == INFINITY ? 0.0f : z[b][4 * q + k];
+            }
+        }
+      }
       Frag df[2][2];
       float part[4] = {};  // (one sum over thousands of rows would round as often)
       auto form = [&](auto checked) {
@@ -808,7 +826,7 @@ __global__ __launch_bounds__(NWS_THREADS, 2) void k_narrow_side(TpOperand own, T
       }
     } else {
       sums += __builtin_bit_cast(float, lane_xor<32>(__builtin_bit_cast(unsigned, sums), lane));
-      if (db && g == 0 && me < n_own) db[me] = live ? sums * out : 0.0f;
+      if (db && g == 0 && me < n_own) db[me] = sums * out;
       if (dw.data) {
         // 32 columns at a time through the wave's block of counts, chunk c of label r at place c ^ (r % 8)
         float* const block = reinterpret_cast<float*>(counts + 4096 * wave);
@@ -825,9 +843,6 @@ __global__ __launch_bounds__(NWS_THREADS, 2) void k_narrow_side(TpOperand own, T
             const f32x4 lo = *reinterpret_cast<const f32x4*>(block + 32 * r + 4 * (c ^ (r & 7)));
             const f32x4 hi = *reinterpret_cast<const f32x4*>(block + 32 * r + 4 * ((c + 1) ^ (r & 7)));
             float v[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
-            if (!live)
-#pragma unroll
-              for (int i = 0; i < 8; ++i) v[i] = 0.0f;
             if (label < n_own && col < d) store8(dw, label, col, min(8, d - col), v);
           }
           __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "wavefront");

@@ -125,3 +125,43 @@ def test_logits_far_from_zero(B, L, dtype):
         far = Call(h, w, lists, torch.full((L,), shift, device="cuda"), dtype=dtype).run().outputs()
         for k in ("dh", "dw", "db"):
             assert torch.equal(far[k], near[k]), (shift, k)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("B,L", [(100, 70_000), (300, 41_000), (320, 41_000), (500, 70_001)])
+def test_infinities_in_a_label_reach_no_row_without_labels(B, L, dtype):
+    # A -inf against a column of ones makes a label's logit -inf in every live row, as a bias of -inf does.  Rows without
+    # labels (and those that fill up the last tile of 64) take part in nothing, whatever 0 times that is.
+    h, w = placed(normal(1, B, 128), dtype), placed(normal(2, L, 128, scale=0.1), dtype)
+    h[:, 5] = 1.0
+    lists = [r or [77] for r in random_lists(3, B, L, 3)]
+    lists[7], lists[B - 1] = [], [-1, L]
+    bias = normal(4, L)
+    for rows in (lists, [r or [3] for r in lists]):
+        rows = [[i for i in r if i not in (40, 1000, L - 1)] or [2] * bool(r) for r in rows]
+        masked = bias.clone()
+        for j in (40, 1000, L - 1):
+            masked[j] = -INF
+        want = {k: v.clone() for k, v in Call(h, w, rows, masked, dtype=dtype).run().outputs().items()}
+        sick = w.clone()
+        sick[40, 5] = sick[1000, 5] = sick[L - 1, 5] = -INF
+        got = Call(h, sick, rows, bias, dtype=dtype).run().outputs()
+        for k in ("loss", "lse", "dw", "db"):
+            assert torch.equal(got[k], want[k]) and bool(want[k].isfinite().all()), k
+        other = [c for c in range(128) if c != 5]  # (0 times the infinity itself is NaN, in the column that has it)
+        assert torch.equal(got["dh"][:, other], want["dh"][:, other])
+
+
+def test_a_label_that_is_not_finite_in_live_rows():
+    # NaN of a live row stays NaN: 0 weights do not hide it
+    B, L = 300, 41_000
+    h, w = placed(normal(1, B, 128), "bf16"), placed(normal(2, L, 128, scale=0.1), "bf16")
+    lists, bias = [[i] for i in range(B)], normal(4, L)
+    lists[9] = []
+    weights = torch.full((B,), 1e-3, device="cuda")
+    weights[8] = 0.0
+    bias[500] = NAN
+    c = Call(h, w, lists, bias, weights, "bf16").run()
+    live = [i for i in range(B) if i != 9]
+    assert bool(c.loss[live].isnan().all()) and float(c.loss[9]) == 0.0 and bool((c.dh[9] == 0).all())
+    assert bool(c.dw.isnan().all()) and bool(c.db[:L].isnan().all()) and bool(c.dh[live].isnan().all())
