@@ -561,73 +561,101 @@ __global__ __launch_bounds__(NWS_THREADS, 2) void k_narrow_side(TpOperand own, T
   };
   issue(t0, 0);
   if (!ROWS) fetch_row(t0);
-  // targets between own and what passes by, listed once: own within the workgroup's, other; then in the order of the tiles
-  // (or of up to 256 groups of them), so that a tile looks at its own alone
+  // Targets between own (first .. last of them) and tiles wa .. wb of what passes by, listed: own within the list's, other;
+  // then in the order of the tiles (or of up to 256 groups of them), so that a tile looks at its own alone.  Returns how many
+  // there are; more than NWS_HITS are not listed (nor all counted: then about how many).
   unsigned* const hits = reinterpret_cast<unsigned*>(smem + NWS_HIT);
   unsigned* const sorted = reinterpret_cast<unsigned*>(smem + NWS_SORT);
   int* const start = reinterpret_cast<int*>(smem + NWS_START);  // [257]
   int* const next = reinterpret_cast<int*>(smem + NWS_AT);
   constexpr int SHIFT = ROWS ? 24 : 18;
   int group = 0;  // tiles of one: 2^group
-  while ((t1 - t0) >> group > 255) ++group;
-  start[tid] = 0;
-  if (tid == 0) hits[0] = start[256] = 0;
-  asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-  __builtin_amdgcn_s_barrier();
-  const int own0 = b0 * NWS_OWN, own1 = min(n_own, b1 * NWS_OWN);
-  if constexpr (ROWS) {
-    const int l0 = t0 * NW_TILE, l1 = min(n_other, t1 * NW_TILE);
-    if (own0 + (tid >> 1) < B && a.y.indptr)
-      each_label(a.y, own0 + (tid >> 1), tid & 1, 2, [&](int id) {
-        if (id >= l0 && id < l1) {
-          const unsigned k = atomicAdd(hits, 1u);
-          if (k < NWS_HITS) hits[1 + k] = (unsigned)(tid >> 1) << SHIFT | (unsigned)id;
+  auto list = [&](int first, int last, int wa, int wb) {
+    __syncthreads();  // (nobody looks at the list before any more)
+    for (group = 0; (wb - wa) >> group > 255;) ++group;
+    start[tid] = 0;
+    if (tid == 0) hits[0] = start[256] = 0;
+    __syncthreads();
+    int n_ids = 0;
+    if constexpr (ROWS) {
+      const int l0 = wa * NW_TILE, l1 = min(n_other, wb * NW_TILE);
+      if (first + (tid >> 1) < last && a.y.indptr)
+        each_label(a.y, first + (tid >> 1), tid & 1, 2, [&](int id) {
+          if (id >= l0 && id < l1) {
+            const unsigned k = atomicAdd(hits, 1u);
+            if (k < NWS_HITS) hits[1 + k] = (unsigned)(tid >> 1) << SHIFT | (unsigned)id;
+          }
+        });
+    } else if (a.y.indptr) {
+      // the rows' lists as one: entries whose label is here, then their rows by bisection
+      const int r0 = wa * NW_TILE, r1 = min(B, wb * NW_TILE);
+      const int64_t begin = *a.y.first, end = begin + a.y.nnz;
+      const int64_t q0 = min(max((int64_t)a.y.indptr[r0], begin), end), q1 = min(max((int64_t)a.y.indptr[r1], q0), end);
+      const int32_t* const ids = a.y.indices + q0;
+      n_ids = (int)(q1 - q0);
+      auto take = [&](unsigned found, auto place) {  // bits: which of a thread's entries
+        if (!found) return;
+        for (unsigned h = atomicAdd(hits, (unsigned)__popc(found)); found && h < NWS_HITS; ++h, found &= found - 1)
+          hits[1 + h] = (unsigned)place(__ffs(found) - 1);
+      };
+      const int whole = n_ids & ~(16 * NWS_THREADS - 1);  // (16 ids a thread on their way at once)
+      int seen = 0;  // a list that is full already is not needed whole
+      for (; seen < whole && __hip_atomic_load(hits, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP) <= NWS_HITS;
+           seen += 16 * NWS_THREADS) {
+        const int q = seen + 4 * tid;
+        i32x4 id[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) id[k] = *reinterpret_cast<const i32x4u*>(ids + q + 4 * NWS_THREADS * k);
+        unsigned found = 0;
+#pragma unroll
+        for (int k = 0; k < 16; ++k) found |= (unsigned)(id[k >> 2][k & 3] >= first && id[k >> 2][k & 3] < last) << k;
+        take(found, [&](int k) { return q + 4 * NWS_THREADS * (k >> 2) + (k & 3); });
+      }
+      if (seen == whole) {
+        for (int q = whole + tid; q < n_ids; q += 8 * NWS_THREADS) {
+          int id[8];
+          unsigned found = 0;
+#pragma unroll
+          for (int k = 0; k < 8; ++k) id[k] = q + k * NWS_THREADS < n_ids ? ids[q + k * NWS_THREADS] : -1;
+#pragma unroll
+          for (int k = 0; k < 8; ++k) found |= (unsigned)(id[k] >= first && id[k] < last) << k;
+          take(found, [&](int k) { return q + k * NWS_THREADS; });
         }
-      });
-  } else if (a.y.indptr) {
-    // the lists as one: entries whose label is here, then their rows by bisection
-    const int64_t first = *a.y.first;
-    const int32_t* const ids = a.y.indices + first;
-    const int nnz = a.y.nnz;
-    auto take = [&](int id, int q) {
-      if (id < own0 || id >= own1) return;
-      const unsigned h = atomicAdd(hits, 1u);
-      if (h < NWS_HITS) hits[1 + h] = (unsigned)q;
-    };
-    const int whole = nnz & ~(16 * NWS_THREADS - 1);  // (16 ids a thread on their way at once)
-    for (int q = 4 * tid; q < whole; q += 16 * NWS_THREADS) {
-      i32x4 id[4];
-#pragma unroll
-      for (int k = 0; k < 4; ++k) id[k] = *reinterpret_cast<const i32x4u*>(ids + q + 4 * NWS_THREADS * k);
-#pragma unroll
-      for (int k = 0; k < 16; ++k) take(id[k >> 2][k & 3], q + 4 * NWS_THREADS * (k >> 2) + (k & 3));
-    }
-    for (int q = whole + tid; q < nnz; q += 8 * NWS_THREADS) {
-      int id[8];
-#pragma unroll
-      for (int k = 0; k < 8; ++k) id[k] = q + k * NWS_THREADS < nnz ? ids[q + k * NWS_THREADS] : -1;
-#pragma unroll
-      for (int k = 0; k < 8; ++k) take(id[k], q + k * NWS_THREADS);
+        seen = n_ids;
+      }
+      if (tid == 0) next[0] = seen;
+      // (of every row or every 2^skip-th where it begins, in LDS: from memory a step takes as long as a tile's products)
+      int skip = 0;
+      while ((r1 - r0 - 1) >> skip > NWS_HITS) ++skip;
+      const int known = ((r1 - r0 - 1) >> skip) + 1;
+      for (int i = tid; i < known; i += NWS_THREADS) sorted[i] = (unsigned)a.y.indptr[r0 + (i << skip)];
+      __syncthreads();
+      const int held = hits[0] <= NWS_HITS ? (int)hits[0] : 0;
+      for (int h = tid; h < held; h += NWS_THREADS) {
+        const int64_t q = q0 + hits[1 + h];
+        int lo = 0, hi = known;  // the last row that does not begin behind q
+        while (hi - lo > 1) {
+          const int mid = (lo + hi) >> 1;
+          if ((int)sorted[mid] <= q) lo = mid;
+          else hi = mid;
+        }
+        lo = r0 + (lo << skip);
+        hi = min(r1, lo + (1 << skip));
+        while (hi - lo > 1) {
+          const int mid = (lo + hi) >> 1;
+          if (a.y.indptr[mid] <= q) lo = mid;
+          else hi = mid;
+        }
+        int s0, s1;
+        label_range(a.y, lo, &s0, &s1);
+        hits[1 + h] = q >= s0 && q < s1 ? (unsigned)(a.y.indices[q] - first) << SHIFT | (unsigned)lo : ~0u;
+      }
     }
     __syncthreads();
-    const int total = min((int)hits[0], NWS_HITS);
-    for (int h = tid; h < total; h += NWS_THREADS) {
-      const int64_t q = first + hits[1 + h];
-      int lo = 0, hi = B;  // the last row that does not begin behind q
-      while (hi - lo > 1) {
-        const int mid = (lo + hi) >> 1;
-        if (a.y.indptr[mid] <= q) lo = mid;
-        else hi = mid;
-      }
-      int q0, q1;
-      label_range(a.y, lo, &q0, &q1);
-      hits[1 + h] = q >= q0 && q < q1 ? (unsigned)(a.y.indices[q] - own0) << SHIFT | (unsigned)lo : ~0u;
-    }
-  }
-  __syncthreads();
-  const int total = (int)hits[0];
-  if (total && total <= NWS_HITS) {
-    auto group_of = [&](unsigned hit) { return (int)((((hit & ((1u << SHIFT) - 1)) >> 6) - t0) >> group); };
+    const int total = (int)hits[0];
+    if (total > NWS_HITS) return ROWS ? total : (int)((int64_t)total * n_ids / max(next[0], min(n_ids, 16 * NWS_THREADS)));
+    if (total == 0) return 0;
+    auto group_of = [&](unsigned hit) { return (int)((((hit & ((1u << SHIFT) - 1)) >> 6) - wa) >> group); };
     for (int h = tid; h < total; h += NWS_THREADS)
       if (hits[1 + h] != ~0u) atomicAdd(start + 1 + group_of(hits[1 + h]), 1);
     __syncthreads();
@@ -642,7 +670,12 @@ __global__ __launch_bounds__(NWS_THREADS, 2) void k_narrow_side(TpOperand own, T
     for (int h = tid; h < total; h += NWS_THREADS)
       if (hits[1 + h] != ~0u) sorted[atomicAdd(next + group_of(hits[1 + h]), 1)] = hits[1 + h];
     __syncthreads();
-  }
+    return total;
+  };
+  // One list for all of it where it fits; else one for each block of own; else as many as it takes, of as many tiles as
+  // should fit if targets were spread evenly, or fewer.  (A tile that has too many by itself looks through its rows' lists.)
+  const int own0 = b0 * NWS_OWN, own1 = min(n_own, b1 * NWS_OWN);
+  int list0 = own0, list_n = own1 - own0, total = 0, wa = t0, wb = t0;  // the list's own, its tiles
   char* const counts = smem + NWS_COUNT;
   // LDS addresses, of which the parts of kk, u, hi, b and q flip bits: formed where they are used (as loop invariants they
   // would take the registers that the sums need)
@@ -671,147 +704,169 @@ __global__ __launch_bounds__(NWS_THREADS, 2) void k_narrow_side(TpOperand own, T
         for (int i = 0; i < 8; ++i) zero = fmaf((float)of[kk][i], 0.0f, zero);
       odd = __ballot(!(zero == 0.0f)) != 0;
     }
-    for (int t = t0; t < t1; ++t) {
-      tp_wait<0>();
-      __builtin_amdgcn_s_barrier();  // the tile is here, and nobody reads the one before
-      asm volatile("" : "+v"(row_at), "+v"(turned_at), "+v"(count_at));
-      const char* const p = smem + buf * NWS_BUF;
-      buf ^= 1;
-      if (t + 1 < t1) issue(t + 1, buf);
-      else if (blk + 1 < b1) issue(t0, buf);
-      bool masked = false;  // labels past the last
-      if constexpr (ROWS) {
-        masked = (t + 1) * NW_TILE > n_other;
-      } else {
-        const NwRow r = nw_row(a, r_top, r_inv, r_share, r_weight, scale);
-        rows[lane] = r.top;
-        rows[64 + lane] = r.fp;
-        rows[128 + lane] = r.fs;
-        fetch_row(t + 1 < t1 ? t + 1 : t0);
-      }
-      // how often a label stands in a row's list: 16-bit counts per own
-      bool any = total > NWS_HITS;
-      const int first = t * NW_TILE, from = (blk - b0) * NWS_OWN + 32 * wave;
-      auto place = [&](unsigned hit, int* o, int* c) {
-        *o = (int)(hit >> SHIFT) - from;
-        *c = (int)(hit & ((1u << SHIFT) - 1)) - first;
-        return *o >= 0 && *o < 32 && *c >= 0 && *c < NW_TILE;
-      };
-      int h0 = 0, h1 = 0;
-      if (total && !any) {
-        h0 = start[(t - t0) >> group];
-        h1 = start[((t - t0) >> group) + 1];
-        bool here = false;
-        int o, c;
-        for (int k = h0 + lane; k < h1; k += 64) here |= place(sorted[k], &o, &c);
-        any = __ballot(here) != 0;
-      }
-      if (any) {
-        auto add = [&](int o, int c) {
-          const int to = nw_dz(32 * wave + o, c >> 2) + 2 * (c & 3);
-          atomicAdd(reinterpret_cast<unsigned*>(counts + (to & ~3)), to & 2 ? 0x10000u : 1u);
-        };
-#pragma unroll
-        for (int k = 0; k < 8; ++k) *reinterpret_cast<uint64_t*>(counts + 4096 * wave + 512 * k + 8 * lane) = 0;
-        __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "wavefront");
-        if (total <= NWS_HITS) {
-          int o, c;
-          for (int k = h0 + lane; k < h1; k += 64)
-            if (place(sorted[k], &o, &c)) add(o, c);
-        } else if constexpr (ROWS) {
-          if (own0 + 32 * wave + (lane >> 1) < B)
-            each_label(a.y, own0 + 32 * wave + (lane >> 1), lane & 1, 2, [&](int id) {
-              const int c = id - first;
-              if (c >= 0 && c < NW_TILE && id < n_other) add(lane >> 1, c);
-            });
-        } else if (first + lane < B) {
-          each_label(a.y, first + lane, 0, 1, [&](int id) {
-            const int o = id - own0 - from;
-            if (o >= 0 && o < 32 && id < n_own) add(o, lane);
-          });
+    if (list_n <= NWS_OWN) {  // a list of each block's own
+      list0 = blk * NWS_OWN;
+      list_n = min(NWS_OWN, n_own - list0);
+      if (blk > b0) wb = t0;
+    }
+    for (int t = t0; t < t1;) {
+      if (t == wb) {
+        wa = t;
+        for (wb = t1;;) {
+          total = list(list0, list0 + list_n, wa, wb);
+          if (total <= NWS_HITS) break;
+          if (list_n > NWS_OWN) {
+            list0 = blk * NWS_OWN;
+            list_n = NWS_OWN;
+            continue;
+          }
+          if (wb - wa == 1) break;
+          const int fit = (int)((int64_t)(wb - wa) * (NWS_HITS * 3 / 4) / total);
+          wb = wa + (fit > 1 ? fit : 1);
         }
       }
-      __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "wavefront");
-      f32x16 z[2];
-      if constexpr (ROWS) {
-        nw_bias(p + NW_WBUF + 256 * wave, g, z);
-      } else {
+      for (; t < wb; ++t) {
+        tp_wait<0>();
+        __builtin_amdgcn_s_barrier();  // the tile is here, and nobody reads the one before
+        asm volatile("" : "+v"(row_at), "+v"(turned_at), "+v"(count_at));
+        const char* const p = smem + buf * NWS_BUF;
+        buf ^= 1;
+        if (t + 1 < t1) issue(t + 1, buf);
+        else if (blk + 1 < b1) issue(t0, buf);
+        bool masked = false;  // labels past the last
+        if constexpr (ROWS) {
+          masked = (t + 1) * NW_TILE > n_other;
+        } else {
+          const NwRow r = nw_row(a, r_top, r_inv, r_share, r_weight, scale);
+          rows[lane] = r.top;
+          rows[64 + lane] = r.fp;
+          rows[128 + lane] = r.fs;
+          fetch_row(t + 1 < t1 ? t + 1 : t0);
+        }
+        // how often a label stands in a row's list: 16-bit counts per own
+        bool any = total > NWS_HITS;
+        const int first = t * NW_TILE, from = blk * NWS_OWN - list0 + 32 * wave;
+        auto place = [&](unsigned hit, int* o, int* c) {
+          *o = (int)(hit >> SHIFT) - from;
+          *c = (int)(hit & ((1u << SHIFT) - 1)) - first;
+          return *o >= 0 && *o < 32 && *c >= 0 && *c < NW_TILE;
+        };
+        int h0 = 0, h1 = 0;
+        if (total && !any) {
+          h0 = start[(t - wa) >> group];
+          h1 = start[((t - wa) >> group) + 1];
+          bool here = false;
+          int o, c;
+          for (int k = h0 + lane; k < h1; k += 64) here |= place(sorted[k], &o, &c);
+          any = __ballot(here) != 0;
+        }
+        if (any) {
+          auto add = [&](int o, int c) {
+            const int to = nw_dz(32 * wave + o, c >> 2) + 2 * (c & 3);
+            atomicAdd(reinterpret_cast<unsigned*>(counts + (to & ~3)), to & 2 ? 0x10000u : 1u);
+          };
 #pragma unroll
-        for (int r = 0; r < 16; ++r) z[0][r] = z[1][r] = own_bias;
-      }
-      Frag f[2][2];
-      auto read = [&](int kk) {
+          for (int k = 0; k < 8; ++k) *reinterpret_cast<uint64_t*>(counts + 4096 * wave + 512 * k + 8 * lane) = 0;
+          __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "wavefront");
+          if (total <= NWS_HITS) {
+            int o, c;
+            for (int k = h0 + lane; k < h1; k += 64)
+              if (place(sorted[k], &o, &c)) add(o, c);
+          } else if constexpr (ROWS) {
+            if (own0 + 32 * wave + (lane >> 1) < B)
+              each_label(a.y, own0 + 32 * wave + (lane >> 1), lane & 1, 2, [&](int id) {
+                const int c = id - first;
+                if (c >= 0 && c < NW_TILE && id < n_other) add(lane >> 1, c);
+              });
+          } else if (first + lane < B) {
+            each_label(a.y, first + lane, 0, 1, [&](int id) {
+              const int o = id - list0 - from;
+              if (o >= 0 && o < 32 && id < n_own) add(o, lane);
+            });
+          }
+        }
+        __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "wavefront");
+        f32x16 z[2];
+        if constexpr (ROWS) {
+          nw_bias(p + NW_WBUF + 256 * wave, g, z);
+        } else {
 #pragma unroll
-        for (int b = 0; b < 2; ++b) f[kk & 1][b] = *reinterpret_cast<const Frag*>(p + (row_at ^ (32 * kk)) + 8192 * b);
-      };
-      read(0);
+          for (int r = 0; r < 16; ++r) z[0][r] = z[1][r] = own_bias;
+        }
+        Frag f[2][2];
+        auto read = [&](int kk) {
 #pragma unroll
-      for (int kk = 0; kk < 8; ++kk) {
-        if (kk + 1 < 8) read(kk + 1);
-        __builtin_amdgcn_sched_barrier(0);
+          for (int b = 0; b < 2; ++b) f[kk & 1][b] = *reinterpret_cast<const Frag*>(p + (row_at ^ (32 * kk)) + 8192 * b);
+        };
+        read(0);
 #pragma unroll
-        for (int b = 0; b < 2; ++b) z[b] = tp_mma(f[kk & 1][b], of[kk], z[b]);
-        __builtin_amdgcn_sched_barrier(0);
-      }
-      if constexpr (!ROWS) {
-        if (odd) {  // (in dh such rows are made zeros when the slabs are joined)
+        for (int kk = 0; kk < 8; ++kk) {
+          if (kk + 1 < 8) read(kk + 1);
+          __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+          for (int b = 0; b < 2; ++b) z[b] = tp_mma(f[kk & 1][b], of[kk], z[b]);
+          __builtin_amdgcn_sched_barrier(0);
+        }
+        if constexpr (!ROWS) {
+          if (odd) {  // (in dh such rows are made zeros when the slabs are joined)
+#pragma unroll
+            for (int b = 0; b < 2; ++b)
+#pragma unroll
+              for (int q = 0; q < 4; ++q) {
+                const f32x4 top = *reinterpret_cast<const f32x4*>(rows + 32 * b + 8 * q + 4 * g);
+#pragma unroll
+                for (int k = 0; k < 4; ++k) z[b][4 * q + k] = top[k] == INFINITY ? 0.0f : z[b][4 * q + k];
+              }
+          }
+        }
+        Frag df[2][2];
+        float part[4] = {};  // (one sum over thousands of rows would round as often)
+        auto form = [&](auto checked) {
 #pragma unroll
           for (int b = 0; b < 2; ++b)
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
-              const f32x4 top = *reinterpret_cast<const f32x4*>(rows + 32 * b + 8 * q + 4 * g);
-#pragma unroll
-              for (int k = 0; k < 4; ++k) z[b][4 * q + k] = top[k] == INFINITY ? 0.0f : z[b][4 * q + k];
-            }
-        }
-      }
-      Frag df[2][2];
-      float part[4] = {};  // (one sum over thousands of rows would round as often)
-      auto form = [&](auto checked) {
-#pragma unroll
-        for (int b = 0; b < 2; ++b)
-#pragma unroll
-          for (int q = 0; q < 4; ++q) {
-            const int c = 32 * b + 8 * q + 4 * g;
-            f32x4 top, fp, fs;
-            if constexpr (!ROWS) {
-              top = *reinterpret_cast<const f32x4*>(rows + c);
-              fp = *reinterpret_cast<const f32x4*>(rows + 64 + c);
-              if (checked) fs = *reinterpret_cast<const f32x4*>(rows + 128 + c);
-            }
-            uint64_t times = 0;
-            if (checked) times = any ? *reinterpret_cast<const uint64_t*>(counts + (count_at ^ (64 * b) ^ (16 * q))) : 0;
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-              float v = exp_fast(z[b][4 * q + k] - (ROWS ? mine.top : top[k])) * (ROWS ? mine.fp : fp[k]);
-              if (checked) {
-                v -= (float)((times >> (16 * k)) & 0xffff) * (ROWS ? mine.fs : fs[k]);
-                if (ROWS && first + c + k >= n_other) v = 0.0f;
+              const int c = 32 * b + 8 * q + 4 * g;
+              f32x4 top, fp, fs;
+              if constexpr (!ROWS) {
+                top = *reinterpret_cast<const f32x4*>(rows + c);
+                fp = *reinterpret_cast<const f32x4*>(rows + 64 + c);
+                if (checked) fs = *reinterpret_cast<const f32x4*>(rows + 128 + c);
               }
-              if constexpr (!ROWS) part[k] += v;
-              df[b][q >> 1][4 * (q & 1) + k] = (T)v;
+              uint64_t times = 0;
+              if (checked) times = any ? *reinterpret_cast<const uint64_t*>(counts + (count_at ^ (64 * b) ^ (16 * q))) : 0;
+#pragma unroll
+              for (int k = 0; k < 4; ++k) {
+                float v = exp_fast(z[b][4 * q + k] - (ROWS ? mine.top : top[k])) * (ROWS ? mine.fp : fp[k]);
+                if (checked) {
+                  v -= (float)((times >> (16 * k)) & 0xffff) * (ROWS ? mine.fs : fs[k]);
+                  if (ROWS && first + c + k >= n_other) v = 0.0f;
+                }
+                if constexpr (!ROWS) part[k] += v;
+                df[b][q >> 1][4 * (q & 1) + k] = (T)v;
+              }
+              __builtin_amdgcn_sched_barrier(0);
             }
-            __builtin_amdgcn_sched_barrier(0);
-          }
-      };
-      if (any || masked) form(std::true_type());
-      else form(std::false_type());
-      if constexpr (!ROWS) sums += (part[0] + part[1]) + (part[2] + part[3]);
-      // dz times what passes by: k in the accumulators' order, 16 c + 8 hi + 4 g + 0..3 of a block
-      Frag uf[4];
-      auto turned = [&](int k) {  // k = 8 b + 4 c + u
-        const char* const q = p + 4096 * (k >> 2);
-        const int to = turned_at ^ (64 * (k & 3));
-        uf[k & 3] = nw_join<T>(tp_turned<T>(q + to), tp_turned<T>(q + (to ^ 32) + 2048));
-      };
+        };
+        if (any || masked) form(std::true_type());
+        else form(std::false_type());
+        if constexpr (!ROWS) sums += (part[0] + part[1]) + (part[2] + part[3]);
+        // dz times what passes by: k in the accumulators' order, 16 c + 8 hi + 4 g + 0..3 of a block
+        Frag uf[4];
+        auto turned = [&](int k) {  // k = 8 b + 4 c + u
+          const char* const q = p + 4096 * (k >> 2);
+          const int to = turned_at ^ (64 * (k & 3));
+          uf[k & 3] = nw_join<T>(tp_turned<T>(q + to), tp_turned<T>(q + (to ^ 32) + 2048));
+        };
 #pragma unroll
-      for (int k = 0; k < 3; ++k) turned(k);
+        for (int k = 0; k < 3; ++k) turned(k);
 #pragma unroll
-      for (int k = 0; k < 16; ++k) {
-        if (k + 3 < 16) turned(k + 3);
-        __builtin_amdgcn_sched_barrier(0);
-        acc[k & 3] = tp_mma(uf[k & 3], df[k >> 3][(k >> 2) & 1], acc[k & 3]);
-        __builtin_amdgcn_sched_barrier(0);
+        for (int k = 0; k < 16; ++k) {
+          if (k + 3 < 16) turned(k + 3);
+          __builtin_amdgcn_sched_barrier(0);
+          acc[k & 3] = tp_mma(uf[k & 3], df[k >> 3][(k >> 2) & 1], acc[k & 3]);
+          __builtin_amdgcn_sched_barrier(0);
+        }
       }
     }
     if constexpr (ROWS) {
@@ -861,9 +916,11 @@ bool narrow_grad_takes(int dtype, int n_rows, int d) { return narrow_takes(dtype
 bool narrow_sides_take(int dtype, int n_rows, int n_labels, int d) {
   return narrow_takes(dtype, d) && n_rows > NW_ROWS && n_rows <= 1 << 18 && n_labels >= 40000;
 }
-// Whether the lists are short enough that a workgroup's share of labels holds its targets (evenly spread: three quarters of
-// what it lists; more, and every tile goes through its rows' lists: 4,096 rows of 75 labels out of 16,400 316 us with the
-// general kernels, 1,190 with these).
+// Whether the lists are short enough that most workgroups list the targets of their share of labels at once (evenly spread: three
+// quarters of what a list holds).  More are right as well, in several lists, but then the general kernels are as fast or
+// faster: 4,096 rows of 300 labels out of 40,001 918 us with them, 1,041 with these.  A few labels that fill lists of their own
+// (ids by a Zipf law of exponent 1.1): 8,192 rows of 75 labels out of 205,443 5,400 and 3,867, 4,096 rows of 40 labels out of
+// 40,001 518 and 590.
 bool narrow_sides_worth(int n_rows, int n_labels, int nnz) {
   const int64_t labels = NWS_OWN * ceil_div(ceil_div(n_labels, NWS_OWN), 512);
   return (int64_t)nnz * labels <= (int64_t)(NWS_HITS * 3 / 4) * n_labels;
