@@ -121,7 +121,8 @@ struct EpiLse {
 // ---- lse and loss --------------------------------------------------------------------------------
 // One workgroup per row.  Target logits are products of their own, 16 lanes each (h and w as the products read them: whole
 // 16-byte pieces).  With `scale` one workgroup more, the first, finds the gradients' scale: the largest finite |weight| of rows
-// that have labels, 1 / B without weights.
+// that have labels, 1 / B without weights; it reads eight rows a thread at once (one at a
+// time, gradients of 2^20 rows of width 16 in rising order of weight waited for it: 7.9 ms, 5.7 so).
 template <typename T>
 __global__ __launch_bounds__(256) void k_loss_rows(const float2* __restrict__ part, int tiles, TpOperand h, TpOperand w,
                                                    int D, int L, const float* __restrict__ bias, IdLists y,
@@ -136,14 +137,32 @@ __global__ __launch_bounds__(256) void k_loss_rows(const float2* __restrict__ pa
   __shared__ int sn[4];
   if (i < 0) {
     float v = 0.0f;
-    if (weights)
-      for (int r = tid; r < B; r += 256) {
-        const float a = fabsf(weights[r]);
-        if (!(a > v) || !(a < INFINITY) || !y.indptr) continue;  // (few lists are looked at)
-        int q0, q1;
-        label_range(y, r, &q0, &q1);
-        while (q0 < q1 && entry(y, q0, L) < 0) ++q0;
-        if (q0 < q1) v = a;
+    if (weights && y.indptr)
+      for (int r0 = tid; r0 < B; r0 += 256 * 8) {
+        float a[8];
+        int q0[8], q1[8];
+        bool live[8] = {}, more = true;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+          const int r = min(r0 + 256 * k, B - 1);
+          a[k] = fabsf(weights[r]);
+          label_range(y, r, &q0[k], &q1[k]);
+        }
+        while (more) {  // an entry of each row that may matter, until one counts
+          int id[8];
+          more = false;
+#pragma unroll
+          for (int k = 0; k < 8; ++k) {
+            const bool look = !live[k] && a[k] > v && a[k] < INFINITY && q0[k] < q1[k];
+            id[k] = look ? entry(y, q0[k]++, L) : -1;
+            more |= look;
+          }
+#pragma unroll
+          for (int k = 0; k < 8; ++k) live[k] |= id[k] >= 0;
+        }
+#pragma unroll
+        for (int k = 0; k < 8; ++k)
+          if (live[k]) v = fmaxf(v, a[k]);
       }
     v = wave_max(v);
     if (lane == 0) sm[wave] = v;

@@ -247,3 +247,21 @@ def test_crowded_labels_cost_little_more_than_even_ones():
             took.append(a.elapsed_time(b))
         best.append(min(took))
     assert best[1] <= 1.6 * best[0], best
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16"])
+def test_the_largest_weight_of_many_rows(dtype):
+    # more rows than are looked at in one go; lists that begin with ids that do not count, and the largest weights on rows
+    # without any that does
+    B, L, D = 5001, 300, 40
+    h, w = placed(normal(1, B, D), dtype), placed(normal(2, L, D, scale=0.3), dtype)
+    lists = [[-1] * (i % 9) + [L] * (i % 3) + [i % L] * (i % 4 != 1) for i in range(B)]
+    up = torch.arange(1, B + 1, dtype=torch.float32).cuda() * 1e-7
+    for weights, largest in ((up, B - 2), (up.flip(0), 0), (-up, 4096 + 7)):
+        weights = weights.clone()
+        weights[4097] = 1e30  # (4097 % 4 == 1: no labels)
+        weights[5] = INF
+        weights[largest] = -3e-3
+        c = Call(h, w, lists, normal(4, L), weights, dtype).run()
+        weights[4097] = weights[5] = 0.0  # (the reference needs finite ones)
+        c.check(lists, dtype)
