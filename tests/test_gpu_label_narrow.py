@@ -265,3 +265,47 @@ def test_the_largest_weight_of_many_rows(dtype):
         c = Call(h, w, lists, normal(4, L), weights, dtype).run()
         weights[4097] = weights[5] = 0.0  # (the reference needs finite ones)
         c.check(lists, dtype)
+
+
+# rows of integers of a few bits: their logits are multiples of 1/16 below 2^6, exact in every order of summation
+PATHS = [(200, 70_000, 128, "bf16"), (256, 30_001, 64, "f16"), (4000, 41_000, 64, "bf16"), (1000, 45_000, 128, "f16"),
+         (300, 3_000, 264, "bf16"), (700, 9_001, 136, "f16"), (300, 3_000, 128, "f32"), (1100, 5_000, 40, "f32"), (20, 20_000, 200, "f32")]
+
+
+def few_bits(B, L, D, dtype):
+    g = torch.Generator().manual_seed(1)
+    h, w = (torch.randint(-2, 3, s, generator=g).float() for s in ((B, D), (L, D)))
+    return placed(h.cuda(), dtype), placed((w / 16).cuda(), dtype)
+
+
+@pytest.mark.parametrize("B,L,D,dtype", PATHS)
+def test_probabilities_of_exact_logits(B, L, D, dtype):
+    # Every row's label is 0, so db of the others is the mean of their probabilities.  One is good to |z - top| + 4 half steps
+    # (the argument's product, the exponential, 1 / sum and two products), 12 or so: of either sign from row to row, so
+    # 12 / sqrt 20 of them are left of 20 rows or more; sums over rows round some 20 times, of either sign.  Together
+    # 7 half steps of 2^-24, 4.2e-7, in the norm.
+    h, w = few_bits(B, L, D, dtype)
+    c = Call(h, w, [[0]] * B, None, dtype=dtype).run()
+    z = h.double() @ w.double().T
+    z_top, lse = z.amax(1), torch.logsumexp(z, 1)
+    want = z.sub_(lse[:, None]).exp_().sum(0) / B
+    off = (c.db[1:L].double() - want[1:]).norm() / want[1:].norm()
+    assert float(off) <= 7 * ref.U, float(off)
+    # (sums of tens of thousands of exponentials, in parts: 20 half steps of 1 at most)
+    assert bool(((c.lse[:B].double() - lse).abs() <= ref.U * (lse.abs() + 20)).all())
+    # In the mean square: lse lies between 8 and 16, where half a step is 8 2^-24, as much over sqrt 3 (4.62) for any part of it;
+    # the logarithm of the sum, below 8, is off by a step of its own at most (8, where it is above 4); the sum by 12 half
+    # steps, of either sign, of each of the exponentials that make it up, 1 together: sqrt(4.62^2 + 8^2 + 1) = 9.3
+    assert bool((lse > 8).all()) and bool((lse < 16).all()) and bool((lse - z_top < 8).all())
+    assert float((c.lse[:B].double() - lse).norm()) <= 9.3 * ref.U * B ** 0.5
+
+
+@pytest.mark.parametrize("B,L,D,dtype", PATHS)
+def test_probabilities_do_not_go_through_the_rounded_log_sum_exp(B, L, D, dtype):
+    # 2^14 in every bias leaves logits exact and takes 10 bits of the log-sum-exp's fraction
+    h, w = few_bits(B, L, D, dtype)
+    lists = random_lists(3, B, L, 3)
+    near = Call(h, w, lists, torch.zeros(L, device="cuda"), dtype=dtype).run().outputs()
+    far = Call(h, w, lists, torch.full((L,), 16384.0, device="cuda"), dtype=dtype).run().outputs()
+    for k in ("dh", "dw", "db"):
+        assert torch.equal(far[k], near[k]), k
