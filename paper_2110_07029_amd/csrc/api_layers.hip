@@ -44,14 +44,16 @@ bool meet(const Span& a, const Span& b) {
   if (!a.at || !b.at) return false;
   const uintptr_t ea = a.at + (a.rows - 1) * a.step + a.width, eb = b.at + (b.rows - 1) * b.step + b.width;
   if (a.at >= eb || b.at >= ea) return false;
-  if (a.rows == 1 || b.rows == 1 || a.step != b.step) return true;
-  const int64_t d = (int64_t)((a.at < b.at ? b.at - a.at : a.step - (int64_t)((a.at - b.at) % a.step)) % a.step);
-  return d < a.width || d + b.width > a.step;
+  if (a.rows == 1 && b.rows == 1) return true;
+  if (a.rows > 1 && b.rows > 1 && a.step != b.step) return true;
+  const int64_t step = a.rows > 1 ? a.step : b.step;  // (one row lies between rows or meets them)
+  const int64_t d = (int64_t)((a.at < b.at ? b.at - a.at : step - (int64_t)((a.at - b.at) % step)) % step);
+  return d < a.width || d + b.width > step;
 }
 bool meet(const asgd_matrix* a, const asgd_matrix* b) { return a && b && meet(span_of(a), span_of(b)); }
 // Whether they do and are not the same matrix.
 bool meet_partly(const asgd_matrix* a, const asgd_matrix* b) {
-  return meet(a, b) && !(a->data == b->data && a->ld == b->ld && a->dtype == b->dtype);
+  return meet(a, b) && !(a->data == b->data && (a->ld == b->ld || a->n_rows == 1) && a->dtype == b->dtype);
 }
 
 asgd_status check_shape(const asgd_matrix* a, const char* name, int rows, int cols) {

@@ -237,3 +237,30 @@ def test_reference_of_layers_and_loss_against_automatic_differentiation():
     assert torch.allclose(out["loss"][0], loss)
     for k, t in zip(("dh", "dw", "db"), torch.autograd.grad((loss * weights).sum(), (x, w, b))):
         assert torch.allclose(out[k][0], t, atol=1e-12), k
+
+
+def test_what_shares_memory_is_found_element_by_element():
+    # outputs of one row and of several against w [n x 8] in rows of 21, wherever they begin.  A matrix of one row has no
+    # stride, whatever its ld says.
+    for n, rows, ld in ((6, 1, 6), (6, 1, 33), (30, 1, 30), (6, 3, 21), (1, 1, 7), (1, 5, 9)):
+        held = {21 * i + j for i in range(n) for j in range(8)}
+        step = ld if rows > 1 else 0
+        for start in range(-max(ld, n) * rows - 8, 21 * n + 8, 1 if n < 10 else 7):
+            taken = {start + i * step + j for i in range(rows) for j in range(n)}
+            call = dict(x=mat(rows, 8, data=at(1)), w=mat(n, 8, 21, data=at(2)), y=mat(rows, n, ld, data=at(2) + 4 * start))
+            if held & taken:
+                refused(E, "overlaps", dense, **call)
+            else:
+                refused(R, "workspace", dense, **call, workspace=Ws(0))
+    # the residual itself, whatever the strides of one row say; of another type it is not itself
+    x, w = mat(1, 8, data=at(1)), mat(6, 8, 9, data=at(2))
+    for ld in (6, 9):
+        refused(R, "workspace", dense, x=x, w=w, y=mat(1, 6, ld, data=at(3)), epilogue=ep(residual=mat(1, 6, data=at(3))), workspace=Ws(0))
+    refused(E, "overlaps", dense, x=x, y=mat(1, 6, data=at(3)), epilogue=ep(residual=mat(1, 6, dtype=BF16, data=at(3))))
+    # the bias's gradient in the gaps between dw's rows
+    for col, fine in ((8, True), (14, True), (7, False), (15, False)):
+        change = dict(dw=mat(6, 8, 20, data=at(5)), db=at(5) + 4 * (40 + col), w=w)
+        if fine:
+            refused(R, "workspace", backward, **change, workspace=Ws(0))
+        else:
+            refused(E, "overlap", backward, **change)
