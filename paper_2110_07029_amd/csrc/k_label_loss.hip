@@ -24,6 +24,7 @@
 // that is only read needs no dz at all.  dz in 16 bits is
 // rounded once, with the target in it (p and the target may nearly cancel); fp16 holds it times 2^15 over the
 // largest weight, so that probabilities down to 2^-29 stay normal.
+#include <float.h>
 #include <math.h>
 
 #include "label_loss_dev.h"
@@ -204,7 +205,8 @@ __global__ __launch_bounds__(256) void k_loss_rows(const float2* __restrict__ pa
       for (int e = 0; e < E; ++e)
         if (id[e] >= 0) {
           n += l == 0;
-          t += d[e] + (bias && l == 0 ? bias[id[e]] : 0.0f);
+          // (times 2^-16: masks of the lowest value, up to 65,535 of them, have a sum as well as a mean)
+          t += 0x1p-16f * (d[e] + (bias && l == 0 ? bias[id[e]] : 0.0f));
         }
     }
   }
@@ -237,7 +239,9 @@ __global__ __launch_bounds__(256) void k_loss_rows(const float2* __restrict__ pa
     top_ws[i] = top;
     inv[i] = 1.0f / s;
     if (lse_out) lse_out[i] = lse;
-    loss[i] = n ? lse - t * sh : 0.0f;
+    float mean = t * (0x1p16f * sh);
+    if (mean == -INFINITY && t > -INFINITY) mean = -FLT_MAX;  // (1 / n rounded up)
+    loss[i] = n ? lse - mean : 0.0f;
   }
 }
 
