@@ -329,3 +329,22 @@ def test_several_masked_labels_in_a_list(dtype, D):
     # and where all labels are masked, lse and the mean are both the lowest value
     c = Call(h, w, [r or [1] for r in lists], torch.full((L,), LOWEST, device="cuda"), dtype=dtype, grads=()).run()
     assert bool((c.lse[:B] == LOWEST).all()) and bool((c.loss[:B].abs() <= 65_537 * ref.U * -LOWEST).all())
+
+
+@pytest.mark.parametrize("low", [LOWEST, -1e10])
+@pytest.mark.parametrize("B,L,D,dtype", [(300, 9_000, 136, "bf16"), (64, 5_000, 264, "f16"), (200, 5_000, 64, "f32"), (3, 30_000, 200, "f32")])
+def test_wider_rows_under_the_same_masks(B, L, D, dtype, low):
+    h, w = placed(normal(1, B, D), dtype), placed(normal(2, L, D, scale=2 * D ** -0.5), dtype)
+    block = torch.arange(L, device="cuda") // 64
+    for masked in (block % 3 == 0, block > 0, block < L // 64):
+        bias = torch.where(masked, low, normal(4, L))
+        free = (~masked).nonzero()[:, 0].tolist()
+        lists = [[free[(7 * i) % len(free)], free[(11 * i + 1) % len(free)]] for i in range(B)]
+        lists[1] = []
+        Call(h, w, lists, bias, dtype=dtype).run().check(lists, dtype)
+    lists = [[i, 2 * i + 500] for i in range(B)]
+    c = Call(h, w, lists, torch.full((L,), LOWEST, device="cuda"), dtype=dtype).run()
+    want = torch.full((L,), 1.0 / L, dtype=torch.float64, device="cuda")
+    ids = torch.tensor(lists, device="cuda").flatten()
+    want.index_add_(0, ids, torch.full_like(ids, -0.5 / B, dtype=torch.float64))
+    assert bool(((c.db[:L].double() - want).abs() <= (B + 8) * ref.U * (1.0 / L + want.abs())).all())
