@@ -11,7 +11,6 @@
 
 namespace asgd {
 
-typedef _Float16 f16;
 typedef unsigned long long u64;
 
 template <typename T>

@@ -7,9 +7,6 @@
 
 namespace asgd {
 
-typedef _Float16 f16;
-typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
-
 // Vectors at any element's address (the hardware takes them; with eight accesses of 2 bytes instead a layer of
 // 777 x 1,001 x 515 out of line took 18 us, it takes 15).
 typedef float f32x4u __attribute__((ext_vector_type(4), aligned(4)));
