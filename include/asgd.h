@@ -538,7 +538,8 @@ enum { ASGD_ACT_NONE = 0, ASGD_ACT_RELU = 1, ASGD_ACT_GELU = 2, ASGD_ACT_SILU = 
 
 /* What follows a product A = X W^T + bias:
  *   Y = residual + drop(act(A))
- * act: none, max(a, 0), a Phi(a) with the normal distribution function Phi,
+ * act: none, max(a, 0), a Phi(a) with the normal distribution function Phi (off
+ * by 2^-22 at most, so that far negative a keep an absolute error of |a| 2^-22),
  * or a / (1 + e^-a).  drop as for asgd_dropout, on Y's rows and columns.
  * Zero-initialise the struct for the product alone. */
 typedef struct asgd_epilogue {
@@ -593,7 +594,9 @@ asgd_status asgd_dropout(const asgd_matrix* x, double p, uint64_t seed, const as
  * device float [B]; dh, dw (any type) and db: each may be NULL.  Without any of
  * the three the workspace of gradients = 0 is enough, otherwise it is that of 1.
  * In 16 bits dz is rounded once to h's type for its two products; db is
- * formed before that.  A logit that is NaN or +inf makes its row's loss and
+ * formed before that.  fp16 holds dz in multiples of 2^-39 of the largest
+ * |weight| among rows with labels at the least (11 bits of it from 2^-29 on), so
+ * rows of far smaller weights keep fewer bits in dh and dw.  A logit that is NaN or +inf makes its row's loss and
  * gradients NaN, and dw and db with them; a label of logit -inf has
  * probability 0. */
 asgd_status asgd_label_loss_workspace(const asgd_matrix* h, const asgd_matrix* w, int32_t gradients, size_t* bytes);

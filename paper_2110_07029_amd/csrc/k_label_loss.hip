@@ -23,7 +23,8 @@
 // gradients' products have).  Forming z twice is the fourth product; storing dz of all labels would take 262 MB, and a loss
 // that is only read needs no dz at all.  dz in 16 bits is
 // rounded once, with the target in it (p and the target may nearly cancel); fp16 holds it times 2^15 over the
-// largest weight, so that probabilities down to 2^-29 stay normal.
+// largest weight, so that probabilities of a row of that weight stay normal down to 2^-29, and of a row of 1/x of it down to
+// x 2^-29: one scale for all, since the products sum over rows.
 #include <float.h>
 #include <math.h>
 

@@ -9,7 +9,7 @@
 //                  registers (dz is fed to the matrix cores as the accumulators hold it, the tile of W read with the k order
 //                  that this gives); dz through LDS, turned around, times h: the tile's rows of dw
 //
-// 256 rows, 670,091 labels, width 128 in bf16, loss and gradients: 234 to 262 us; the general kernels took 638.  W is read
+// 256 rows, 670,091 labels, width 128 in bf16, loss and gradients: 245 to 260 us; the general kernels took 638.  W is read
 // twice and dw written once, 515 MB (101 us at a copy's rate); four products of 44 GFLOP.
 //
 // LDS rows of W and h are 256 bytes; chunk c (16 bytes) of row r lies at place c ^ (4 (r % 4) + r / 4 % 4), which makes both
@@ -125,8 +125,9 @@ __device__ __forceinline__ void nw_logits(const char* w, const typename TpMma<T>
 // all).
 // Four waves with 64 rows each: what a wave reads of a tile serves two products.  Two workgroups share a compute unit, so
 // that one's exponentials meet the other's products.  Bound by issue: per tile and wave 32 products and 64 exponentials a
-// lane with their sums and maxima, of which a part overlaps.  256 rows against 670,091 labels: 62 us (eight waves with 32 rows
-// each 68).
+// lane with their sums and maxima, of which a part overlaps.  256 rows against 670,091 labels: 65 us (62 with a power of two
+// as the base, one operation less for each exponential, which masks of large values do not allow; eight waves with 32 rows
+// each 6 more).
 constexpr int NWF_THREADS = 256, NWF_BUFS = 2;
 constexpr int NWF_LDS = NWF_BUFS * (NW_WBUF + 4 * 256);
 
@@ -214,10 +215,11 @@ __global__ __launch_bounds__(NWF_THREADS, 2) void k_narrow_lse(TpOperand h, TpOp
 
 // ---- gradients ---------------------------------------------------------------------------------------
 // Workgroup = a range of tiles with all the rows; one per compute unit (h, two tiles of W and dz fill its LDS).  Eight waves
-// own 32 rows each for z, dz and dh, and one of the eight 32 x 32 blocks of dw.  256 rows, 670,091 labels: 165 to 180 us.
+// own 32 rows each for z, dz and dh, and one of the eight 32 x 32 blocks of dw.  256 rows, 670,091 labels: 170 to 185 us.
 // Bound by latency: two barriers per tile, and what stands between them (LDS reads, dz's arithmetic, products) waits for
 // each other in a wave while its SIMD has one more.  Four waves of 64 rows in 512 registers took 320 us, dz's exponentials
-// between the products of dh 790 (spills).  Where dw has the operands' type it leaves in 16-byte stores.
+// between the products of dh 790 (spills).  All 256 registers of a lane are taken; two or four more, which rows whose targets
+// do not fit the list need, lie in scratch.  Where dw has the operands' type it leaves in 16-byte stores.
 constexpr int NWG_BUFS = 2, NWG_HITS = 1023;
 constexpr int NWG_H = 0, NWG_DZ = NWG_H + NW_ROWS * 256, NWG_W = NWG_DZ + NW_ROWS * 128;
 constexpr int NWG_HIT = NWG_W + NWG_BUFS * (NW_WBUF + NW_BIAS), NWG_SUM = NWG_HIT + 4 * (NWG_HITS + 1);
@@ -236,18 +238,16 @@ __device__ __forceinline__ float nw_sum_lanes(float (&v)[32], int lane) {
     v[k] = __builtin_bit_cast(float, (unsigned)s[0]) + __builtin_bit_cast(float, (unsigned)s[1]);
   }
   auto halve = [&](int half, bool up, auto other) {
+#pragma unroll
     for (int k = 0; k < half; ++k) {
       const float keep = up ? v[k + half] : v[k], give = up ? v[k] : v[k + half];
       v[k] = keep + __builtin_bit_cast(float, other(__builtin_bit_cast(unsigned, give)));
     }
   };
-#pragma unroll
-  for (int k = 0; k < 1; ++k) {
-    halve(8, lane & 8, [&](unsigned x) { return lane_xor<8>(x, lane); });
-    halve(4, lane & 4, [&](unsigned x) { return lane_xor<4>(x, lane); });
-    halve(2, lane & 2, [&](unsigned x) { return lane_xor<2>(x, lane); });
-    halve(1, lane & 1, [&](unsigned x) { return lane_xor<1>(x, lane); });
-  }
+  halve(8, lane & 8, [&](unsigned x) { return lane_xor<8>(x, lane); });
+  halve(4, lane & 4, [&](unsigned x) { return lane_xor<4>(x, lane); });
+  halve(2, lane & 2, [&](unsigned x) { return lane_xor<2>(x, lane); });
+  halve(1, lane & 1, [&](unsigned x) { return lane_xor<1>(x, lane); });
   return v[0];
 }
 
@@ -503,8 +503,9 @@ __global__ __launch_bounds__(NW_THREADS) void k_narrow_grad(TpOperand h, TpOpera
 // One side of the product in registers, 32 per wave, with the sums of its gradient; the other passes by in tiles of 64
 // through LDS.  Rows in registers give dh, labels dw and db: z is formed once more for each (and its exponentials), but dz
 // leaves its registers for neither.  Four waves, two workgroups per compute unit, one barrier per tile.  406 rows, 225,682
-// labels, width 128 in bf16: dh 70 us, dw and db 94 (the general kernels' dz, 183 MB written and read twice, and its products
-// 245); the whole call 304 -> 198.  For up to 256 rows k_narrow_grad, which forms z once for both, is faster.
+// labels, width 128 in bf16: dh 70 to 76 us, dw and db 94 to 104 (the general kernels' dz, 183 MB written and read twice, and
+// its products 245); the whole call 304 -> 198 to 215.  For up to 256 rows k_narrow_grad, which forms z once for both, is
+// faster.
 constexpr int NWS_THREADS = 256, NWS_OWN = 128, NWS_HITS = 2047;
 constexpr int NWS_BUF = NW_WBUF + 4 * 256, NWS_COUNT = 2 * NWS_BUF, NWS_ROW = NWS_COUNT + NWS_OWN * 128;
 constexpr int NWS_HIT = NWS_ROW + 4 * 3 * 256, NWS_SORT = NWS_HIT + 4 * (NWS_HITS + 1), NWS_START = NWS_SORT + 4 * (NWS_HITS + 1);
