@@ -314,7 +314,8 @@ __global__ __launch_bounds__(NW_THREADS) void k_narrow_grad(TpOperand h, TpOpera
   }
   const bool live = sh > 0.0f;
   const float out = alpha * scale, fs = f * sh;
-  // targets among this workgroup's labels, listed once
+  // targets among this workgroup's labels, listed once (more than the list holds: every tile goes through the rows' lists, which
+  // takes 256 rows x 670,091 labels of 75 targets a row from 304 us to 530 where all are among 2,000 labels; general kernels 638)
   int* const hits = reinterpret_cast<int*>(smem + NWG_HIT);
   if (tid == 0) hits[0] = 0;
   asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
